@@ -195,7 +195,10 @@ def _ha():
 
 
 def _own_decode(s):
-    o, state = _ha().ha_la_gla_decode(s["q"], s["k"], s["v"], s["g"], s["state"])
+    """To another state, so that every pass starts from the same one; that buffer is kept."""
+    if "state_out" not in s:
+        s["state_out"] = torch.empty_like(s["state"])
+    o, state = _ha().ha_la_gla_decode(s["q"], s["k"], s["v"], s["g"], s["state"], state_out=s["state_out"])
     return {"o": o, "state": state}
 
 
