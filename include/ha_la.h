@@ -1,9 +1,11 @@
 /*
  * ha_la.h -- C ABI of the B200 (sm_100a) delta-rule linear-attention prefill library.
  *
- * One operation: the chunkwise-parallel prefill of a Gated DeltaNet (GDN) layer
+ * First the chunkwise-parallel prefill of a Gated DeltaNet (GDN) layer
  * (scalar log-gate per head per token) or its Kimi-Delta-Attention (KDA)
- * variant (log-gate per key channel).
+ * variant (log-gate per key channel), with its decoding step; further down what
+ * stands next to it in a hybrid model: gated linear attention (forward, backward,
+ * one token) and the norms on both sides of a block (forward, backward).
  *
  * Paper passages that define the operation:
  *   - Section 2.1, "Architecture of Linear-Attention Hybrids": a fixed-size
@@ -235,6 +237,135 @@ typedef struct {
 /* Enqueue one decoding step on `cuda_stream`.  Returns HA_LA_OK or an error code; launches one
  * kernel (none when N == 0).                                                                      */
 int ha_la_decode(const ha_la_decode_args* args, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Gated linear attention: the recurrence above without the delta correction (no beta: what is written does not depend on
+ * what the state already holds), scalar log-gate per V-head and token, for serving and for training.  Per sequence and
+ * V-head j (QK-head jq = j / (HV/HK)), h (d_k x d_v) starting at h0 or zero, for each token t in order:
+ *     h <- exp(g[t,j]) h + k[t,jq] v[t,j]^T          o[t,j] = scale * h^T q[t,jq]          hT = h after the last token
+ * and backwards, with dh (the gradient of the state) starting at dhT or zero behind the last token:
+ *     dh <- dh + scale * q_t do_t^T      dv_t = dh^T k_t      dk_t = dh v_t      dq_t = scale * h_t do_t
+ *     dg_t = exp(g_t) <h_{t-1}, dh>      dh <- exp(g_t) dh                       dh0 = dh in front of the first token
+ * dq and dk of a QK-head are the sums over its V-heads.  (The paper's models mix such layers with GDN and KDA ones; it
+ * prints no equations for them.)
+ *
+ * Evaluated by chunks: 64 tokens in fp32 (fp32 inputs, or d = 64), 128 on the tensor cores (bf16, d = 128).  Cumulative
+ * log-gates are held in 64 bits.  States, dg and dh0 have fp32 accuracy on both paths (operands that go into a state are
+ * split into two bf16 pieces); o, dq, dk and dv of the tensor-core path come of bf16 operands with fp32 sums.  Results are
+ * the same bits from run to run: nothing is added atomically.
+ *
+ * Conventions as for ha_la_prefill (device pointers, caller's stream, no allocation, no synchronisation, may be captured,
+ * a workspace belongs to one call at a time).  The same log-gates: finite, <= 0 (very negative ones, that make exp(g)
+ * zero, are fine, and so is minus infinity).  No other value is read beyond what the sequence owns: NaN or infinities of one sequence do not reach
+ * another.  Outputs must not overlap inputs or each other, except that hT may be exactly h0, and dh0 exactly dhT.   */
+typedef struct {
+  int32_t dtype;          /* ha_la_dtype of q, k, v, o, do_, dq, dk, dv                       */
+  int32_t batch;          /* B; must be 1 when cu_seqlens != NULL                            */
+  int32_t seqlen;         /* T per batch row; TOTAL packed tokens when cu_seqlens != NULL    */
+  int32_t num_qk_heads;   /* HK                                                              */
+  int32_t num_v_heads;    /* HV, a multiple of HK                                            */
+  int32_t d_k, d_v;       /* d_k == d_v, 64 or 128                                           */
+  float   scale;
+  const void*  q;         /* [B, T, HK, d_k] contiguous; 16-byte aligned, as are k, v and the other tensors of that type */
+  const void*  k;         /* [B, T, HK, d_k]                                                 */
+  const void*  v;         /* [B, T, HV, d_v]                                                 */
+  const float* g;         /* [B, T, HV] log-gate                                             */
+  const float* h0;        /* [N, HV, d_k, d_v] or NULL (zeros); N = B or num_seqs            */
+  const int32_t* cu_seqlens; /* as in ha_la_prefill_args                                     */
+  int32_t num_seqs;
+  int32_t max_seqlen;
+  void*   o;              /* forward: [B, T, HV, d_v]                                        */
+  float*  hT;             /* forward: [N, HV, d_k, d_v] or NULL (not wanted)                 */
+  const void*  do_;       /* backward: gradient of o                                         */
+  const float* dhT;       /* backward: gradient of hT, or NULL (zeros)                       */
+  void*   dq;             /* backward: [B, T, HK, d_k]                                       */
+  void*   dk;             /* backward: [B, T, HK, d_k]                                       */
+  void*   dv;             /* backward: [B, T, HV, d_v]                                       */
+  float*  dg;             /* backward: [B, T, HV]                                            */
+  float*  dh0;            /* backward: [N, HV, d_k, d_v] or NULL (not wanted)                */
+  void*   workspace;      /* >= ha_la_gla_workspace_bytes(), 256-byte aligned                */
+  size_t  workspace_bytes;
+  int32_t* status_word;   /* optional device int32; the caller zeroes it before the call     */
+} ha_la_gla_args;
+
+/* Host only: bytes of scratch that ha_la_gla_prefill (backward = 0) or ha_la_gla_backward (1) needs for these shapes.
+ * Pointers are not followed; whether cu_seqlens is NULL or num_seqs > 0 tells packed batches.  */
+int ha_la_gla_workspace_bytes(const ha_la_gla_args* args, int backward, size_t* out_bytes);
+/* "tc" (tcgen05 tensor cores: bf16, d = 128), "simt" (fp32) or NULL if unsupported.  Host only. */
+const char* ha_la_gla_path(const ha_la_gla_args* args);
+int ha_la_gla_prefill(const ha_la_gla_args* args, void* cuda_stream);
+int ha_la_gla_backward(const ha_la_gla_args* args, void* cuda_stream);
+
+/* One token per sequence, in fp32: h_out = exp(g) h_in + k v^T, o = scale h_out^T q.  The struct is that of ha_la_decode;
+ * variant and beta are not read.  h_out may be exactly h_in.                                  */
+int ha_la_gla_decode(const ha_la_decode_args* args, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * The norms on both sides of a block.  rms(x) = sqrt(mean(x^2) + eps) over a row's `cols` values; rows are contiguous, one
+ * behind the other; weights and their gradients fp32, everything else of `dtype`; all arithmetic fp32, rounded once at the
+ * end.  1 <= cols <= 16384, any rows >= 0.  Tensors of `dtype` that are 16-byte aligned are read and written 16 bytes at a
+ * time whatever `cols` is; others element by element.
+ *
+ * ha_la_gated_norm, behind the recurrence (a row is a head's d_v channels) or before it (without z):
+ *     y = x / rms(x) * w * act(z)          act = silu (z sigmoid(z)) or sigmoid; z == NULL: no gate
+ *   ha_la_gated_norm_backward: dx, dz (z given), dw from dy, x, w, z.
+ *   y may be exactly x or z; dx exactly dy or x, dz exactly z (or dy or x, if dx is not).
+ * ha_la_add_norm, where a block's output x joins the residual stream r and the next block begins:
+ *     f = x, or x / rms(x) * w_post (w_post given);  r_out = r + scale * f;  y = r_out / rms(r_out) * w
+ *   y is made from r_out before it is rounded.  ha_la_add_norm_backward: dr, dx, dw, dw_post from dy, dr_out (the
+ *   gradient that r_out has from elsewhere; NULL: none), x and r_out as stored.
+ *   r_out may be exactly r, y exactly x (or r, if r_out is not); dr exactly dr_out, dx exactly dy.
+ * Otherwise outputs must not overlap inputs or each other.
+ * The backward passes sum the weights' gradients over rows in a fixed order (the same bits from run to run) and need a
+ * workspace; the forward passes need none and ignore it.                                          */
+typedef enum { HA_LA_ACT_SILU = 0, HA_LA_ACT_SIGMOID = 1 } ha_la_activation;
+
+typedef struct {
+  int32_t dtype;          /* ha_la_dtype of x, z, y, dy, dx, dz                              */
+  int32_t activation;     /* ha_la_activation, read when z != NULL                           */
+  int64_t rows;
+  int32_t cols;
+  float   eps;            /* >= 0                                                            */
+  const void*  x;
+  const float* w;         /* [cols]                                                          */
+  const void*  z;         /* or NULL                                                         */
+  void*   y;              /* forward                                                         */
+  const void*  dy;        /* backward                                                        */
+  void*   dx;
+  void*   dz;             /* backward, with z                                                */
+  float*  dw;             /* backward: [cols]                                                */
+  void*   workspace;      /* backward: >= ha_la_gated_norm_workspace_bytes(), 256-byte aligned */
+  size_t  workspace_bytes;
+} ha_la_gated_norm_args;
+
+typedef struct {
+  int32_t dtype;          /* ha_la_dtype of x, r, y, r_out, dy, dr_out, dx, dr               */
+  int32_t cols;
+  int64_t rows;
+  float   scale;
+  float   eps;            /* >= 0                                                            */
+  const void*  x;
+  const void*  r;         /* forward                                                         */
+  const float* w;         /* [cols]                                                          */
+  const float* w_post;    /* [cols] or NULL                                                  */
+  void*   y;              /* forward                                                         */
+  void*   r_out;          /* forward: written; backward: read                                */
+  const void*  dy;        /* backward                                                        */
+  const void*  dr_out;    /* backward, or NULL                                               */
+  void*   dx;
+  void*   dr;
+  float*  dw;             /* backward: [cols]                                                */
+  float*  dw_post;        /* backward, with w_post: [cols]                                   */
+  void*   workspace;      /* backward: >= ha_la_add_norm_workspace_bytes(), 256-byte aligned */
+  size_t  workspace_bytes;
+} ha_la_add_norm_args;
+
+int ha_la_gated_norm_workspace_bytes(const ha_la_gated_norm_args* args, size_t* out_bytes);   /* host only */
+int ha_la_gated_norm(const ha_la_gated_norm_args* args, void* cuda_stream);
+int ha_la_gated_norm_backward(const ha_la_gated_norm_args* args, void* cuda_stream);
+int ha_la_add_norm_workspace_bytes(const ha_la_add_norm_args* args, size_t* out_bytes);       /* host only */
+int ha_la_add_norm(const ha_la_add_norm_args* args, void* cuda_stream);
+int ha_la_add_norm_backward(const ha_la_add_norm_args* args, void* cuda_stream);
 
 /* Test hook for the device-side bounded waits (the paper has no counterpart).  Every wait inside the
  * kernels is on an mbarrier; it gives up after a fixed number of polls, records HA_LA_ERR_TIMEOUT in

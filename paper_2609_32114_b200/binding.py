@@ -35,6 +35,17 @@ EXPORTS = (
     "ha_la_prefill_num_segments",
     "ha_la_prefill_num_runs",
     "ha_la_decode",
+    "ha_la_gla_workspace_bytes",
+    "ha_la_gla_path",
+    "ha_la_gla_prefill",
+    "ha_la_gla_backward",
+    "ha_la_gla_decode",
+    "ha_la_gated_norm_workspace_bytes",
+    "ha_la_gated_norm",
+    "ha_la_gated_norm_backward",
+    "ha_la_add_norm_workspace_bytes",
+    "ha_la_add_norm",
+    "ha_la_add_norm_backward",
     "ha_la_debug_wait_timeout",
     "ha_la_status_string",
     "ha_la_version",
@@ -98,7 +109,7 @@ class HaLaError(RuntimeError):
 
 
 _lib = None
-_call = None          # the native half of ha_la_prefill / ha_la_decode (csrc/torch_call.cpp), once loaded
+_call = None          # the native half of the torch entry points (csrc/torch_call.cpp), once loaded
 _call_lib = None      # ... and the library it is bound to
 
 
@@ -143,6 +154,9 @@ def load_library(path: Optional[str] = None):
     lib.ha_la_status_string.restype = ctypes.c_char_p
     lib.ha_la_version.argtypes = []
     lib.ha_la_version.restype = ctypes.c_int
+    from . import layer
+
+    layer.declare(lib)
     if path is None:
         _lib = lib
     return lib
@@ -166,9 +180,16 @@ def _torch_call():
         _call = mod
     if _call_lib is not lib:
         _call.bind(*(ctypes.cast(f, ctypes.c_void_p).value
-                     for f in (lib.ha_la_prefill, lib.ha_la_prefill_workspace_bytes, lib.ha_la_decode)))
+                     for f in (lib.ha_la_prefill, lib.ha_la_prefill_workspace_bytes, lib.ha_la_decode,
+                               lib.ha_la_gla_prefill, lib.ha_la_gla_backward, lib.ha_la_gla_workspace_bytes, lib.ha_la_gla_decode,
+                               lib.ha_la_gated_norm, lib.ha_la_gated_norm_backward, lib.ha_la_gated_norm_workspace_bytes,
+                               lib.ha_la_add_norm, lib.ha_la_add_norm_backward, lib.ha_la_add_norm_workspace_bytes)))
         _call_lib = lib
     return _call
+
+
+def _native():
+    return _call if _call_lib is not None else _torch_call()
 
 
 def status_string(status: int) -> str:

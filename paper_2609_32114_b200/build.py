@@ -23,7 +23,8 @@ INCLUDE = os.path.join(ROOT, "include")
 # (object name, source, extra flags)
 UNITS = [("api", "api.cu", []), ("plan", "plan.cu", []), ("tc", "tc.cu", []), ("tc_tp", "tc_tp.cu", []), ("tc_kda", "tc_kda.cu", []),
          ("tc_walk", "tc_walk.cu", []), ("tc_span", "tc_span.cu", []),
-         ("noalloc", "noalloc.cu", []), ("decode", "decode.cu", []), ("fp32_d64", "fp32_d64.cu", [])] + [
+         ("noalloc", "noalloc.cu", []), ("decode", "decode.cu", []), ("fp32_d64", "fp32_d64.cu", []),
+         ("norm", "norm.cu", []), ("gla_api", "gla/api.cu", []), ("gla_decode", "gla/decode.cu", []), ("gla_simt", "gla/simt.cu", [])] + [
     (f"simt{u}", "simt.cu", [f"-DHA_LA_SIMT_UNIT={u}"]) for u in range(5)
 ] + [
     (f"fp32_{u}", "fp32.cu", [f"-DHA_LA_FP32_UNIT={u}"]) for u in range(5)
@@ -37,7 +38,7 @@ def _nvcc() -> str:
 
 def _headers_mtime() -> float:
     t = os.path.getmtime(os.path.abspath(__file__))
-    for d in (CSRC, INCLUDE):
+    for d in (CSRC, os.path.join(CSRC, "gla"), INCLUDE):
         for f in os.listdir(d):
             if f.endswith((".cuh", ".h")):
                 t = max(t, os.path.getmtime(os.path.join(d, f)))

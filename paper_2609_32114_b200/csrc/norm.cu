@@ -1,0 +1,693 @@
+// The norms on both sides of a block (ha_la_gated_norm, ha_la_add_norm in ha_la.h), forward and backward.
+//
+//   gated_norm   y = x rs w act(z)                     rs = 1 / sqrt(mean(x^2) + eps) of the row
+//     backward   with dn = dy w act(z):  dx = rs (dn - x rs^2 mean(dn x)),  dz = dy x rs w act'(z),  dw = sum over rows of dy x rs act(z)
+//   add_norm     r' = r + s f,  f = x or x rx w_post;  y = r' rs w
+//     backward   with dn = dy w:  dr = dr' + rs (dn - r' rs^2 mean(dn r')),  dw = sum dy r' rs;  df = s dr, and with a norm behind the block
+//                dw_post = sum df x rx,  dx = rx (dm - x rx^2 mean(dm x)) with dm = df w_post
+// Nothing is kept from the forward pass: the row is there anyway, so its norm costs no traffic.  The sums that do not wait for one another
+// go through one reduction (mean(dn x) is taken of x, not of x rs), so a row needs one, two with w_post.
+//
+// What bounds them is HBM, and latency in small calls.  A row lies in registers, 16 bytes of each tensor to a thread: rows of up to 32
+// vectors are shared by 1, 2, 4 .. 32 neighbouring lanes, longer ones by a CTA.  A row that does not start on a 16-byte boundary is
+// read in aligned vectors all the same, with the neighbours' values at its ends masked: a group's rows are a multiple of 8 apart, so the
+// column that an element of a thread holds is the same in every row, weights stay in registers and so do the sums for dw, which
+// a second kernel adds up over CTAs in order (no atomics: the same bits every time).  Rows in flight: the next row of the backward loops is
+// loaded before the present one is reduced.
+#include "common.cuh"
+
+namespace ha_la {
+
+namespace {
+
+constexpr int kSubThreads = 256;                         // CTA of the short rows (several rows to a warp or to a CTA)
+constexpr int kMaxCols = 16384;
+constexpr int kReduceThreads = 256;
+
+struct NormParams {
+  const void *x, *z, *r, *dy, *dr_out;                   // z: the gate; r: residual stream (backward: behind the addition)
+  const float *w, *w_post;
+  void *y, *r_out, *dx, *dz, *dr;
+  float *part;                                           // backward: [CTA][1 or 2][cols] sums of a CTA's rows
+  long long rows;
+  int cols, group;                                       // group: lanes that share a row (short rows)
+  int sigmoid;
+  float eps, scale;
+};
+
+// ---------------------------------------------------------------- vectors of a row
+
+template <typename In, int VEC> struct Raw { In e[VEC]; };
+template <> struct Raw<__nv_bfloat16, 8> { uint4 v; };
+template <> struct Raw<float, 4> { float4 v; };
+
+__device__ __forceinline__ void to_floats(const Raw<__nv_bfloat16, 8>& a, float (&f)[8]) {
+  const uint32_t w[4] = {a.v.x, a.v.y, a.v.z, a.v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(w[i] << 16);
+    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void to_floats(const Raw<float, 4>& a, float (&f)[4]) { f[0] = a.v.x; f[1] = a.v.y; f[2] = a.v.z; f[3] = a.v.w; }
+template <typename In> __device__ __forceinline__ void to_floats(const Raw<In, 1>& a, float (&f)[1]) { f[0] = to_f32(a.e[0]); }
+__device__ __forceinline__ Raw<__nv_bfloat16, 8> from_floats(const float (&f)[8], __nv_bfloat16) {
+  Raw<__nv_bfloat16, 8> a;
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&b);
+  }
+  a.v = make_uint4(w[0], w[1], w[2], w[3]);
+  return a;
+}
+__device__ __forceinline__ Raw<float, 4> from_floats(const float (&f)[4], float) { return {make_float4(f[0], f[1], f[2], f[3])}; }
+template <typename In> __device__ __forceinline__ Raw<In, 1> from_floats(const float (&f)[1], In) { return {{from_f32<In>(f[0])}}; }
+
+// Which part of a row a thread holds: NV vectors of VEC elements, the group's threads one behind the other, the first one's first vector `shift`
+// elements in front of the row's start, on a 16-byte boundary.
+template <typename In, int VEC, int NV, bool SUB>
+struct Rows {
+  int t, threads, shift, cols;
+  long long row, step, rows, total;                      // this group's first row, rows between its rows
+  __device__ __forceinline__ explicit Rows(const NormParams& p) {
+    threads = SUB ? p.group : blockDim.x;
+    t = SUB ? threadIdx.x & (p.group - 1) : threadIdx.x;
+    const int groups = SUB ? kSubThreads / p.group : 1;
+    row = SUB ? (long long)blockIdx.x * groups + threadIdx.x / p.group : blockIdx.x;
+    step = (long long)gridDim.x * groups;                // (a multiple of VEC unless a group has one row only)
+    rows = p.rows;
+    cols = p.cols;
+    total = p.rows * p.cols;
+    shift = (int)((row * cols) & (VEC - 1));
+  }
+  // the loop over a group's rows goes on as long as any group of the CTA has one: its threads meet in the sums
+  __device__ __forceinline__ bool on(long long r) const {
+    return SUB ? r - threadIdx.x / threads < rows : r < rows;
+  }
+  __device__ __forceinline__ int col(int i, int e) const { return VEC * (t + i * threads) - shift + e; }
+  __device__ __forceinline__ bool in(int i, int e) const { return (unsigned)col(i, e) < (unsigned)cols; }
+  __device__ __forceinline__ bool any(int i) const { return col(i, VEC - 1) >= 0 && col(i, 0) < cols; }
+  __device__ __forceinline__ bool whole(int i) const { return col(i, 0) >= 0 && col(i, VEC - 1) < cols; }
+  __device__ __forceinline__ Raw<In, VEC> load(const void* base, long long r, int i) const {
+    Raw<In, VEC> a = {};
+    if (r < rows && any(i)) {
+      const long long at = r * cols + col(i, 0);         // (>= 0: a whole vector of the tensor, or the one at its end)
+      const In* src = reinterpret_cast<const In*>(base) + at;
+      if (at + VEC <= total) a = *reinterpret_cast<const Raw<In, VEC>*>(src);
+      else {
+        In* e = reinterpret_cast<In*>(&a);
+        for (int k = 0; k < VEC && at + k < total; ++k) e[k] = src[k];
+      }
+    }
+    return a;
+  }
+  __device__ __forceinline__ void unpack(const Raw<In, VEC>& a, int i, float (&f)[VEC]) const {
+    to_floats(a, f);
+    if (VEC > 1 && !whole(i)) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) f[e] = in(i, e) ? f[e] : 0.f;
+    }
+  }
+  __device__ __forceinline__ void store(void* base, long long r, int i, const float (&f)[VEC]) const {
+    if (r >= rows || !any(i)) return;
+    In* dst = reinterpret_cast<In*>(base) + r * cols + col(i, 0);
+    if (whole(i)) {
+      *reinterpret_cast<Raw<In, VEC>*>(dst) = from_floats(f, In());
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (in(i, e)) dst[e] = from_f32<In>(f[e]);
+    }
+  }
+  __device__ __forceinline__ void vector(const float* w, int i, float (&f)[VEC]) const {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) f[e] = in(i, e) ? w[col(i, e)] : 0.f;
+  }
+};
+
+// Sums of N values over the threads that share a row; every thread gets them.  `slot`: this call's shared memory, two used in turn
+// so that one barrier is enough.
+template <int N, bool SUB>
+__device__ __forceinline__ void row_sum(float (&v)[N], int group, float (*slot)[N]) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    if (SUB && o >= group) continue;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  }
+  if constexpr (!SUB) {
+    const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+    if (lane == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) slot[threadIdx.x >> 5][i] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float s = lane < warps ? slot[lane][i] : 0.f;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      v[i] = s;
+    }
+  }
+}
+
+// s = 1 / (1 + e^-z) and 1 - s, both from e^-|z| <= 1, so that neither is a difference of near numbers.
+__device__ __forceinline__ float sigmoid_of(float z, float* rest = nullptr) {
+  const float e = __expf(-fabsf(z)), big = __fdividef(1.f, 1.f + e), small = e * big;
+  if (rest) *rest = z < 0.f ? big : small;
+  return z < 0.f ? small : big;
+}
+
+// A CTA's sums over its rows, from the threads' registers to part[CTA][which][cols]: short rows are added up group by group in shared memory.
+template <typename In, int VEC, int NV, bool SUB>
+__device__ __forceinline__ void put_sums(const Rows<In, VEC, NV, SUB>& at, const float (&acc)[NV][VEC], float* part, float* sum, int group) {
+  if constexpr (!SUB) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (at.in(i, e)) part[at.col(i, e)] = acc[i][e];
+  } else {
+    const int mine = threadIdx.x / group, groups = kSubThreads / group;
+    __syncthreads();
+    for (int c = threadIdx.x; c < at.cols; c += kSubThreads) sum[c] = 0.f;
+    for (int g = 0; g < groups; ++g) {
+      __syncthreads();
+      if (g == mine) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (at.in(0, e)) sum[at.col(0, e)] += acc[0][e];
+      }
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < at.cols; c += kSubThreads) part[c] = sum[c];
+  }
+}
+
+// ---------------------------------------------------------------- kernels (THREADS: kSubThreads for the short rows, else the most a CTA has)
+
+template <typename In, int VEC, int NV, int THREADS>
+__global__ void __launch_bounds__(THREADS) gated_norm_kernel(NormParams p) {
+  constexpr bool SUB = THREADS == kSubThreads;
+  __shared__ float red[2][32][1];
+  const Rows<In, VEC, NV, SUB> at(p);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  float w[NV][VEC];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) at.vector(p.w, i, w[i]);
+  int turn = 0;
+  for (long long row = at.row; at.on(row); row += at.step) {
+    Raw<In, VEC> rx[NV], rz[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) rx[i] = at.load(p.x, row, i);
+    if (p.z) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) rz[i] = at.load(p.z, row, i);
+    }
+    float s[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float x[VEC];
+      at.unpack(rx[i], i, x);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s[0] = fmaf(x[e], x[e], s[0]);
+    }
+    row_sum<1, SUB>(s, p.group, red[turn]);
+    turn ^= 1;
+    const float rs = rsqrtf(s[0] / at.cols + p.eps);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float x[VEC], z[VEC];
+      at.unpack(rx[i], i, x);
+      if (p.z) at.unpack(rz[i], i, z);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        x[e] = x[e] * rs * w[i][e];
+        if (p.z) x[e] *= p.sigmoid ? sigmoid_of(z[e]) : z[e] * sigmoid_of(z[e]);
+      }
+      at.store(p.y, row, i, x);
+    }
+  }
+}
+
+template <typename In, int VEC, int NV, int THREADS>
+__global__ void __launch_bounds__(THREADS) gated_norm_back_kernel(NormParams p) {
+  constexpr bool SUB = THREADS == kSubThreads;
+  __shared__ float red[2][32][2];
+  __shared__ float sum[SUB ? 32 * VEC : 1];
+  const Rows<In, VEC, NV, SUB> at(p);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  float w[NV][VEC], dw[NV][VEC];
+  Raw<In, VEC> rx[NV], rz[NV], rd[NV];
+  auto load = [&](long long row) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      rx[i] = at.load(p.x, row, i);
+      rd[i] = at.load(p.dy, row, i);
+      if (p.z) rz[i] = at.load(p.z, row, i);
+    }
+  };
+  load(at.row);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    at.vector(p.w, i, w[i]);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) dw[i][e] = 0.f;
+  }
+  int turn = 0;
+  for (long long row = at.row; at.on(row); row += at.step) {
+    float x[NV][VEC], d[NV][VEC], a[NV][VEC], slope[NV][VEC];   // a = act(z)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      at.unpack(rx[i], i, x[i]);
+      at.unpack(rd[i], i, d[i]);
+      if (p.z) at.unpack(rz[i], i, a[i]);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        float rest;
+        const float z = p.z ? a[i][e] : 0.f, s = sigmoid_of(z, &rest);
+        a[i][e] = p.z ? (p.sigmoid ? s : z * s) : 1.f;
+        slope[i][e] = p.sigmoid ? s * rest : s * (1.f + z * rest);
+      }
+    }
+    load(row + at.step);
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        s[0] = fmaf(x[i][e], x[i][e], s[0]);
+        s[1] = fmaf(d[i][e] * w[i][e] * a[i][e], x[i][e], s[1]);
+      }
+    row_sum<2, SUB>(s, p.group, red[turn]);
+    turn ^= 1;
+    const float rs = rsqrtf(s[0] / at.cols + p.eps), m = rs * rs * (s[1] / at.cols);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float dx[VEC], dz[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float dn = d[i][e] * x[i][e] * rs;
+        dx[e] = rs * (d[i][e] * w[i][e] * a[i][e] - x[i][e] * m);
+        dz[e] = dn * w[i][e] * slope[i][e];
+        dw[i][e] = fmaf(dn, a[i][e], dw[i][e]);
+      }
+      at.store(p.dx, row, i, dx);
+      if (p.z) at.store(p.dz, row, i, dz);
+    }
+  }
+  put_sums<In, VEC, NV, SUB>(at, dw, p.part + (size_t)blockIdx.x * p.cols, sum, p.group);
+}
+
+template <typename In, int VEC, int NV, int THREADS, bool POST>
+__global__ void __launch_bounds__(THREADS) add_norm_kernel(NormParams p) {
+  constexpr bool SUB = THREADS == kSubThreads;
+  __shared__ float red[2][32][1];
+  const Rows<In, VEC, NV, SUB> at(p);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  float w[NV][VEC], wp[NV][VEC];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    at.vector(p.w, i, w[i]);
+    if (POST) at.vector(p.w_post, i, wp[i]);
+  }
+  int turn = 0;
+  for (long long row = at.row; at.on(row); row += at.step) {
+    Raw<In, VEC> rx[NV], rr[NV];
+    float r[NV][VEC];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      rx[i] = at.load(p.x, row, i);
+      rr[i] = at.load(p.r, row, i);
+    }
+    float s[1] = {0.f}, fs = p.scale;
+    if (POST) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        float x[VEC];
+        at.unpack(rx[i], i, x);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s[0] = fmaf(x[e], x[e], s[0]);
+      }
+      row_sum<1, SUB>(s, p.group, red[turn]);
+      turn ^= 1;
+      fs = p.scale * rsqrtf(s[0] / at.cols + p.eps);
+      s[0] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float x[VEC];
+      at.unpack(rx[i], i, x);
+      at.unpack(rr[i], i, r[i]);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        r[i][e] = fmaf(fs, POST ? x[e] * wp[i][e] : x[e], r[i][e]);
+        s[0] = fmaf(r[i][e], r[i][e], s[0]);
+      }
+      at.store(p.r_out, row, i, r[i]);
+    }
+    row_sum<1, SUB>(s, p.group, red[turn]);
+    turn ^= 1;
+    const float rs = rsqrtf(s[0] / at.cols + p.eps);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) r[i][e] *= rs * w[i][e];
+      at.store(p.y, row, i, r[i]);
+    }
+  }
+}
+
+template <typename In, int VEC, int NV, int THREADS, bool POST>
+__global__ void __launch_bounds__(THREADS) add_norm_back_kernel(NormParams p) {
+  constexpr bool SUB = THREADS == kSubThreads;
+  __shared__ float red[2][32][3];
+  __shared__ float red1[2][32][1];
+  __shared__ float sum[SUB ? 32 * VEC : 1];
+  const Rows<In, VEC, NV, SUB> at(p);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  float w[NV][VEC], wp[NV][VEC], dw[NV][VEC], dwp[NV][VEC];
+  Raw<In, VEC> rx[NV], rr[NV], rd[NV], rg[NV];
+  auto load = [&](long long row) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      rr[i] = at.load(p.r, row, i);
+      rd[i] = at.load(p.dy, row, i);
+      if (POST) rx[i] = at.load(p.x, row, i);
+      if (p.dr_out) rg[i] = at.load(p.dr_out, row, i);
+    }
+  };
+  load(at.row);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    at.vector(p.w, i, w[i]);
+    if (POST) at.vector(p.w_post, i, wp[i]);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) dw[i][e] = dwp[i][e] = 0.f;
+  }
+  int turn = 0;
+  for (long long row = at.row; at.on(row); row += at.step) {
+    float r[NV][VEC], d[NV][VEC], x[NV][VEC], g[NV][VEC];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      at.unpack(rr[i], i, r[i]);
+      at.unpack(rd[i], i, d[i]);
+      if (POST) at.unpack(rx[i], i, x[i]);
+      if (p.dr_out) at.unpack(rg[i], i, g[i]);
+    }
+    load(row + at.step);
+    float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        s[0] = fmaf(r[i][e], r[i][e], s[0]);
+        s[1] = fmaf(d[i][e] * w[i][e], r[i][e], s[1]);
+        if (POST) s[2] = fmaf(x[i][e], x[i][e], s[2]);
+      }
+    row_sum<3, SUB>(s, p.group, red[turn]);
+    const float rs = rsqrtf(s[0] / at.cols + p.eps), m = rs * rs * (s[1] / at.cols);
+    float u[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        dw[i][e] = fmaf(d[i][e] * rs, r[i][e], dw[i][e]);
+        r[i][e] = rs * (d[i][e] * w[i][e] - r[i][e] * m);            // dr
+        if (p.dr_out) r[i][e] += g[i][e];
+        if (POST) u[0] = fmaf(r[i][e] * wp[i][e], x[i][e], u[0]);
+      }
+      at.store(p.dr, row, i, r[i]);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) r[i][e] *= p.scale;              // df
+      if (!POST) at.store(p.dx, row, i, r[i]);
+    }
+    if (POST) {
+      row_sum<1, SUB>(u, p.group, red1[turn]);
+      const float rx_ = rsqrtf(s[2] / at.cols + p.eps), mx = rx_ * rx_ * (p.scale * u[0] / at.cols);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          dwp[i][e] = fmaf(r[i][e] * rx_, x[i][e], dwp[i][e]);
+          r[i][e] = rx_ * (r[i][e] * wp[i][e] - x[i][e] * mx);
+        }
+        at.store(p.dx, row, i, r[i]);
+      }
+    }
+    turn ^= 1;
+  }
+  float* part = p.part + (size_t)blockIdx.x * (POST ? 2 : 1) * p.cols;
+  put_sums<In, VEC, NV, SUB>(at, dw, part, sum, p.group);
+  if (POST) put_sums<In, VEC, NV, SUB>(at, dwp, part + p.cols, sum, p.group);
+}
+
+// Sums of the CTAs' sums: a warp's lanes have 32 neighbouring columns, its eight warps every eighth CTA.  blockIdx.y: which vector.
+__global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const float* part, int ctas, int cols, int both, float* dw, float* dw_post) {
+  __shared__ float s[kReduceThreads / 32][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  float a[4] = {0.f, 0.f, 0.f, 0.f};
+  if (c < cols) {
+    const float* src = part + (size_t)blockIdx.y * cols + c;
+    const size_t stride = (size_t)both * cols;
+    int i = warp;
+    for (; i + 24 < ctas; i += 32)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) a[k] += src[(i + 8 * k) * stride];
+    for (; i < ctas; i += 8) a[0] += src[i * stride];
+  }
+  s[warp][lane] = (a[0] + a[1]) + (a[2] + a[3]);
+  __syncthreads();
+  if (warp == 0 && c < cols) {
+    float t = 0.f;
+#pragma unroll
+    for (int k = 0; k < kReduceThreads / 32; ++k) t += s[k][lane];
+    (blockIdx.y ? dw_post : dw)[c] = t;
+  }
+}
+
+// ---------------------------------------------------------------- host
+
+struct Shape { int vec, nv, group, threads, groups; bool sub; };   // group: lanes of a row (sub), groups: rows of a CTA at once
+
+// `fast`: every tensor 16-byte aligned
+Shape shape_of(int cols, bool bf16, bool fast) {
+  Shape s;
+  s.vec = fast ? (bf16 ? 8 : 4) : 1;
+  const int vectors = cols % s.vec ? (cols + s.vec - 1) / s.vec + 1 : cols / s.vec;   // of the worst start
+  s.sub = vectors <= 32;
+  s.group = 1;
+  s.nv = 1;
+  if (s.sub) {
+    while (s.group < vectors) s.group *= 2;
+    s.threads = kSubThreads;
+    s.groups = kSubThreads / s.group;
+  } else {
+    while (s.nv * 1024 < vectors) s.nv *= 2;
+    s.threads = ((vectors + s.nv - 1) / s.nv + 31) / 32 * 32;
+    s.groups = 1;
+  }
+  return s;
+}
+
+// CTAs: one per `groups` rows up to `most` threads on an SM; rows of a group a multiple of 8 apart where it has several.
+int ctas_of(const Shape& s, long long rows, int most_threads) {
+  const long long need = (rows + s.groups - 1) / s.groups;
+  const long long most = (long long)sm_count() * (most_threads / s.threads > 0 ? most_threads / s.threads : 1);
+  long long n = need < most ? need : most;
+  if (n < need) n = (n + 7) / 8 * 8;
+  return (int)(n > 0 ? n : 1);
+}
+
+// Threads of an SM in the backward kernels, whose CTAs keep sums: more would only lengthen the second kernel.
+constexpr int kBackThreads = 1024, kForwardThreads = 16384;
+
+int back_ctas(int cols, bool bf16, long long rows) {     // (of the workspace: either way of reading)
+  const int a = ctas_of(shape_of(cols, bf16, true), rows, kBackThreads), b = ctas_of(shape_of(cols, bf16, false), rows, kBackThreads);
+  return a > b ? a : b;
+}
+
+template <typename... Args>
+cudaError_t start(void (*kernel)(Args...), dim3 grid, int threads, cudaStream_t stream, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+enum Kind { kGated, kGatedBack, kAdd, kAddBack };
+
+template <typename In, int VEC, int NV, int THREADS>
+cudaError_t pick(Kind kind, const NormParams& p, int ctas, int threads, cudaStream_t stream) {
+  void (*k)(NormParams) = nullptr;
+  switch (kind) {
+    case kGated: k = gated_norm_kernel<In, VEC, NV, THREADS>; break;
+    case kGatedBack: k = gated_norm_back_kernel<In, VEC, NV, THREADS>; break;
+    case kAdd: k = p.w_post ? add_norm_kernel<In, VEC, NV, THREADS, true> : add_norm_kernel<In, VEC, NV, THREADS, false>; break;
+    case kAddBack: k = p.w_post ? add_norm_back_kernel<In, VEC, NV, THREADS, true> : add_norm_back_kernel<In, VEC, NV, THREADS, false>; break;
+  }
+  return start(k, dim3((unsigned)ctas), threads, stream, p);
+}
+
+template <typename In, int VEC>
+cudaError_t by_length(Kind kind, const NormParams& p, const Shape& s, int ctas, cudaStream_t stream) {
+  if (s.sub) return pick<In, VEC, 1, kSubThreads>(kind, p, ctas, s.threads, stream);
+  if (s.nv == 1) return s.threads <= 512 ? pick<In, VEC, 1, 512>(kind, p, ctas, s.threads, stream) : pick<In, VEC, 1, 1024>(kind, p, ctas, s.threads, stream);
+  if (s.nv == 2) return pick<In, VEC, 2, 1024>(kind, p, ctas, s.threads, stream);
+  if (s.nv == 4) return pick<In, VEC, 4, 1024>(kind, p, ctas, s.threads, stream);   // (bf16, 16 bytes at a time: 2049 vectors are the most)
+  if constexpr (VEC <= 4) {
+    if (s.nv == 8) return pick<In, VEC, 8, 1024>(kind, p, ctas, s.threads, stream);   // (fp32: 4097)
+  }
+  if constexpr (VEC == 1) return pick<In, VEC, 16, 1024>(kind, p, ctas, s.threads, stream);
+  return cudaErrorInvalidValue;
+}
+
+cudaError_t run(Kind kind, NormParams& p, int dtype, uintptr_t addresses, float* dw, float* dw_post, cudaStream_t stream) {
+  const bool bf16 = dtype == HA_LA_BF16, fast = !(addresses & 15), back = kind == kGatedBack || kind == kAddBack;
+  const Shape s = shape_of(p.cols, bf16, fast);
+  p.group = s.group;
+  const int ctas = ctas_of(s, p.rows, back ? kBackThreads : kForwardThreads);
+  cudaError_t e = bf16 ? (fast ? by_length<__nv_bfloat16, 8>(kind, p, s, ctas, stream) : by_length<__nv_bfloat16, 1>(kind, p, s, ctas, stream))
+                       : (fast ? by_length<float, 4>(kind, p, s, ctas, stream) : by_length<float, 1>(kind, p, s, ctas, stream));
+  if (e != cudaSuccess || !back) return e;
+  const int both = dw_post ? 2 : 1;
+  return start(norm_reduce_kernel, dim3((unsigned)((p.cols + 31) / 32), (unsigned)both), kReduceThreads, stream,
+               (const float*)p.part, ctas, p.cols, both, dw, dw_post);
+}
+
+int check(int dtype, long long rows, int cols, float eps) {
+  if (dtype != HA_LA_BF16 && dtype != HA_LA_FP32) return HA_LA_ERR_INVALID_ARG;
+  if (rows < 0 || cols < 1 || !(eps >= 0.f)) return HA_LA_ERR_INVALID_ARG;
+  if (cols > kMaxCols || rows > (1LL << 46) / cols) return HA_LA_ERR_UNSUPPORTED;
+  return HA_LA_OK;
+}
+
+// the tensors of `dtype` have to start on one of its elements, fp32 vectors too
+bool misaligned(int dtype, uintptr_t tensors, uintptr_t vectors) { return (tensors & (dtype == HA_LA_BF16 ? 1 : 3)) || (vectors & 3); }
+
+template <typename... P> uintptr_t any_of(P... p) { return (... | (uintptr_t)p); }
+
+int bytes(int dtype, long long rows, int cols, float eps, int both, size_t* out) {
+  if (!out) return HA_LA_ERR_INVALID_ARG;
+  const int rc = check(dtype, rows, cols, eps);
+  if (rc != HA_LA_OK) return rc;
+  *out = align_up((size_t)back_ctas(cols, dtype == HA_LA_BF16, rows) * both * cols * sizeof(float), 256);
+  return HA_LA_OK;
+}
+
+// Gradients of weights without a row
+int no_rows(float* dw, float* dw_post, int cols, cudaStream_t stream) {
+  if (cudaMemsetAsync(dw, 0, sizeof(float) * cols, stream) != cudaSuccess) return HA_LA_ERR_CUDA;
+  if (dw_post && cudaMemsetAsync(dw_post, 0, sizeof(float) * cols, stream) != cudaSuccess) return HA_LA_ERR_CUDA;
+  return HA_LA_OK;
+}
+
+bool workspace_ok(const void* ws, size_t have, size_t need) { return ws && !((uintptr_t)ws & 255) && have >= need; }
+
+}  // namespace
+
+}  // namespace ha_la
+
+using namespace ha_la;
+
+extern "C" {
+
+int ha_la_gated_norm_workspace_bytes(const ha_la_gated_norm_args* a, size_t* out_bytes) {
+  if (!a) return HA_LA_ERR_INVALID_ARG;
+  return bytes(a->dtype, a->rows, a->cols, a->eps, 1, out_bytes);
+}
+
+int ha_la_gated_norm(const ha_la_gated_norm_args* a, void* cuda_stream) {
+  if (!a) return HA_LA_ERR_INVALID_ARG;
+  const int rc = check(a->dtype, a->rows, a->cols, a->eps);
+  if (rc != HA_LA_OK) return rc;
+  if (a->z && a->activation != HA_LA_ACT_SILU && a->activation != HA_LA_ACT_SIGMOID) return HA_LA_ERR_INVALID_ARG;
+  if (a->rows == 0) return HA_LA_OK;
+  if (!a->x || !a->w || !a->y) return HA_LA_ERR_INVALID_ARG;
+  const uintptr_t at = any_of(a->x, a->z, a->y);
+  if (misaligned(a->dtype, at, (uintptr_t)a->w)) return HA_LA_ERR_INVALID_ARG;
+  NormParams p = {};
+  p.x = a->x; p.z = a->z; p.w = a->w; p.y = a->y;
+  p.rows = a->rows; p.cols = a->cols; p.eps = a->eps;
+  p.sigmoid = a->activation == HA_LA_ACT_SIGMOID;
+  return run(kGated, p, a->dtype, at, nullptr, nullptr, reinterpret_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? HA_LA_OK : HA_LA_ERR_CUDA;
+}
+
+int ha_la_gated_norm_backward(const ha_la_gated_norm_args* a, void* cuda_stream) {
+  if (!a) return HA_LA_ERR_INVALID_ARG;
+  size_t need = 0;
+  const int rc = bytes(a->dtype, a->rows, a->cols, a->eps, 1, &need);
+  if (rc != HA_LA_OK) return rc;
+  if (a->z && a->activation != HA_LA_ACT_SILU && a->activation != HA_LA_ACT_SIGMOID) return HA_LA_ERR_INVALID_ARG;
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  if (!a->dw || ((uintptr_t)a->dw & 3)) return HA_LA_ERR_INVALID_ARG;
+  if (a->rows == 0) return no_rows(a->dw, nullptr, a->cols, stream);
+  if (!a->x || !a->w || !a->dy || !a->dx || (a->z && !a->dz)) return HA_LA_ERR_INVALID_ARG;
+  const uintptr_t at = any_of(a->x, a->z, a->dy, a->dx, a->z ? a->dz : nullptr);
+  if (misaligned(a->dtype, at, (uintptr_t)a->w)) return HA_LA_ERR_INVALID_ARG;
+  if (!workspace_ok(a->workspace, a->workspace_bytes, need)) return HA_LA_ERR_WORKSPACE;
+  NormParams p = {};
+  p.x = a->x; p.z = a->z; p.w = a->w; p.dy = a->dy; p.dx = a->dx; p.dz = a->dz;
+  p.part = reinterpret_cast<float*>(a->workspace);
+  p.rows = a->rows; p.cols = a->cols; p.eps = a->eps;
+  p.sigmoid = a->activation == HA_LA_ACT_SIGMOID;
+  return run(kGatedBack, p, a->dtype, at, a->dw, nullptr, stream) == cudaSuccess ? HA_LA_OK : HA_LA_ERR_CUDA;
+}
+
+int ha_la_add_norm_workspace_bytes(const ha_la_add_norm_args* a, size_t* out_bytes) {
+  if (!a) return HA_LA_ERR_INVALID_ARG;
+  return bytes(a->dtype, a->rows, a->cols, a->eps, a->w_post ? 2 : 1, out_bytes);
+}
+
+int ha_la_add_norm(const ha_la_add_norm_args* a, void* cuda_stream) {
+  if (!a) return HA_LA_ERR_INVALID_ARG;
+  const int rc = check(a->dtype, a->rows, a->cols, a->eps);
+  if (rc != HA_LA_OK) return rc;
+  if (!(a->scale == a->scale)) return HA_LA_ERR_INVALID_ARG;
+  if (a->rows == 0) return HA_LA_OK;
+  if (!a->x || !a->r || !a->w || !a->y || !a->r_out) return HA_LA_ERR_INVALID_ARG;
+  const uintptr_t at = any_of(a->x, a->r, a->y, a->r_out);
+  if (misaligned(a->dtype, at, any_of(a->w, a->w_post))) return HA_LA_ERR_INVALID_ARG;
+  NormParams p = {};
+  p.x = a->x; p.r = a->r; p.w = a->w; p.w_post = a->w_post; p.y = a->y; p.r_out = a->r_out;
+  p.rows = a->rows; p.cols = a->cols; p.eps = a->eps; p.scale = a->scale;
+  return run(kAdd, p, a->dtype, at, nullptr, nullptr, reinterpret_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? HA_LA_OK : HA_LA_ERR_CUDA;
+}
+
+int ha_la_add_norm_backward(const ha_la_add_norm_args* a, void* cuda_stream) {
+  if (!a) return HA_LA_ERR_INVALID_ARG;
+  size_t need = 0;
+  const int rc = bytes(a->dtype, a->rows, a->cols, a->eps, a->w_post ? 2 : 1, &need);
+  if (rc != HA_LA_OK) return rc;
+  if (!(a->scale == a->scale)) return HA_LA_ERR_INVALID_ARG;
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  if (!a->dw || (a->w_post && !a->dw_post) || (any_of(a->dw, a->dw_post) & 3)) return HA_LA_ERR_INVALID_ARG;
+  float* dw_post = a->w_post ? a->dw_post : nullptr;
+  if (a->rows == 0) return no_rows(a->dw, dw_post, a->cols, stream);
+  if (!a->r_out || !a->w || !a->dy || !a->dx || !a->dr || (a->w_post && !a->x)) return HA_LA_ERR_INVALID_ARG;
+  const uintptr_t at = any_of(a->w_post ? a->x : nullptr, a->r_out, a->dy, a->dr_out, a->dx, a->dr);
+  if (misaligned(a->dtype, at, any_of(a->w, a->w_post))) return HA_LA_ERR_INVALID_ARG;
+  if (!workspace_ok(a->workspace, a->workspace_bytes, need)) return HA_LA_ERR_WORKSPACE;
+  NormParams p = {};
+  p.x = a->x; p.r = a->r_out; p.w = a->w; p.w_post = a->w_post; p.dy = a->dy; p.dr_out = a->dr_out; p.dx = a->dx; p.dr = a->dr;
+  p.part = reinterpret_cast<float*>(a->workspace);
+  p.rows = a->rows; p.cols = a->cols; p.eps = a->eps; p.scale = a->scale;
+  return run(kAddBack, p, a->dtype, at, a->dw, dw_post, stream) == cudaSuccess ? HA_LA_OK : HA_LA_ERR_CUDA;
+}
+
+}  // extern "C"
