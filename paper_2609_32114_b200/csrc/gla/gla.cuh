@@ -54,6 +54,8 @@ size_t simt_bytes(const Problem& p, bool back, Work* w, void* base);
 cudaError_t launch_simt_forward(const Call& c, cudaStream_t stream);
 cudaError_t launch_simt_backward(const Call& c, cudaStream_t stream);
 cudaError_t launch_combine(const Call& c, bool reverse, cudaStream_t stream);
+// N x HV chains of `count` states each, one behind the other at [n][i][head]: total, s in place, from `first` (or zero)
+cudaError_t launch_chain(const float* total, float* s, const float* first, int count, int N, int HV, int per_state, bool reverse, cudaStream_t stream);
 cudaError_t launch_head_sums(const Call& c, cudaStream_t stream);
 
 template <typename... Args>

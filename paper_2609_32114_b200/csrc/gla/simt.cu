@@ -523,6 +523,12 @@ cudaError_t launch_combine(const Call& c, bool reverse, cudaStream_t stream) {
   return reverse ? start(gla_combine_kernel<true>, grid, kThreads, 0, stream, p) : start(gla_combine_kernel<false>, grid, kThreads, 0, stream, p);
 }
 
+cudaError_t launch_chain(const float* total, float* s, const float* first, int count, int N, int HV, int per_state, bool reverse, cudaStream_t stream) {
+  const CombineParams p{total, s, first, nullptr, nullptr, count, HV, per_state};
+  const dim3 grid((unsigned)((size_t)N * HV * (per_state / (4 * kThreads))));
+  return reverse ? start(gla_combine_kernel<true>, grid, kThreads, 0, stream, p) : start(gla_combine_kernel<false>, grid, kThreads, 0, stream, p);
+}
+
 cudaError_t launch_head_sums(const Call& c, cudaStream_t stream) {
   if (c.p.HV == c.p.HK) return cudaSuccess;
   SumParams p;

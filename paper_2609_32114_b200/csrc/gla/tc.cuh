@@ -1,0 +1,150 @@
+// Tensor-core path of gated linear attention (bf16, d = 128): what its kernels share.
+//
+// Steps of 128 tokens.  Tiles are [2][128 rows][64 columns] bf16, 32 KiB, rows of 128 bytes with the 128-byte swizzle: as TMA brings q, k, v and do
+// (rows = tokens), and as the state kernel writes the images of a state (rows = keys, columns = value channels).  Such a tile
+// is an operand either way round: K-major over its columns, MN-major over its rows.  What threads make (P, the scaled keys) goes to
+// tensor memory as A operand, so no thread writes shared memory that the tensor cores read, but for the rows behind the end of a sequence.
+#pragma once
+
+#include <cuda.h>
+
+#include <type_traits>
+
+#include "gla.cuh"
+#include "../fp32_common.cuh"
+#include "../tc_common.cuh"
+#include "../tc_mma.cuh"
+
+namespace ha_la {
+namespace gla {
+
+using namespace ptx;
+
+constexpr int kComputeWarps = 16;
+constexpr double kLog2e = 1.4426950408889634;
+
+// Cumulative log2-gates of a step's tokens 4 lane .. 4 lane + 3 (one warp), in 64 bits.  Tokens past the end have gate 0.
+__device__ __forceinline__ void scan_gates(const float* g, int HV, int j, Geom c, int lane, double (&G)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int t = 4 * lane + e;
+    G[e] = t < c.L ? gate(g[(size_t)(c.tok0 + t) * HV + j]) * kLog2e : 0.0;
+  }
+  G[1] += G[0];
+  G[2] += G[1];
+  G[3] += G[2];
+  double s = G[3];
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const double y = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += y;
+  }
+  const double before = s - G[3];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) G[e] += before;
+}
+
+// What e^{G_i - G_j} is made of.  Off the diagonal blocks of 16 tokens it factors through the gates at the blocks' edges, all exponents
+// <= 0: er[i] = 2^(G_i - R_I), ec[j] = 2^(R_{J+1} - G_j), bb[I][J] = 2^(R_I - R_{J+1}) (zero where J >= I), R_I = G of block I's first token.
+// Near the diagonal it is taken of the difference, G = hi + lo: sums of closed gates leave a float no bits for what comes behind.
+struct StepGates {
+  float hi[kStep], lo[kStep], er[kStep], ec[kStep];
+  float eg[kStep], el[kStep];                              // e^{G_i}, e^{G_L - G_j}
+  float bb[64];
+  float total;                                             // e^{G_L}
+  float pad[3];
+};
+
+__device__ __forceinline__ void fill_gates(StepGates* s, const double (&G)[4], int lane) {
+  const double R = __shfl_sync(0xffffffffu, G[0], lane & ~3), R1 = __shfl_sync(0xffffffffu, G[0], min((lane & ~3) + 4, 31)),
+               GL = __shfl_sync(0xffffffffu, G[3], 31);
+  float4 hi, lo, er, ec, eg, el;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    (&hi.x)[e] = (float)G[e];
+    (&lo.x)[e] = (float)(G[e] - (double)(&hi.x)[e]);
+    (&er.x)[e] = ex2((float)(G[e] - R));
+    (&ec.x)[e] = ex2(fminf((float)(R1 - G[e]), 0.f));      // (the last block's, which nothing uses, would be of the wrong sign)
+    (&eg.x)[e] = ex2((float)G[e]);
+    (&el.x)[e] = ex2((float)(GL - G[e]));
+  }
+  reinterpret_cast<float4*>(s->hi)[lane] = hi;
+  reinterpret_cast<float4*>(s->lo)[lane] = lo;
+  reinterpret_cast<float4*>(s->er)[lane] = er;
+  reinterpret_cast<float4*>(s->ec)[lane] = ec;
+  reinterpret_cast<float4*>(s->eg)[lane] = eg;
+  reinterpret_cast<float4*>(s->el)[lane] = el;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int I = (2 * lane + e) >> 3, J = (2 * lane + e) & 7;
+    const double rI = __shfl_sync(0xffffffffu, G[0], 4 * I), rJ = __shfl_sync(0xffffffffu, G[0], min(4 * J + 4, 31));
+    s->bb[2 * lane + e] = J < I ? ex2((float)(rI - rJ)) : 0.f;
+  }
+  if (lane == 0) s->total = ex2((float)GL);
+}
+
+// Rows L .. 127 of a tile to zero, by `n` threads: what lies behind a sequence may be NaN, and zero weights would not mask that.
+__device__ __forceinline__ void clear_rows(uint8_t* tile, int L, int tid, int n) {
+  for (int i = tid; i < (kStep - L) * 16; i += n)
+    *reinterpret_cast<uint4*>(tile + (i & 1) * 16384 + (L + (i >> 4)) * 128 + ((i >> 1) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// A tile's descriptors as B operand: over its columns (k index = columns, N = rows) or over its rows (k index = rows, N = columns), and
+// what a step of 16 k adds.
+__device__ __forceinline__ uint64_t desc_cols(uint32_t tile) { return smem_desc(tile, 16, 1024, kSwizzle128B); }
+__device__ __forceinline__ uint64_t desc_rows(uint32_t tile) { return smem_desc(tile, 16384, 1024, kSwizzle128B); }
+__device__ __forceinline__ uint32_t step_cols(int ks) { return (uint32_t)((ks >> 2) * 16384 + (ks & 3) * 32) >> 4; }
+__device__ __forceinline__ uint32_t step_rows(int ks) { return (uint32_t)(ks * 2048) >> 4; }
+constexpr uint32_t kIdCols = idesc_bf16(128, 128, false, false), kIdRows = idesc_bf16(128, 128, false, true);
+
+// D (+)= A B over 128 k, one thread: both tiles over their columns; A over its columns and B over its rows; A in tensor memory.
+__device__ __forceinline__ void mma_cols(uint32_t d, uint32_t a, uint32_t b, bool add) {
+  const uint64_t da = desc_cols(a), db = desc_cols(b);
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks) umma_ss(d, da + step_cols(ks), db + step_cols(ks), kIdCols, add || ks > 0);
+}
+__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, bool add) {
+  const uint64_t da = desc_cols(a), db = desc_rows(b);
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks) umma_ss(d, da + step_cols(ks), db + step_rows(ks), kIdRows, add || ks > 0);
+}
+__device__ __forceinline__ void mma_tmem_rows(uint32_t d, uint32_t a, uint32_t b, bool add) {
+  const uint64_t db = desc_rows(b);
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks) umma_ts(d, a + 8 * ks, db + step_rows(ks), kIdRows, add || ks > 0);
+}
+
+// Sequences as the state kernel walks them
+struct Seqs {
+  const int32_t *tok0, *len, *chunk0, *order;              // the plan kernel's tables, or NULL: equal-length rows
+  int T_row, cps;
+};
+
+struct TcWork {
+  uint8_t* image;                                          // [slot][V-head] states in front of the steps as tiles: bf16, backward two pieces
+  uint8_t* image_back;                                     // ... gradients behind them
+  float *part, *part_back;                                 // [sequence][segment][V-head] fp32 states
+  float *total, *total_back;                               // ... and decays
+};
+
+struct TcCall {
+  const Call* c;
+  CUtensorMap q, k, v, d_o;
+  Seqs seqs;
+  TcWork w;
+  int nseg;
+};
+
+int segments(const Problem& p, bool back);
+size_t tc_bytes(const Problem& p, bool back, TcWork* tw, Work* w, void* base);
+cudaError_t launch_tc_forward(const Call& c, PlanView plan, const TcWork& w, cudaStream_t stream);
+cudaError_t launch_tc_backward(const Call& c, PlanView plan, const TcWork& w, cudaStream_t stream);
+cudaError_t launch_tc_states(const TcCall& t, bool sums, cudaStream_t stream);
+cudaError_t launch_tc_out(const TcCall& t, cudaStream_t stream);
+cudaError_t launch_tc_local_back(const TcCall& t, cudaStream_t stream);
+
+}  // namespace gla
+
+bool make_map_tile(CUtensorMap* m, const void* base, int T, int H);   // tc.cu
+
+}  // namespace ha_la

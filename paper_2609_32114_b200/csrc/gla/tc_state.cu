@@ -1,0 +1,256 @@
+// States of gated linear attention on the tensor cores: the state in front of every step, and in the backward pass the gradient of the
+// state behind every step, as bf16 tiles that the output and gradient kernels take as operands.
+//
+//   forward   h  <- e^{G_L} h  + sum_j (e^{G_L - G_j} k_j) v_j^T        in the order of the steps
+//   reverse   dh <- e^{G_L} dh + sum_i (scale e^{G_i} q_i) do_i^T       against it
+// A CTA walks a run of a (sequence, V-head)'s steps, a whole state in registers (32 values of a key's row to each of 512 threads).  A step is one
+// product, D[key][value channel] = A B: A the scaled keys, transposed to tensor memory (lane = key channel, columns = tokens) as two bf16
+// pieces, 2^-17 of the value left out, so that the sum keeps the accuracy of fp32; B the values' tile as it is.  Nothing of the product waits for
+// the state, so the next step's keys are scaled under this one's product, and the chain through the steps is one multiply-add.
+//
+// What bounds it: the tiles and images through HBM when many CTAs run (96 KiB a step forward, 128 backward), else a CTA's steps, bound by the
+// scaling warps' instructions.  Few (sequence, V-head) pairs are cut into segments: a first launch sums each from zero,
+// gla_combine_kernel (simt.cu) chains the sums, and this launch walks all segments from their true starts.
+#include "tc.cuh"
+
+namespace ha_la {
+namespace gla {
+
+namespace {
+
+constexpr int kStages = 3;
+constexpr uint32_t kStageB = 2 * kTileBytes;
+constexpr int kThreads = 32 * (kComputeWarps + 3);         // compute warps, producer, MMA issue, gates
+constexpr uint32_t OFF_W = kStages * kStageB;              // [2] weights of a step's tokens, and its decay
+constexpr uint32_t kWeightB = (kStep + 4) * 4;
+constexpr uint32_t OFF_BAR = OFF_W + 2 * kWeightB;
+constexpr int kBars = 2 * kStages + 8;
+constexpr uint32_t kSmem = OFF_BAR + kBars * 8 + 16;
+static_assert(kSmem <= 227 * 1024, "shared memory budget");
+constexpr uint32_t TM_A = 0, TM_D = 256;                   // operand: [2] (hi 64 | lo 64 columns); product: [2] 128 columns
+
+struct StateParams {
+  const float* g;
+  Seqs seqs;
+  const float* first[2];                                   // [direction] start states, [sequence][V-head], or NULL
+  float* last[2];
+  uint8_t* image[2];
+  float *part[2], *total[2];
+  int HK, HV, nseg;
+  float scale;
+  int32_t* status;
+};
+
+// PIECES: bf16 tiles that an image has; 0: the segments' sums from zero are all that is wanted
+template <int PIECES>
+__global__ void __launch_bounds__(kThreads, 1)
+gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                    const __grid_constant__ CUtensorMap map_do, StateParams p) {
+  extern __shared__ __align__(1024) uint8_t sm[];
+  uint64_t* bar = reinterpret_cast<uint64_t*>(sm + OFF_BAR);
+  uint64_t* full = bar;                                    // [kStages] tiles of a step
+  uint64_t* empty = bar + kStages;                         // [kStages] its product complete
+  uint64_t* weights = bar + 2 * kStages;                   // [2] of step c in set c % 2
+  uint64_t* used = weights + 2;                            // [2] ... and done with
+  uint64_t* operand = used + 2;                            // [2] scaled keys in tensor memory
+  uint64_t* product = operand + 2;                         // [2]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + kBars);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const bool rev = blockIdx.y;
+  const int seg = blockIdx.x % p.nseg, nj = blockIdx.x / p.nseg, j = nj % p.HV, jq = j / (p.HV / p.HK);
+
+  if (tid == 0) {
+    for (int i = 0; i < kBars; ++i) mbar_init(&bar[i], &bar[i] >= used && &bar[i] < product ? kComputeWarps : 1);
+    *abort_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == 0) tmem_alloc(tmem_slot, 512);
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // this CTA's steps: c = 0 .. count - 1 in the order it walks them
+  int n = nj / p.HV, tok0 = n * p.seqs.T_row, len = p.seqs.T_row, slot0 = n * p.seqs.cps;
+  if (p.seqs.tok0) {
+    n = p.seqs.order[n];                                   // (the longest sequences first)
+    tok0 = p.seqs.tok0[n];
+    len = p.seqs.len[n];
+    slot0 = p.seqs.chunk0[n];
+  }
+  const int steps = (len + kStep - 1) / kStep, per_seg = (steps + p.nseg - 1) / p.nseg;
+  const int s0 = min(seg * per_seg, steps);
+  const bool unused = PIECES == 0 && seg == (rev ? 0 : p.nseg - 1);   // (nothing starts from what the last segment adds)
+  const int count = unused ? 0 : min(per_seg, steps - s0);
+  auto index = [&](int c) { return s0 + (rev ? count - 1 - c : c); };   // step of the sequence
+  auto geom = [&](int c) { return Geom{tok0 + index(c) * kStep, min(kStep, len - index(c) * kStep)}; };
+
+  if (warp == kComputeWarps) {
+    // ------------------------------------------------------------ tiles
+    if (elect_one()) {
+      for (int c = 0; c < count; ++c) {
+        const int st = c % kStages, t0 = geom(c).tok0;
+        if (c >= kStages) mbar_wait(&empty[st], (c / kStages - 1) & 1, abort_flag);
+        if (*abort_flag) break;
+        mbar_expect_tx(&full[st], kStageB);
+        tma_load_4d(sm + st * kStageB, rev ? &map_q : &map_k, &full[st], 0, jq, t0, 0);
+        tma_load_4d(sm + st * kStageB + kTileBytes, rev ? &map_do : &map_v, &full[st], 0, j, t0, 0);
+      }
+    }
+    __syncwarp();
+  } else if (warp == kComputeWarps + 1) {
+    // ------------------------------------------------------------ products
+    if (elect_one()) {
+      for (int c = 0; c < count; ++c) {
+        const int st = c % kStages, b = c & 1;
+        mbar_wait(&full[st], (c / kStages) & 1, abort_flag);
+        mbar_wait(&operand[b], (c >> 1) & 1, abort_flag);
+        tc_fence_after_sync();
+        const uint32_t tile = smem_u32(sm + st * kStageB + kTileBytes);
+        mma_tmem_rows(TM_D + 128 * b, TM_A + 128 * b, tile, false);
+        mma_tmem_rows(TM_D + 128 * b, TM_A + 128 * b + 64, tile, true);
+        umma_commit(&product[b]);
+        umma_commit(&empty[st]);
+      }
+    }
+    __syncwarp();
+  } else if (warp == kComputeWarps + 2) {
+    // ------------------------------------------------------------ gates
+    for (int c = 0; c < count; ++c) {
+      double G[4];
+      scan_gates(p.g, p.HV, j, geom(c), lane, G);
+      if (c > 1) mbar_wait(&used[c & 1], ((c >> 1) - 1) & 1, abort_flag);
+      __syncwarp();
+      float* w = reinterpret_cast<float*>(sm + OFF_W + (c & 1) * kWeightB);
+      const double GL = __shfl_sync(0xffffffffu, G[3], 31);
+      float4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) (&x.x)[e] = rev ? p.scale * ex2((float)G[e]) : ex2((float)(GL - G[e]));
+      reinterpret_cast<float4*>(w)[lane] = x;
+      if (lane == 0) w[kStep] = ex2((float)GL);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&weights[c & 1]);
+      __syncwarp();
+    }
+  } else {
+    // ------------------------------------------------------------ scaling, state
+    const int q = warp & 3, g = warp >> 2;                 // lanes 32 q .. (keys), columns: tokens of the operand or value channels 32 g ..
+    const int key = 32 * q + lane;
+    const uint32_t lanes = static_cast<uint32_t>(32 * q) << 16;
+    float h[32];                                           // [key][32 g ..]
+    const size_t unit = (size_t)n * p.HV + j, part = ((size_t)n * p.nseg + seg) * p.HV + j;
+    const size_t at = (size_t)key * kStep + 32 * g;
+    {
+      const float* src = PIECES == 0 ? nullptr : p.nseg > 1 ? p.part[rev] + part * 16384 : p.first[rev] ? p.first[rev] + unit * 16384 : nullptr;
+#pragma unroll
+      for (int k = 0; k < 32; k += 4) {
+        const float4 x = src ? *reinterpret_cast<const float4*>(src + at + k) : make_float4(0.f, 0.f, 0.f, 0.f);
+        h[k] = x.x; h[k + 1] = x.y; h[k + 2] = x.z; h[k + 3] = x.w;
+      }
+    }
+    float total = 1.f;
+    auto scale_keys = [&](int c) {
+      const int st = c % kStages, b = c & 1, L = geom(c).L;
+      uint8_t* tile = sm + st * kStageB;
+      mbar_wait(&weights[b], (c >> 1) & 1, abort_flag);
+      mbar_wait(&full[st], (c / kStages) & 1, abort_flag);
+      __syncwarp();
+      if (L < kStep) {                                     // (a product's rows past the end: weight 0 is not enough for NaN)
+        clear_rows(tile + kTileBytes, L, tid, 32 * kComputeWarps);
+        fence_proxy_async_smem();
+      }
+      const float* w = reinterpret_cast<const float*>(sm + OFF_W + b * kWeightB) + 32 * g;
+      const uint8_t* src = tile + (key >> 6) * 16384 + 32 * g * 128 + (key & 7) * 2;
+      const int chunk = (key & 63) >> 3;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t hi[8], lo[8];
+#pragma unroll
+        for (int t = 0; t < 16; t += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(w + 16 * half + t);
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 16 * half + t + e;
+            const uint16_t v = *reinterpret_cast<const uint16_t*>(src + r * 128 + ((chunk ^ (r & 7)) << 4));
+            x[e] = 32 * g + r < L ? __uint_as_float((uint32_t)v << 16) * (&f.x)[e] : 0.f;
+          }
+          split_bf16(x[0], x[1], hi[t / 2], lo[t / 2]);
+          split_bf16(x[2], x[3], hi[t / 2 + 1], lo[t / 2 + 1]);
+        }
+        tmem_st8(TM_A + 128 * b + lanes + 16 * g + 8 * half, hi);
+        tmem_st8(TM_A + 128 * b + 64 + lanes + 16 * g + 8 * half, lo);
+      }
+      tmem_st_wait();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&operand[b]);
+    };
+    if (count > 0) scale_keys(0);
+    for (int c = 0; c < count; ++c) {
+      const int b = c & 1;
+      if (c + 1 < count) scale_keys(c + 1);
+      if constexpr (PIECES > 0) {
+        uint8_t* row = p.image[rev] + ((size_t)(slot0 + index(c)) * p.HV + j) * (PIECES * kTileBytes) + (g >> 1) * 16384 + key * 128;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint4 hi, lo;
+          split_bf16(h[8 * k], h[8 * k + 1], hi.x, lo.x);
+          split_bf16(h[8 * k + 2], h[8 * k + 3], hi.y, lo.y);
+          split_bf16(h[8 * k + 4], h[8 * k + 5], hi.z, lo.z);
+          split_bf16(h[8 * k + 6], h[8 * k + 7], hi.w, lo.w);
+          const int off = ((4 * (g & 1) + k) ^ (key & 7)) << 4;
+          *reinterpret_cast<uint4*>(row + off) = hi;
+          if (PIECES == 2) *reinterpret_cast<uint4*>(row + kTileBytes + off) = lo;
+        }
+      }
+      const float decay = reinterpret_cast<const float*>(sm + OFF_W + b * kWeightB)[kStep];
+      mbar_wait(&product[b], (c >> 1) & 1, abort_flag);
+      __syncwarp();
+      tc_fence_after_sync();
+      uint32_t d[32];
+      tmem_ld32(TM_D + 128 * b + lanes + 32 * g, d);
+      tmem_ld_wait();
+#pragma unroll
+      for (int k = 0; k < 32; ++k) h[k] = fmaf(decay, h[k], __uint_as_float(d[k]));
+      total *= decay;
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&used[b]);
+    }
+    float* dst = PIECES == 0 ? p.part[rev] + part * 16384 : seg == (rev ? 0 : p.nseg - 1) && p.last[rev] ? p.last[rev] + unit * 16384 : nullptr;
+    if (dst) {
+#pragma unroll
+      for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(dst + at + k) = make_float4(h[k], h[k + 1], h[k + 2], h[k + 3]);
+    }
+    if (PIECES == 0 && tid == 0) p.total[rev][part] = total;
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  if (tid == 0 && *abort_flag) report_timeout(p.status);
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(*tmem_slot, 512);
+}
+
+}  // namespace
+
+cudaError_t launch_tc_states(const TcCall& t, bool sums, cudaStream_t stream) {
+  const Call& c = *t.c;
+  StateParams p = {};
+  p.g = c.a.g; p.seqs = t.seqs;
+  p.first[0] = c.a.h0; p.first[1] = c.a.dhT;
+  p.last[0] = c.back ? nullptr : c.a.hT; p.last[1] = c.a.dh0;
+  p.image[0] = t.w.image; p.image[1] = t.w.image_back;
+  p.part[0] = t.w.part; p.part[1] = t.w.part_back;
+  p.total[0] = t.w.total; p.total[1] = t.w.total_back;
+  p.HK = c.p.HK; p.HV = c.p.HV; p.nseg = t.nseg; p.scale = c.p.scale; p.status = c.a.status_word;
+  const dim3 grid((unsigned)((size_t)c.p.N * c.p.HV * t.nseg), c.back ? 2 : 1);
+  auto kernel = sums ? gla_tc_state_kernel<0> : c.back ? gla_tc_state_kernel<2> : gla_tc_state_kernel<1>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+  return e != cudaSuccess ? e : start(kernel, grid, kThreads, kSmem, stream, t.q, t.k, t.v, t.d_o, p);
+}
+
+}  // namespace gla
+}  // namespace ha_la
