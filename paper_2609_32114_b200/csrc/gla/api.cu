@@ -5,10 +5,10 @@ using namespace ha_la;
 
 namespace {
 
-bool on_tensor_cores(const Problem& p, bool back) { return p.dtype == HA_LA_BF16 && p.dk == 128 && !back; }
+bool on_tensor_cores(const Problem& p) { return p.dtype == HA_LA_BF16 && p.dk == 128; }
 
 // Shapes only.  Fills `p`.
-int make_problem(const ha_la_gla_args* a, bool back, Problem* p) {
+int make_problem(const ha_la_gla_args* a, Problem* p) {
   if (!a) return HA_LA_ERR_INVALID_ARG;
   if (a->dtype != HA_LA_BF16 && a->dtype != HA_LA_FP32) return HA_LA_ERR_INVALID_ARG;
   if (a->batch < 1 || a->seqlen < 0) return HA_LA_ERR_INVALID_ARG;
@@ -32,7 +32,7 @@ int make_problem(const ha_la_gla_args* a, bool back, Problem* p) {
   p->dv = a->d_v;
   p->scale = a->scale;
   p->varlen = varlen ? 1 : 0;
-  p->step = on_tensor_cores(*p, back) ? 128 : 64;
+  p->step = on_tensor_cores(*p) ? 128 : 64;
   const long long step = p->step;
   long long chunks;
   if (varlen) {
@@ -54,7 +54,7 @@ int make_problem(const ha_la_gla_args* a, bool back, Problem* p) {
 size_t plan_part(const Problem& p) { return p.varlen ? plan_bytes(p) : 0; }
 
 size_t bytes_of(const Problem& p, bool back) {
-  const size_t n = on_tensor_cores(p, back) ? gla::tc_bytes(p, back, nullptr, nullptr, nullptr) : gla::simt_bytes(p, back, nullptr, nullptr);
+  const size_t n = on_tensor_cores(p) ? gla::tc_bytes(p, back, nullptr, nullptr, nullptr) : gla::simt_bytes(p, back, nullptr, nullptr);
   return align_up(plan_part(p) + n, 256);
 }
 
@@ -62,7 +62,7 @@ template <typename... P> uintptr_t any_of(P... p) { return (... | (uintptr_t)p);
 
 int run(const ha_la_gla_args* a, bool back, cudaStream_t stream) {
   gla::Call c = {};
-  const int rc = make_problem(a, back, &c.p);
+  const int rc = make_problem(a, &c.p);
   if (rc != HA_LA_OK) return rc;
   c.a = *a;
   c.back = back;
@@ -84,7 +84,7 @@ int run(const ha_la_gla_args* a, bool back, cudaStream_t stream) {
   c.chunks = {plan.chunk_tok0, plan.chunk_len, plan.seq_chunk0, c.p.T_row, c.p.max_seq_chunks, c.p.step};
   void* scratch = reinterpret_cast<char*>(a->workspace) + plan_part(c.p);
   cudaError_t e;
-  if (on_tensor_cores(c.p, back)) {
+  if (on_tensor_cores(c.p)) {
     gla::TcWork w = {};
     gla::tc_bytes(c.p, back, &w, &c.w, scratch);
     e = back ? gla::launch_tc_backward(c, plan, w, stream) : gla::launch_tc_forward(c, plan, w, stream);
@@ -102,7 +102,7 @@ extern "C" {
 int ha_la_gla_workspace_bytes(const ha_la_gla_args* args, int backward, size_t* out_bytes) {
   if (!out_bytes) return HA_LA_ERR_INVALID_ARG;
   Problem p;
-  const int rc = make_problem(args, backward != 0, &p);
+  const int rc = make_problem(args, &p);
   if (rc != HA_LA_OK) return rc;
   *out_bytes = bytes_of(p, backward != 0);
   return HA_LA_OK;
@@ -110,8 +110,8 @@ int ha_la_gla_workspace_bytes(const ha_la_gla_args* args, int backward, size_t* 
 
 const char* ha_la_gla_path(const ha_la_gla_args* args) {
   Problem p;
-  if (make_problem(args, false, &p) != HA_LA_OK) return nullptr;
-  return on_tensor_cores(p, false) ? "tc" : "simt";
+  if (make_problem(args, &p) != HA_LA_OK) return nullptr;
+  return on_tensor_cores(p) ? "tc" : "simt";
 }
 
 int ha_la_gla_prefill(const ha_la_gla_args* a, void* cuda_stream) { return run(a, false, reinterpret_cast<cudaStream_t>(cuda_stream)); }

@@ -36,6 +36,7 @@ size_t tc_bytes(const Problem& p, bool back, TcWork* tw, Work* w, void* base) {
     take(tw ? &tw->image_back : nullptr, units * kTileBytes * 2);
     take(tw ? &tw->part_back : nullptr, parts * 65536);
     take(tw ? &tw->total_back : nullptr, parts * 4);
+    take(tw ? &tw->sums : nullptr, local_back_bytes());
     take(w ? &w->dq : nullptr, shared);
     take(w ? &w->dk : nullptr, shared);
   }
@@ -81,7 +82,7 @@ cudaError_t launch_tc_backward(const Call& c, PlanView plan, const TcWork& w, cu
   TcCall t;
   cudaError_t e = make(&t, c, plan, w);
   if (e == cudaSuccess) e = states(t, stream);
-  if (e == cudaSuccess) e = cudaErrorNotSupported;
+  if (e == cudaSuccess) e = launch_tc_local_back(t, stream);
   return e == cudaSuccess ? launch_head_sums(c, stream) : e;
 }
 

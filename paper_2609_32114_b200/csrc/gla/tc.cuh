@@ -125,6 +125,7 @@ struct TcWork {
   uint8_t* image_back;                                     // ... gradients behind them
   float *part, *part_back;                                 // [sequence][segment][V-head] fp32 states
   float *total, *total_back;                               // ... and decays
+  float* sums;                                             // backward: what the gradient kernel's CTAs pass on
 };
 
 struct TcCall {
@@ -141,6 +142,7 @@ cudaError_t launch_tc_forward(const Call& c, PlanView plan, const TcWork& w, cud
 cudaError_t launch_tc_backward(const Call& c, PlanView plan, const TcWork& w, cudaStream_t stream);
 cudaError_t launch_tc_states(const TcCall& t, bool sums, cudaStream_t stream);
 cudaError_t launch_tc_out(const TcCall& t, cudaStream_t stream);
+size_t local_back_bytes();
 cudaError_t launch_tc_local_back(const TcCall& t, cudaStream_t stream);
 
 }  // namespace gla

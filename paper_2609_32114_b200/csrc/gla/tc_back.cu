@@ -1,0 +1,528 @@
+// Gradients of gated linear attention on the tensor cores, step by step and independent of one another once the states in front of the steps and the
+// gradients behind them are there (gla.cuh has the formulas).
+//
+// A persistent CTA per SM takes (step, V-head) units: sixteen products of 128^3 a unit,
+//   S = Q K^T   dP = dO V^T   and both transposed, as the operands dS (rows i), dS^T and P^T (rows j) are wanted by lanes of tensor memory;
+//   dq: dS K, dO h^T    dk: dS^T Q, V dh^T    dv: P^T dO, K dh
+// The parts by the states are products of their own, for their rows are scaled by e^{G_i} (e^{G_L - G_j}) behind them, and because x_i and y_j, what
+// dg is a sum of, come of them alone: with h and dh as two bf16 pieces they keep the accuracy of fp32.  E = S dS is taken of the fp32
+// accumulators.  P and dS are rounded to bf16 for the products that give dq, dk and dv, which are rounded to bf16 anyway.
+//
+// Shared memory has seven slots for the eight tiles of a unit (Q, K, dO, V, two pieces of h and of dh; the last goes where dO was), assigned anew each unit so
+// that what the next unit needs first goes where this one is done first.  Tensor memory: four regions of 128 columns,
+//   R0: S | dP^T | dq by h | dv by dh      R1: dP | dq by dS | dk by dS      R2: S^T | dv by P      R3: operands dS, then dS^T and P^T | dk by dh
+// One more warp scans the next unit's gates and adds up dg of the last one; the sums over a row's columns, which four warps share, pass through a
+// few KiB of workspace that stay in L2.
+// What bounds it: 352 KiB of tiles, images and gradients a unit, and a unit's dependent phases (measured below, tc_back in the figures of the call).
+#include "tc.cuh"
+
+namespace ha_la {
+namespace gla {
+
+namespace {
+
+constexpr int kSlots = 7;
+constexpr int kThreads = 32 * (kComputeWarps + 3);
+struct BackGates { float hi[kStep], lo[kStep], er[kStep], ec[kStep], bb[64], ghi, glo; float pad[2]; };   // (as StepGates; G_L = ghi + glo)
+constexpr uint32_t OFF_G = kSlots * kTileBytes;
+constexpr uint32_t OFF_BAR = OFF_G + sizeof(BackGates);
+constexpr int kBars = 2 * kSlots + 16;
+constexpr uint32_t kSmem = OFF_BAR + kBars * 8 + 16;
+static_assert(kSmem <= 227 * 1024 && sizeof(BackGates) % 16 == 0, "shared memory budget");
+constexpr uint32_t R0 = 0, R1 = 128, R2 = 256, R3 = 384;
+enum { kQ, kK, kDO, kV, kHH, kHL, kDH, kDL };              // tiles in the order they are loaded; kDL lies where kDO was
+
+struct BackParams {
+  const float* g;
+  Chunks chunks;
+  const uint8_t *image, *image_back;
+  void *dq, *dk, *dv;
+  float *dg, *part_q, *part_k;                             // part_q, part_k: fp32 parts of heads that several V-heads share, or NULL
+  float* sums;                                             // [CTA][2][kSums]
+  int HK, HV;
+  float scale;
+  long long units;
+  int32_t* status;
+};
+
+// The slots' roles in this unit, and the parity of their next fill
+struct Slots {
+  int s[kSlots] = {0, 1, 2, 3, 4, 5, 6};
+  uint32_t parity = 0;
+  __device__ __forceinline__ int at(int tile) const { return s[tile == kDL ? kDO : tile]; }
+  __device__ __forceinline__ uint32_t fill(int tile) const { return (parity >> at(tile) & 1) ^ (tile == kDL ? 1 : 0); }
+  __device__ __forceinline__ void next() {
+    parity ^= 0x7f ^ (1u << s[kDO]);
+    const int k = s[kK], o = s[kDO], v = s[kV], hh = s[kHH], hl = s[kHL], dh = s[kDH];
+    s[kK] = hh; s[kDO] = hl; s[kV] = dh; s[kHH] = v; s[kHL] = o; s[kDH] = k;
+  }
+};
+
+__global__ void __launch_bounds__(kThreads, 1)
+gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                   const __grid_constant__ CUtensorMap map_do, BackParams p) {
+  extern __shared__ __align__(1024) uint8_t sm[];
+  BackGates* s = reinterpret_cast<BackGates*>(sm + OFF_G);
+  uint64_t* bar = reinterpret_cast<uint64_t*>(sm + OFF_BAR);
+  uint64_t *full = bar, *empty = bar + kSlots;             // [kSlots]
+  uint64_t* one = bar + 2 * kSlots;                        // by one thread or by the tensor cores:
+  uint64_t *gates = one, *b_s = one + 1, *b_dpt = one + 2, *b_dq1 = one + 3, *b_dq2 = one + 4, *b_dv = one + 5, *b_dk = one + 6;
+  uint64_t* all = one + 7;                                 // by the compute warps:
+  uint64_t *g_free = all, *clean = all + 1, *e1 = all + 2, *e2 = all + 3, *e_q = all + 4, *e_v = all + 5, *e_d = all + 6, *e_k = all + 7;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + kBars);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < kBars; ++i) mbar_init(&bar[i], &bar[i] >= all ? kComputeWarps : 1);
+    *abort_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == 0) tmem_alloc(tmem_slot, 512);
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  struct Unit { Geom c; int j; size_t sj; };
+  auto unit = [&](int u) {
+    const long long i = blockIdx.x + (long long)u * gridDim.x;
+    Unit x{{0, 0}, 0, 0};
+    if (i >= p.units) return x;
+    const int slot = (int)((unsigned)i / (unsigned)p.HV);
+    x.j = (int)i - slot * p.HV;
+    x.sj = (size_t)i;
+    x.c = geom_of(p.chunks, slot);
+    return x;
+  };
+  const int R = p.HV / p.HK;
+  constexpr int kSums = 2 * 4 * kStep + kComputeWarps;     // [4][128] x + R - C, [4][128] y, [16] parts of <h, dh>
+  float* sums = p.sums + (size_t)blockIdx.x * 2 * kSums;
+  Slots sl;
+
+  if (warp == kComputeWarps) {
+    // ------------------------------------------------------------ tiles
+    if (elect_one()) {
+      Unit x = unit(0);
+      while (x.c.L > 0 && !*abort_flag) {
+        const Unit after = unit((int)((x.sj - blockIdx.x) / gridDim.x) + 1);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          const int at = sl.at(t);
+          mbar_wait(&empty[at], sl.fill(t) ^ 1, abort_flag);
+          if (*abort_flag) break;
+          uint8_t* dst = sm + at * kTileBytes;
+          mbar_expect_tx(&full[at], kTileBytes);
+          if (t == kQ) tma_load_4d(dst, &map_q, &full[at], 0, x.j / R, x.c.tok0, 0);
+          else if (t == kK) tma_load_4d(dst, &map_k, &full[at], 0, x.j / R, x.c.tok0, 0);
+          else if (t == kDO) tma_load_4d(dst, &map_do, &full[at], 0, x.j, x.c.tok0, 0);
+          else if (t == kV) tma_load_4d(dst, &map_v, &full[at], 0, x.j, x.c.tok0, 0);
+          else bulk_load(dst, (t < kDH ? p.image : p.image_back) + (2 * x.sj + (t == kHL || t == kDL)) * kTileBytes, kTileBytes, &full[at]);
+        }
+        sl.next();
+        x = after;
+      }
+    }
+    __syncwarp();
+  } else if (warp == kComputeWarps + 1) {
+    // ------------------------------------------------------------ products
+    if (elect_one()) {
+      Unit x = unit(0);
+      uint32_t tails = 0;
+      int last_k = 0;
+      for (int u = 0; x.c.L > 0; ++u) {
+        const Unit after = unit(u + 1);
+        const uint32_t ph = u & 1;
+        auto tile = [&](int t) { return smem_u32(sm + sl.at(t) * kTileBytes); };
+        auto wait = [&](uint64_t* b, uint32_t parity) {
+          mbar_wait(b, parity, abort_flag);
+          tc_fence_after_sync();
+        };
+        auto loaded = [&](int t) { wait(&full[sl.at(t)], sl.fill(t)); };
+        loaded(kQ);
+        loaded(kK);
+        if (x.c.L < kStep) wait(clean, tails++ & 1);
+        if (u > 0) wait(e_v, ph ^ 1);
+        mma_cols(R0, tile(kQ), tile(kK), false);           // S
+        mma_cols(R2, tile(kK), tile(kQ), false);           // S^T
+        if (u > 0) {
+          wait(e_k, ph ^ 1);
+          mbar_arrive(&empty[last_k]);                     // (its products are complete)
+        }
+        loaded(kDO);
+        loaded(kV);
+        mma_cols(R1, tile(kDO), tile(kV), false);          // dP
+        umma_commit(b_s);
+        wait(e1, ph);
+        mma_cols(R0, tile(kV), tile(kDO), false);          // dP^T
+        umma_commit(b_dpt);
+        mma_tmem_rows(R1, R3, tile(kK), false);            // dS K
+        umma_commit(b_dq1);
+        wait(e2, ph);
+        mma_tmem_rows(R2, R3 + 64, tile(kDO), false);      // P^T dO
+        loaded(kHH);
+        mma_cols(R0, tile(kDO), tile(kHH), false);         // dO h^T
+        loaded(kHL);
+        mma_cols(R0, tile(kDO), tile(kHL), true);
+        umma_commit(b_dq2);
+        umma_commit(&empty[sl.at(kDO)]);
+        wait(e_q, ph);
+        loaded(kDH);
+        mma_rows(R0, tile(kK), tile(kDH), false);          // K dh
+        umma_commit(b_dv);
+        mma_tmem_rows(R1, R3, tile(kQ), false);            // dS^T Q
+        umma_commit(&empty[sl.at(kQ)]);
+        mma_cols(R3, tile(kV), tile(kDH), false);          // V dh^T
+        loaded(kDL);
+        mma_cols(R3, tile(kV), tile(kDL), true);
+        umma_commit(b_dk);
+        umma_commit(&empty[sl.at(kV)]);
+        wait(e_d, ph);
+        mbar_arrive(&empty[sl.at(kHH)]);
+        mbar_arrive(&empty[sl.at(kHL)]);
+        umma_commit(&empty[sl.at(kDH)]);
+        umma_commit(&empty[sl.at(kDL)]);
+        last_k = sl.at(kK);
+        sl.next();
+        x = after;
+      }
+    }
+    __syncwarp();
+  } else if (warp == kComputeWarps + 2) {
+    // ------------------------------------------------------------ gates; dg of the unit before
+    Unit x = unit(0), before{{0, 0}, 0, 0};
+    float total = 0.f;
+    for (int u = 0; x.c.L > 0 || before.c.L > 0; ++u) {
+      const Unit after = x.c.L > 0 ? unit(u + 1) : x;
+      float next_total = 0.f;
+      if (x.c.L > 0) {
+        double G[4];
+        scan_gates(p.g, p.HV, x.j, x.c, lane, G);
+        const double Rb = __shfl_sync(0xffffffffu, G[0], lane & ~3), R1b = __shfl_sync(0xffffffffu, G[0], min((lane & ~3) + 4, 31)),
+                     GL = __shfl_sync(0xffffffffu, G[3], 31);
+        float4 hi, lo, er, ec;
+        float bb[2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          (&hi.x)[e] = (float)G[e];
+          (&lo.x)[e] = (float)(G[e] - (double)(&hi.x)[e]);
+          (&er.x)[e] = ex2((float)(G[e] - Rb));
+          (&ec.x)[e] = ex2(fminf((float)(R1b - G[e]), 0.f));
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int I = (2 * lane + e) >> 3, J = (2 * lane + e) & 7;
+          const double rI = __shfl_sync(0xffffffffu, G[0], 4 * I), rJ = __shfl_sync(0xffffffffu, G[0], min(4 * J + 4, 31));
+          bb[e] = J < I ? ex2((float)(rI - rJ)) : 0.f;
+        }
+        next_total = ex2((float)GL);
+        if (u > 0) mbar_wait(g_free, (u - 1) & 1, abort_flag);
+        __syncwarp();
+        reinterpret_cast<float4*>(s->hi)[lane] = hi;
+        reinterpret_cast<float4*>(s->lo)[lane] = lo;
+        reinterpret_cast<float4*>(s->er)[lane] = er;
+        reinterpret_cast<float4*>(s->ec)[lane] = ec;
+        reinterpret_cast<float2*>(s->bb)[lane] = make_float2(bb[0], bb[1]);
+        if (lane == 0) {
+          s->ghi = (float)GL;
+          s->glo = (float)(GL - (double)(float)GL);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(gates);
+        __syncwarp();
+      }
+      if (before.c.L > 0) {
+        mbar_wait(e_k, (u - 1) & 1, abort_flag);           // (the last of the unit's sums are written ahead of it)
+        __syncwarp();
+        const float* f = sums + ((u - 1) & 1) * kSums;
+        double z[4] = {0.0, 0.0, 0.0, 0.0}, y[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 a = __ldcg(reinterpret_cast<const float4*>(f + g * kStep) + lane), b = __ldcg(reinterpret_cast<const float4*>(f + 4 * kStep + g * kStep) + lane);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { z[e] += (&a.x)[e]; y[e] += (&b.x)[e]; }
+        }
+        double dot = lane < kComputeWarps ? (double)__ldcg(f + 8 * kStep + lane) : 0.0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+        dot *= total;
+        z[2] += z[3]; z[1] += z[2]; z[0] += z[1];          // z: over this and later tokens, y: over earlier ones
+        const double y3 = y[3], y012 = y[0] + y[1] + y[2];
+        double zs = z[0], ys = y012 + y3;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const double a = __shfl_down_sync(0xffffffffu, zs, o), b = __shfl_up_sync(0xffffffffu, ys, o);
+          if (lane + o < 32) zs += a;
+          if (lane >= o) ys += b;
+        }
+        const double behind = zs - z[0], front = ys - (y012 + y3);
+        const double yy[4] = {front, front + y[0], front + y[0] + y[1], front + y012};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (4 * lane + e < before.c.L)
+            p.dg[(size_t)(before.c.tok0 + 4 * lane + e) * p.HV + before.j] = (float)(z[e] + behind + yy[e] + dot);
+      }
+      total = next_total;
+      before = x;
+      x = after;
+    }
+  } else {
+    // ------------------------------------------------------------ operands, gradients
+    const int q = warp & 3, g = warp >> 2, i = 32 * q + lane;     // row (token, key), columns 32 g ..
+    const uint32_t lanes = static_cast<uint32_t>(32 * q) << 16;
+    auto arrive = [&](uint64_t* b) {
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(b);
+    };
+    auto wait = [&](uint64_t* b, uint32_t parity) {
+      mbar_wait(b, parity, abort_flag);
+      __syncwarp();
+      tc_fence_after_sync();
+    };
+    auto seen = [&](int t) {                               // (loaded long ago; this thread's own look at it)
+      if (!mbar_test_wait(&full[sl.at(t)], sl.fill(t))) mbar_wait(&full[sl.at(t)], sl.fill(t), abort_flag);
+      __syncwarp();
+    };
+    // 16-byte piece k of this thread's 32 columns in its row of a tile
+    auto piece = [&](int at, int k) {
+      return *reinterpret_cast<const uint4*>(sm + at * kTileBytes + (g >> 1) * 16384 + i * 128 + (((4 * (g & 1) + k) ^ (i & 7)) << 4));
+    };
+    // out = a f + b, 32 columns of a row; dot: of a f with the tile's row
+    auto gradient = [&](uint32_t first, uint32_t second, float f, int dot_with, float* dot, uint64_t* read, __nv_bfloat16* out, float* part, bool valid) {
+      uint32_t a[32], b[32];
+      tmem_ld32(first + lanes + 32 * g, a);
+      tmem_ld32(second + lanes + 32 * g, b);
+      uint4 r[4];
+      if (dot_with >= 0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) r[k] = piece(dot_with, k);
+      }
+      tmem_ld_wait();
+      arrive(read);
+      float d = 0.f;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) {
+        const float v = f * __uint_as_float(a[k]);
+        if (dot_with >= 0) {
+          const uint32_t w = (&r[k >> 3].x)[(k >> 1) & 3];
+          d = fmaf(v, __uint_as_float(k & 1 ? w & 0xffff0000u : w << 16), d);
+        }
+        a[k] = __float_as_uint(v + __uint_as_float(b[k]));
+      }
+      if (dot_with >= 0) *dot = d;
+      if (!valid) return;
+      if (part) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) reinterpret_cast<uint4*>(part)[k] = make_uint4(a[4 * k], a[4 * k + 1], a[4 * k + 2], a[4 * k + 3]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          reinterpret_cast<uint4*>(out)[k] =
+              make_uint4(pack_bf16(as_f2(a[8 * k], a[8 * k + 1])), pack_bf16(as_f2(a[8 * k + 2], a[8 * k + 3])),
+                         pack_bf16(as_f2(a[8 * k + 4], a[8 * k + 5])), pack_bf16(as_f2(a[8 * k + 6], a[8 * k + 7])));
+      }
+    };
+    Unit x = unit(0);
+    for (int u = 0; x.c.L > 0; ++u) {
+      const Unit after = unit(u + 1);
+      const uint32_t ph = u & 1;
+      mbar_wait(gates, ph, abort_flag);
+      if (x.c.L < kStep) {                                 // (rows behind the sequence may be NaN)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          mbar_wait(&full[sl.at(t)], sl.fill(t), abort_flag);
+          clear_rows(sm + sl.at(t) * kTileBytes, x.c.L, tid, 32 * kComputeWarps);
+        }
+        fence_proxy_async_smem();
+        arrive(clean);
+      }
+      const float hi = s->hi[i], lo = s->lo[i];
+      const float eg = p.scale * ex2(hi + lo), el = ex2((s->ghi - hi) + (s->glo - lo));
+      float z = 0.f;                                       // x_i + R_i - C_i of these columns
+
+      // ---- dS (row i, columns j) as operand; R_i
+      wait(b_s, ph);
+      {
+        uint32_t w[16];
+        if (g <= q) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            uint32_t rs[16], rp[16];
+            tmem_ld16(R0 + lanes + 32 * g + 16 * b, rs);
+            tmem_ld16(R1 + lanes + 32 * g + 16 * b, rp);
+            float dec[16];
+            if (g < q) {
+              const float f = p.scale * s->er[i] * s->bb[8 * (i >> 4) + 2 * g + b];
+#pragma unroll
+              for (int k = 0; k < 16; k += 4) {
+                const float4 e = *reinterpret_cast<const float4*>(&s->ec[32 * g + 16 * b + k]);
+                dec[k] = f * e.x; dec[k + 1] = f * e.y; dec[k + 2] = f * e.z; dec[k + 3] = f * e.w;
+              }
+            } else {
+#pragma unroll
+              for (int k = 0; k < 16; ++k)
+                dec[k] = 16 * b + k <= lane ? p.scale * ex2((hi - s->hi[32 * g + 16 * b + k]) + (lo - s->lo[32 * g + 16 * b + k])) : 0.f;
+            }
+            tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              dec[k] *= __uint_as_float(rp[k]);
+              if (g < q || 16 * b + k < lane) z = fmaf(dec[k], __uint_as_float(rs[k]), z);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[8 * b + k] = pack_bf16(dec[2 * k], dec[2 * k + 1]);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) w[k] = 0u;
+        }
+        tmem_st16(R3 + lanes + 16 * g, w);
+        tmem_st_wait();
+        arrive(e1);
+      }
+      // ---- P^T and dS^T (row j, columns i) as operands; C_j
+      wait(b_dpt, ph);
+      {
+        uint32_t wp[16], ws[16];
+        if (g >= q) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            uint32_t rs[16], rp[16];
+            tmem_ld16(R2 + lanes + 32 * g + 16 * b, rs);
+            tmem_ld16(R0 + lanes + 32 * g + 16 * b, rp);
+            float dec[16];
+            if (g > q) {
+              const float f = p.scale * s->ec[i] * s->bb[8 * (2 * g + b) + (i >> 4)];
+#pragma unroll
+              for (int k = 0; k < 16; k += 4) {
+                const float4 e = *reinterpret_cast<const float4*>(&s->er[32 * g + 16 * b + k]);
+                dec[k] = f * e.x; dec[k + 1] = f * e.y; dec[k + 2] = f * e.z; dec[k + 3] = f * e.w;
+              }
+            } else {
+#pragma unroll
+              for (int k = 0; k < 16; ++k)
+                dec[k] = 16 * b + k >= lane ? p.scale * ex2((s->hi[32 * g + 16 * b + k] - hi) + (s->lo[32 * g + 16 * b + k] - lo)) : 0.f;
+            }
+            tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < 16; k += 2) {
+              float ds[2];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                ds[e] = dec[k + e] * __uint_as_float(rp[k + e]);
+                if (g > q || 16 * b + k + e > lane) z = fmaf(-ds[e], __uint_as_float(rs[k + e]), z);
+              }
+              wp[8 * b + k / 2] = pack_bf16(dec[k] * __uint_as_float(rs[k]), dec[k + 1] * __uint_as_float(rs[k + 1]));
+              ws[8 * b + k / 2] = pack_bf16(ds[0], ds[1]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) wp[k] = ws[k] = 0u;
+        }
+        wait(b_dq1, ph);                                   // (dS has been read where dS^T goes)
+        tmem_st16(R3 + lanes + 16 * g, ws);
+        tmem_st16(R3 + 64 + lanes + 16 * g, wp);
+        tmem_st_wait();
+        arrive(e2);
+        if (lane == 0) mbar_arrive(g_free);
+      }
+      const bool valid = i < x.c.L;
+      const size_t row = (size_t)(x.c.tok0 + i), at_v = (row * p.HV + x.j) * 128 + 32 * g, at_k = (row * p.HK + x.j / R) * 128 + 32 * g;
+      float* mine = sums + ph * kSums;
+      // ---- dq
+      float d = 0.f;
+      wait(b_dq2, ph);
+      seen(kQ);
+      gradient(R0, R1, eg, sl.at(kQ), &d, e_q, reinterpret_cast<__nv_bfloat16*>(p.dq) + at_k, p.part_q ? p.part_q + at_v : nullptr, valid);
+      __stcg(mine + g * kStep + i, z + d);
+      // ---- dv
+      wait(b_dv, ph);
+      gradient(R0, R2, el, -1, nullptr, e_v, reinterpret_cast<__nv_bfloat16*>(p.dv) + at_v, nullptr, valid);
+      // ---- <h, dh>
+      d = 0.f;
+#pragma unroll
+      for (int t = kHH; t <= kDL; ++t) seen(t);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint4 a = piece(sl.at(kHH), k), b = piece(sl.at(kHL), k), c = piece(sl.at(kDH), k), e = piece(sl.at(kDL), k);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float2 a2 = unpack_bf16((&a.x)[w]), b2 = unpack_bf16((&b.x)[w]), c2 = unpack_bf16((&c.x)[w]), e2_ = unpack_bf16((&e.x)[w]);
+          d = fmaf(a2.x + b2.x, c2.x + e2_.x, d);
+          d = fmaf(a2.y + b2.y, c2.y + e2_.y, d);
+        }
+      }
+      arrive(e_d);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+      if (lane == 0) __stcg(mine + 8 * kStep + warp, d);
+      // ---- dk
+      wait(b_dk, ph);
+      seen(kK);
+      {
+        uint32_t a[32], b[32];
+        tmem_ld32(R3 + lanes + 32 * g, a);
+        tmem_ld32(R1 + lanes + 32 * g, b);
+        uint4 r[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) r[k] = piece(sl.at(kK), k);
+        tmem_ld_wait();
+        d = 0.f;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          const float v = el * __uint_as_float(a[k]);
+          const uint32_t w = (&r[k >> 3].x)[(k >> 1) & 3];
+          d = fmaf(v, __uint_as_float(k & 1 ? w & 0xffff0000u : w << 16), d);
+          a[k] = __float_as_uint(v + __uint_as_float(b[k]));
+        }
+        __stcg(mine + 4 * kStep + g * kStep + i, d);
+        arrive(e_k);                                       // (with the unit's sums ahead of it)
+        if (valid) {
+          if (p.part_k) {
+            uint4* out = reinterpret_cast<uint4*>(p.part_k + at_v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) out[k] = make_uint4(a[4 * k], a[4 * k + 1], a[4 * k + 2], a[4 * k + 3]);
+          } else {
+            uint4* out = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.dk) + at_k);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              out[k] = make_uint4(pack_bf16(as_f2(a[8 * k], a[8 * k + 1])), pack_bf16(as_f2(a[8 * k + 2], a[8 * k + 3])),
+                                  pack_bf16(as_f2(a[8 * k + 4], a[8 * k + 5])), pack_bf16(as_f2(a[8 * k + 6], a[8 * k + 7])));
+          }
+        }
+      }
+      sl.next();
+      x = after;
+    }
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  if (tid == 0 && *abort_flag) report_timeout(p.status);
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(*tmem_slot, 512);
+}
+
+}  // namespace
+
+size_t local_back_bytes() { return (size_t)sm_count() * 2 * (2 * 4 * kStep + kComputeWarps) * 4; }
+
+cudaError_t launch_tc_local_back(const TcCall& t, cudaStream_t stream) {
+  const Call& c = *t.c;
+  BackParams p;
+  p.g = c.a.g; p.chunks = c.chunks; p.image = t.w.image; p.image_back = t.w.image_back;
+  p.dq = c.a.dq; p.dk = c.a.dk; p.dv = c.a.dv; p.dg = c.a.dg;
+  p.part_q = c.p.HV != c.p.HK ? c.w.dq : nullptr;
+  p.part_k = c.p.HV != c.p.HK ? c.w.dk : nullptr;
+  p.sums = t.w.sums;
+  p.HK = c.p.HK; p.HV = c.p.HV; p.scale = c.p.scale; p.status = c.a.status_word;
+  p.units = (long long)c.p.max_chunks * c.p.HV;
+  if (p.units == 0) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(gla_tc_back_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+  const unsigned grid = (unsigned)(p.units < sm_count() ? p.units : sm_count());
+  return e != cudaSuccess ? e : start(gla_tc_back_kernel, dim3(grid), kThreads, kSmem, stream, t.q, t.k, t.v, t.d_o, p);
+}
+
+}  // namespace gla
+}  // namespace ha_la

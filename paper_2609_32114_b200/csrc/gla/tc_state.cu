@@ -1,11 +1,12 @@
 // States of gated linear attention on the tensor cores: the state in front of every step, and in the backward pass the gradient of the
 // state behind every step, as bf16 tiles that the output and gradient kernels take as operands.
 //
-//   forward   h  <- e^{G_L} h  + sum_j (e^{G_L - G_j} k_j) v_j^T        in the order of the steps
-//   reverse   dh <- e^{G_L} dh + sum_i (scale e^{G_i} q_i) do_i^T       against it
+//   forward   h  <- e^{G_L} h  + sum_j (e^{G_L - G_j} k_j) v_j^T                       in the order of the steps
+//   reverse   dh <- e^{G_L} dh + scale e^{G_0} sum_i (e^{G_i - G_0} q_i) do_i^T        against it
 // A CTA walks a run of a (sequence, V-head)'s steps, a whole state in registers (32 values of a key's row to each of 512 threads).  A step is one
 // product, D[key][value channel] = A B: A the scaled keys, transposed to tensor memory (lane = key channel, columns = tokens) as two bf16
-// pieces, 2^-17 of the value left out, so that the sum keeps the accuracy of fp32; B the values' tile as it is.  Nothing of the product waits for
+// pieces, 2^-17 of the value left out, so that the sum keeps the accuracy of fp32 (and nothing left out of the token next to the state, whose
+// weight is one: with scale e^{G_0} in the weights dh0 had 1.5 times the error); B the values' tile as it is.  Nothing of the product waits for
 // the state, so the next step's keys are scaled under this one's product, and the chain through the steps is one multiply-add.
 //
 // What bounds it: the tiles and images through HBM when many CTAs run (96 KiB a step forward, 128 backward), else a CTA's steps, bound by the
@@ -21,7 +22,7 @@ namespace {
 constexpr int kStages = 3;
 constexpr uint32_t kStageB = 2 * kTileBytes;
 constexpr int kThreads = 32 * (kComputeWarps + 3);         // compute warps, producer, MMA issue, gates
-constexpr uint32_t OFF_W = kStages * kStageB;              // [2] weights of a step's tokens, and its decay
+constexpr uint32_t OFF_W = kStages * kStageB;              // [2] weights of a step's tokens, its decay, its sum's factor
 constexpr uint32_t kWeightB = (kStep + 4) * 4;
 constexpr uint32_t OFF_BAR = OFF_W + 2 * kWeightB;
 constexpr int kBars = 2 * kStages + 8;
@@ -124,12 +125,15 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       if (c > 1) mbar_wait(&used[c & 1], ((c >> 1) - 1) & 1, abort_flag);
       __syncwarp();
       float* w = reinterpret_cast<float*>(sm + OFF_W + (c & 1) * kWeightB);
-      const double GL = __shfl_sync(0xffffffffu, G[3], 31);
+      const double GL = __shfl_sync(0xffffffffu, G[3], 31), G0 = __shfl_sync(0xffffffffu, G[0], 0);
       float4 x;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) (&x.x)[e] = rev ? p.scale * ex2((float)G[e]) : ex2((float)(GL - G[e]));
+      for (int e = 0; e < 4; ++e) (&x.x)[e] = ex2((float)(rev ? G[e] - G0 : GL - G[e]));
       reinterpret_cast<float4*>(w)[lane] = x;
-      if (lane == 0) w[kStep] = ex2((float)GL);
+      if (lane == 0) {
+        w[kStep] = ex2((float)GL);
+        w[kStep + 1] = rev ? p.scale * ex2((float)G0) : 1.f;
+      }
       __syncwarp();
       if (lane == 0) mbar_arrive(&weights[c & 1]);
       __syncwarp();
@@ -206,7 +210,8 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           if (PIECES == 2) *reinterpret_cast<uint4*>(row + kTileBytes + off) = lo;
         }
       }
-      const float decay = reinterpret_cast<const float*>(sm + OFF_W + b * kWeightB)[kStep];
+      const float2 f = *reinterpret_cast<const float2*>(sm + OFF_W + b * kWeightB + kStep * 4);
+      const float decay = f.x;
       mbar_wait(&product[b], (c >> 1) & 1, abort_flag);
       __syncwarp();
       tc_fence_after_sync();
@@ -214,7 +219,7 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       tmem_ld32(TM_D + 128 * b + lanes + 32 * g, d);
       tmem_ld_wait();
 #pragma unroll
-      for (int k = 0; k < 32; ++k) h[k] = fmaf(decay, h[k], __uint_as_float(d[k]));
+      for (int k = 0; k < 32; ++k) h[k] = fmaf(decay, h[k], f.y * __uint_as_float(d[k]));
       total *= decay;
       tc_fence_before_sync();
       __syncwarp();
