@@ -39,7 +39,7 @@ struct Work {                                              // workspace behind t
   float* total;                                            // [slot][V-head] e^{G_L}
   float* h;                                                // what a chunk adds to the state, then the state in front of it
   float* dh;                                               // backward: what it adds to the gradient, then the gradient behind it
-  float *dq, *dk;                                          // backward, several V-heads per QK-head: [token][V-head][d] fp32
+  float *dq, *dk;                                          // backward, several V-heads per QK-head: fp32 parts [token][V-head or run of them][d]
 };
 
 struct Call {                                              // one call, as the launchers take it
@@ -56,7 +56,7 @@ cudaError_t launch_simt_backward(const Call& c, cudaStream_t stream);
 cudaError_t launch_combine(const Call& c, bool reverse, cudaStream_t stream);
 // N x HV chains of `count` states each, one behind the other at [n][i][head]: total, s in place, from `first` (or zero)
 cudaError_t launch_chain(const float* total, float* s, const float* first, int count, int N, int HV, int per_state, bool reverse, cudaStream_t stream);
-cudaError_t launch_head_sums(const Call& c, cudaStream_t stream);
+cudaError_t launch_head_sums(const Call& c, int parts, cudaStream_t stream);   // of dq, dk: `parts` per token, HK heads
 
 template <typename... Args>
 cudaError_t start(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, cudaStream_t stream, Args... args) {

@@ -490,7 +490,7 @@ cudaError_t backward(const Call& c, cudaStream_t stream) {
   if (e == cudaSuccess) e = launch_combine(c, true, stream);
   if (e != cudaSuccess || c.p.max_chunks == 0) return e;
   e = launch(gla_back_kernel<In, D>, smem_back(D), c, stream);
-  return e == cudaSuccess ? launch_head_sums(c, stream) : e;
+  return e == cudaSuccess ? launch_head_sums(c, c.p.HV, stream) : e;
 }
 
 }  // namespace
@@ -529,11 +529,11 @@ cudaError_t launch_chain(const float* total, float* s, const float* first, int c
   return reverse ? start(gla_combine_kernel<true>, grid, kThreads, 0, stream, p) : start(gla_combine_kernel<false>, grid, kThreads, 0, stream, p);
 }
 
-cudaError_t launch_head_sums(const Call& c, cudaStream_t stream) {
-  if (c.p.HV == c.p.HK) return cudaSuccess;
+cudaError_t launch_head_sums(const Call& c, int parts, cudaStream_t stream) {
+  if (parts == c.p.HK) return cudaSuccess;
   SumParams p;
   p.dq = c.w.dq; p.dk = c.w.dk; p.out_q = c.a.dq; p.out_k = c.a.dk;
-  p.n = (size_t)c.p.T_total * c.p.HK * c.p.dk; p.R = c.p.HV / c.p.HK; p.per_head = c.p.dk;
+  p.n = (size_t)c.p.T_total * c.p.HK * c.p.dk; p.R = parts / c.p.HK; p.per_head = c.p.dk;
   const dim3 grid((unsigned)((p.n / 4 + kThreads - 1) / kThreads), 2);
   return c.p.dtype == HA_LA_BF16 ? start(gla_sum_kernel<__nv_bfloat16>, grid, kThreads, 0, stream, p) : start(gla_sum_kernel<float>, grid, kThreads, 0, stream, p);
 }

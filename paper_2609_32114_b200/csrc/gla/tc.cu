@@ -32,13 +32,15 @@ size_t tc_bytes(const Problem& p, bool back, TcWork* tw, Work* w, void* base) {
   take(tw ? &tw->part : nullptr, parts * 65536);
   take(tw ? &tw->total : nullptr, parts * 4);
   if (back) {
-    const size_t shared = p.HV != p.HK ? (size_t)p.T_total * p.HV * 128 * 4 : 0;
+    const int per = heads_per_run(p);
+    const size_t parts_of = p.HV / per != p.HK ? (size_t)p.T_total * (p.HV / per) * 128 * 4 : 0;
     take(tw ? &tw->image_back : nullptr, units * kTileBytes * 2);
     take(tw ? &tw->part_back : nullptr, parts * 65536);
     take(tw ? &tw->total_back : nullptr, parts * 4);
     take(tw ? &tw->sums : nullptr, local_back_bytes());
-    take(w ? &w->dq : nullptr, shared);
-    take(w ? &w->dk : nullptr, shared);
+    take(tw ? &tw->shared : nullptr, per > 1 ? (size_t)sm_count() * 2 * 65536 : 0);
+    take(w ? &w->dq : nullptr, parts_of);
+    take(w ? &w->dk : nullptr, parts_of);
   }
   return at;
 }
@@ -83,7 +85,7 @@ cudaError_t launch_tc_backward(const Call& c, PlanView plan, const TcWork& w, cu
   cudaError_t e = make(&t, c, plan, w);
   if (e == cudaSuccess) e = states(t, stream);
   if (e == cudaSuccess) e = launch_tc_local_back(t, stream);
-  return e == cudaSuccess ? launch_head_sums(c, stream) : e;
+  return e == cudaSuccess ? launch_head_sums(c, c.p.HV / heads_per_run(c.p), stream) : e;
 }
 
 }  // namespace gla

@@ -89,6 +89,32 @@ __device__ __forceinline__ void clear_rows(uint8_t* tile, int L, int tid, int n)
     *reinterpret_cast<uint4*>(tile + (i & 1) * 16384 + (L + (i >> 4)) * 128 + ((i >> 1) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
 }
 
+// Four lanes that hold four 16-byte pieces of a row each exchange them: v[i] becomes this lane's (lane % 4) piece of the row of lane i of the four.
+// A warp's store of v[i] then covers 64 bytes of eight rows instead of 16 of thirty-two: a store takes the memory pipe a cycle for every
+// 128-byte line it touches, and with a row to a thread the stores were what bounded the state kernel (4.9 us a step with two images)
+// and the gradients (15 us a unit).
+__device__ __forceinline__ void exchange4(uint4 (&v)[4], int lane) {
+  auto swap = [](uint4& mine, uint4& theirs, bool keep_second, int with) {
+    const uint4 send = keep_second ? mine : theirs;
+    uint4 got;
+    got.x = __shfl_xor_sync(0xffffffffu, send.x, with);
+    got.y = __shfl_xor_sync(0xffffffffu, send.y, with);
+    got.z = __shfl_xor_sync(0xffffffffu, send.z, with);
+    got.w = __shfl_xor_sync(0xffffffffu, send.w, with);
+    if (keep_second) mine = got;
+    else theirs = got;
+  };
+  swap(v[0], v[1], lane & 1, 1);
+  swap(v[2], v[3], lane & 1, 1);
+  swap(v[0], v[2], lane & 2, 2);
+  swap(v[1], v[3], lane & 2, 2);
+}
+
+// Polls once before it waits: mbarrier.try_wait costs its caller some 150 cycles even when the phase is over.
+__device__ __forceinline__ void wait_for(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  if (!mbar_test_wait(bar, parity)) mbar_wait(bar, parity, abort_flag);
+}
+
 // A tile's descriptors as B operand: over its columns (k index = columns, N = rows) or over its rows (k index = rows, N = columns), and
 // what a step of 16 k adds.
 __device__ __forceinline__ uint64_t desc_cols(uint32_t tile) { return smem_desc(tile, 16, 1024, kSwizzle128B); }
@@ -125,6 +151,7 @@ struct TcWork {
   uint8_t* image_back;                                     // ... gradients behind them
   float *part, *part_back;                                 // [sequence][segment][V-head] fp32 states
   float *total, *total_back;                               // ... and decays
+  float4* shared;                                          // ... and add up over V-heads
   float* sums;                                             // backward: what the gradient kernel's CTAs pass on
 };
 
@@ -143,6 +170,7 @@ cudaError_t launch_tc_backward(const Call& c, PlanView plan, const TcWork& w, cu
 cudaError_t launch_tc_states(const TcCall& t, bool sums, cudaStream_t stream);
 cudaError_t launch_tc_out(const TcCall& t, cudaStream_t stream);
 size_t local_back_bytes();
+int heads_per_run(const Problem& p);
 cudaError_t launch_tc_local_back(const TcCall& t, cudaStream_t stream);
 
 }  // namespace gla

@@ -37,9 +37,10 @@ struct BackParams {
   Chunks chunks;
   const uint8_t *image, *image_back;
   void *dq, *dk, *dv;
-  float *dg, *part_q, *part_k;                             // part_q, part_k: fp32 parts of heads that several V-heads share, or NULL
+  float *dg, *part_q, *part_k;                             // part_q, part_k: [token][run of V-heads][128] fp32, where a q/k head has several runs, or NULL
   float* sums;                                             // [CTA][2][kSums]
-  int HK, HV;
+  float4* shared;                                          // [CTA][dq, dk][8][512 threads], runs of several V-heads
+  int HK, HV, per;                                         // per: V-heads of a run
   float scale;
   long long units;
   int32_t* status;
@@ -84,18 +85,21 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  struct Unit { Geom c; int j; size_t sj; };
+  // A CTA takes runs of `per` V-heads that share a q/k head, of one step: dq and dk add up over them.
+  struct Unit { Geom c; int j, r; size_t sj; };            // r: V-head of the run; L = 0: no unit
+  const int R = p.HV / p.HK, runs = p.HV / p.per;
   auto unit = [&](int u) {
-    const long long i = blockIdx.x + (long long)u * gridDim.x;
-    Unit x{{0, 0}, 0, 0};
+    const int n = u / p.per;
+    const long long i = blockIdx.x + (long long)n * gridDim.x;
+    Unit x{{0, 0}, 0, 0, 0};
     if (i >= p.units) return x;
-    const int slot = (int)((unsigned)i / (unsigned)p.HV);
-    x.j = (int)i - slot * p.HV;
-    x.sj = (size_t)i;
+    const int slot = (int)((unsigned)i / (unsigned)runs);
+    x.r = u - n * p.per;
+    x.j = ((int)i - slot * runs) * p.per + x.r;
+    x.sj = (size_t)slot * p.HV + x.j;
     x.c = geom_of(p.chunks, slot);
     return x;
   };
-  const int R = p.HV / p.HK;
   constexpr int kSums = 2 * 4 * kStep + kComputeWarps;     // [4][128] x + R - C, [4][128] y, [16] parts of <h, dh>
   float* sums = p.sums + (size_t)blockIdx.x * 2 * kSums;
   Slots sl;
@@ -104,12 +108,12 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     // ------------------------------------------------------------ tiles
     if (elect_one()) {
       Unit x = unit(0);
-      while (x.c.L > 0 && !*abort_flag) {
-        const Unit after = unit((int)((x.sj - blockIdx.x) / gridDim.x) + 1);
+      for (int u = 0; x.c.L > 0 && !*abort_flag; ++u) {
+        const Unit after = unit(u + 1);
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
           const int at = sl.at(t);
-          mbar_wait(&empty[at], sl.fill(t) ^ 1, abort_flag);
+          wait_for(&empty[at], sl.fill(t) ^ 1, abort_flag);
           if (*abort_flag) break;
           uint8_t* dst = sm + at * kTileBytes;
           mbar_expect_tx(&full[at], kTileBytes);
@@ -135,7 +139,7 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const uint32_t ph = u & 1;
         auto tile = [&](int t) { return smem_u32(sm + sl.at(t) * kTileBytes); };
         auto wait = [&](uint64_t* b, uint32_t parity) {
-          mbar_wait(b, parity, abort_flag);
+          wait_for(b, parity, abort_flag);
           tc_fence_after_sync();
         };
         auto loaded = [&](int t) { wait(&full[sl.at(t)], sl.fill(t)); };
@@ -190,7 +194,7 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     __syncwarp();
   } else if (warp == kComputeWarps + 2) {
     // ------------------------------------------------------------ gates; dg of the unit before
-    Unit x = unit(0), before{{0, 0}, 0, 0};
+    Unit x = unit(0), before{{0, 0}, 0, 0, 0};
     float total = 0.f;
     for (int u = 0; x.c.L > 0 || before.c.L > 0; ++u) {
       const Unit after = x.c.L > 0 ? unit(u + 1) : x;
@@ -216,7 +220,7 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           bb[e] = J < I ? ex2((float)(rI - rJ)) : 0.f;
         }
         next_total = ex2((float)GL);
-        if (u > 0) mbar_wait(g_free, (u - 1) & 1, abort_flag);
+        if (u > 0) wait_for(g_free, (u - 1) & 1, abort_flag);
         __syncwarp();
         reinterpret_cast<float4*>(s->hi)[lane] = hi;
         reinterpret_cast<float4*>(s->lo)[lane] = lo;
@@ -232,7 +236,7 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         __syncwarp();
       }
       if (before.c.L > 0) {
-        mbar_wait(e_k, (u - 1) & 1, abort_flag);           // (the last of the unit's sums are written ahead of it)
+        wait_for(e_k, (u - 1) & 1, abort_flag);           // (the last of the unit's sums are written ahead of it)
         __syncwarp();
         const float* f = sums + ((u - 1) & 1) * kSums;
         double z[4] = {0.0, 0.0, 0.0, 0.0}, y[4] = {0.0, 0.0, 0.0, 0.0};
@@ -276,62 +280,102 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       if (lane == 0) mbar_arrive(b);
     };
     auto wait = [&](uint64_t* b, uint32_t parity) {
-      mbar_wait(b, parity, abort_flag);
+      wait_for(b, parity, abort_flag);
       __syncwarp();
       tc_fence_after_sync();
     };
     auto seen = [&](int t) {                               // (loaded long ago; this thread's own look at it)
-      if (!mbar_test_wait(&full[sl.at(t)], sl.fill(t))) mbar_wait(&full[sl.at(t)], sl.fill(t), abort_flag);
+      wait_for(&full[sl.at(t)], sl.fill(t), abort_flag);
       __syncwarp();
     };
     // 16-byte piece k of this thread's 32 columns in its row of a tile
     auto piece = [&](int at, int k) {
       return *reinterpret_cast<const uint4*>(sm + at * kTileBytes + (g >> 1) * 16384 + i * 128 + (((4 * (g & 1) + k) ^ (i & 7)) << 4));
     };
-    // out = a f + b, 32 columns of a row; dot: of a f with the tile's row
-    auto gradient = [&](uint32_t first, uint32_t second, float f, int dot_with, float* dot, uint64_t* read, __nv_bfloat16* out, float* part, bool valid) {
+    // a f + b, 32 columns of a row.  With `tile`: base + a f . (the tile's row) to `sum`.  With `acc`: added to what the run's V-heads before
+    // left there, and left there for the next ones.  `read` follows the sum.
+    auto gradient = [&](uint32_t first, uint32_t second, float f, int tile, float base, float* sum, uint64_t* read, const Unit& x, float4* acc,
+                        void* out, float* part, int heads, int head) {
       uint32_t a[32], b[32];
       tmem_ld32(first + lanes + 32 * g, a);
       tmem_ld32(second + lanes + 32 * g, b);
-      uint4 r[4];
-      if (dot_with >= 0) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) r[k] = piece(dot_with, k);
-      }
       tmem_ld_wait();
-      arrive(read);
-      float d = 0.f;
+      if (tile < 0) arrive(read);
 #pragma unroll
-      for (int k = 0; k < 32; ++k) {
-        const float v = f * __uint_as_float(a[k]);
-        if (dot_with >= 0) {
-          const uint32_t w = (&r[k >> 3].x)[(k >> 1) & 3];
-          d = fmaf(v, __uint_as_float(k & 1 ? w & 0xffff0000u : w << 16), d);
+      for (int k = 0; k < 32; ++k) a[k] = __float_as_uint(f * __uint_as_float(a[k]));
+      if (tile >= 0) {
+        float d = base;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint4 r = piece(tile, k);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const float2 t = unpack_bf16((&r.x)[w]);
+            d = fmaf(__uint_as_float(a[8 * k + 2 * w]), t.x, d);
+            d = fmaf(__uint_as_float(a[8 * k + 2 * w + 1]), t.y, d);
+          }
         }
-        a[k] = __float_as_uint(v + __uint_as_float(b[k]));
+        __stcg(sum, d);
+        arrive(read);
       }
-      if (dot_with >= 0) *dot = d;
-      if (!valid) return;
-      if (part) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) reinterpret_cast<uint4*>(part)[k] = make_uint4(a[4 * k], a[4 * k + 1], a[4 * k + 2], a[4 * k + 3]);
+      for (int k = 0; k < 32; ++k) a[k] = __float_as_uint(__uint_as_float(a[k]) + __uint_as_float(b[k]));
+      if (acc) {
+        float4* mine = acc + tid;
+        if (x.r > 0) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float4 t = __ldcg(mine + 512 * k);
+            a[4 * k] = __float_as_uint(__uint_as_float(a[4 * k]) + t.x);
+            a[4 * k + 1] = __float_as_uint(__uint_as_float(a[4 * k + 1]) + t.y);
+            a[4 * k + 2] = __float_as_uint(__uint_as_float(a[4 * k + 2]) + t.z);
+            a[4 * k + 3] = __float_as_uint(__uint_as_float(a[4 * k + 3]) + t.w);
+          }
+        }
+        if (x.r < p.per - 1) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            __stcg(mine + 512 * k, make_float4(__uint_as_float(a[4 * k]), __uint_as_float(a[4 * k + 1]), __uint_as_float(a[4 * k + 2]), __uint_as_float(a[4 * k + 3])));
+          return;
+        }
+      }
+      const int row = 32 * q + (lane & ~3), left = x.c.L - row;
+      if (part) {
+        float* dst = part + ((size_t)(x.c.tok0 + row) * heads + head) * 128 + 32 * g + 4 * (lane & 3);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint4 o[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[k] = make_uint4(a[16 * half + 4 * k], a[16 * half + 4 * k + 1], a[16 * half + 4 * k + 2], a[16 * half + 4 * k + 3]);
+          exchange4(o, lane);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (k < left) *reinterpret_cast<uint4*>(dst + (size_t)k * heads * 128 + 16 * half) = o[k];
+        }
       } else {
+        uint4 o[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          reinterpret_cast<uint4*>(out)[k] =
-              make_uint4(pack_bf16(as_f2(a[8 * k], a[8 * k + 1])), pack_bf16(as_f2(a[8 * k + 2], a[8 * k + 3])),
-                         pack_bf16(as_f2(a[8 * k + 4], a[8 * k + 5])), pack_bf16(as_f2(a[8 * k + 6], a[8 * k + 7])));
+          o[k] = make_uint4(pack_bf16(as_f2(a[8 * k], a[8 * k + 1])), pack_bf16(as_f2(a[8 * k + 2], a[8 * k + 3])),
+                            pack_bf16(as_f2(a[8 * k + 4], a[8 * k + 5])), pack_bf16(as_f2(a[8 * k + 6], a[8 * k + 7])));
+        exchange4(o, lane);
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(out) + ((size_t)(x.c.tok0 + row) * heads + head) * 128 + 32 * g + 8 * (lane & 3);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (k < left) *reinterpret_cast<uint4*>(dst + (size_t)k * heads * 128) = o[k];
       }
     };
+    float4* shared_q = p.per > 1 ? p.shared + (size_t)blockIdx.x * 2 * 8 * 512 : nullptr;
+    float4* shared_k = p.per > 1 ? shared_q + 8 * 512 : nullptr;
     Unit x = unit(0);
     for (int u = 0; x.c.L > 0; ++u) {
       const Unit after = unit(u + 1);
       const uint32_t ph = u & 1;
-      mbar_wait(gates, ph, abort_flag);
+      wait_for(gates, ph, abort_flag);
       if (x.c.L < kStep) {                                 // (rows behind the sequence may be NaN)
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          mbar_wait(&full[sl.at(t)], sl.fill(t), abort_flag);
+          wait_for(&full[sl.at(t)], sl.fill(t), abort_flag);
           clear_rows(sm + sl.at(t) * kTileBytes, x.c.L, tid, 32 * kComputeWarps);
         }
         fence_proxy_async_smem();
@@ -428,20 +472,17 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         arrive(e2);
         if (lane == 0) mbar_arrive(g_free);
       }
-      const bool valid = i < x.c.L;
-      const size_t row = (size_t)(x.c.tok0 + i), at_v = (row * p.HV + x.j) * 128 + 32 * g, at_k = (row * p.HK + x.j / R) * 128 + 32 * g;
+      const int head_k = x.j / R, run = x.j / p.per, heads_k = p.part_q ? runs : p.HK, out_k = p.part_q ? run : head_k;
       float* mine = sums + ph * kSums;
       // ---- dq
-      float d = 0.f;
       wait(b_dq2, ph);
       seen(kQ);
-      gradient(R0, R1, eg, sl.at(kQ), &d, e_q, reinterpret_cast<__nv_bfloat16*>(p.dq) + at_k, p.part_q ? p.part_q + at_v : nullptr, valid);
-      __stcg(mine + g * kStep + i, z + d);
+      gradient(R0, R1, eg, sl.at(kQ), z, mine + g * kStep + i, e_q, x, shared_q, p.dq, p.part_q, heads_k, out_k);
       // ---- dv
       wait(b_dv, ph);
-      gradient(R0, R2, el, -1, nullptr, e_v, reinterpret_cast<__nv_bfloat16*>(p.dv) + at_v, nullptr, valid);
+      gradient(R0, R2, el, -1, 0.f, nullptr, e_v, x, nullptr, p.dv, nullptr, p.HV, x.j);
       // ---- <h, dh>
-      d = 0.f;
+      float d = 0.f;
 #pragma unroll
       for (int t = kHH; t <= kDL; ++t) seen(t);
 #pragma unroll
@@ -458,41 +499,10 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
       if (lane == 0) __stcg(mine + 8 * kStep + warp, d);
-      // ---- dk
+      // ---- dk (with the unit's sums ahead of its e_k)
       wait(b_dk, ph);
       seen(kK);
-      {
-        uint32_t a[32], b[32];
-        tmem_ld32(R3 + lanes + 32 * g, a);
-        tmem_ld32(R1 + lanes + 32 * g, b);
-        uint4 r[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) r[k] = piece(sl.at(kK), k);
-        tmem_ld_wait();
-        d = 0.f;
-#pragma unroll
-        for (int k = 0; k < 32; ++k) {
-          const float v = el * __uint_as_float(a[k]);
-          const uint32_t w = (&r[k >> 3].x)[(k >> 1) & 3];
-          d = fmaf(v, __uint_as_float(k & 1 ? w & 0xffff0000u : w << 16), d);
-          a[k] = __float_as_uint(v + __uint_as_float(b[k]));
-        }
-        __stcg(mine + 4 * kStep + g * kStep + i, d);
-        arrive(e_k);                                       // (with the unit's sums ahead of it)
-        if (valid) {
-          if (p.part_k) {
-            uint4* out = reinterpret_cast<uint4*>(p.part_k + at_v);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) out[k] = make_uint4(a[4 * k], a[4 * k + 1], a[4 * k + 2], a[4 * k + 3]);
-          } else {
-            uint4* out = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.dk) + at_k);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              out[k] = make_uint4(pack_bf16(as_f2(a[8 * k], a[8 * k + 1])), pack_bf16(as_f2(a[8 * k + 2], a[8 * k + 3])),
-                                  pack_bf16(as_f2(a[8 * k + 4], a[8 * k + 5])), pack_bf16(as_f2(a[8 * k + 6], a[8 * k + 7])));
-          }
-        }
-      }
+      gradient(R3, R1, el, sl.at(kK), 0.f, mine + 4 * kStep + g * kStep + i, e_k, x, shared_k, p.dk, p.part_k, heads_k, out_k);
       sl.next();
       x = after;
     }
@@ -506,6 +516,15 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
 }  // namespace
 
+// V-heads of a q/k head that one CTA takes one behind the other, so that dq and dk add up on the way: as many as leave two runs to an SM.
+// (Four heads per q/k head apart and summed by a kernel of their own instead: see the figures in tc.cu.)
+int heads_per_run(const Problem& p) {
+  const int R = p.HV / p.HK;
+  for (int per = R; per > 1; --per)
+    if (R % per == 0 && (long long)p.max_chunks * (p.HV / per) >= 2 * sm_count()) return per;
+  return 1;
+}
+
 size_t local_back_bytes() { return (size_t)sm_count() * 2 * (2 * 4 * kStep + kComputeWarps) * 4; }
 
 cudaError_t launch_tc_local_back(const TcCall& t, cudaStream_t stream) {
@@ -513,11 +532,12 @@ cudaError_t launch_tc_local_back(const TcCall& t, cudaStream_t stream) {
   BackParams p;
   p.g = c.a.g; p.chunks = c.chunks; p.image = t.w.image; p.image_back = t.w.image_back;
   p.dq = c.a.dq; p.dk = c.a.dk; p.dv = c.a.dv; p.dg = c.a.dg;
-  p.part_q = c.p.HV != c.p.HK ? c.w.dq : nullptr;
-  p.part_k = c.p.HV != c.p.HK ? c.w.dk : nullptr;
-  p.sums = t.w.sums;
+  p.per = heads_per_run(c.p);
+  p.part_q = c.p.HV / p.per != c.p.HK ? c.w.dq : nullptr;
+  p.part_k = c.p.HV / p.per != c.p.HK ? c.w.dk : nullptr;
+  p.sums = t.w.sums; p.shared = t.w.shared;
   p.HK = c.p.HK; p.HV = c.p.HV; p.scale = c.p.scale; p.status = c.a.status_word;
-  p.units = (long long)c.p.max_chunks * c.p.HV;
+  p.units = (long long)c.p.max_chunks * (c.p.HV / p.per);
   if (p.units == 0) return cudaSuccess;
   const cudaError_t e = cudaFuncSetAttribute(gla_tc_back_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
   const unsigned grid = (unsigned)(p.units < sm_count() ? p.units : sm_count());

@@ -77,7 +77,7 @@ gla_tc_out_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
       int slot = 0;
       uint32_t round = 0;
       auto next = [&]() {                                  // the ring's next slot, free
-        if (round > 0) mbar_wait(&empty[slot], (round - 1) & 1, abort_flag);
+        if (round > 0) wait_for(&empty[slot], (round - 1) & 1, abort_flag);
         return !*abort_flag;
       };
       auto done = [&]() { if (++slot == kSlots) { slot = 0; ++round; } };
@@ -110,20 +110,20 @@ gla_tc_out_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
           ph[t] = ((kTiles * u + t) / kSlots) & 1;
         }
         auto tile = [&](int t) { return smem_u32(sm + s[t] * kTileBytes); };
-        mbar_wait(&full[s[0]], ph[0], abort_flag);
-        mbar_wait(&full[s[1]], ph[1], abort_flag);
+        wait_for(&full[s[0]], ph[0], abort_flag);
+        wait_for(&full[s[1]], ph[1], abort_flag);
         tc_fence_after_sync();
         mma_cols(TM_S, tile(0), tile(1), false);           // (the unit before has read its S: its P was made)
         umma_commit(made_s);
         umma_commit(&empty[s[1]]);
-        mbar_wait(&full[s[2]], ph[2], abort_flag);
-        if (u > 0) mbar_wait(&used[(u - 1) & 1], ((u - 1) >> 1) & 1, abort_flag);
+        wait_for(&full[s[2]], ph[2], abort_flag);
+        if (u > 0) wait_for(&used[(u - 1) & 1], ((u - 1) >> 1) & 1, abort_flag);
         tc_fence_after_sync();
         mma_rows(TM_O1, tile(0), tile(2), false);
         umma_commit(&empty[s[0]]);
         umma_commit(&empty[s[2]]);
-        mbar_wait(&full[s[3]], ph[3], abort_flag);
-        mbar_wait(made_p, u & 1, abort_flag);
+        wait_for(&full[s[3]], ph[3], abort_flag);
+        wait_for(made_p, u & 1, abort_flag);
         tc_fence_after_sync();
         mma_tmem_rows(TM_O2, TM_P, tile(3), false);
         umma_commit(made_o);
@@ -139,7 +139,7 @@ gla_tc_out_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
       if (x.c.L <= 0) break;
       double G[4];
       scan_gates(p.g, p.HV, x.j, x.c, lane, G);
-      if (u > 1) mbar_wait(&used[u & 1], ((u >> 1) - 1) & 1, abort_flag);
+      if (u > 1) wait_for(&used[u & 1], ((u >> 1) - 1) & 1, abort_flag);
       __syncwarp();
       fill_gates(reinterpret_cast<StepGates*>(sm + OFF_G) + (u & 1), G, lane);
       __syncwarp();
@@ -159,14 +159,14 @@ gla_tc_out_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     for (int u = 0; x.c.L > 0; ++u) {
       const Unit after = unit(u + 1);
       const StepGates* s = reinterpret_cast<const StepGates*>(sm + OFF_G) + (u & 1);
-      mbar_wait(&gates[u & 1], (u >> 1) & 1, abort_flag);
+      wait_for(&gates[u & 1], (u >> 1) & 1, abort_flag);
       if (x.c.L < kStep) {                                 // (rows behind the sequence: their zero in P is not enough for NaN)
         const int sv = (kTiles * u + 3) % kSlots;
-        mbar_wait(&full[sv], ((kTiles * u + 3) / kSlots) & 1, abort_flag);
+        wait_for(&full[sv], ((kTiles * u + 3) / kSlots) & 1, abort_flag);
         clear_rows(sm + sv * kTileBytes, x.c.L, tid, 32 * kComputeWarps);
         fence_proxy_async_smem();
       }
-      mbar_wait(made_s, u & 1, abort_flag);
+      wait_for(made_s, u & 1, abort_flag);
       __syncwarp();
       tc_fence_after_sync();
       if (g <= q) {
@@ -205,7 +205,7 @@ gla_tc_out_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
       __syncwarp();
       if (lane == 0) mbar_arrive(made_p);
       const float eg = p.scale * s->eg[i];
-      mbar_wait(made_o, u & 1, abort_flag);
+      wait_for(made_o, u & 1, abort_flag);
       __syncwarp();
       tc_fence_after_sync();
       uint32_t a[32], b[32];
@@ -215,14 +215,18 @@ gla_tc_out_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&used[u & 1]);
-      if (i < x.c.L) {
-        uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.o) + ((size_t)(x.c.tok0 + i) * p.HV + x.j) * 128 + 32 * g);
-        auto val = [&](int k) { return fmaf(eg, __uint_as_float(a[k]), p.scale * __uint_as_float(b[k])); };
+      auto val = [&](int k) { return fmaf(eg, __uint_as_float(a[k]), p.scale * __uint_as_float(b[k])); };
+      uint4 o[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          dst[k] = make_uint4(pack_bf16(val(8 * k), val(8 * k + 1)), pack_bf16(val(8 * k + 2), val(8 * k + 3)),
-                              pack_bf16(val(8 * k + 4), val(8 * k + 5)), pack_bf16(val(8 * k + 6), val(8 * k + 7)));
-      }
+      for (int k = 0; k < 4; ++k)
+        o[k] = make_uint4(pack_bf16(val(8 * k), val(8 * k + 1)), pack_bf16(val(8 * k + 2), val(8 * k + 3)),
+                          pack_bf16(val(8 * k + 4), val(8 * k + 5)), pack_bf16(val(8 * k + 6), val(8 * k + 7)));
+      exchange4(o, lane);
+      const int row = 32 * q + (lane & ~3);
+      __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.o) + ((size_t)(x.c.tok0 + row) * p.HV + x.j) * 128 + 32 * g + 8 * (lane & 3);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (row + k < x.c.L) *reinterpret_cast<uint4*>(dst + (size_t)k * p.HV * 128) = o[k];
       x = after;
     }
   }

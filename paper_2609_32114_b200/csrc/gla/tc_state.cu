@@ -93,7 +93,7 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     if (elect_one()) {
       for (int c = 0; c < count; ++c) {
         const int st = c % kStages, t0 = geom(c).tok0;
-        if (c >= kStages) mbar_wait(&empty[st], (c / kStages - 1) & 1, abort_flag);
+        if (c >= kStages) wait_for(&empty[st], (c / kStages - 1) & 1, abort_flag);
         if (*abort_flag) break;
         mbar_expect_tx(&full[st], kStageB);
         tma_load_4d(sm + st * kStageB, rev ? &map_q : &map_k, &full[st], 0, jq, t0, 0);
@@ -106,8 +106,8 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     if (elect_one()) {
       for (int c = 0; c < count; ++c) {
         const int st = c % kStages, b = c & 1;
-        mbar_wait(&full[st], (c / kStages) & 1, abort_flag);
-        mbar_wait(&operand[b], (c >> 1) & 1, abort_flag);
+        wait_for(&full[st], (c / kStages) & 1, abort_flag);
+        wait_for(&operand[b], (c >> 1) & 1, abort_flag);
         tc_fence_after_sync();
         const uint32_t tile = smem_u32(sm + st * kStageB + kTileBytes);
         mma_tmem_rows(TM_D + 128 * b, TM_A + 128 * b, tile, false);
@@ -122,7 +122,7 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     for (int c = 0; c < count; ++c) {
       double G[4];
       scan_gates(p.g, p.HV, j, geom(c), lane, G);
-      if (c > 1) mbar_wait(&used[c & 1], ((c >> 1) - 1) & 1, abort_flag);
+      if (c > 1) wait_for(&used[c & 1], ((c >> 1) - 1) & 1, abort_flag);
       __syncwarp();
       float* w = reinterpret_cast<float*>(sm + OFF_W + (c & 1) * kWeightB);
       const double GL = __shfl_sync(0xffffffffu, G[3], 31), G0 = __shfl_sync(0xffffffffu, G[0], 0);
@@ -158,8 +158,8 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     auto scale_keys = [&](int c) {
       const int st = c % kStages, b = c & 1, L = geom(c).L;
       uint8_t* tile = sm + st * kStageB;
-      mbar_wait(&weights[b], (c >> 1) & 1, abort_flag);
-      mbar_wait(&full[st], (c / kStages) & 1, abort_flag);
+      wait_for(&weights[b], (c >> 1) & 1, abort_flag);
+      wait_for(&full[st], (c / kStages) & 1, abort_flag);
       __syncwarp();
       if (L < kStep) {                                     // (a product's rows past the end: weight 0 is not enough for NaN)
         clear_rows(tile + kTileBytes, L, tid, 32 * kComputeWarps);
@@ -197,22 +197,27 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       const int b = c & 1;
       if (c + 1 < count) scale_keys(c + 1);
       if constexpr (PIECES > 0) {
-        uint8_t* row = p.image[rev] + ((size_t)(slot0 + index(c)) * p.HV + j) * (PIECES * kTileBytes) + (g >> 1) * 16384 + key * 128;
+        uint8_t* image = p.image[rev] + ((size_t)(slot0 + index(c)) * p.HV + j) * (PIECES * kTileBytes) + (g >> 1) * 16384;
+        uint4 hi[4], lo[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            if (PIECES == 2) split_bf16(h[8 * k + 2 * w], h[8 * k + 2 * w + 1], (&hi[k].x)[w], (&lo[k].x)[w]);
+            else (&hi[k].x)[w] = pack_bf16(h[8 * k + 2 * w], h[8 * k + 2 * w + 1]);
+          }
+        exchange4(hi, lane);
+        if (PIECES == 2) exchange4(lo, lane);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          uint4 hi, lo;
-          split_bf16(h[8 * k], h[8 * k + 1], hi.x, lo.x);
-          split_bf16(h[8 * k + 2], h[8 * k + 3], hi.y, lo.y);
-          split_bf16(h[8 * k + 4], h[8 * k + 5], hi.z, lo.z);
-          split_bf16(h[8 * k + 6], h[8 * k + 7], hi.w, lo.w);
-          const int off = ((4 * (g & 1) + k) ^ (key & 7)) << 4;
-          *reinterpret_cast<uint4*>(row + off) = hi;
-          if (PIECES == 2) *reinterpret_cast<uint4*>(row + kTileBytes + off) = lo;
+          const int row = 32 * q + (lane & ~3) + k, off = row * 128 + (((4 * (g & 1) + (lane & 3)) ^ (row & 7)) << 4);
+          *reinterpret_cast<uint4*>(image + off) = hi[k];
+          if (PIECES == 2) *reinterpret_cast<uint4*>(image + kTileBytes + off) = lo[k];
         }
       }
       const float2 f = *reinterpret_cast<const float2*>(sm + OFF_W + b * kWeightB + kStep * 4);
       const float decay = f.x;
-      mbar_wait(&product[b], (c >> 1) & 1, abort_flag);
+      wait_for(&product[b], (c >> 1) & 1, abort_flag);
       __syncwarp();
       tc_fence_after_sync();
       uint32_t d[32];

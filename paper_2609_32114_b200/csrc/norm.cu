@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kSubThreads = 256;                         // CTA of the short rows (several rows to a warp or to a CTA)
 constexpr int kMaxCols = 16384;
-constexpr int kReduceThreads = 256;
+constexpr int kReduceThreads = 1024;
 
 struct NormParams {
   const void *x, *z, *r, *dy, *dr_out;                   // z: the gate; r: residual stream (backward: behind the addition)
@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(THREADS) add_norm_back_kernel(NormParams p) {
   if (POST) put_sums<In, VEC, NV, SUB>(at, dwp, part + p.cols, sum, p.group);
 }
 
-// Sums of the CTAs' sums: a warp's lanes have 32 neighbouring columns, its eight warps every eighth CTA.  blockIdx.y: which vector.
+// Sums of the CTAs' sums: a warp's lanes have 32 neighbouring columns, the 32 warps every 32nd CTA.  blockIdx.y: which vector.
 __global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const float* part, int ctas, int cols, int both, float* dw, float* dw_post) {
   __shared__ float s[kReduceThreads / 32][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
@@ -460,10 +460,11 @@ __global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const float
     const float* src = part + (size_t)blockIdx.y * cols + c;
     const size_t stride = (size_t)both * cols;
     int i = warp;
-    for (; i + 24 < ctas; i += 32)
+    constexpr int kWarps = kReduceThreads / 32;
+    for (; i + 3 * kWarps < ctas; i += 4 * kWarps)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) a[k] += src[(i + 8 * k) * stride];
-    for (; i < ctas; i += 8) a[0] += src[i * stride];
+      for (int k = 0; k < 4; ++k) a[k] += src[(i + k * kWarps) * stride];
+    for (; i < ctas; i += kWarps) a[0] += src[i * stride];
   }
   s[warp][lane] = (a[0] + a[1]) + (a[2] + a[3]);
   __syncthreads();
