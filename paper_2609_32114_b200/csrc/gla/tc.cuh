@@ -23,13 +23,19 @@ using namespace ptx;
 constexpr int kComputeWarps = 16;
 constexpr double kLog2e = 1.4426950408889634;
 
-// Cumulative log2-gates of a step's tokens 4 lane .. 4 lane + 3 (one warp), in 64 bits.  Tokens past the end have gate 0.
-__device__ __forceinline__ void scan_gates(const float* g, int HV, int j, Geom c, int lane, double (&G)[4]) {
+// Log-gates of a step's tokens 4 lane .. 4 lane + 3 (one warp; 0 past the end), and cumulative, times log2 e, in 64 bits.
+__device__ __forceinline__ float4 fetch_gates(const float* g, int HV, int j, Geom c, int lane) {
+  float4 x;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const int t = 4 * lane + e;
-    G[e] = t < c.L ? gate(g[(size_t)(c.tok0 + t) * HV + j]) * kLog2e : 0.0;
+    (&x.x)[e] = t < c.L ? g[(size_t)(c.tok0 + t) * HV + j] : 0.f;
   }
+  return x;
+}
+__device__ __forceinline__ void scan_gates(float4 x, int lane, double (&G)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) G[e] = gate((&x.x)[e]) * kLog2e;
   G[1] += G[0];
   G[2] += G[1];
   G[3] += G[2];

@@ -196,12 +196,14 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     // ------------------------------------------------------------ gates; dg of the unit before
     Unit x = unit(0), before{{0, 0}, 0, 0, 0};
     float total = 0.f;
+    float4 raw = fetch_gates(p.g, p.HV, x.j, x.c, lane);
     for (int u = 0; x.c.L > 0 || before.c.L > 0; ++u) {
       const Unit after = x.c.L > 0 ? unit(u + 1) : x;
       float next_total = 0.f;
       if (x.c.L > 0) {
         double G[4];
-        scan_gates(p.g, p.HV, x.j, x.c, lane, G);
+        scan_gates(raw, lane, G);
+        raw = fetch_gates(p.g, p.HV, after.j, after.c, lane);
         const double Rb = __shfl_sync(0xffffffffu, G[0], lane & ~3), R1b = __shfl_sync(0xffffffffu, G[0], min((lane & ~3) + 4, 31)),
                      GL = __shfl_sync(0xffffffffu, G[3], 31);
         float4 hi, lo, er, ec;

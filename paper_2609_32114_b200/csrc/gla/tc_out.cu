@@ -134,11 +134,13 @@ gla_tc_out_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     __syncwarp();
   } else if (warp == kComputeWarps + 2) {
     // ------------------------------------------------------------ gates
-    for (int u = 0;; ++u) {
-      const Unit x = unit(u);
-      if (x.c.L <= 0) break;
+    Unit x = unit(0);
+    float4 raw = fetch_gates(p.g, p.HV, x.j, x.c, lane);
+    for (int u = 0; x.c.L > 0; ++u) {
       double G[4];
-      scan_gates(p.g, p.HV, x.j, x.c, lane, G);
+      scan_gates(raw, lane, G);
+      x = unit(u + 1);
+      raw = fetch_gates(p.g, p.HV, x.j, x.c, lane);        // (nothing where there is no unit)
       if (u > 1) wait_for(&used[u & 1], ((u >> 1) - 1) & 1, abort_flag);
       __syncwarp();
       fill_gates(reinterpret_cast<StepGates*>(sm + OFF_G) + (u & 1), G, lane);

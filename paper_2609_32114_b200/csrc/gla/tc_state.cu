@@ -24,7 +24,9 @@ constexpr uint32_t kStageB = 2 * kTileBytes;
 constexpr int kThreads = 32 * (kComputeWarps + 3);         // compute warps, producer, MMA issue, gates
 constexpr uint32_t OFF_W = kStages * kStageB;              // [2] weights of a step's tokens, its decay, its sum's factor
 constexpr uint32_t kWeightB = (kStep + 4) * 4;
-constexpr uint32_t OFF_BAR = OFF_W + 2 * kWeightB;
+constexpr uint32_t OFF_STAGE = OFF_W + 2 * kWeightB;       // image rows on their way out, [16 warps][32 rows][32 columns]
+constexpr uint32_t kWarpStage = 2048;
+constexpr uint32_t OFF_BAR = OFF_STAGE + kComputeWarps * kWarpStage;
 constexpr int kBars = 2 * kStages + 8;
 constexpr uint32_t kSmem = OFF_BAR + kBars * 8 + 16;
 static_assert(kSmem <= 227 * 1024, "shared memory budget");
@@ -119,9 +121,11 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     __syncwarp();
   } else if (warp == kComputeWarps + 2) {
     // ------------------------------------------------------------ gates
+    float4 raw = count > 0 ? fetch_gates(p.g, p.HV, j, geom(0), lane) : make_float4(0.f, 0.f, 0.f, 0.f);
     for (int c = 0; c < count; ++c) {
       double G[4];
-      scan_gates(p.g, p.HV, j, geom(c), lane, G);
+      scan_gates(raw, lane, G);
+      if (c + 1 < count) raw = fetch_gates(p.g, p.HV, j, geom(c + 1), lane);
       if (c > 1) wait_for(&used[c & 1], ((c >> 1) - 1) & 1, abort_flag);
       __syncwarp();
       float* w = reinterpret_cast<float*>(sm + OFF_W + (c & 1) * kWeightB);
@@ -161,31 +165,28 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       wait_for(&weights[b], (c >> 1) & 1, abort_flag);
       wait_for(&full[st], (c / kStages) & 1, abort_flag);
       __syncwarp();
-      if (L < kStep) {                                     // (a product's rows past the end: weight 0 is not enough for NaN)
+      if (L < kStep) {                                     // (rows behind the sequence may be NaN, which no weight of zero masks)
+        clear_rows(tile, L, tid, 32 * kComputeWarps);
         clear_rows(tile + kTileBytes, L, tid, 32 * kComputeWarps);
         fence_proxy_async_smem();
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * kComputeWarps) : "memory");
       }
-      const float* w = reinterpret_cast<const float*>(sm + OFF_W + b * kWeightB) + 32 * g;
-      const uint8_t* src = tile + (key >> 6) * 16384 + 32 * g * 128 + (key & 7) * 2;
-      const int chunk = (key & 63) >> 3;
+      // 16 keys x 16 tokens at a time, transposed by ldmatrix; this lane's tokens are 2 (lane % 4), + 1 of each eight
+      const float* w = reinterpret_cast<const float*>(sm + OFF_W + b * kWeightB) + 32 * g + 2 * (lane & 3);
+      const uint32_t keys = smem_u32(tile) + (q >> 1) * 16384;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        uint32_t hi[8], lo[8];
+      for (int tk = 0; tk < 32; tk += 16) {
+        const float2 f0 = *reinterpret_cast<const float2*>(w + tk), f1 = *reinterpret_cast<const float2*>(w + tk + 8);
 #pragma unroll
-        for (int t = 0; t < 16; t += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(w + 16 * half + t);
-          float x[4];
+        for (int hl = 0; hl < 2; ++hl) {
+          uint32_t x[4], hi[4], lo[4];
+          ldsm4t(x, keys + sw128_offset(32 * g + tk + (lane >> 4) * 8 + (lane & 7), (4 * q + 2 * hl + ((lane >> 3) & 1)) & 7));
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 16 * half + t + e;
-            const uint16_t v = *reinterpret_cast<const uint16_t*>(src + r * 128 + ((chunk ^ (r & 7)) << 4));
-            x[e] = 32 * g + r < L ? __uint_as_float((uint32_t)v << 16) * (&f.x)[e] : 0.f;
-          }
-          split_bf16(x[0], x[1], hi[t / 2], lo[t / 2]);
-          split_bf16(x[2], x[3], hi[t / 2 + 1], lo[t / 2 + 1]);
+          for (int e = 0; e < 4; ++e) split_bf16(mul2(unpack_bf16(x[e]), e < 2 ? f0 : f1), hi[e], lo[e]);
+          const uint32_t at = TM_A + 128 * b + lanes + (static_cast<uint32_t>(16 * hl) << 16) + 16 * g + tk / 2;
+          tmem_st_16x128b_x2(at, hi);
+          tmem_st_16x128b_x2(at + 64, lo);
         }
-        tmem_st8(TM_A + 128 * b + lanes + 16 * g + 8 * half, hi);
-        tmem_st8(TM_A + 128 * b + 64 + lanes + 16 * g + 8 * half, lo);
       }
       tmem_st_wait();
       tc_fence_before_sync();
@@ -203,20 +204,27 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         for (int k = 0; k < 4; ++k)
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
-            if (PIECES == 2) split_bf16(h[8 * k + 2 * w], h[8 * k + 2 * w + 1], (&hi[k].x)[w], (&lo[k].x)[w]);
-            else (&hi[k].x)[w] = pack_bf16(h[8 * k + 2 * w], h[8 * k + 2 * w + 1]);
+            const float2 x = make_float2(h[8 * k + 2 * w], h[8 * k + 2 * w + 1]);
+            if (PIECES == 2) split_bf16(x, (&hi[k].x)[w], (&lo[k].x)[w]);
+            else (&hi[k].x)[w] = pack_bf16(x);
           }
-        exchange4(hi, lane);
-        if (PIECES == 2) exchange4(lo, lane);
+        // by way of shared memory, so that a store covers 64 bytes of eight rows: a row to a thread it takes the memory pipe four times as long
+        uint8_t* mine = sm + OFF_STAGE + warp * kWarpStage;
+        auto put = [&](const uint4 (&x)[4], uint8_t* dst) {
+          __syncwarp();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int row = 32 * q + (lane & ~3) + k, off = row * 128 + (((4 * (g & 1) + (lane & 3)) ^ (row & 7)) << 4);
-          *reinterpret_cast<uint4*>(image + off) = hi[k];
-          if (PIECES == 2) *reinterpret_cast<uint4*>(image + kTileBytes + off) = lo[k];
-        }
+          for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(mine + sw64_offset(lane, k)) = x[k];
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int r = 8 * k + (lane >> 2), row = 32 * q + r;
+            *reinterpret_cast<uint4*>(dst + row * 128 + (((4 * (g & 1) + (lane & 3)) ^ (row & 7)) << 4)) = *reinterpret_cast<const uint4*>(mine + sw64_offset(r, lane & 3));
+          }
+        };
+        put(hi, image);
+        if (PIECES == 2) put(lo, image + kTileBytes);
       }
       const float2 f = *reinterpret_cast<const float2*>(sm + OFF_W + b * kWeightB + kStep * 4);
-      const float decay = f.x;
       wait_for(&product[b], (c >> 1) & 1, abort_flag);
       __syncwarp();
       tc_fence_after_sync();
@@ -224,8 +232,12 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       tmem_ld32(TM_D + 128 * b + lanes + 32 * g, d);
       tmem_ld_wait();
 #pragma unroll
-      for (int k = 0; k < 32; ++k) h[k] = fmaf(decay, h[k], f.y * __uint_as_float(d[k]));
-      total *= decay;
+      for (int k = 0; k < 32; k += 2) {
+        const float2 x = fma2(make_float2(f.x, f.x), make_float2(h[k], h[k + 1]), mul2(make_float2(f.y, f.y), as_f2(d[k], d[k + 1])));
+        h[k] = x.x;
+        h[k + 1] = x.y;
+      }
+      total *= f.x;
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&used[b]);

@@ -80,6 +80,17 @@ __device__ __forceinline__ void split_bf16(float x, float y, uint32_t& hi, uint3
   const float2 h = unpack_bf16(hi);
   lo = pack_bf16(x - h.x, y - h.y);
 }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {   // two fp32 sums in one instruction
+  float2 c;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(c.x), "=f"(c.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return c;
+}
+// ... of a pair, its difference from the high part in one instruction
+__device__ __forceinline__ void split_bf16(float2 x, uint32_t& hi, uint32_t& lo) {
+  hi = pack_bf16(x);
+  lo = pack_bf16(fma2(unpack_bf16(hi), make_float2(-1.f, -1.f), x));
+}
 __device__ __forceinline__ float ex2(float x) {          // 2^x, flushes to zero for very negative x
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -247,6 +247,12 @@ __device__ __forceinline__ void tmem_st_16x256b_x1(uint32_t taddr, const uint32_
   asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1, %2, %3, %4};"
                ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
+// Shape 16x128b: 16 lanes by 8 columns; registers 0, 1 of thread t are column t % 4 of lanes t / 4 and t / 4 + 8, registers 2, 3
+// column 4 + t % 4: a 16 x 16 fragment of 16-bit values, as ldmatrix brings it, in its own order.
+__device__ __forceinline__ void tmem_st_16x128b_x2(uint32_t taddr, const uint32_t (&r)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1, %2, %3, %4};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
 // Registers -> tensor memory, shape 32x32b: thread t of the warp writes 16 consecutive 32-bit columns of lane
 // (taddr.lane + t).  Used for bf16 A operands kept in tensor memory (two K-neighbours per column, low half first).
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
