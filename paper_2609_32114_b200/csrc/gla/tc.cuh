@@ -140,10 +140,12 @@ __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, boo
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) umma_ss(d, da + step_cols(ks), db + step_rows(ks), kIdRows, add || ks > 0);
 }
+// (`pitch`: columns from one 32 k of A to the next)
+template <int pitch = 16>
 __device__ __forceinline__ void mma_tmem_rows(uint32_t d, uint32_t a, uint32_t b, bool add) {
   const uint64_t db = desc_rows(b);
 #pragma unroll
-  for (int ks = 0; ks < 8; ++ks) umma_ts(d, a + 8 * ks, db + step_rows(ks), kIdRows, add || ks > 0);
+  for (int ks = 0; ks < 8; ++ks) umma_ts(d, a + pitch * (ks >> 1) + 8 * (ks & 1), db + step_rows(ks), kIdRows, add || ks > 0);
 }
 
 // Sequences as the state kernel walks them

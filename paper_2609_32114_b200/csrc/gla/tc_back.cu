@@ -8,12 +8,15 @@
 // dg is a sum of, come of them alone: with h and dh as two bf16 pieces they keep the accuracy of fp32.  E = S dS is taken of the fp32
 // accumulators.  P and dS are rounded to bf16 for the products that give dq, dk and dv, which are rounded to bf16 anyway.
 //
-// Shared memory has seven slots for the eight tiles of a unit (Q, K, dO, V, two pieces of h and of dh; the last goes where dO was), assigned anew each unit so
+// Shared memory has seven slots for the eight tiles of a unit (Q, K, dO, V, two pieces of h and of dh; the last goes where Q was), assigned anew each unit so
 // that what the next unit needs first goes where this one is done first.  Tensor memory: four regions of 128 columns,
-//   R0: S | dP^T | dq by h | dv by dh      R1: dP | dq by dS | dk by dS      R2: S^T | dv by P      R3: operands dS, then dS^T and P^T | dk by dh
+//   R0: S, then dS | dq by h | dv by P      R1: dP | dq by dS | dk by dS      R2: S^T, then P^T | dv by dh      R3: dP^T, then dS^T | dk by dh
+// An operand lies over the scores that it is made of: a warp writes its 32 columns, 16 words, over the first half of the 32 accumulator columns
+// that it alone has read, and a product's steps of 16 k go from one such half to the next.  So all four scores become operands in one phase, in which the
+// triangles on either side of the diagonal share out evenly over the warps (dS below it, the transposed ones above).
 // One more warp scans the next unit's gates and adds up dg of the last one; the sums over a row's columns, which four warps share, pass through a
 // few KiB of workspace that stay in L2.
-// What bounds it: 352 KiB of tiles, images and gradients a unit, and a unit's dependent phases (measured below, tc_back in the figures of the call).
+// What bounds it: 352 KiB of tiles, images and gradients a unit, and a unit's dependent phases.
 #include "tc.cuh"
 
 namespace ha_la {
@@ -26,11 +29,11 @@ constexpr int kThreads = 32 * (kComputeWarps + 3);
 struct BackGates { float hi[kStep], lo[kStep], er[kStep], ec[kStep], bb[64], ghi, glo; float pad[2]; };   // (as StepGates; G_L = ghi + glo)
 constexpr uint32_t OFF_G = kSlots * kTileBytes;
 constexpr uint32_t OFF_BAR = OFF_G + sizeof(BackGates);
-constexpr int kBars = 2 * kSlots + 16;
+constexpr int kBars = 2 * kSlots + 12;
 constexpr uint32_t kSmem = OFF_BAR + kBars * 8 + 16;
 static_assert(kSmem <= 227 * 1024 && sizeof(BackGates) % 16 == 0, "shared memory budget");
 constexpr uint32_t R0 = 0, R1 = 128, R2 = 256, R3 = 384;
-enum { kQ, kK, kDO, kV, kHH, kHL, kDH, kDL };              // tiles in the order they are loaded; kDL lies where kDO was
+enum { kQ, kK, kDO, kV, kHH, kHL, kDH, kDL };              // tiles in the order they are loaded; kDL lies where kQ was
 
 struct BackParams {
   const float* g;
@@ -50,12 +53,12 @@ struct BackParams {
 struct Slots {
   int s[kSlots] = {0, 1, 2, 3, 4, 5, 6};
   uint32_t parity = 0;
-  __device__ __forceinline__ int at(int tile) const { return s[tile == kDL ? kDO : tile]; }
+  __device__ __forceinline__ int at(int tile) const { return s[tile == kDL ? kQ : tile]; }
   __device__ __forceinline__ uint32_t fill(int tile) const { return (parity >> at(tile) & 1) ^ (tile == kDL ? 1 : 0); }
   __device__ __forceinline__ void next() {
-    parity ^= 0x7f ^ (1u << s[kDO]);
-    const int k = s[kK], o = s[kDO], v = s[kV], hh = s[kHH], hl = s[kHL], dh = s[kDH];
-    s[kK] = hh; s[kDO] = hl; s[kV] = dh; s[kHH] = v; s[kHL] = o; s[kDH] = k;
+    parity ^= 0x7f ^ (1u << s[kQ]);
+    const int q = s[kQ], k = s[kK], o = s[kDO], hh = s[kHH], hl = s[kHL], dh = s[kDH];
+    s[kQ] = o; s[kK] = hh; s[kDO] = hl; s[kHH] = dh; s[kHL] = q; s[kDH] = k;   // (V stays)
   }
 };
 
@@ -67,9 +70,9 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   uint64_t* bar = reinterpret_cast<uint64_t*>(sm + OFF_BAR);
   uint64_t *full = bar, *empty = bar + kSlots;             // [kSlots]
   uint64_t* one = bar + 2 * kSlots;                        // by one thread or by the tensor cores:
-  uint64_t *gates = one, *b_s = one + 1, *b_dpt = one + 2, *b_dq1 = one + 3, *b_dq2 = one + 4, *b_dv = one + 5, *b_dk = one + 6;
-  uint64_t* all = one + 7;                                 // by the compute warps:
-  uint64_t *g_free = all, *clean = all + 1, *e1 = all + 2, *e2 = all + 3, *e_q = all + 4, *e_v = all + 5, *e_d = all + 6, *e_k = all + 7;
+  uint64_t *gates = one, *b_s = one + 1, *b_dq = one + 2, *b_dv = one + 3, *b_dk = one + 4;
+  uint64_t* all = one + 5;                                 // by the compute warps:
+  uint64_t *g_free = all, *clean = all + 1, *e_s = all + 2, *e_q = all + 3, *e_v = all + 4, *e_d = all + 5, *e_k = all + 6;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -156,26 +159,23 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         loaded(kDO);
         loaded(kV);
         mma_cols(R1, tile(kDO), tile(kV), false);          // dP
+        mma_cols(R3, tile(kV), tile(kDO), false);          // dP^T
         umma_commit(b_s);
-        wait(e1, ph);
-        mma_cols(R0, tile(kV), tile(kDO), false);          // dP^T
-        umma_commit(b_dpt);
-        mma_tmem_rows(R1, R3, tile(kK), false);            // dS K
-        umma_commit(b_dq1);
-        wait(e2, ph);
-        mma_tmem_rows(R2, R3 + 64, tile(kDO), false);      // P^T dO
+        wait(e_s, ph);
+        mma_tmem_rows<32>(R1, R0, tile(kK), false);        // dS K
         loaded(kHH);
         mma_cols(R0, tile(kDO), tile(kHH), false);         // dO h^T
         loaded(kHL);
         mma_cols(R0, tile(kDO), tile(kHL), true);
-        umma_commit(b_dq2);
-        umma_commit(&empty[sl.at(kDO)]);
+        umma_commit(b_dq);
         wait(e_q, ph);
-        loaded(kDH);
-        mma_rows(R0, tile(kK), tile(kDH), false);          // K dh
-        umma_commit(b_dv);
-        mma_tmem_rows(R1, R3, tile(kQ), false);            // dS^T Q
+        mma_tmem_rows<32>(R1, R3, tile(kQ), false);        // dS^T Q
         umma_commit(&empty[sl.at(kQ)]);
+        mma_tmem_rows<32>(R0, R2, tile(kDO), false);       // P^T dO
+        umma_commit(&empty[sl.at(kDO)]);
+        loaded(kDH);
+        mma_rows(R2, tile(kK), tile(kDH), false);          // K dh
+        umma_commit(b_dv);
         mma_cols(R3, tile(kV), tile(kDH), false);          // V dh^T
         loaded(kDL);
         mma_cols(R3, tile(kV), tile(kDL), true);
@@ -303,25 +303,23 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       tmem_ld32(second + lanes + 32 * g, b);
       tmem_ld_wait();
       if (tile < 0) arrive(read);
-#pragma unroll
-      for (int k = 0; k < 32; ++k) a[k] = __float_as_uint(f * __uint_as_float(a[k]));
       if (tile >= 0) {
-        float d = base;
+        float2 d = make_float2(0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const uint4 r = piece(tile, k);
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const float2 t = unpack_bf16((&r.x)[w]);
-            d = fmaf(__uint_as_float(a[8 * k + 2 * w]), t.x, d);
-            d = fmaf(__uint_as_float(a[8 * k + 2 * w + 1]), t.y, d);
-          }
+          for (int w = 0; w < 4; ++w) d = fma2(as_f2(a[8 * k + 2 * w], a[8 * k + 2 * w + 1]), unpack_bf16((&r.x)[w]), d);
         }
-        __stcg(sum, d);
+        __stcg(sum, fmaf(f, d.x + d.y, base));
         arrive(read);
       }
 #pragma unroll
-      for (int k = 0; k < 32; ++k) a[k] = __float_as_uint(__uint_as_float(a[k]) + __uint_as_float(b[k]));
+      for (int k = 0; k < 32; k += 2) {
+        const float2 v = fma2(as_f2(a[k], a[k + 1]), make_float2(f, f), as_f2(b[k], b[k + 1]));
+        a[k] = __float_as_uint(v.x);
+        a[k + 1] = __float_as_uint(v.y);
+      }
       if (acc) {
         float4* mine = acc + tid;
         if (x.r > 0) {
@@ -385,104 +383,88 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       }
       const float hi = s->hi[i], lo = s->lo[i];
       const float eg = p.scale * ex2(hi + lo), el = ex2((s->ghi - hi) + (s->glo - lo));
-      float z = 0.f;                                       // x_i + R_i - C_i of these columns
 
-      // ---- dS (row i, columns j) as operand; R_i
+      // ---- operands: dS (row i, columns j <= i), and with the roles of rows and columns exchanged P^T and dS^T; R_i - C_i of these columns
       wait(b_s, ph);
-      {
-        uint32_t w[16];
+      float2 zr = make_float2(0.f, 0.f), zc = make_float2(0.f, 0.f);
+      // decays of 16 columns from 32 g + 16 b, masked; `below`: of columns before the row
+      auto decays = [&](bool below, int b, float2 (&dec)[8]) {
+        if (g != q) {
+          const float f = p.scale * (below ? s->er[i] * s->bb[8 * (i >> 4) + 2 * g + b] : s->ec[i] * s->bb[8 * (2 * g + b) + (i >> 4)]);
+          const float* e = (below ? s->ec : s->er) + 32 * g + 16 * b;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float4 c = *reinterpret_cast<const float4*>(e + 4 * k);
+            dec[2 * k] = mul2(make_float2(f, f), make_float2(c.x, c.y));
+            dec[2 * k + 1] = mul2(make_float2(f, f), make_float2(c.z, c.w));
+          }
+        } else {
+          const float2 sign = below ? make_float2(-1.f, -1.f) : make_float2(1.f, 1.f);
+          const float h0 = below ? hi : -hi, l0 = below ? lo : -lo;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int at = 16 * b + 2 * k;
+            const float2 a = fma2(*reinterpret_cast<const float2*>(&s->hi[32 * g + at]), sign, make_float2(h0, h0)),
+                         c = fma2(*reinterpret_cast<const float2*>(&s->lo[32 * g + at]), sign, make_float2(l0, l0));
+            dec[k].x = (below ? at <= lane : at >= lane) ? p.scale * ex2(a.x + c.x) : 0.f;
+            dec[k].y = (below ? at + 1 <= lane : at + 1 >= lane) ? p.scale * ex2(a.y + c.y) : 0.f;
+          }
+        }
+      };
+      // ds = dec dP; z += ds S but on the diagonal
+      auto score = [&](const float2 dec, float2 dp, float2 sc, int at, float2& z) {
+        const float2 ds = mul2(dec, dp);
+        z = fma2(g != q ? ds : make_float2(at == lane ? 0.f : ds.x, at + 1 == lane ? 0.f : ds.y), sc, z);
+        return pack_bf16(ds);
+      };
+      const uint32_t slice = lanes + 32 * g;
+#pragma unroll 1
+      for (int b = 0; b < 2; ++b) {
+        uint32_t w[8] = {};
         if (g <= q) {
+          uint32_t rs[16], rp[16];
+          tmem_ld16(R0 + slice + 16 * b, rs);
+          tmem_ld16(R1 + slice + 16 * b, rp);
+          float2 dec[8];
+          decays(true, b, dec);
+          tmem_ld_wait();
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            uint32_t rs[16], rp[16];
-            tmem_ld16(R0 + lanes + 32 * g + 16 * b, rs);
-            tmem_ld16(R1 + lanes + 32 * g + 16 * b, rp);
-            float dec[16];
-            if (g < q) {
-              const float f = p.scale * s->er[i] * s->bb[8 * (i >> 4) + 2 * g + b];
-#pragma unroll
-              for (int k = 0; k < 16; k += 4) {
-                const float4 e = *reinterpret_cast<const float4*>(&s->ec[32 * g + 16 * b + k]);
-                dec[k] = f * e.x; dec[k + 1] = f * e.y; dec[k + 2] = f * e.z; dec[k + 3] = f * e.w;
-              }
-            } else {
-#pragma unroll
-              for (int k = 0; k < 16; ++k)
-                dec[k] = 16 * b + k <= lane ? p.scale * ex2((hi - s->hi[32 * g + 16 * b + k]) + (lo - s->lo[32 * g + 16 * b + k])) : 0.f;
-            }
-            tmem_ld_wait();
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              dec[k] *= __uint_as_float(rp[k]);
-              if (g < q || 16 * b + k < lane) z = fmaf(dec[k], __uint_as_float(rs[k]), z);
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) w[8 * b + k] = pack_bf16(dec[2 * k], dec[2 * k + 1]);
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < 16; ++k) w[k] = 0u;
+          for (int k = 0; k < 8; ++k) w[k] = score(dec[k], as_f2(rp[2 * k], rp[2 * k + 1]), as_f2(rs[2 * k], rs[2 * k + 1]), 16 * b + 2 * k, zr);
         }
-        tmem_st16(R3 + lanes + 16 * g, w);
-        tmem_st_wait();
-        arrive(e1);
+        tmem_st8(R0 + slice + 8 * b, w);
       }
-      // ---- P^T and dS^T (row j, columns i) as operands; C_j
-      wait(b_dpt, ph);
-      {
-        uint32_t wp[16], ws[16];
+#pragma unroll 1
+      for (int b = 0; b < 2; ++b) {
+        uint32_t wp[8] = {}, ws[8] = {};
         if (g >= q) {
+          uint32_t rs[16], rp[16];
+          tmem_ld16(R2 + slice + 16 * b, rs);
+          tmem_ld16(R3 + slice + 16 * b, rp);
+          float2 dec[8];
+          decays(false, b, dec);
+          tmem_ld_wait();
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            uint32_t rs[16], rp[16];
-            tmem_ld16(R2 + lanes + 32 * g + 16 * b, rs);
-            tmem_ld16(R0 + lanes + 32 * g + 16 * b, rp);
-            float dec[16];
-            if (g > q) {
-              const float f = p.scale * s->ec[i] * s->bb[8 * (2 * g + b) + (i >> 4)];
-#pragma unroll
-              for (int k = 0; k < 16; k += 4) {
-                const float4 e = *reinterpret_cast<const float4*>(&s->er[32 * g + 16 * b + k]);
-                dec[k] = f * e.x; dec[k + 1] = f * e.y; dec[k + 2] = f * e.z; dec[k + 3] = f * e.w;
-              }
-            } else {
-#pragma unroll
-              for (int k = 0; k < 16; ++k)
-                dec[k] = 16 * b + k >= lane ? p.scale * ex2((s->hi[32 * g + 16 * b + k] - hi) + (s->lo[32 * g + 16 * b + k] - lo)) : 0.f;
-            }
-            tmem_ld_wait();
-#pragma unroll
-            for (int k = 0; k < 16; k += 2) {
-              float ds[2];
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                ds[e] = dec[k + e] * __uint_as_float(rp[k + e]);
-                if (g > q || 16 * b + k + e > lane) z = fmaf(-ds[e], __uint_as_float(rs[k + e]), z);
-              }
-              wp[8 * b + k / 2] = pack_bf16(dec[k] * __uint_as_float(rs[k]), dec[k + 1] * __uint_as_float(rs[k + 1]));
-              ws[8 * b + k / 2] = pack_bf16(ds[0], ds[1]);
-            }
+          for (int k = 0; k < 8; ++k) {
+            wp[k] = pack_bf16(mul2(dec[k], as_f2(rs[2 * k], rs[2 * k + 1])));
+            ws[k] = score(dec[k], as_f2(rp[2 * k], rp[2 * k + 1]), as_f2(rs[2 * k], rs[2 * k + 1]), 16 * b + 2 * k, zc);
           }
-        } else {
-#pragma unroll
-          for (int k = 0; k < 16; ++k) wp[k] = ws[k] = 0u;
         }
-        wait(b_dq1, ph);                                   // (dS has been read where dS^T goes)
-        tmem_st16(R3 + lanes + 16 * g, ws);
-        tmem_st16(R3 + 64 + lanes + 16 * g, wp);
-        tmem_st_wait();
-        arrive(e2);
-        if (lane == 0) mbar_arrive(g_free);
+        tmem_st8(R2 + slice + 8 * b, wp);
+        tmem_st8(R3 + slice + 8 * b, ws);
       }
+      tmem_st_wait();
+      arrive(e_s);
+      if (lane == 0) mbar_arrive(g_free);
+      const float z = (zr.x + zr.y) - (zc.x + zc.y);
       const int head_k = x.j / R, run = x.j / p.per, heads_k = p.part_q ? runs : p.HK, out_k = p.part_q ? run : head_k;
       float* mine = sums + ph * kSums;
       // ---- dq
-      wait(b_dq2, ph);
+      wait(b_dq, ph);
       seen(kQ);
       gradient(R0, R1, eg, sl.at(kQ), z, mine + g * kStep + i, e_q, x, shared_q, p.dq, p.part_q, heads_k, out_k);
       // ---- dv
       wait(b_dv, ph);
-      gradient(R0, R2, el, -1, 0.f, nullptr, e_v, x, nullptr, p.dv, nullptr, p.HV, x.j);
+      gradient(R2, R0, el, -1, 0.f, nullptr, e_v, x, nullptr, p.dv, nullptr, p.HV, x.j);
       // ---- <h, dh>
       float d = 0.f;
 #pragma unroll
