@@ -91,6 +91,7 @@ __device__ __forceinline__ void fill_gates(StepGates* s, const double (&G)[4], i
 
 // Rows L .. 127 of a tile to zero, by `n` threads: what lies behind a sequence may be NaN, and zero weights would not mask that.
 __device__ __forceinline__ void clear_rows(uint8_t* tile, int L, int tid, int n) {
+#pragma unroll 1
   for (int i = tid; i < (kStep - L) * 16; i += n)
     *reinterpret_cast<uint4*>(tile + (i & 1) * 16384 + (L + (i >> 4)) * 128 + ((i >> 1) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
 }
@@ -116,9 +117,12 @@ __device__ __forceinline__ void exchange4(uint4 (&v)[4], int lane) {
   swap(v[1], v[3], lane & 2, 2);
 }
 
-// Polls once before it waits: mbarrier.try_wait costs its caller some 150 cycles even when the phase is over.
+// Polls once before it waits: mbarrier.try_wait costs its caller some 150 cycles even when the phase is over.  The wait itself is a function of
+// its own: in line it is a KiB of instructions at each of some sixty places, and the gradient kernel's warps waited for instructions a quarter of
+// their time.
+static __device__ __noinline__ void wait_long(uint64_t* bar, uint32_t parity, volatile int* abort_flag) { mbar_wait(bar, parity, abort_flag); }
 __device__ __forceinline__ void wait_for(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  if (!mbar_test_wait(bar, parity)) mbar_wait(bar, parity, abort_flag);
+  if (!mbar_test_wait(bar, parity)) wait_long(bar, parity, abort_flag);
 }
 
 // A tile's descriptors as B operand: over its columns (k index = columns, N = rows) or over its rows (k index = rows, N = columns), and

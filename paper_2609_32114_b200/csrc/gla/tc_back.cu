@@ -72,7 +72,7 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   uint64_t* one = bar + 2 * kSlots;                        // by one thread or by the tensor cores:
   uint64_t *gates = one, *b_s = one + 1, *b_dq = one + 2, *b_dv = one + 3, *b_dk = one + 4;
   uint64_t* all = one + 5;                                 // by the compute warps:
-  uint64_t *g_free = all, *clean = all + 1, *e_s = all + 2, *e_q = all + 3, *e_v = all + 4, *e_d = all + 5, *e_k = all + 6;
+  uint64_t *g_free = all, *clean = all + 1, *e_s = all + 2, *e_d = all + 3, *e_q = all + 4, *e_v = all + 5, *e_k = all + 6;   // (e_q, e_v, e_k and b_dq, b_dv, b_dk in a row)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -110,11 +110,12 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   if (warp == kComputeWarps) {
     // ------------------------------------------------------------ tiles
     if (elect_one()) {
-      Unit x = unit(0);
-      for (int u = 0; x.c.L > 0 && !*abort_flag; ++u) {
-        const Unit after = unit(u + 1);
+      Unit x{{0, 1}, 0, 0, 0};
+      for (int u = -1; x.c.L > 0 && !*abort_flag; ++u) {
+        const Unit after = unit(u + 1);                    // (its look-ups under the waits, here and below)
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
+          if (u < 0) break;
           const int at = sl.at(t);
           wait_for(&empty[at], sl.fill(t) ^ 1, abort_flag);
           if (*abort_flag) break;
@@ -126,7 +127,7 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           else if (t == kV) tma_load_4d(dst, &map_v, &full[at], 0, x.j, x.c.tok0, 0);
           else bulk_load(dst, (t < kDH ? p.image : p.image_back) + (2 * x.sj + (t == kHL || t == kDL)) * kTileBytes, kTileBytes, &full[at]);
         }
-        sl.next();
+        if (u >= 0) sl.next();
         x = after;
       }
     }
@@ -134,11 +135,15 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   } else if (warp == kComputeWarps + 1) {
     // ------------------------------------------------------------ products
     if (elect_one()) {
-      Unit x = unit(0);
+      Unit x{{0, 1}, 0, 0, 0};
       uint32_t tails = 0;
       int last_k = 0;
-      for (int u = 0; x.c.L > 0; ++u) {
+      for (int u = -1; x.c.L > 0; ++u) {
         const Unit after = unit(u + 1);
+        if (u < 0) {
+          x = after;
+          continue;
+        }
         const uint32_t ph = u & 1;
         auto tile = [&](int t) { return smem_u32(sm + sl.at(t) * kTileBytes); };
         auto wait = [&](uint64_t* b, uint32_t parity) {
@@ -290,204 +295,181 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       wait_for(&full[sl.at(t)], sl.fill(t), abort_flag);
       __syncwarp();
     };
-    // 16-byte piece k of this thread's 32 columns in its row of a tile
+    // 16-byte piece k of this thread's 32 columns in its row of the tile in a slot
     auto piece = [&](int at, int k) {
       return *reinterpret_cast<const uint4*>(sm + at * kTileBytes + (g >> 1) * 16384 + i * 128 + (((4 * (g & 1) + k) ^ (i & 7)) << 4));
     };
-    // a f + b, 32 columns of a row.  With `tile`: base + a f . (the tile's row) to `sum`.  With `acc`: added to what the run's V-heads before
-    // left there, and left there for the next ones.  `read` follows the sum.
-    auto gradient = [&](uint32_t first, uint32_t second, float f, int tile, float base, float* sum, uint64_t* read, const Unit& x, float4* acc,
-                        void* out, float* part, int heads, int head) {
-      uint32_t a[32], b[32];
-      tmem_ld32(first + lanes + 32 * g, a);
-      tmem_ld32(second + lanes + 32 * g, b);
-      tmem_ld_wait();
-      if (tile < 0) arrive(read);
-      if (tile >= 0) {
-        float2 d = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint4 r = piece(tile, k);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) d = fma2(as_f2(a[8 * k + 2 * w], a[8 * k + 2 * w + 1]), unpack_bf16((&r.x)[w]), d);
-        }
-        __stcg(sum, fmaf(f, d.x + d.y, base));
-        arrive(read);
-      }
-#pragma unroll
-      for (int k = 0; k < 32; k += 2) {
-        const float2 v = fma2(as_f2(a[k], a[k + 1]), make_float2(f, f), as_f2(b[k], b[k + 1]));
-        a[k] = __float_as_uint(v.x);
-        a[k + 1] = __float_as_uint(v.y);
-      }
-      if (acc) {
-        float4* mine = acc + tid;
-        if (x.r > 0) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float4 t = __ldcg(mine + 512 * k);
-            a[4 * k] = __float_as_uint(__uint_as_float(a[4 * k]) + t.x);
-            a[4 * k + 1] = __float_as_uint(__uint_as_float(a[4 * k + 1]) + t.y);
-            a[4 * k + 2] = __float_as_uint(__uint_as_float(a[4 * k + 2]) + t.z);
-            a[4 * k + 3] = __float_as_uint(__uint_as_float(a[4 * k + 3]) + t.w);
-          }
-        }
-        if (x.r < p.per - 1) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            __stcg(mine + 512 * k, make_float4(__uint_as_float(a[4 * k]), __uint_as_float(a[4 * k + 1]), __uint_as_float(a[4 * k + 2]), __uint_as_float(a[4 * k + 3])));
-          return;
-        }
-      }
-      const int row = 32 * q + (lane & ~3), left = x.c.L - row;
-      if (part) {
-        float* dst = part + ((size_t)(x.c.tok0 + row) * heads + head) * 128 + 32 * g + 4 * (lane & 3);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint4 o[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) o[k] = make_uint4(a[16 * half + 4 * k], a[16 * half + 4 * k + 1], a[16 * half + 4 * k + 2], a[16 * half + 4 * k + 3]);
-          exchange4(o, lane);
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (k < left) *reinterpret_cast<uint4*>(dst + (size_t)k * heads * 128 + 16 * half) = o[k];
-        }
-      } else {
-        uint4 o[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          o[k] = make_uint4(pack_bf16(as_f2(a[8 * k], a[8 * k + 1])), pack_bf16(as_f2(a[8 * k + 2], a[8 * k + 3])),
-                            pack_bf16(as_f2(a[8 * k + 4], a[8 * k + 5])), pack_bf16(as_f2(a[8 * k + 6], a[8 * k + 7])));
-        exchange4(o, lane);
-        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(out) + ((size_t)(x.c.tok0 + row) * heads + head) * 128 + 32 * g + 8 * (lane & 3);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (k < left) *reinterpret_cast<uint4*>(dst + (size_t)k * heads * 128) = o[k];
-      }
-    };
-    float4* shared_q = p.per > 1 ? p.shared + (size_t)blockIdx.x * 2 * 8 * 512 : nullptr;
-    float4* shared_k = p.per > 1 ? shared_q + 8 * 512 : nullptr;
-    Unit x = unit(0);
-    for (int u = 0; x.c.L > 0; ++u) {
+    float4* acc = p.per > 1 ? p.shared + (size_t)blockIdx.x * 2 * 8 * 512 + tid : nullptr;
+    // What the loop over units executes has to stay small, or the warps wait for their instructions: one body for the operands below and above the
+    // diagonal, one for the three gradients.
+    Unit x{{0, 1}, 0, 0, 0};
+    for (int u = -1; x.c.L > 0; ++u) {
       const Unit after = unit(u + 1);
-      const uint32_t ph = u & 1;
-      wait_for(gates, ph, abort_flag);
-      if (x.c.L < kStep) {                                 // (rows behind the sequence may be NaN)
+      if (u >= 0) {
+        const uint32_t ph = u & 1;
+        wait_for(gates, ph, abort_flag);
+        if (x.c.L < kStep) {                               // (rows behind the sequence may be NaN)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          wait_for(&full[sl.at(t)], sl.fill(t), abort_flag);
-          clear_rows(sm + sl.at(t) * kTileBytes, x.c.L, tid, 32 * kComputeWarps);
+          for (int t = 0; t < 4; ++t) {
+            wait_for(&full[sl.at(t)], sl.fill(t), abort_flag);
+            clear_rows(sm + sl.at(t) * kTileBytes, x.c.L, tid, 32 * kComputeWarps);
+          }
+          fence_proxy_async_smem();
+          arrive(clean);
         }
-        fence_proxy_async_smem();
-        arrive(clean);
-      }
-      const float hi = s->hi[i], lo = s->lo[i];
-      const float eg = p.scale * ex2(hi + lo), el = ex2((s->ghi - hi) + (s->glo - lo));
+        const float hi = s->hi[i], lo = s->lo[i];
+        const float eg = p.scale * ex2(hi + lo), el = ex2((s->ghi - hi) + (s->glo - lo));
 
-      // ---- operands: dS (row i, columns j <= i), and with the roles of rows and columns exchanged P^T and dS^T; R_i - C_i of these columns
-      wait(b_s, ph);
-      float2 zr = make_float2(0.f, 0.f), zc = make_float2(0.f, 0.f);
-      // decays of 16 columns from 32 g + 16 b, masked; `below`: of columns before the row
-      auto decays = [&](bool below, int b, float2 (&dec)[8]) {
-        if (g != q) {
-          const float f = p.scale * (below ? s->er[i] * s->bb[8 * (i >> 4) + 2 * g + b] : s->ec[i] * s->bb[8 * (2 * g + b) + (i >> 4)]);
-          const float* e = (below ? s->ec : s->er) + 32 * g + 16 * b;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float4 c = *reinterpret_cast<const float4*>(e + 4 * k);
-            dec[2 * k] = mul2(make_float2(f, f), make_float2(c.x, c.y));
-            dec[2 * k + 1] = mul2(make_float2(f, f), make_float2(c.z, c.w));
-          }
-        } else {
-          const float2 sign = below ? make_float2(-1.f, -1.f) : make_float2(1.f, 1.f);
-          const float h0 = below ? hi : -hi, l0 = below ? lo : -lo;
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int at = 16 * b + 2 * k;
-            const float2 a = fma2(*reinterpret_cast<const float2*>(&s->hi[32 * g + at]), sign, make_float2(h0, h0)),
-                         c = fma2(*reinterpret_cast<const float2*>(&s->lo[32 * g + at]), sign, make_float2(l0, l0));
-            dec[k].x = (below ? at <= lane : at >= lane) ? p.scale * ex2(a.x + c.x) : 0.f;
-            dec[k].y = (below ? at + 1 <= lane : at + 1 >= lane) ? p.scale * ex2(a.y + c.y) : 0.f;
-          }
-        }
-      };
-      // ds = dec dP; z += ds S but on the diagonal
-      auto score = [&](const float2 dec, float2 dp, float2 sc, int at, float2& z) {
-        const float2 ds = mul2(dec, dp);
-        z = fma2(g != q ? ds : make_float2(at == lane ? 0.f : ds.x, at + 1 == lane ? 0.f : ds.y), sc, z);
-        return pack_bf16(ds);
-      };
-      const uint32_t slice = lanes + 32 * g;
+        // ---- operands, 16 columns at a time: dS (row i, columns j <= i), then with the roles of rows and columns exchanged P^T and dS^T;
+        // z: R_i - C_i of these columns
+        wait(b_s, ph);
+        const uint32_t slice = lanes + 32 * g;
+        float z = 0.f;
 #pragma unroll 1
-      for (int b = 0; b < 2; ++b) {
-        uint32_t w[8] = {};
-        if (g <= q) {
-          uint32_t rs[16], rp[16];
-          tmem_ld16(R0 + slice + 16 * b, rs);
-          tmem_ld16(R1 + slice + 16 * b, rp);
-          float2 dec[8];
-          decays(true, b, dec);
-          tmem_ld_wait();
+        for (int turn = 0; turn < 4; ++turn) {
+          asm volatile("" : "+r"(turn));
+          const int above = turn >> 1, b = turn & 1;
+          uint32_t wp[8] = {}, ws[8] = {};
+          if (above ? g >= q : g <= q) {
+            uint32_t rs[16], rp[16];
+            tmem_ld16((above ? R2 : R0) + slice + 16 * b, rs);
+            tmem_ld16((above ? R3 : R1) + slice + 16 * b, rp);
+            float2 dec[8];                                 // decay, mask and scale
+            if (g != q) {
+              const float f = p.scale * (above ? s->ec[i] * s->bb[8 * (2 * g + b) + (i >> 4)] : s->er[i] * s->bb[8 * (i >> 4) + 2 * g + b]);
+              const float* e = (above ? s->er : s->ec) + 32 * g + 16 * b;
 #pragma unroll
-          for (int k = 0; k < 8; ++k) w[k] = score(dec[k], as_f2(rp[2 * k], rp[2 * k + 1]), as_f2(rs[2 * k], rs[2 * k + 1]), 16 * b + 2 * k, zr);
+              for (int k = 0; k < 4; ++k) {
+                const float4 c = *reinterpret_cast<const float4*>(e + 4 * k);
+                dec[2 * k] = mul2(make_float2(f, f), make_float2(c.x, c.y));
+                dec[2 * k + 1] = mul2(make_float2(f, f), make_float2(c.z, c.w));
+              }
+            } else {
+              const float sign = above ? 1.f : -1.f;
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const int at = 16 * b + 2 * k;
+                const float2 a = fma2(*reinterpret_cast<const float2*>(&s->hi[32 * g + at]), make_float2(sign, sign), make_float2(-sign * hi, -sign * hi)),
+                             c = fma2(*reinterpret_cast<const float2*>(&s->lo[32 * g + at]), make_float2(sign, sign), make_float2(-sign * lo, -sign * lo));
+                dec[k].x = (above ? at >= lane : at <= lane) ? p.scale * ex2(a.x + c.x) : 0.f;
+                dec[k].y = (above ? at + 1 >= lane : at + 1 <= lane) ? p.scale * ex2(a.y + c.y) : 0.f;
+              }
+            }
+            tmem_ld_wait();
+            float2 zz = make_float2(0.f, 0.f);
+            const int diag = g == q ? lane - 16 * b : -1;  // the column whose E counts for neither
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float2 sc = as_f2(rs[2 * k], rs[2 * k + 1]), ds = mul2(dec[k], as_f2(rp[2 * k], rp[2 * k + 1]));
+              wp[k] = pack_bf16(mul2(dec[k], sc));
+              ws[k] = pack_bf16(ds);
+              zz = fma2(make_float2(2 * k == diag ? 0.f : ds.x, 2 * k + 1 == diag ? 0.f : ds.y), sc, zz);
+            }
+            z += above ? -(zz.x + zz.y) : zz.x + zz.y;
+          }
+          tmem_st8((above ? R3 : R0) + slice + 8 * b, ws);
+          if (above) tmem_st8(R2 + slice + 8 * b, wp);
         }
-        tmem_st8(R0 + slice + 8 * b, w);
-      }
+        tmem_st_wait();
+        arrive(e_s);
+        if (lane == 0) mbar_arrive(g_free);
+
+        // ---- dq, dv, dk: a f + b, a the part by the state; with the sums x_i, y_i of a f . (the row of q, k) ahead of e_q, e_k
+        float* mine = sums + ph * kSums;
 #pragma unroll 1
-      for (int b = 0; b < 2; ++b) {
-        uint32_t wp[8] = {}, ws[8] = {};
-        if (g >= q) {
-          uint32_t rs[16], rp[16];
-          tmem_ld16(R2 + slice + 16 * b, rs);
-          tmem_ld16(R3 + slice + 16 * b, rp);
-          float2 dec[8];
-          decays(false, b, dec);
-          tmem_ld_wait();
+        for (int o = 0; o < 3; ++o) {
+          asm volatile("" : "+r"(o));                      // (not three copies of the body)
+          if (o == 2) {                                    // <h, dh>, under the products for dk
+            float2 d = make_float2(0.f, 0.f);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            wp[k] = pack_bf16(mul2(dec[k], as_f2(rs[2 * k], rs[2 * k + 1])));
-            ws[k] = score(dec[k], as_f2(rp[2 * k], rp[2 * k + 1]), as_f2(rs[2 * k], rs[2 * k + 1]), 16 * b + 2 * k, zc);
+            for (int t = kHH; t <= kDL; ++t) seen(t);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint4 h1 = piece(sl.at(kHH), k), h2 = piece(sl.at(kHL), k), d1 = piece(sl.at(kDH), k), d2 = piece(sl.at(kDL), k);
+#pragma unroll
+              for (int w = 0; w < 4; ++w)
+                d = fma2(add2(unpack_bf16((&h1.x)[w]), unpack_bf16((&h2.x)[w])), add2(unpack_bf16((&d1.x)[w]), unpack_bf16((&d2.x)[w])), d);
+            }
+            arrive(e_d);
+            float sum = d.x + d.y;
+#pragma unroll
+            for (int e = 16; e > 0; e >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, e);
+            if (lane == 0) __stcg(mine + 8 * kStep + warp, sum);
+          }
+          wait(b_dq + o, ph);
+          uint32_t a[32], c[32];
+          tmem_ld32((o == 0 ? R0 : o == 1 ? R2 : R3) + slice, a);
+          tmem_ld32((o == 1 ? R0 : R1) + slice, c);
+          const float f = o == 0 ? eg : el;
+          tmem_ld_wait();
+          if (o != 1) {
+            const int tile = o == 0 ? kQ : kK;
+            seen(tile);
+            float2 d = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint4 r = piece(sl.at(tile), k);
+#pragma unroll
+              for (int w = 0; w < 4; ++w) d = fma2(as_f2(a[8 * k + 2 * w], a[8 * k + 2 * w + 1]), unpack_bf16((&r.x)[w]), d);
+            }
+            __stcg(mine + (o == 0 ? 0 : 4 * kStep) + g * kStep + i, fmaf(f, d.x + d.y, o == 0 ? z : 0.f));
+          }
+          arrive(e_q + o);
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) {
+            const float2 v = fma2(as_f2(a[k], a[k + 1]), make_float2(f, f), as_f2(c[k], c[k + 1]));
+            a[k] = __float_as_uint(v.x);
+            a[k + 1] = __float_as_uint(v.y);
+          }
+          if (o != 1 && acc) {                             // added to what the run's V-heads before left, and left for the next ones
+            float4* part = acc + (o == 0 ? 0 : 8 * 512);
+            if (x.r > 0) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const float4 t = __ldcg(part + 512 * k);
+                const float2 v0 = add2(as_f2(a[4 * k], a[4 * k + 1]), make_float2(t.x, t.y)), v1 = add2(as_f2(a[4 * k + 2], a[4 * k + 3]), make_float2(t.z, t.w));
+                a[4 * k] = __float_as_uint(v0.x); a[4 * k + 1] = __float_as_uint(v0.y);
+                a[4 * k + 2] = __float_as_uint(v1.x); a[4 * k + 3] = __float_as_uint(v1.y);
+              }
+            }
+            if (x.r < p.per - 1) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                __stcg(part + 512 * k, make_float4(__uint_as_float(a[4 * k]), __uint_as_float(a[4 * k + 1]), __uint_as_float(a[4 * k + 2]), __uint_as_float(a[4 * k + 3])));
+              continue;
+            }
+          }
+          const int row = 32 * q + (lane & ~3), left = x.c.L - row;
+          const bool parts = o != 1 && p.part_q;
+          const int heads = o == 1 ? p.HV : parts ? runs : p.HK, head = o == 1 ? x.j : parts ? x.j / p.per : x.j / R;
+          const size_t at = ((size_t)(x.c.tok0 + row) * heads + head) * 128 + 32 * g, pitch = (size_t)heads * 128;
+          if (parts) {
+            float* dst = (o == 0 ? p.part_q : p.part_k) + at + 4 * (lane & 3);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              uint4 v[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) v[k] = make_uint4(a[16 * half + 4 * k], a[16 * half + 4 * k + 1], a[16 * half + 4 * k + 2], a[16 * half + 4 * k + 3]);
+              exchange4(v, lane);
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                if (k < left) *reinterpret_cast<uint4*>(dst + k * pitch + 16 * half) = v[k];
+            }
+          } else {
+            uint4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              v[k] = make_uint4(pack_bf16(as_f2(a[8 * k], a[8 * k + 1])), pack_bf16(as_f2(a[8 * k + 2], a[8 * k + 3])),
+                                pack_bf16(as_f2(a[8 * k + 4], a[8 * k + 5])), pack_bf16(as_f2(a[8 * k + 6], a[8 * k + 7])));
+            exchange4(v, lane);
+            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(o == 0 ? p.dq : o == 1 ? p.dv : p.dk) + at + 8 * (lane & 3);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (k < left) *reinterpret_cast<uint4*>(dst + k * pitch) = v[k];
           }
         }
-        tmem_st8(R2 + slice + 8 * b, wp);
-        tmem_st8(R3 + slice + 8 * b, ws);
+        sl.next();
       }
-      tmem_st_wait();
-      arrive(e_s);
-      if (lane == 0) mbar_arrive(g_free);
-      const float z = (zr.x + zr.y) - (zc.x + zc.y);
-      const int head_k = x.j / R, run = x.j / p.per, heads_k = p.part_q ? runs : p.HK, out_k = p.part_q ? run : head_k;
-      float* mine = sums + ph * kSums;
-      // ---- dq
-      wait(b_dq, ph);
-      seen(kQ);
-      gradient(R0, R1, eg, sl.at(kQ), z, mine + g * kStep + i, e_q, x, shared_q, p.dq, p.part_q, heads_k, out_k);
-      // ---- dv
-      wait(b_dv, ph);
-      gradient(R2, R0, el, -1, 0.f, nullptr, e_v, x, nullptr, p.dv, nullptr, p.HV, x.j);
-      // ---- <h, dh>
-      float d = 0.f;
-#pragma unroll
-      for (int t = kHH; t <= kDL; ++t) seen(t);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint4 a = piece(sl.at(kHH), k), b = piece(sl.at(kHL), k), c = piece(sl.at(kDH), k), e = piece(sl.at(kDL), k);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const float2 a2 = unpack_bf16((&a.x)[w]), b2 = unpack_bf16((&b.x)[w]), c2 = unpack_bf16((&c.x)[w]), e2_ = unpack_bf16((&e.x)[w]);
-          d = fmaf(a2.x + b2.x, c2.x + e2_.x, d);
-          d = fmaf(a2.y + b2.y, c2.y + e2_.y, d);
-        }
-      }
-      arrive(e_d);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-      if (lane == 0) __stcg(mine + 8 * kStep + warp, d);
-      // ---- dk (with the unit's sums ahead of its e_k)
-      wait(b_dk, ph);
-      seen(kK);
-      gradient(R3, R1, el, sl.at(kK), 0.f, mine + 4 * kStep + g * kStep + i, e_k, x, shared_k, p.dk, p.part_k, heads_k, out_k);
-      sl.next();
       x = after;
     }
   }
