@@ -96,33 +96,38 @@ __device__ __forceinline__ void clear_rows(uint8_t* tile, int L, int tid, int n)
     *reinterpret_cast<uint4*>(tile + (i & 1) * 16384 + (L + (i >> 4)) * 128 + ((i >> 1) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// Four lanes that hold four 16-byte pieces of a row each exchange them: v[i] becomes this lane's (lane % 4) piece of the row of lane i of the four.
-// A warp's store of v[i] then covers 64 bytes of eight rows instead of 16 of thirty-two: a store takes the memory pipe a cycle for every
-// 128-byte line it touches, and with a row to a thread the stores were what bounded the state kernel (4.9 us a step with two images)
-// and the gradients (15 us a unit).
+// Two (four) lanes that hold two (four) 16-byte pieces of a row each exchange them: v[i] becomes this lane's piece of the row of lane i of the
+// two (four).  A warp's store of v[i] then covers 32 (64) bytes of sixteen (eight) rows instead of 16 of thirty-two: a store takes the memory pipe
+// a cycle for every 128-byte line it touches.
+__device__ __forceinline__ void exchange(uint4& first, uint4& second, bool keep_second, int with) {
+  const uint4 send = keep_second ? first : second;
+  uint4 got;
+  got.x = __shfl_xor_sync(0xffffffffu, send.x, with);
+  got.y = __shfl_xor_sync(0xffffffffu, send.y, with);
+  got.z = __shfl_xor_sync(0xffffffffu, send.z, with);
+  got.w = __shfl_xor_sync(0xffffffffu, send.w, with);
+  if (keep_second) first = got;
+  else second = got;
+}
+__device__ __forceinline__ void exchange2(uint4 (&v)[2], int lane) { exchange(v[0], v[1], lane & 1, 1); }
 __device__ __forceinline__ void exchange4(uint4 (&v)[4], int lane) {
-  auto swap = [](uint4& mine, uint4& theirs, bool keep_second, int with) {
-    const uint4 send = keep_second ? mine : theirs;
-    uint4 got;
-    got.x = __shfl_xor_sync(0xffffffffu, send.x, with);
-    got.y = __shfl_xor_sync(0xffffffffu, send.y, with);
-    got.z = __shfl_xor_sync(0xffffffffu, send.z, with);
-    got.w = __shfl_xor_sync(0xffffffffu, send.w, with);
-    if (keep_second) mine = got;
-    else theirs = got;
-  };
-  swap(v[0], v[1], lane & 1, 1);
-  swap(v[2], v[3], lane & 1, 1);
-  swap(v[0], v[2], lane & 2, 2);
-  swap(v[1], v[3], lane & 2, 2);
+  exchange(v[0], v[1], lane & 1, 1);
+  exchange(v[2], v[3], lane & 1, 1);
+  exchange(v[0], v[2], lane & 2, 2);
+  exchange(v[1], v[3], lane & 2, 2);
 }
 
-// Polls once before it waits: mbarrier.try_wait costs its caller some 150 cycles even when the phase is over.  The wait itself is a function of
-// its own: in line it is a KiB of instructions at each of some sixty places, and the gradient kernel's warps waited for instructions a quarter of
-// their time.
-static __device__ __noinline__ void wait_long(uint64_t* bar, uint32_t parity, volatile int* abort_flag) { mbar_wait(bar, parity, abort_flag); }
+// mbar_wait, with a look ahead of it (mbarrier.try_wait costs its caller some 150 cycles even when the phase is over) and its loop not unrolled: at some
+// sixty places that is most of the gradient kernel's instructions, for which its warps waited a quarter of their time.  (As a function of its own it is
+// shorter still, but what is live across a call does not all stay in registers, and there is hardly any L1 left for the stack.)
 __device__ __forceinline__ void wait_for(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-  if (!mbar_test_wait(bar, parity)) wait_long(bar, parity, abort_flag);
+  if (mbar_test_wait(bar, parity)) return;
+#pragma unroll 1
+  for (uint32_t it = 0; it < kSpinLimit; ++it) {
+    if (mbar_try_wait(bar, parity)) return;
+    if ((it & 255u) == 255u && *abort_flag) return;
+  }
+  *abort_flag = 1;
 }
 
 // A tile's descriptors as B operand: over its columns (k index = columns, N = rows) or over its rows (k index = rows, N = columns), and
@@ -144,12 +149,12 @@ __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, boo
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) umma_ss(d, da + step_cols(ks), db + step_rows(ks), kIdRows, add || ks > 0);
 }
-// (`pitch`: columns from one 32 k of A to the next)
-template <int pitch = 16>
+// (`pitch`: columns from one 16 k of A to the next)
+template <int pitch = 8>
 __device__ __forceinline__ void mma_tmem_rows(uint32_t d, uint32_t a, uint32_t b, bool add) {
   const uint64_t db = desc_rows(b);
 #pragma unroll
-  for (int ks = 0; ks < 8; ++ks) umma_ts(d, a + pitch * (ks >> 1) + 8 * (ks & 1), db + step_rows(ks), kIdRows, add || ks > 0);
+  for (int ks = 0; ks < 8; ++ks) umma_ts(d, a + pitch * ks, db + step_rows(ks), kIdRows, add || ks > 0);
 }
 
 // Sequences as the state kernel walks them

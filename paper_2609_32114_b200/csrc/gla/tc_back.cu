@@ -8,12 +8,14 @@
 // dg is a sum of, come of them alone: with h and dh as two bf16 pieces they keep the accuracy of fp32.  E = S dS is taken of the fp32
 // accumulators.  P and dS are rounded to bf16 for the products that give dq, dk and dv, which are rounded to bf16 anyway.
 //
-// Shared memory has seven slots for the eight tiles of a unit (Q, K, dO, V, two pieces of h and of dh; the last goes where Q was), assigned anew each unit so
-// that what the next unit needs first goes where this one is done first.  Tensor memory: four regions of 128 columns,
+// Shared memory has seven slots for a unit's tiles: K, Q, dO, V, two pieces of h, two of dh.  V makes room for the second piece of dh once the scores are
+// made and is loaded again, out of L2, where the first piece of h was: so all pieces are there for <h, dh> while the products for dq run, and the slots come free
+// over the length of a unit, each for what is needed next.  (An SM gets some 32 bytes a cycle when all load, 1000 cycles for a tile.  With <h, dh> at the
+// end the last piece of dh and the next unit's K came 4000 cycles late each, of 25000 a unit.)  Tensor memory: four regions of 128 columns,
 //   R0: S, then dS | dq by h | dv by P      R1: dP | dq by dS | dk by dS      R2: S^T, then P^T | dv by dh      R3: dP^T, then dS^T | dk by dh
-// An operand lies over the scores that it is made of: a warp writes its 32 columns, 16 words, over the first half of the 32 accumulator columns
-// that it alone has read, and a product's steps of 16 k go from one such half to the next.  So all four scores become operands in one phase, in which the
-// triangles on either side of the diagonal share out evenly over the warps (dS below it, the transposed ones above).
+// An operand lies over the scores that it is made of: a warp writes 16 columns of it, 8 words, over the first half of the 16 accumulator columns
+// that it alone has read, and a product's steps of 16 k go from one such place to the next.  So all four scores become operands in one phase, in which
+// the blocks of 32 x 16 on either side of the diagonal (dS below it, the transposed ones above) share out evenly: ten to the four warps of a quarter.
 // One more warp scans the next unit's gates and adds up dg of the last one; the sums over a row's columns, which four warps share, pass through a
 // few KiB of workspace that stay in L2.
 // What bounds it: 352 KiB of tiles, images and gradients a unit, and a unit's dependent phases.
@@ -26,14 +28,15 @@ namespace {
 
 constexpr int kSlots = 7;
 constexpr int kThreads = 32 * (kComputeWarps + 3);
-struct BackGates { float hi[kStep], lo[kStep], er[kStep], ec[kStep], bb[64], ghi, glo; float pad[2]; };   // (as StepGates; G_L = ghi + glo)
+// As StepGates, G_L = ghi + glo; and which unit these are the gates of: first token, tokens (0: no more units), V-head, V-head of the run; its run's and its q/k head
+struct BackGates { float hi[kStep], lo[kStep], er[kStep], ec[kStep], bb[64], ghi, glo; int part_head, qk_head; int4 unit; };
 constexpr uint32_t OFF_G = kSlots * kTileBytes;
 constexpr uint32_t OFF_BAR = OFF_G + sizeof(BackGates);
 constexpr int kBars = 2 * kSlots + 12;
 constexpr uint32_t kSmem = OFF_BAR + kBars * 8 + 16;
 static_assert(kSmem <= 227 * 1024 && sizeof(BackGates) % 16 == 0, "shared memory budget");
 constexpr uint32_t R0 = 0, R1 = 128, R2 = 256, R3 = 384;
-enum { kQ, kK, kDO, kV, kHH, kHL, kDH, kDL };              // tiles in the order they are loaded; kDL lies where kQ was
+enum { kK, kQ, kDO, kV, kHH, kHL, kDH, kDL, kV2, kTiles };   // tiles in the order they are loaded; kDL lies where kV was, kV2 where kHH was
 
 struct BackParams {
   const float* g;
@@ -49,18 +52,20 @@ struct BackParams {
   int32_t* status;
 };
 
-// The slots' roles in this unit, and the parity of their next fill
-struct Slots {
-  int s[kSlots] = {0, 1, 2, 3, 4, 5, 6};
-  uint32_t parity = 0;
-  __device__ __forceinline__ int at(int tile) const { return s[tile == kDL ? kQ : tile]; }
-  __device__ __forceinline__ uint32_t fill(int tile) const { return (parity >> at(tile) & 1) ^ (tile == kDL ? 1 : 0); }
-  __device__ __forceinline__ void next() {
-    parity ^= 0x7f ^ (1u << s[kQ]);
-    const int q = s[kQ], k = s[kK], o = s[kDO], hh = s[kHH], hl = s[kHL], dh = s[kDH];
-    s[kQ] = o; s[kK] = hh; s[kDO] = hl; s[kHH] = dh; s[kHL] = q; s[kDH] = k;   // (V stays)
-  }
-};
+// Slot of a tile of the CTA's unit u, and the parity of its fill there.  Q, dO and V have slots of their own; K, the pieces of h and the first of dh go round
+// four, each unit where the next one of that order was the unit before.
+__device__ __forceinline__ int slot_of(int tile, int u) {
+  if (tile == kQ) return 4;
+  if (tile == kDO) return 5;
+  if (tile == kV || tile == kDL) return 6;
+  return ((tile == kK ? 0 : tile == kHL ? 1 : tile == kDH ? 3 : 2) + u) & 3;
+}
+__device__ __forceinline__ uint32_t fill_of(int tile, int u) {
+  if (tile == kQ || tile == kDO) return u & 1;
+  if (tile == kV || tile == kDL) return tile == kDL;
+  const int since = (slot_of(tile, u) - 2) & 3;            // the first unit in which this slot was filled twice
+  return (u + ((u + 3 - since) >> 2) + (tile == kV2 ? 1 : 0)) & 1;
+}
 
 __global__ void __launch_bounds__(kThreads, 1)
 gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -105,7 +110,6 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   };
   constexpr int kSums = 2 * 4 * kStep + kComputeWarps;     // [4][128] x + R - C, [4][128] y, [16] parts of <h, dh>
   float* sums = p.sums + (size_t)blockIdx.x * 2 * kSums;
-  Slots sl;
 
   if (warp == kComputeWarps) {
     // ------------------------------------------------------------ tiles
@@ -113,21 +117,28 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       Unit x{{0, 1}, 0, 0, 0};
       for (int u = -1; x.c.L > 0 && !*abort_flag; ++u) {
         const Unit after = unit(u + 1);                    // (its look-ups under the waits, here and below)
+        if (after.c.L > 0) {                               // on the way to L2 while this unit is at work: out of HBM a tile takes 1.8 - 2.8 us
+          tma_prefetch_4d(&map_q, 0, after.j / R, after.c.tok0, 0);
+          tma_prefetch_4d(&map_k, 0, after.j / R, after.c.tok0, 0);
+          tma_prefetch_4d(&map_do, 0, after.j, after.c.tok0, 0);
+          tma_prefetch_4d(&map_v, 0, after.j, after.c.tok0, 0);
+          bulk_prefetch(p.image + 2 * after.sj * kTileBytes, 2 * kTileBytes);
+          bulk_prefetch(p.image_back + 2 * after.sj * kTileBytes, 2 * kTileBytes);
+        }
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
+        for (int t = 0; t < kTiles; ++t) {
           if (u < 0) break;
-          const int at = sl.at(t);
-          wait_for(&empty[at], sl.fill(t) ^ 1, abort_flag);
+          const int at = slot_of(t, u);
+          wait_for(&empty[at], fill_of(t, u) ^ 1, abort_flag);
           if (*abort_flag) break;
           uint8_t* dst = sm + at * kTileBytes;
           mbar_expect_tx(&full[at], kTileBytes);
           if (t == kQ) tma_load_4d(dst, &map_q, &full[at], 0, x.j / R, x.c.tok0, 0);
           else if (t == kK) tma_load_4d(dst, &map_k, &full[at], 0, x.j / R, x.c.tok0, 0);
           else if (t == kDO) tma_load_4d(dst, &map_do, &full[at], 0, x.j, x.c.tok0, 0);
-          else if (t == kV) tma_load_4d(dst, &map_v, &full[at], 0, x.j, x.c.tok0, 0);
+          else if (t == kV || t == kV2) tma_load_4d(dst, &map_v, &full[at], 0, x.j, x.c.tok0, 0);
           else bulk_load(dst, (t < kDH ? p.image : p.image_back) + (2 * x.sj + (t == kHL || t == kDL)) * kTileBytes, kTileBytes, &full[at]);
         }
-        if (u >= 0) sl.next();
         x = after;
       }
     }
@@ -145,12 +156,12 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           continue;
         }
         const uint32_t ph = u & 1;
-        auto tile = [&](int t) { return smem_u32(sm + sl.at(t) * kTileBytes); };
+        auto tile = [&](int t) { return smem_u32(sm + slot_of(t, u) * kTileBytes); };
         auto wait = [&](uint64_t* b, uint32_t parity) {
           wait_for(b, parity, abort_flag);
           tc_fence_after_sync();
         };
-        auto loaded = [&](int t) { wait(&full[sl.at(t)], sl.fill(t)); };
+        auto loaded = [&](int t) { wait(&full[slot_of(t, u)], fill_of(t, u)); };
         loaded(kQ);
         loaded(kK);
         if (x.c.L < kStep) wait(clean, tails++ & 1);
@@ -166,33 +177,34 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         mma_cols(R1, tile(kDO), tile(kV), false);          // dP
         mma_cols(R3, tile(kV), tile(kDO), false);          // dP^T
         umma_commit(b_s);
+        umma_commit(&empty[slot_of(kV, u)]);
         wait(e_s, ph);
-        mma_tmem_rows<32>(R1, R0, tile(kK), false);        // dS K
+        mma_tmem_rows<16>(R1, R0, tile(kK), false);        // dS K
         loaded(kHH);
         mma_cols(R0, tile(kDO), tile(kHH), false);         // dO h^T
         loaded(kHL);
         mma_cols(R0, tile(kDO), tile(kHL), true);
         umma_commit(b_dq);
+        wait(e_d, ph);
+        umma_commit(&empty[slot_of(kHH, u)]);
+        umma_commit(&empty[slot_of(kHL, u)]);
         wait(e_q, ph);
-        mma_tmem_rows<32>(R1, R3, tile(kQ), false);        // dS^T Q
-        umma_commit(&empty[sl.at(kQ)]);
-        mma_tmem_rows<32>(R0, R2, tile(kDO), false);       // P^T dO
-        umma_commit(&empty[sl.at(kDO)]);
+        mma_tmem_rows<16>(R1, R3, tile(kQ), false);        // dS^T Q
+        umma_commit(&empty[slot_of(kQ, u)]);
+        mma_tmem_rows<16>(R0, R2, tile(kDO), false);       // P^T dO
+        umma_commit(&empty[slot_of(kDO, u)]);
         loaded(kDH);
         mma_rows(R2, tile(kK), tile(kDH), false);          // K dh
         umma_commit(b_dv);
-        mma_cols(R3, tile(kV), tile(kDH), false);          // V dh^T
+        loaded(kV2);
+        mma_cols(R3, tile(kV2), tile(kDH), false);         // V dh^T
         loaded(kDL);
-        mma_cols(R3, tile(kV), tile(kDL), true);
+        mma_cols(R3, tile(kV2), tile(kDL), true);
         umma_commit(b_dk);
-        umma_commit(&empty[sl.at(kV)]);
-        wait(e_d, ph);
-        mbar_arrive(&empty[sl.at(kHH)]);
-        mbar_arrive(&empty[sl.at(kHL)]);
-        umma_commit(&empty[sl.at(kDH)]);
-        umma_commit(&empty[sl.at(kDL)]);
-        last_k = sl.at(kK);
-        sl.next();
+        umma_commit(&empty[slot_of(kV2, u)]);
+        umma_commit(&empty[slot_of(kDH, u)]);
+        umma_commit(&empty[slot_of(kDL, u)]);
+        last_k = slot_of(kK, u);
         x = after;
       }
     }
@@ -202,10 +214,10 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     Unit x = unit(0), before{{0, 0}, 0, 0, 0};
     float total = 0.f;
     float4 raw = fetch_gates(p.g, p.HV, x.j, x.c, lane);
-    for (int u = 0; x.c.L > 0 || before.c.L > 0; ++u) {
+    for (int u = 0; x.c.L > 0 || before.c.L > 0 || u == 0; ++u) {
       const Unit after = x.c.L > 0 ? unit(u + 1) : x;
       float next_total = 0.f;
-      if (x.c.L > 0) {
+      {                                                    // (behind the last unit: that there are no more)
         double G[4];
         scan_gates(raw, lane, G);
         raw = fetch_gates(p.g, p.HV, after.j, after.c, lane);
@@ -237,6 +249,9 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         if (lane == 0) {
           s->ghi = (float)GL;
           s->glo = (float)(GL - (double)(float)GL);
+          s->unit = make_int4(x.c.tok0, x.c.L, x.j, x.r);
+          s->part_head = x.j / p.per;
+          s->qk_head = x.j / R;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(gates);
@@ -291,8 +306,9 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       __syncwarp();
       tc_fence_after_sync();
     };
+    int u = 0;
     auto seen = [&](int t) {                               // (loaded long ago; this thread's own look at it)
-      wait_for(&full[sl.at(t)], sl.fill(t), abort_flag);
+      wait_for(&full[slot_of(t, u)], fill_of(t, u), abort_flag);
       __syncwarp();
     };
     // 16-byte piece k of this thread's 32 columns in its row of the tile in a slot
@@ -302,17 +318,20 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     float4* acc = p.per > 1 ? p.shared + (size_t)blockIdx.x * 2 * 8 * 512 + tid : nullptr;
     // What the loop over units executes has to stay small, or the warps wait for their instructions: one body for the operands below and above the
     // diagonal, one for the three gradients.
-    Unit x{{0, 1}, 0, 0, 0};
-    for (int u = -1; x.c.L > 0; ++u) {
-      const Unit after = unit(u + 1);
-      if (u >= 0) {
+    struct { Geom c; int j, r, out; } x;                   // out: head of dq, dk
+    const bool by_run = p.part_q;
+    for (;; ++u) {
+      {
         const uint32_t ph = u & 1;
         wait_for(gates, ph, abort_flag);
+        const int4 at_unit = s->unit;
+        x = {{at_unit.x, *abort_flag ? 0 : at_unit.y}, at_unit.z, at_unit.w, by_run ? s->part_head : s->qk_head};
+        if (x.c.L <= 0) break;
         if (x.c.L < kStep) {                               // (rows behind the sequence may be NaN)
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
-            wait_for(&full[sl.at(t)], sl.fill(t), abort_flag);
-            clear_rows(sm + sl.at(t) * kTileBytes, x.c.L, tid, 32 * kComputeWarps);
+            wait_for(&full[slot_of(t, u)], fill_of(t, u), abort_flag);
+            clear_rows(sm + slot_of(t, u) * kTileBytes, x.c.L, tid, 32 * kComputeWarps);
           }
           fence_proxy_async_smem();
           arrive(clean);
@@ -325,152 +344,167 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         wait(b_s, ph);
         const uint32_t slice = lanes + 32 * g;
         float z = 0.f;
+        {                                                  // zeros on the other side of the diagonal
+          const uint32_t none[8] = {};
+          if (g > q) {
+            tmem_st8(R0 + slice, none);
+            tmem_st8(R0 + slice + 16, none);
+          }
+          if (g < q) {
+            tmem_st8(R2 + slice, none);
+            tmem_st8(R2 + slice + 16, none);
+            tmem_st8(R3 + slice, none);
+            tmem_st8(R3 + slice + 16, none);
+          }
+        }
 #pragma unroll 1
-        for (int turn = 0; turn < 4; ++turn) {
-          asm volatile("" : "+r"(turn));
-          const int above = turn >> 1, b = turn & 1;
-          uint32_t wp[8] = {}, ws[8] = {};
-          if (above ? g >= q : g <= q) {
-            uint32_t rs[16], rp[16];
-            tmem_ld16((above ? R2 : R0) + slice + 16 * b, rs);
-            tmem_ld16((above ? R3 : R1) + slice + 16 * b, rp);
-            float2 dec[8];                                 // decay, mask and scale
-            if (g != q) {
-              const float f = p.scale * (above ? s->ec[i] * s->bb[8 * (2 * g + b) + (i >> 4)] : s->er[i] * s->bb[8 * (i >> 4) + 2 * g + b]);
-              const float* e = (above ? s->er : s->ec) + 32 * g + 16 * b;
+        for (int n = g; n < 10; n += 4) {                  // block n of the quarter: 2 q + 2 below the diagonal, then 8 - 2 q above
+          const bool above = n >= 2 * q + 2;
+          const int b = above ? n - 2 : n;                 // block of 16 columns
+          const uint32_t at = lanes + 16 * b;
+          uint32_t rs[16], rp[16], wp[8], ws[8];
+          tmem_ld16((above ? R2 : R0) + at, rs);
+          tmem_ld16((above ? R3 : R1) + at, rp);
+          float2 dec[8];                                   // decay, mask and scale
+          if (b >> 1 != q) {
+            const float f = p.scale * (above ? s->ec[i] * s->bb[8 * b + (i >> 4)] : s->er[i] * s->bb[8 * (i >> 4) + b]);
+            const float* e = (above ? s->er : s->ec) + 16 * b;
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const float4 c = *reinterpret_cast<const float4*>(e + 4 * k);
-                dec[2 * k] = mul2(make_float2(f, f), make_float2(c.x, c.y));
-                dec[2 * k + 1] = mul2(make_float2(f, f), make_float2(c.z, c.w));
-              }
-            } else {
-              const float sign = above ? 1.f : -1.f;
-#pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const int at = 16 * b + 2 * k;
-                const float2 a = fma2(*reinterpret_cast<const float2*>(&s->hi[32 * g + at]), make_float2(sign, sign), make_float2(-sign * hi, -sign * hi)),
-                             c = fma2(*reinterpret_cast<const float2*>(&s->lo[32 * g + at]), make_float2(sign, sign), make_float2(-sign * lo, -sign * lo));
-                dec[k].x = (above ? at >= lane : at <= lane) ? p.scale * ex2(a.x + c.x) : 0.f;
-                dec[k].y = (above ? at + 1 >= lane : at + 1 <= lane) ? p.scale * ex2(a.y + c.y) : 0.f;
-              }
+            for (int k = 0; k < 4; ++k) {
+              const float4 c = *reinterpret_cast<const float4*>(e + 4 * k);
+              dec[2 * k] = mul2(make_float2(f, f), make_float2(c.x, c.y));
+              dec[2 * k + 1] = mul2(make_float2(f, f), make_float2(c.z, c.w));
             }
-            tmem_ld_wait();
-            float2 zz = make_float2(0.f, 0.f);
-            const int diag = g == q ? lane - 16 * b : -1;  // the column whose E counts for neither
+          } else {
+            const float sign = above ? 1.f : -1.f;
+            const int to = i - 16 * b;                     // the row's own column
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              const float2 sc = as_f2(rs[2 * k], rs[2 * k + 1]), ds = mul2(dec[k], as_f2(rp[2 * k], rp[2 * k + 1]));
-              wp[k] = pack_bf16(mul2(dec[k], sc));
-              ws[k] = pack_bf16(ds);
-              zz = fma2(make_float2(2 * k == diag ? 0.f : ds.x, 2 * k + 1 == diag ? 0.f : ds.y), sc, zz);
+              const float2 a = fma2(*reinterpret_cast<const float2*>(&s->hi[16 * b + 2 * k]), make_float2(sign, sign), make_float2(-sign * hi, -sign * hi)),
+                           c = fma2(*reinterpret_cast<const float2*>(&s->lo[16 * b + 2 * k]), make_float2(sign, sign), make_float2(-sign * lo, -sign * lo));
+              dec[k].x = (above ? 2 * k >= to : 2 * k <= to) ? p.scale * ex2(a.x + c.x) : 0.f;
+              dec[k].y = (above ? 2 * k + 1 >= to : 2 * k + 1 <= to) ? p.scale * ex2(a.y + c.y) : 0.f;
             }
-            z += above ? -(zz.x + zz.y) : zz.x + zz.y;
           }
-          tmem_st8((above ? R3 : R0) + slice + 8 * b, ws);
-          if (above) tmem_st8(R2 + slice + 8 * b, wp);
+          tmem_ld_wait();
+          float2 zz = make_float2(0.f, 0.f);
+          const int diag = i - 16 * b;                     // the column whose E counts for neither (none, where it is not of these 16)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float2 sc = as_f2(rs[2 * k], rs[2 * k + 1]), ds = mul2(dec[k], as_f2(rp[2 * k], rp[2 * k + 1]));
+            wp[k] = pack_bf16(mul2(dec[k], sc));
+            ws[k] = pack_bf16(ds);
+            zz = fma2(make_float2(2 * k == diag ? 0.f : ds.x, 2 * k + 1 == diag ? 0.f : ds.y), sc, zz);
+          }
+          z += above ? -(zz.x + zz.y) : zz.x + zz.y;
+          tmem_st8((above ? R3 : R0) + at, ws);
+          if (above) tmem_st8(R2 + at, wp);
         }
         tmem_st_wait();
         arrive(e_s);
         if (lane == 0) mbar_arrive(g_free);
 
-        // ---- dq, dv, dk: a f + b, a the part by the state; with the sums x_i, y_i of a f . (the row of q, k) ahead of e_q, e_k
+        // ---- <h, dh>, under the products for dq
         float* mine = sums + ph * kSums;
+        {
+          float2 d = make_float2(0.f, 0.f);
+          seen(kHH);
+          seen(kHL);
+          seen(kDH);
+          seen(kDL);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint4 h1 = piece(slot_of(kHH, u), k), h2 = piece(slot_of(kHL, u), k), d1 = piece(slot_of(kDH, u), k), d2 = piece(slot_of(kDL, u), k);
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              d = fma2(add2(unpack_bf16((&h1.x)[w]), unpack_bf16((&h2.x)[w])), add2(unpack_bf16((&d1.x)[w]), unpack_bf16((&d2.x)[w])), d);
+          }
+          arrive(e_d);
+          float sum = d.x + d.y;
+#pragma unroll
+          for (int e = 16; e > 0; e >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, e);
+          if (lane == 0) __stcg(mine + 8 * kStep + warp, sum);
+        }
+
+        // ---- dq, dv, dk: a f + c, a the part by the state; with the sums x_i, y_i of a f . (the row of q, k) ahead of e_q, e_k
 #pragma unroll 1
         for (int o = 0; o < 3; ++o) {
           asm volatile("" : "+r"(o));                      // (not three copies of the body)
-          if (o == 2) {                                    // <h, dh>, under the products for dk
-            float2 d = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int t = kHH; t <= kDL; ++t) seen(t);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint4 h1 = piece(sl.at(kHH), k), h2 = piece(sl.at(kHL), k), d1 = piece(sl.at(kDH), k), d2 = piece(sl.at(kDL), k);
-#pragma unroll
-              for (int w = 0; w < 4; ++w)
-                d = fma2(add2(unpack_bf16((&h1.x)[w]), unpack_bf16((&h2.x)[w])), add2(unpack_bf16((&d1.x)[w]), unpack_bf16((&d2.x)[w])), d);
-            }
-            arrive(e_d);
-            float sum = d.x + d.y;
-#pragma unroll
-            for (int e = 16; e > 0; e >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, e);
-            if (lane == 0) __stcg(mine + 8 * kStep + warp, sum);
-          }
           wait(b_dq + o, ph);
-          uint32_t a[32], c[32];
-          tmem_ld32((o == 0 ? R0 : o == 1 ? R2 : R3) + slice, a);
-          tmem_ld32((o == 1 ? R0 : R1) + slice, c);
+          if (o != 1) seen(o == 0 ? kQ : kK);
           const float f = o == 0 ? eg : el;
-          tmem_ld_wait();
-          if (o != 1) {
-            const int tile = o == 0 ? kQ : kK;
-            seen(tile);
-            float2 d = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint4 r = piece(sl.at(tile), k);
-#pragma unroll
-              for (int w = 0; w < 4; ++w) d = fma2(as_f2(a[8 * k + 2 * w], a[8 * k + 2 * w + 1]), unpack_bf16((&r.x)[w]), d);
+          const bool parts = o != 1 && by_run;
+          const int heads = o == 1 ? p.HV : by_run ? runs : p.HK;
+          const size_t row0 = ((size_t)(x.c.tok0 + 32 * q) * heads + (o == 1 ? x.j : x.out)) * 128 + 32 * g, pitch = (size_t)heads * 128;
+          float2 d = make_float2(0.f, 0.f);
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {           // of the 32 columns
+            uint32_t a[16], c[16];
+            tmem_ld16((o == 0 ? R0 : o == 1 ? R2 : R3) + slice + 16 * half, a);
+            tmem_ld16((o == 1 ? R0 : R1) + slice + 16 * half, c);
+            uint4 t[2] = {};
+            if (o != 1) {
+              t[0] = piece((o == 0 ? slot_of(kQ, u) : slot_of(kK, u)), 2 * half);
+              t[1] = piece((o == 0 ? slot_of(kQ, u) : slot_of(kK, u)), 2 * half + 1);
             }
-            __stcg(mine + (o == 0 ? 0 : 4 * kStep) + g * kStep + i, fmaf(f, d.x + d.y, o == 0 ? z : 0.f));
-          }
-          arrive(e_q + o);
+            tmem_ld_wait();
 #pragma unroll
-          for (int k = 0; k < 32; k += 2) {
-            const float2 v = fma2(as_f2(a[k], a[k + 1]), make_float2(f, f), as_f2(c[k], c[k + 1]));
-            a[k] = __float_as_uint(v.x);
-            a[k + 1] = __float_as_uint(v.y);
-          }
-          if (o != 1 && acc) {                             // added to what the run's V-heads before left, and left for the next ones
-            float4* part = acc + (o == 0 ? 0 : 8 * 512);
-            if (x.r > 0) {
+            for (int k = 0; k < 8; ++k) d = fma2(as_f2(a[2 * k], a[2 * k + 1]), unpack_bf16((&t[k >> 2].x)[k & 3]), d);
+            if (half == 1) {
+              // (behind the sequence y is of whatever V's second loading brought)
+              if (o != 1) __stcg(mine + (o == 0 ? 0 : 4 * kStep) + g * kStep + i, i < x.c.L ? fmaf(f, d.x + d.y, o == 0 ? z : 0.f) : 0.f);
+              arrive(e_q + o);
+            }
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const float4 t = __ldcg(part + 512 * k);
-                const float2 v0 = add2(as_f2(a[4 * k], a[4 * k + 1]), make_float2(t.x, t.y)), v1 = add2(as_f2(a[4 * k + 2], a[4 * k + 3]), make_float2(t.z, t.w));
-                a[4 * k] = __float_as_uint(v0.x); a[4 * k + 1] = __float_as_uint(v0.y);
-                a[4 * k + 2] = __float_as_uint(v1.x); a[4 * k + 3] = __float_as_uint(v1.y);
+            for (int k = 0; k < 16; k += 2) {
+              const float2 v = fma2(as_f2(a[k], a[k + 1]), make_float2(f, f), as_f2(c[k], c[k + 1]));
+              a[k] = __float_as_uint(v.x);
+              a[k + 1] = __float_as_uint(v.y);
+            }
+            if (o != 1 && acc) {                           // added to what the run's V-heads before left, and left for the next ones
+              float4* part = acc + (o == 0 ? 0 : 8 * 512) + 4 * 512 * half;
+              if (x.r > 0) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const float4 y = __ldcg(part + 512 * k);
+                  const float2 v0 = add2(as_f2(a[4 * k], a[4 * k + 1]), make_float2(y.x, y.y)), v1 = add2(as_f2(a[4 * k + 2], a[4 * k + 3]), make_float2(y.z, y.w));
+                  a[4 * k] = __float_as_uint(v0.x); a[4 * k + 1] = __float_as_uint(v0.y);
+                  a[4 * k + 2] = __float_as_uint(v1.x); a[4 * k + 3] = __float_as_uint(v1.y);
+                }
+              }
+              if (x.r < p.per - 1) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  __stcg(part + 512 * k, make_float4(__uint_as_float(a[4 * k]), __uint_as_float(a[4 * k + 1]), __uint_as_float(a[4 * k + 2]), __uint_as_float(a[4 * k + 3])));
+                continue;
               }
             }
-            if (x.r < p.per - 1) {
-#pragma unroll
-              for (int k = 0; k < 8; ++k)
-                __stcg(part + 512 * k, make_float4(__uint_as_float(a[4 * k]), __uint_as_float(a[4 * k + 1]), __uint_as_float(a[4 * k + 2]), __uint_as_float(a[4 * k + 3])));
-              continue;
-            }
-          }
-          const int row = 32 * q + (lane & ~3), left = x.c.L - row;
-          const bool parts = o != 1 && p.part_q;
-          const int heads = o == 1 ? p.HV : parts ? runs : p.HK, head = o == 1 ? x.j : parts ? x.j / p.per : x.j / R;
-          const size_t at = ((size_t)(x.c.tok0 + row) * heads + head) * 128 + 32 * g, pitch = (size_t)heads * 128;
-          if (parts) {
-            float* dst = (o == 0 ? p.part_q : p.part_k) + at + 4 * (lane & 3);
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
+            if (parts) {
+              const int row = lane & ~3;
               uint4 v[4];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) v[k] = make_uint4(a[16 * half + 4 * k], a[16 * half + 4 * k + 1], a[16 * half + 4 * k + 2], a[16 * half + 4 * k + 3]);
+              for (int k = 0; k < 4; ++k) v[k] = make_uint4(a[4 * k], a[4 * k + 1], a[4 * k + 2], a[4 * k + 3]);
               exchange4(v, lane);
+              float* dst = (o == 0 ? p.part_q : p.part_k) + row0 + row * pitch + 16 * half + 4 * (lane & 3);
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                if (k < left) *reinterpret_cast<uint4*>(dst + k * pitch + 16 * half) = v[k];
+                if (32 * q + row + k < x.c.L) *reinterpret_cast<uint4*>(dst + k * pitch) = v[k];
+            } else {
+              const int row = lane & ~1;
+              uint4 v[2];
+#pragma unroll
+              for (int k = 0; k < 2; ++k)
+                v[k] = make_uint4(pack_bf16(as_f2(a[8 * k], a[8 * k + 1])), pack_bf16(as_f2(a[8 * k + 2], a[8 * k + 3])),
+                                  pack_bf16(as_f2(a[8 * k + 4], a[8 * k + 5])), pack_bf16(as_f2(a[8 * k + 6], a[8 * k + 7])));
+              exchange2(v, lane);
+              __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(o == 0 ? p.dq : o == 1 ? p.dv : p.dk) + row0 + row * pitch + 16 * half + 8 * (lane & 1);
+#pragma unroll
+              for (int k = 0; k < 2; ++k)
+                if (32 * q + row + k < x.c.L) *reinterpret_cast<uint4*>(dst + k * pitch) = v[k];
             }
-          } else {
-            uint4 v[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              v[k] = make_uint4(pack_bf16(as_f2(a[8 * k], a[8 * k + 1])), pack_bf16(as_f2(a[8 * k + 2], a[8 * k + 3])),
-                                pack_bf16(as_f2(a[8 * k + 4], a[8 * k + 5])), pack_bf16(as_f2(a[8 * k + 6], a[8 * k + 7])));
-            exchange4(v, lane);
-            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(o == 0 ? p.dq : o == 1 ? p.dv : p.dk) + at + 8 * (lane & 3);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (k < left) *reinterpret_cast<uint4*>(dst + k * pitch) = v[k];
           }
         }
-        sl.next();
       }
-      x = after;
     }
   }
   tc_fence_before_sync();
