@@ -117,14 +117,6 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       Unit x{{0, 1}, 0, 0, 0};
       for (int u = -1; x.c.L > 0 && !*abort_flag; ++u) {
         const Unit after = unit(u + 1);                    // (its look-ups under the waits, here and below)
-        if (after.c.L > 0) {                               // on the way to L2 while this unit is at work: out of HBM a tile takes 1.8 - 2.8 us
-          tma_prefetch_4d(&map_q, 0, after.j / R, after.c.tok0, 0);
-          tma_prefetch_4d(&map_k, 0, after.j / R, after.c.tok0, 0);
-          tma_prefetch_4d(&map_do, 0, after.j, after.c.tok0, 0);
-          tma_prefetch_4d(&map_v, 0, after.j, after.c.tok0, 0);
-          bulk_prefetch(p.image + 2 * after.sj * kTileBytes, 2 * kTileBytes);
-          bulk_prefetch(p.image_back + 2 * after.sj * kTileBytes, 2 * kTileBytes);
-        }
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
           if (u < 0) break;
@@ -436,72 +428,70 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           const bool parts = o != 1 && by_run;
           const int heads = o == 1 ? p.HV : by_run ? runs : p.HK;
           const size_t row0 = ((size_t)(x.c.tok0 + 32 * q) * heads + (o == 1 ? x.j : x.out)) * 128 + 32 * g, pitch = (size_t)heads * 128;
-          float2 d = make_float2(0.f, 0.f);
-#pragma unroll 1
-          for (int half = 0; half < 2; ++half) {           // of the 32 columns
-            uint32_t a[16], c[16];
-            tmem_ld16((o == 0 ? R0 : o == 1 ? R2 : R3) + slice + 16 * half, a);
-            tmem_ld16((o == 1 ? R0 : R1) + slice + 16 * half, c);
-            uint4 t[2] = {};
-            if (o != 1) {
-              t[0] = piece((o == 0 ? slot_of(kQ, u) : slot_of(kK, u)), 2 * half);
-              t[1] = piece((o == 0 ? slot_of(kQ, u) : slot_of(kK, u)), 2 * half + 1);
+          uint32_t a[32], c[32];
+          tmem_ld32((o == 0 ? R0 : o == 1 ? R2 : R3) + slice, a);
+          tmem_ld32((o == 1 ? R0 : R1) + slice, c);
+          tmem_ld_wait();
+          if (o != 1) {
+            float2 d = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint4 t = piece(o == 0 ? slot_of(kQ, u) : slot_of(kK, u), k);
+#pragma unroll
+              for (int w = 0; w < 4; ++w) d = fma2(as_f2(a[8 * k + 2 * w], a[8 * k + 2 * w + 1]), unpack_bf16((&t.x)[w]), d);
             }
-            tmem_ld_wait();
+            // (behind the sequence y is of whatever V's second loading brought)
+            __stcg(mine + (o == 0 ? 0 : 4 * kStep) + g * kStep + i, i < x.c.L ? fmaf(f, d.x + d.y, o == 0 ? z : 0.f) : 0.f);
+          }
+          arrive(e_q + o);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) d = fma2(as_f2(a[2 * k], a[2 * k + 1]), unpack_bf16((&t[k >> 2].x)[k & 3]), d);
-            if (half == 1) {
-              // (behind the sequence y is of whatever V's second loading brought)
-              if (o != 1) __stcg(mine + (o == 0 ? 0 : 4 * kStep) + g * kStep + i, i < x.c.L ? fmaf(f, d.x + d.y, o == 0 ? z : 0.f) : 0.f);
-              arrive(e_q + o);
-            }
+          for (int k = 0; k < 32; k += 2) {
+            const float2 v = fma2(as_f2(a[k], a[k + 1]), make_float2(f, f), as_f2(c[k], c[k + 1]));
+            a[k] = __float_as_uint(v.x);
+            a[k + 1] = __float_as_uint(v.y);
+          }
+          if (o != 1 && acc) {                             // added to what the run's V-heads before left, and left for the next ones
+            float4* part = acc + (o == 0 ? 0 : 8 * 512);
+            if (x.r > 0) {
 #pragma unroll
-            for (int k = 0; k < 16; k += 2) {
-              const float2 v = fma2(as_f2(a[k], a[k + 1]), make_float2(f, f), as_f2(c[k], c[k + 1]));
-              a[k] = __float_as_uint(v.x);
-              a[k + 1] = __float_as_uint(v.y);
-            }
-            if (o != 1 && acc) {                           // added to what the run's V-heads before left, and left for the next ones
-              float4* part = acc + (o == 0 ? 0 : 8 * 512) + 4 * 512 * half;
-              if (x.r > 0) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  const float4 y = __ldcg(part + 512 * k);
-                  const float2 v0 = add2(as_f2(a[4 * k], a[4 * k + 1]), make_float2(y.x, y.y)), v1 = add2(as_f2(a[4 * k + 2], a[4 * k + 3]), make_float2(y.z, y.w));
-                  a[4 * k] = __float_as_uint(v0.x); a[4 * k + 1] = __float_as_uint(v0.y);
-                  a[4 * k + 2] = __float_as_uint(v1.x); a[4 * k + 3] = __float_as_uint(v1.y);
-                }
-              }
-              if (x.r < p.per - 1) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  __stcg(part + 512 * k, make_float4(__uint_as_float(a[4 * k]), __uint_as_float(a[4 * k + 1]), __uint_as_float(a[4 * k + 2]), __uint_as_float(a[4 * k + 3])));
-                continue;
+              for (int k = 0; k < 8; ++k) {
+                const float4 y = __ldcg(part + 512 * k);
+                const float2 v0 = add2(as_f2(a[4 * k], a[4 * k + 1]), make_float2(y.x, y.y)), v1 = add2(as_f2(a[4 * k + 2], a[4 * k + 3]), make_float2(y.z, y.w));
+                a[4 * k] = __float_as_uint(v0.x); a[4 * k + 1] = __float_as_uint(v0.y);
+                a[4 * k + 2] = __float_as_uint(v1.x); a[4 * k + 3] = __float_as_uint(v1.y);
               }
             }
-            if (parts) {
-              const int row = lane & ~3;
+            if (x.r < p.per - 1) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                __stcg(part + 512 * k, make_float4(__uint_as_float(a[4 * k]), __uint_as_float(a[4 * k + 1]), __uint_as_float(a[4 * k + 2]), __uint_as_float(a[4 * k + 3])));
+              continue;
+            }
+          }
+          const int row = lane & ~3, left = x.c.L - 32 * q - row;
+          if (parts) {
+            float* dst = (o == 0 ? p.part_q : p.part_k) + row0 + row * pitch + 4 * (lane & 3);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
               uint4 v[4];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) v[k] = make_uint4(a[4 * k], a[4 * k + 1], a[4 * k + 2], a[4 * k + 3]);
+              for (int k = 0; k < 4; ++k) v[k] = make_uint4(a[16 * half + 4 * k], a[16 * half + 4 * k + 1], a[16 * half + 4 * k + 2], a[16 * half + 4 * k + 3]);
               exchange4(v, lane);
-              float* dst = (o == 0 ? p.part_q : p.part_k) + row0 + row * pitch + 16 * half + 4 * (lane & 3);
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                if (32 * q + row + k < x.c.L) *reinterpret_cast<uint4*>(dst + k * pitch) = v[k];
-            } else {
-              const int row = lane & ~1;
-              uint4 v[2];
-#pragma unroll
-              for (int k = 0; k < 2; ++k)
-                v[k] = make_uint4(pack_bf16(as_f2(a[8 * k], a[8 * k + 1])), pack_bf16(as_f2(a[8 * k + 2], a[8 * k + 3])),
-                                  pack_bf16(as_f2(a[8 * k + 4], a[8 * k + 5])), pack_bf16(as_f2(a[8 * k + 6], a[8 * k + 7])));
-              exchange2(v, lane);
-              __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(o == 0 ? p.dq : o == 1 ? p.dv : p.dk) + row0 + row * pitch + 16 * half + 8 * (lane & 1);
-#pragma unroll
-              for (int k = 0; k < 2; ++k)
-                if (32 * q + row + k < x.c.L) *reinterpret_cast<uint4*>(dst + k * pitch) = v[k];
+                if (k < left) *reinterpret_cast<uint4*>(dst + k * pitch + 16 * half) = v[k];
             }
+          } else {
+            uint4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              v[k] = make_uint4(pack_bf16(as_f2(a[8 * k], a[8 * k + 1])), pack_bf16(as_f2(a[8 * k + 2], a[8 * k + 3])),
+                                pack_bf16(as_f2(a[8 * k + 4], a[8 * k + 5])), pack_bf16(as_f2(a[8 * k + 6], a[8 * k + 7])));
+            exchange4(v, lane);
+            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(o == 0 ? p.dq : o == 1 ? p.dv : p.dk) + row0 + row * pitch + 8 * (lane & 3);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (k < left) *reinterpret_cast<uint4*>(dst + k * pitch) = v[k];
           }
         }
       }
