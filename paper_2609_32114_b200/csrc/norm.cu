@@ -12,9 +12,11 @@
 // vectors are shared by 1, 2, 4 .. 32 neighbouring lanes, longer ones by a CTA.  A row that does not start on a 16-byte boundary is
 // read in aligned vectors all the same, with the neighbours' values at its ends masked: a group's rows are a multiple of 8 apart, so the
 // column that an element of a thread holds is the same in every row, weights stay in registers and so do the sums for dw, which
-// a second kernel adds up over CTAs in order (no atomics: the same bits every time).  Rows in flight: the next row of the backward loops is
-// loaded before the present one is reduced.
+// a second kernel adds up over CTAs in order (no atomics: the same bits every time).  Rows in flight: the backward loops copy the next rows to shared
+// memory asynchronously, each thread for itself; with the next row in registers instead 262144 rows of 128 took 89 us instead of FIGURE_GATED, 16384
+// of 2048 with both norms 105 instead of FIGURE_ADD.
 #include "common.cuh"
+#include "tc_mma.cuh"
 
 namespace ha_la {
 
@@ -65,9 +67,61 @@ __device__ __forceinline__ Raw<__nv_bfloat16, 8> from_floats(const float (&f)[8]
 __device__ __forceinline__ Raw<float, 4> from_floats(const float (&f)[4], float) { return {make_float4(f[0], f[1], f[2], f[3])}; }
 template <typename In> __device__ __forceinline__ Raw<In, 1> from_floats(const float (&f)[1], In) { return {{from_f32<In>(f[0])}}; }
 
+// Elementwise arithmetic on what a thread holds of a row, two to an instruction where there are two.
+template <int N> struct Vec {
+  float v[N];
+  __device__ __forceinline__ float& operator[](int i) { return v[i]; }
+  __device__ __forceinline__ float operator[](int i) const { return v[i]; }
+};
+template <int N> __device__ __forceinline__ Vec<N> all_of(float x) {
+  Vec<N> r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = x;
+  return r;
+}
+template <int N> __device__ __forceinline__ Vec<N> mul(const Vec<N>& a, const Vec<N>& b) {
+  Vec<N> r;
+  if constexpr (N == 1) r[0] = a[0] * b[0];
+  else {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const float2 x = ptx::mul2(make_float2(a[i], a[i + 1]), make_float2(b[i], b[i + 1]));
+      r[i] = x.x;
+      r[i + 1] = x.y;
+    }
+  }
+  return r;
+}
+template <int N> __device__ __forceinline__ Vec<N> fma(const Vec<N>& a, const Vec<N>& b, const Vec<N>& c) {
+  Vec<N> r;
+  if constexpr (N == 1) r[0] = fmaf(a[0], b[0], c[0]);
+  else {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const float2 x = ptx::fma2(make_float2(a[i], a[i + 1]), make_float2(b[i], b[i + 1]), make_float2(c[i], c[i + 1]));
+      r[i] = x.x;
+      r[i + 1] = x.y;
+    }
+  }
+  return r;
+}
+template <int N> __device__ __forceinline__ Vec<N> mul(const Vec<N>& a, float b) { return mul(a, all_of<N>(b)); }
+template <int N> __device__ __forceinline__ Vec<N> fma(const Vec<N>& a, float b, const Vec<N>& c) { return fma(a, all_of<N>(b), c); }
+// s + the sum of a b
+template <int N> __device__ __forceinline__ float dot(const Vec<N>& a, const Vec<N>& b, float s) {
+  if constexpr (N == 1) return fmaf(a[0], b[0], s);
+  else {
+    float2 x = make_float2(s, 0.f);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) x = ptx::fma2(make_float2(a[i], a[i + 1]), make_float2(b[i], b[i + 1]), x);
+    return x.x + x.y;
+  }
+}
+
 // Which part of a row a thread holds: NV vectors of VEC elements, the group's threads one behind the other, the first one's first vector `shift`
 // elements in front of the row's start, on a 16-byte boundary.
-template <typename In, int VEC, int NV, bool SUB>
+// FULL: rows are whole vectors, so they all start on a boundary.
+template <typename In, int VEC, int NV, bool SUB, bool FULL>
 struct Rows {
   int t, threads, shift, cols;
   long long row, step, rows, total;                      // this group's first row, rows between its rows
@@ -80,22 +134,22 @@ struct Rows {
     rows = p.rows;
     cols = p.cols;
     total = p.rows * p.cols;
-    shift = (int)((row * cols) & (VEC - 1));
+    shift = FULL ? 0 : (int)((row * cols) & (VEC - 1));
   }
   // the loop over a group's rows goes on as long as any group of the CTA has one: its threads meet in the sums
   __device__ __forceinline__ bool on(long long r) const {
     return SUB ? r - threadIdx.x / threads < rows : r < rows;
   }
-  __device__ __forceinline__ int col(int i, int e) const { return VEC * (t + i * threads) - shift + e; }
-  __device__ __forceinline__ bool in(int i, int e) const { return (unsigned)col(i, e) < (unsigned)cols; }
-  __device__ __forceinline__ bool any(int i) const { return col(i, VEC - 1) >= 0 && col(i, 0) < cols; }
-  __device__ __forceinline__ bool whole(int i) const { return col(i, 0) >= 0 && col(i, VEC - 1) < cols; }
+  __device__ __forceinline__ int col(int i, int e) const { return VEC * (t + i * threads) - (FULL ? 0 : shift) + e; }
+  __device__ __forceinline__ bool in(int i, int e) const { return FULL ? col(i, 0) < cols : (unsigned)col(i, e) < (unsigned)cols; }
+  __device__ __forceinline__ bool any(int i) const { return FULL ? col(i, 0) < cols : col(i, VEC - 1) >= 0 && col(i, 0) < cols; }
+  __device__ __forceinline__ bool whole(int i) const { return FULL ? col(i, 0) < cols : col(i, 0) >= 0 && col(i, VEC - 1) < cols; }
   __device__ __forceinline__ Raw<In, VEC> load(const void* base, long long r, int i) const {
     Raw<In, VEC> a = {};
     if (r < rows && any(i)) {
       const long long at = r * cols + col(i, 0);         // (>= 0: a whole vector of the tensor, or the one at its end)
       const In* src = reinterpret_cast<const In*>(base) + at;
-      if (at + VEC <= total) a = *reinterpret_cast<const Raw<In, VEC>*>(src);
+      if (FULL || at + VEC <= total) a = *reinterpret_cast<const Raw<In, VEC>*>(src);
       else {
         In* e = reinterpret_cast<In*>(&a);
         for (int k = 0; k < VEC && at + k < total; ++k) e[k] = src[k];
@@ -103,29 +157,98 @@ struct Rows {
     }
     return a;
   }
-  __device__ __forceinline__ void unpack(const Raw<In, VEC>& a, int i, float (&f)[VEC]) const {
-    to_floats(a, f);
-    if (VEC > 1 && !whole(i)) {
+  __device__ __forceinline__ Vec<VEC> unpack(const Raw<In, VEC>& a, int i) const {
+    Vec<VEC> f;
+    to_floats(a, f.v);
+    if (!FULL && VEC > 1 && !whole(i)) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) f[e] = in(i, e) ? f[e] : 0.f;
     }
+    return f;
   }
-  __device__ __forceinline__ void store(void* base, long long r, int i, const float (&f)[VEC]) const {
+  __device__ __forceinline__ void store(void* base, long long r, int i, const Vec<VEC>& f) const {
     if (r >= rows || !any(i)) return;
     In* dst = reinterpret_cast<In*>(base) + r * cols + col(i, 0);
     if (whole(i)) {
-      *reinterpret_cast<Raw<In, VEC>*>(dst) = from_floats(f, In());
+      *reinterpret_cast<Raw<In, VEC>*>(dst) = from_floats(f.v, In());
     } else {
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
         if (in(i, e)) dst[e] = from_f32<In>(f[e]);
     }
   }
-  __device__ __forceinline__ void vector(const float* w, int i, float (&f)[VEC]) const {
+  __device__ __forceinline__ Vec<VEC> vector(const float* w, int i) const {
+    Vec<VEC> f;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) f[e] = in(i, e) ? w[col(i, e)] : 0.f;
+    return f;
   }
 };
+
+// The next rows' vectors of N tensors, a thread's own.  Where a row is one vector to a thread, copied asynchronously to shared memory ahead of
+// the kRows rows that are worked on together (one's arithmetic under the other's sums); else the next row's in registers.  Copies of less than 16
+// bytes (the tensor's end, no row) fill up with zeros.
+template <typename In, int VEC, int NV, int THREADS, bool FULL, int N>
+struct Ahead {
+  static constexpr bool kAsync = VEC > 1 && NV == 1, SUB = THREADS == kSubThreads;
+  static constexpr int kRows = kAsync && THREADS <= 512 ? 2 : 1, kStages = kAsync ? (kRows == 2 ? 6 : 3) : 1;   // rows in shared memory
+  Raw<In, VEC> raw[N][NV];
+  const void* base[N];
+  int st = 0;
+  __device__ __forceinline__ uint4* slot(int stage, int n) const {
+    extern __shared__ __align__(16) uint4 ahead_rows[];
+    return ahead_rows + ((size_t)stage * N + n) * blockDim.x + threadIdx.x;
+  }
+  __device__ __forceinline__ void fetch(const Rows<In, VEC, NV, SUB, FULL>& at, long long row, int stage) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if constexpr (kAsync) {
+        if (base[n]) {
+          const bool there = row < at.rows && at.any(0);
+          const long long from = there ? row * at.cols + at.col(0, 0) : 0, left = (at.total - from) * (long long)sizeof(In);
+          const int bytes = there ? (!FULL && left < 16 ? (int)left : 16) : 0;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(slot(stage, n))),
+                       "l"(reinterpret_cast<const In*>(base[n]) + from), "r"(bytes) : "memory");
+        }
+      } else if (base[n]) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) raw[n][i] = at.load(base[n], row, i);
+      }
+    }
+    if constexpr (kAsync) asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  __device__ __forceinline__ void start(const Rows<In, VEC, NV, SUB, FULL>& at) {
+#pragma unroll
+    for (int k = 0; k < (kAsync ? kStages - kRows : 1); ++k) fetch(at, at.row + k * at.step, k);
+  }
+  // the vectors of `row` and the next one or none to use(p, n, i, raw); copies for later ones
+  template <typename F> __device__ __forceinline__ void next(const Rows<In, VEC, NV, SUB, FULL>& at, long long row, F use) {
+    if constexpr (kAsync) {
+#pragma unroll
+      for (int p = 0; p < kRows; ++p) {
+        int to = st + kStages - kRows + p;
+        fetch(at, row + (kStages - kRows + p) * at.step, to >= kStages ? to - kStages : to);
+      }
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - kRows) : "memory");
+#pragma unroll
+      for (int p = 0; p < kRows; ++p)
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          if (base[n]) use(p, n, 0, *reinterpret_cast<const Raw<In, VEC>*>(slot(st + p, n)));
+      st = st + kRows == kStages ? 0 : st + kRows;
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (base[n]) use(0, n, i, raw[n][i]);
+      fetch(at, row + at.step, 0);
+    }
+  }
+};
+constexpr size_t ahead_bytes(int vec, int nv, int threads, bool sub, int tensors) {
+  return vec > 1 && nv == 1 ? (size_t)(!sub && threads > 512 ? 3 : 6) * tensors * threads * 16 : 0;
+}
 
 // Sums of N values over the threads that share a row; every thread gets them.  `slot`: this call's shared memory, two used in turn
 // so that one barrier is enough.
@@ -156,14 +279,17 @@ __device__ __forceinline__ void row_sum(float (&v)[N], int group, float (*slot)[
 
 // s = 1 / (1 + e^-z) and 1 - s, both from e^-|z| <= 1, so that neither is a difference of near numbers.
 __device__ __forceinline__ float sigmoid_of(float z, float* rest = nullptr) {
-  const float e = __expf(-fabsf(z)), big = __fdividef(1.f, 1.f + e), small = e * big;
+  const float e = ptx::ex2(-1.4426950408889634f * fabsf(z));
+  float big;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(big) : "f"(1.f + e));
+  const float small = e * big;
   if (rest) *rest = z < 0.f ? big : small;
   return z < 0.f ? small : big;
 }
 
 // A CTA's sums over its rows, from the threads' registers to part[CTA][which][cols]: short rows are added up group by group in shared memory.
-template <typename In, int VEC, int NV, bool SUB>
-__device__ __forceinline__ void put_sums(const Rows<In, VEC, NV, SUB>& at, const float (&acc)[NV][VEC], float* part, float* sum, int group) {
+template <typename In, int VEC, int NV, bool SUB, bool FULL>
+__device__ __forceinline__ void put_sums(const Rows<In, VEC, NV, SUB, FULL>& at, const Vec<VEC> (&acc)[NV], float* part, float* sum, int group) {
   if constexpr (!SUB) {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -189,16 +315,16 @@ __device__ __forceinline__ void put_sums(const Rows<In, VEC, NV, SUB>& at, const
 
 // ---------------------------------------------------------------- kernels (THREADS: kSubThreads for the short rows, else the most a CTA has)
 
-template <typename In, int VEC, int NV, int THREADS>
+template <typename In, int VEC, int NV, int THREADS, bool FULL>
 __global__ void __launch_bounds__(THREADS) gated_norm_kernel(NormParams p) {
   constexpr bool SUB = THREADS == kSubThreads;
   __shared__ float red[2][32][1];
-  const Rows<In, VEC, NV, SUB> at(p);
+  const Rows<In, VEC, NV, SUB, FULL> at(p);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  float w[NV][VEC];
+  Vec<VEC> w[NV];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) at.vector(p.w, i, w[i]);
+  for (int i = 0; i < NV; ++i) w[i] = at.vector(p.w, i);
   int turn = 0;
   for (long long row = at.row; at.on(row); row += at.step) {
     Raw<In, VEC> rx[NV], rz[NV];
@@ -209,132 +335,121 @@ __global__ void __launch_bounds__(THREADS) gated_norm_kernel(NormParams p) {
       for (int i = 0; i < NV; ++i) rz[i] = at.load(p.z, row, i);
     }
     float s[1] = {0.f};
+    Vec<VEC> x[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      float x[VEC];
-      at.unpack(rx[i], i, x);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) s[0] = fmaf(x[e], x[e], s[0]);
+      x[i] = at.unpack(rx[i], i);
+      s[0] = dot(x[i], x[i], s[0]);
     }
     row_sum<1, SUB>(s, p.group, red[turn]);
     turn ^= 1;
     const float rs = rsqrtf(s[0] / at.cols + p.eps);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      float x[VEC], z[VEC];
-      at.unpack(rx[i], i, x);
-      if (p.z) at.unpack(rz[i], i, z);
+      Vec<VEC> y = mul(mul(x[i], rs), w[i]);
+      if (p.z) {
+        Vec<VEC> z = at.unpack(rz[i], i);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        x[e] = x[e] * rs * w[i][e];
-        if (p.z) x[e] *= p.sigmoid ? sigmoid_of(z[e]) : z[e] * sigmoid_of(z[e]);
+        for (int e = 0; e < VEC; ++e) z[e] = p.sigmoid ? sigmoid_of(z[e]) : z[e] * sigmoid_of(z[e]);
+        y = mul(y, z);
       }
-      at.store(p.y, row, i, x);
+      at.store(p.y, row, i, y);
     }
   }
 }
 
-template <typename In, int VEC, int NV, int THREADS>
+template <typename In, int VEC, int NV, int THREADS, bool FULL>
 __global__ void __launch_bounds__(THREADS) gated_norm_back_kernel(NormParams p) {
   constexpr bool SUB = THREADS == kSubThreads;
-  __shared__ float red[2][32][2];
+  __shared__ float red[2][32][2 * Ahead<In, VEC, NV, THREADS, FULL, 3>::kRows];
   __shared__ float sum[SUB ? 32 * VEC : 1];
-  const Rows<In, VEC, NV, SUB> at(p);
+  const Rows<In, VEC, NV, SUB, FULL> at(p);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  float w[NV][VEC], dw[NV][VEC];
-  Raw<In, VEC> rx[NV], rz[NV], rd[NV];
-  auto load = [&](long long row) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      rx[i] = at.load(p.x, row, i);
-      rd[i] = at.load(p.dy, row, i);
-      if (p.z) rz[i] = at.load(p.z, row, i);
-    }
-  };
-  load(at.row);
+  Vec<VEC> w[NV], dw[NV];
+  Ahead<In, VEC, NV, THREADS, FULL, 3> rows;
+  rows.base[0] = p.x; rows.base[1] = p.dy; rows.base[2] = p.z;
+  rows.start(at);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    at.vector(p.w, i, w[i]);
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) dw[i][e] = 0.f;
+    w[i] = at.vector(p.w, i);
+    dw[i] = all_of<VEC>(0.f);
   }
   int turn = 0;
-  for (long long row = at.row; at.on(row); row += at.step) {
-    float x[NV][VEC], d[NV][VEC], a[NV][VEC], slope[NV][VEC];   // a = act(z)
+  constexpr int P = decltype(rows)::kRows;
+  for (long long row = at.row; at.on(row); row += P * at.step) {
+    Vec<VEC> x[P][NV], d[P][NV], a[P][NV], slope[P][NV];   // a = act(z)
+    rows.next(at, row, [&](int q, int n, int i, const Raw<In, VEC>& v) { (n == 0 ? x[q][i] : n == 1 ? d[q][i] : a[q][i]) = at.unpack(v, i); });
+    float s[2 * P];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      at.unpack(rx[i], i, x[i]);
-      at.unpack(rd[i], i, d[i]);
-      if (p.z) at.unpack(rz[i], i, a[i]);
+    for (int q = 0; q < P; ++q) {
+      s[2 * q] = s[2 * q + 1] = 0.f;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        float rest;
-        const float z = p.z ? a[i][e] : 0.f, s = sigmoid_of(z, &rest);
-        a[i][e] = p.z ? (p.sigmoid ? s : z * s) : 1.f;
-        slope[i][e] = p.sigmoid ? s * rest : s * (1.f + z * rest);
+      for (int i = 0; i < NV; ++i) {
+        if (p.z) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            float rest;
+            const float z = a[q][i][e], g = sigmoid_of(z, &rest);
+            a[q][i][e] = p.sigmoid ? g : z * g;
+            slope[q][i][e] = p.sigmoid ? g * rest : fmaf(a[q][i][e], rest, g);   // (silu: g (1 + z rest))
+          }
+          slope[q][i] = mul(slope[q][i], mul(d[q][i], w[i]));   // dz = slope d w x rs
+          d[q][i] = mul(d[q][i], a[q][i]);
+        }
+        s[2 * q] = dot(x[q][i], x[q][i], s[2 * q]);
+        s[2 * q + 1] = dot(mul(d[q][i], w[i]), x[q][i], s[2 * q + 1]);
       }
     }
-    load(row + at.step);
-    float s[2] = {0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        s[0] = fmaf(x[i][e], x[i][e], s[0]);
-        s[1] = fmaf(d[i][e] * w[i][e] * a[i][e], x[i][e], s[1]);
-      }
-    row_sum<2, SUB>(s, p.group, red[turn]);
+    row_sum<2 * P, SUB>(s, p.group, red[turn]);
     turn ^= 1;
-    const float rs = rsqrtf(s[0] / at.cols + p.eps), m = rs * rs * (s[1] / at.cols);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      float dx[VEC], dz[VEC];
+    for (int q = 0; q < P; ++q) {
+      const float rs = rsqrtf(s[2 * q] / at.cols + p.eps), m = -rs * rs * rs * (s[2 * q + 1] / at.cols);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const float dn = d[i][e] * x[i][e] * rs;
-        dx[e] = rs * (d[i][e] * w[i][e] * a[i][e] - x[i][e] * m);
-        dz[e] = dn * w[i][e] * slope[i][e];
-        dw[i][e] = fmaf(dn, a[i][e], dw[i][e]);
+      for (int i = 0; i < NV; ++i) {
+        const Vec<VEC> t = mul(d[q][i], rs);
+        at.store(p.dx, row + q * at.step, i, fma(t, w[i], mul(x[q][i], m)));
+        if (P == 1 || row + q * at.step < at.rows) dw[i] = fma(t, x[q][i], dw[i]);
+        if (p.z) at.store(p.dz, row + q * at.step, i, mul(slope[q][i], mul(x[q][i], rs)));
       }
-      at.store(p.dx, row, i, dx);
-      if (p.z) at.store(p.dz, row, i, dz);
     }
   }
-  put_sums<In, VEC, NV, SUB>(at, dw, p.part + (size_t)blockIdx.x * p.cols, sum, p.group);
+  put_sums(at, dw, p.part + (size_t)blockIdx.x * p.cols, sum, p.group);
 }
 
-template <typename In, int VEC, int NV, int THREADS, bool POST>
+template <typename In, int VEC, int NV, int THREADS, bool FULL, bool POST>
 __global__ void __launch_bounds__(THREADS) add_norm_kernel(NormParams p) {
   constexpr bool SUB = THREADS == kSubThreads;
   __shared__ float red[2][32][1];
-  const Rows<In, VEC, NV, SUB> at(p);
+  const Rows<In, VEC, NV, SUB, FULL> at(p);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  float w[NV][VEC], wp[NV][VEC];
+  Vec<VEC> w[NV], wp[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    at.vector(p.w, i, w[i]);
-    if (POST) at.vector(p.w_post, i, wp[i]);
+    w[i] = at.vector(p.w, i);
+    if (POST) wp[i] = at.vector(p.w_post, i);
   }
   int turn = 0;
   for (long long row = at.row; at.on(row); row += at.step) {
     Raw<In, VEC> rx[NV], rr[NV];
-    float r[NV][VEC];
+    Vec<VEC> x[NV], r[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       rx[i] = at.load(p.x, row, i);
       rr[i] = at.load(p.r, row, i);
     }
     float s[1] = {0.f}, fs = p.scale;
-    if (POST) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        float x[VEC];
-        at.unpack(rx[i], i, x);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) s[0] = fmaf(x[e], x[e], s[0]);
+    for (int i = 0; i < NV; ++i) {
+      x[i] = at.unpack(rx[i], i);
+      if (POST) {
+        s[0] = dot(x[i], x[i], s[0]);
+        x[i] = mul(x[i], wp[i]);
       }
+    }
+    if (POST) {
       row_sum<1, SUB>(s, p.group, red[turn]);
       turn ^= 1;
       fs = p.scale * rsqrtf(s[0] / at.cols + p.eps);
@@ -342,111 +457,94 @@ __global__ void __launch_bounds__(THREADS) add_norm_kernel(NormParams p) {
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      float x[VEC];
-      at.unpack(rx[i], i, x);
-      at.unpack(rr[i], i, r[i]);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        r[i][e] = fmaf(fs, POST ? x[e] * wp[i][e] : x[e], r[i][e]);
-        s[0] = fmaf(r[i][e], r[i][e], s[0]);
-      }
+      r[i] = fma(x[i], fs, at.unpack(rr[i], i));
+      s[0] = dot(r[i], r[i], s[0]);
       at.store(p.r_out, row, i, r[i]);
     }
     row_sum<1, SUB>(s, p.group, red[turn]);
     turn ^= 1;
     const float rs = rsqrtf(s[0] / at.cols + p.eps);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) r[i][e] *= rs * w[i][e];
-      at.store(p.y, row, i, r[i]);
-    }
+    for (int i = 0; i < NV; ++i) at.store(p.y, row, i, mul(mul(r[i], rs), w[i]));
   }
 }
 
-template <typename In, int VEC, int NV, int THREADS, bool POST>
+template <typename In, int VEC, int NV, int THREADS, bool FULL, bool POST>
 __global__ void __launch_bounds__(THREADS) add_norm_back_kernel(NormParams p) {
   constexpr bool SUB = THREADS == kSubThreads;
-  __shared__ float red[2][32][3];
-  __shared__ float red1[2][32][1];
+  constexpr int kR = Ahead<In, VEC, NV, THREADS, FULL, 3>::kRows;
+  __shared__ float red[2][32][3 * kR];
+  __shared__ float red1[2][32][kR];
   __shared__ float sum[SUB ? 32 * VEC : 1];
-  const Rows<In, VEC, NV, SUB> at(p);
+  const Rows<In, VEC, NV, SUB, FULL> at(p);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  float w[NV][VEC], wp[NV][VEC], dw[NV][VEC], dwp[NV][VEC];
-  Raw<In, VEC> rx[NV], rr[NV], rd[NV], rg[NV];
-  auto load = [&](long long row) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      rr[i] = at.load(p.r, row, i);
-      rd[i] = at.load(p.dy, row, i);
-      if (POST) rx[i] = at.load(p.x, row, i);
-      if (p.dr_out) rg[i] = at.load(p.dr_out, row, i);
-    }
-  };
-  load(at.row);
+  Vec<VEC> w[NV], wp[NV], dw[NV], dwp[NV];
+  Ahead<In, VEC, NV, THREADS, FULL, POST ? 4 : 3> rows;
+  rows.base[0] = p.r; rows.base[1] = p.dy; rows.base[2] = p.dr_out;
+  if constexpr (POST) rows.base[3] = p.x;
+  rows.start(at);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    at.vector(p.w, i, w[i]);
-    if (POST) at.vector(p.w_post, i, wp[i]);
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) dw[i][e] = dwp[i][e] = 0.f;
+    w[i] = at.vector(p.w, i);
+    if (POST) wp[i] = at.vector(p.w_post, i);
+    dw[i] = dwp[i] = all_of<VEC>(0.f);
   }
   int turn = 0;
-  for (long long row = at.row; at.on(row); row += at.step) {
-    float r[NV][VEC], d[NV][VEC], x[NV][VEC], g[NV][VEC];
+  constexpr int P = decltype(rows)::kRows;
+  for (long long row = at.row; at.on(row); row += P * at.step) {
+    Vec<VEC> r[P][NV], d[P][NV], x[P][NV], g[P][NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      at.unpack(rr[i], i, r[i]);
-      at.unpack(rd[i], i, d[i]);
-      if (POST) at.unpack(rx[i], i, x[i]);
-      if (p.dr_out) at.unpack(rg[i], i, g[i]);
-    }
-    load(row + at.step);
-    float s[3] = {0.f, 0.f, 0.f};
+    for (int q = 0; q < P; ++q)
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+      for (int i = 0; i < NV; ++i) g[q][i] = all_of<VEC>(0.f);
+    rows.next(at, row, [&](int q, int n, int i, const Raw<In, VEC>& v) {
+      (n == 0 ? r[q][i] : n == 1 ? d[q][i] : n == 2 ? g[q][i] : x[q][i]) = at.unpack(v, i);
+    });
+    float s[3 * P], u[P];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        s[0] = fmaf(r[i][e], r[i][e], s[0]);
-        s[1] = fmaf(d[i][e] * w[i][e], r[i][e], s[1]);
-        if (POST) s[2] = fmaf(x[i][e], x[i][e], s[2]);
-      }
-    row_sum<3, SUB>(s, p.group, red[turn]);
-    const float rs = rsqrtf(s[0] / at.cols + p.eps), m = rs * rs * (s[1] / at.cols);
-    float u[1] = {0.f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        dw[i][e] = fmaf(d[i][e] * rs, r[i][e], dw[i][e]);
-        r[i][e] = rs * (d[i][e] * w[i][e] - r[i][e] * m);            // dr
-        if (p.dr_out) r[i][e] += g[i][e];
-        if (POST) u[0] = fmaf(r[i][e] * wp[i][e], x[i][e], u[0]);
-      }
-      at.store(p.dr, row, i, r[i]);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) r[i][e] *= p.scale;              // df
-      if (!POST) at.store(p.dx, row, i, r[i]);
-    }
-    if (POST) {
-      row_sum<1, SUB>(u, p.group, red1[turn]);
-      const float rx_ = rsqrtf(s[2] / at.cols + p.eps), mx = rx_ * rx_ * (p.scale * u[0] / at.cols);
+    for (int q = 0; q < P; ++q) {
+      s[3 * q] = s[3 * q + 1] = s[3 * q + 2] = u[q] = 0.f;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
+        s[3 * q] = dot(r[q][i], r[q][i], s[3 * q]);
+        s[3 * q + 1] = dot(mul(d[q][i], w[i]), r[q][i], s[3 * q + 1]);
+        if (POST) s[3 * q + 2] = dot(x[q][i], x[q][i], s[3 * q + 2]);
+      }
+    }
+    row_sum<3 * P, SUB>(s, p.group, red[turn]);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          dwp[i][e] = fmaf(r[i][e] * rx_, x[i][e], dwp[i][e]);
-          r[i][e] = rx_ * (r[i][e] * wp[i][e] - x[i][e] * mx);
+    for (int q = 0; q < P; ++q) {
+      const float rs = rsqrtf(s[3 * q] / at.cols + p.eps), m = -rs * rs * rs * (s[3 * q + 1] / at.cols);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const Vec<VEC> t = mul(d[q][i], rs);
+        if (P == 1 || row + q * at.step < at.rows) dw[i] = fma(t, r[q][i], dw[i]);
+        r[q][i] = fma(t, w[i], fma(r[q][i], m, g[q][i]));              // dr
+        if (POST) u[q] = dot(mul(r[q][i], wp[i]), x[q][i], u[q]);
+        at.store(p.dr, row + q * at.step, i, r[q][i]);
+        r[q][i] = mul(r[q][i], p.scale);                               // df
+        if (!POST) at.store(p.dx, row + q * at.step, i, r[q][i]);
+      }
+    }
+    if (POST) {
+      row_sum<P, SUB>(u, p.group, red1[turn]);
+#pragma unroll
+      for (int q = 0; q < P; ++q) {
+        const float rx = rsqrtf(s[3 * q + 2] / at.cols + p.eps), mx = -rx * rx * rx * (p.scale * u[q] / at.cols);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const Vec<VEC> t = mul(r[q][i], rx);
+          if (P == 1 || row + q * at.step < at.rows) dwp[i] = fma(t, x[q][i], dwp[i]);
+          at.store(p.dx, row + q * at.step, i, fma(t, wp[i], mul(x[q][i], mx)));
         }
-        at.store(p.dx, row, i, r[i]);
       }
     }
     turn ^= 1;
   }
   float* part = p.part + (size_t)blockIdx.x * (POST ? 2 : 1) * p.cols;
-  put_sums<In, VEC, NV, SUB>(at, dw, part, sum, p.group);
-  if (POST) put_sums<In, VEC, NV, SUB>(at, dwp, part + p.cols, sum, p.group);
+  put_sums(at, dw, part, sum, p.group);
+  if (POST) put_sums(at, dwp, part + p.cols, sum, p.group);
 }
 
 // Sums of the CTAs' sums: a warp's lanes have 32 neighbouring columns, the 32 warps every 32nd CTA.  blockIdx.y: which vector.
@@ -478,13 +576,14 @@ __global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const float
 
 // ---------------------------------------------------------------- host
 
-struct Shape { int vec, nv, group, threads, groups; bool sub; };   // group: lanes of a row (sub), groups: rows of a CTA at once
+struct Shape { int vec, nv, group, threads, groups; bool sub, full; };   // group: lanes of a row (sub), groups: rows of a CTA at once
 
 // `fast`: every tensor 16-byte aligned
 Shape shape_of(int cols, bool bf16, bool fast) {
   Shape s;
   s.vec = fast ? (bf16 ? 8 : 4) : 1;
-  const int vectors = cols % s.vec ? (cols + s.vec - 1) / s.vec + 1 : cols / s.vec;   // of the worst start
+  s.full = cols % s.vec == 0;
+  const int vectors = !s.full ? (cols + s.vec - 1) / s.vec + 1 : cols / s.vec;   // of the worst start
   s.sub = vectors <= 32;
   s.group = 1;
   s.nv = 1;
@@ -509,7 +608,7 @@ int ctas_of(const Shape& s, long long rows, int most_threads) {
   return (int)(n > 0 ? n : 1);
 }
 
-// Threads of an SM in the backward kernels, whose CTAs keep sums: more would only lengthen the second kernel.
+// Threads of an SM: the backward kernels' CTAs keep sums, so there are no more of them than run at a time (see pick), this many at most.
 constexpr int kBackThreads = 1024, kForwardThreads = 16384;
 
 int back_ctas(int cols, bool bf16, long long rows) {     // (of the workspace: either way of reading)
@@ -518,10 +617,11 @@ int back_ctas(int cols, bool bf16, long long rows) {     // (of the workspace: e
 }
 
 template <typename... Args>
-cudaError_t start(void (*kernel)(Args...), dim3 grid, int threads, cudaStream_t stream, Args... args) {
+cudaError_t start(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, cudaStream_t stream, Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -533,41 +633,60 @@ cudaError_t start(void (*kernel)(Args...), dim3 grid, int threads, cudaStream_t 
 
 enum Kind { kGated, kGatedBack, kAdd, kAddBack };
 
-template <typename In, int VEC, int NV, int THREADS>
-cudaError_t pick(Kind kind, const NormParams& p, int ctas, int threads, cudaStream_t stream) {
+template <typename In, int VEC, int NV, int THREADS, bool FULL>
+cudaError_t pick(Kind kind, const NormParams& p, int& ctas, int threads, cudaStream_t stream) {
   void (*k)(NormParams) = nullptr;
   switch (kind) {
-    case kGated: k = gated_norm_kernel<In, VEC, NV, THREADS>; break;
-    case kGatedBack: k = gated_norm_back_kernel<In, VEC, NV, THREADS>; break;
-    case kAdd: k = p.w_post ? add_norm_kernel<In, VEC, NV, THREADS, true> : add_norm_kernel<In, VEC, NV, THREADS, false>; break;
-    case kAddBack: k = p.w_post ? add_norm_back_kernel<In, VEC, NV, THREADS, true> : add_norm_back_kernel<In, VEC, NV, THREADS, false>; break;
+    case kGated: k = gated_norm_kernel<In, VEC, NV, THREADS, FULL>; break;
+    case kGatedBack: k = gated_norm_back_kernel<In, VEC, NV, THREADS, FULL>; break;
+    case kAdd: k = p.w_post ? add_norm_kernel<In, VEC, NV, THREADS, FULL, true> : add_norm_kernel<In, VEC, NV, THREADS, FULL, false>; break;
+    case kAddBack: k = p.w_post ? add_norm_back_kernel<In, VEC, NV, THREADS, FULL, true> : add_norm_back_kernel<In, VEC, NV, THREADS, FULL, false>; break;
   }
-  return start(k, dim3((unsigned)ctas), threads, stream, p);
+  size_t smem = 0;
+  if (kind == kGatedBack || kind == kAddBack) {
+    smem = ahead_bytes(VEC, NV, threads, THREADS == kSubThreads, kind == kAddBack && p.w_post ? 4 : 3);
+    cudaError_t e = smem > 0 ? cudaFuncSetAttribute(reinterpret_cast<const void*>(k), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+    int resident = 1;
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, k, threads, smem);
+    if (e != cudaSuccess) return e;
+    const int most = (sm_count() * (resident > 0 ? resident : 1) + 7) / 8 * 8;   // (rows of a CTA stay a multiple of 8 apart)
+    if (ctas > most) ctas = most;
+  }
+  return start(k, dim3((unsigned)ctas), threads, smem, stream, p);
 }
 
-template <typename In, int VEC>
-cudaError_t by_length(Kind kind, const NormParams& p, const Shape& s, int ctas, cudaStream_t stream) {
-  if (s.sub) return pick<In, VEC, 1, kSubThreads>(kind, p, ctas, s.threads, stream);
-  if (s.nv == 1) return s.threads <= 512 ? pick<In, VEC, 1, 512>(kind, p, ctas, s.threads, stream) : pick<In, VEC, 1, 1024>(kind, p, ctas, s.threads, stream);
-  if (s.nv == 2) return pick<In, VEC, 2, 1024>(kind, p, ctas, s.threads, stream);
-  if (s.nv == 4) return pick<In, VEC, 4, 1024>(kind, p, ctas, s.threads, stream);   // (bf16, 16 bytes at a time: 2049 vectors are the most)
+template <typename In, int VEC, bool FULL>
+cudaError_t by_length(Kind kind, const NormParams& p, const Shape& s, int& ctas, cudaStream_t stream) {
+  if (s.sub) return pick<In, VEC, 1, kSubThreads, FULL>(kind, p, ctas, s.threads, stream);
+  if (s.nv == 1) return s.threads <= 512 ? pick<In, VEC, 1, 512, FULL>(kind, p, ctas, s.threads, stream) : pick<In, VEC, 1, 1024, FULL>(kind, p, ctas, s.threads, stream);
+  if (s.nv == 2) return pick<In, VEC, 2, 1024, FULL>(kind, p, ctas, s.threads, stream);
+  if (s.nv == 4) return pick<In, VEC, 4, 1024, FULL>(kind, p, ctas, s.threads, stream);   // (bf16, 16 bytes at a time: 2049 vectors are the most)
   if constexpr (VEC <= 4) {
-    if (s.nv == 8) return pick<In, VEC, 8, 1024>(kind, p, ctas, s.threads, stream);   // (fp32: 4097)
+    if (s.nv == 8) return pick<In, VEC, 8, 1024, FULL>(kind, p, ctas, s.threads, stream);   // (fp32: 4097)
   }
-  if constexpr (VEC == 1) return pick<In, VEC, 16, 1024>(kind, p, ctas, s.threads, stream);
+  if constexpr (VEC == 1) return pick<In, VEC, 16, 1024, FULL>(kind, p, ctas, s.threads, stream);
   return cudaErrorInvalidValue;
+}
+
+// (element by element all rows are whole)
+template <typename In, int VEC>
+cudaError_t by_start(Kind kind, const NormParams& p, const Shape& s, int& ctas, cudaStream_t stream) {
+  if constexpr (VEC > 1) {
+    if (!s.full) return by_length<In, VEC, false>(kind, p, s, ctas, stream);
+  }
+  return by_length<In, VEC, true>(kind, p, s, ctas, stream);
 }
 
 cudaError_t run(Kind kind, NormParams& p, int dtype, uintptr_t addresses, float* dw, float* dw_post, cudaStream_t stream) {
   const bool bf16 = dtype == HA_LA_BF16, fast = !(addresses & 15), back = kind == kGatedBack || kind == kAddBack;
   const Shape s = shape_of(p.cols, bf16, fast);
   p.group = s.group;
-  const int ctas = ctas_of(s, p.rows, back ? kBackThreads : kForwardThreads);
-  cudaError_t e = bf16 ? (fast ? by_length<__nv_bfloat16, 8>(kind, p, s, ctas, stream) : by_length<__nv_bfloat16, 1>(kind, p, s, ctas, stream))
-                       : (fast ? by_length<float, 4>(kind, p, s, ctas, stream) : by_length<float, 1>(kind, p, s, ctas, stream));
+  int ctas = ctas_of(s, p.rows, back ? kBackThreads : kForwardThreads);
+  cudaError_t e = bf16 ? (fast ? by_start<__nv_bfloat16, 8>(kind, p, s, ctas, stream) : by_start<__nv_bfloat16, 1>(kind, p, s, ctas, stream))
+                       : (fast ? by_start<float, 4>(kind, p, s, ctas, stream) : by_start<float, 1>(kind, p, s, ctas, stream));
   if (e != cudaSuccess || !back) return e;
   const int both = dw_post ? 2 : 1;
-  return start(norm_reduce_kernel, dim3((unsigned)((p.cols + 31) / 32), (unsigned)both), kReduceThreads, stream,
+  return start(norm_reduce_kernel, dim3((unsigned)((p.cols + 31) / 32), (unsigned)both), kReduceThreads, 0, stream,
                (const float*)p.part, ctas, p.cols, both, dw, dw_post);
 }
 
