@@ -13,8 +13,8 @@
 // read in aligned vectors all the same, with the neighbours' values at its ends masked: a group's rows are a multiple of 8 apart, so the
 // column that an element of a thread holds is the same in every row, weights stay in registers and so do the sums for dw, which
 // a second kernel adds up over CTAs in order (no atomics: the same bits every time).  Rows in flight: the backward loops copy the next rows to shared
-// memory asynchronously, each thread for itself; with the next row in registers instead 262144 rows of 128 took 89 us instead of FIGURE_GATED, 16384
-// of 2048 with both norms 105 instead of FIGURE_ADD.
+// memory asynchronously, each thread for itself; with the next row in registers instead 262144 rows of 128 took 89 us instead of 73, 16384
+// of 2048 with both norms 105 instead of 91.
 #include "common.cuh"
 #include "tc_mma.cuh"
 
@@ -125,6 +125,10 @@ template <typename In, int VEC, int NV, bool SUB, bool FULL>
 struct Rows {
   int t, threads, shift, cols;
   long long row, step, rows, total;                      // this group's first row, rows between its rows
+  // Of rows that start anywhere: the bits of a vector that are the row's, and for a vector at one of its ends (not both) the pieces of 8, 4 and
+  // 2 bytes that it is stored in, as 1 + the piece's place or 0.  The same for every row of the group; kept for the first vector of a thread only.
+  uint4 mask;
+  uint32_t pieces;
   __device__ __forceinline__ explicit Rows(const NormParams& p) {
     threads = SUB ? p.group : blockDim.x;
     t = SUB ? threadIdx.x & (p.group - 1) : threadIdx.x;
@@ -135,6 +139,37 @@ struct Rows {
     cols = p.cols;
     total = p.rows * p.cols;
     shift = FULL ? 0 : (int)((row * cols) & (VEC - 1));
+    pieces = 0;
+    if constexpr (!FULL && VEC > 1) {
+      const int first = max(0, -col(0, 0)), end = min(VEC, cols - col(0, 0));   // elements of the vector that are the row's
+      uint32_t m[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        m[k] = 0;
+#pragma unroll
+        for (int e = k * VEC / 4; e < (k + 1) * VEC / 4; ++e)
+          if (e >= first && e < end) m[k] |= VEC == 4 ? 0xffffffffu : 0xffffu << 16 * (e & 1);
+      }
+      mask = make_uint4(m[0], m[1], m[2], m[3]);
+      if (end - first > 0 && end - first < VEC && (first == 0 || end == VEC)) {
+        // a run from `first` up to the vector's end: the smaller pieces come first; one from its start up to `end`: the larger ones do
+        const int unit = 16 / VEC, n = (end - first) * unit;   // bytes
+        const int base = first * unit;
+        int at2 = -1, at4 = -1, at8 = -1;
+        if (first > 0) {
+          int o = base;
+          if (n & 2) { at2 = o; o += 2; }
+          if (n & 4) { at4 = o; o += 4; }
+          if (n & 8) at8 = o;
+        } else {
+          int o = 0;
+          if (n & 8) { at8 = o; o += 8; }
+          if (n & 4) { at4 = o; o += 4; }
+          if (n & 2) at2 = o;
+        }
+        pieces = (uint32_t)(at8 + 1) | (uint32_t)(at4 + 1) << 8 | (uint32_t)(at2 + 1) << 16 | 1u << 24;
+      }
+    }
   }
   // the loop over a group's rows goes on as long as any group of the CTA has one: its threads meet in the sums
   __device__ __forceinline__ bool on(long long r) const {
@@ -159,6 +194,12 @@ struct Rows {
   }
   __device__ __forceinline__ Vec<VEC> unpack(const Raw<In, VEC>& a, int i) const {
     Vec<VEC> f;
+    if constexpr (!FULL && VEC > 1 && NV == 1) {
+      uint4 w = *reinterpret_cast<const uint4*>(&a);
+      w.x &= mask.x; w.y &= mask.y; w.z &= mask.z; w.w &= mask.w;
+      to_floats(*reinterpret_cast<const Raw<In, VEC>*>(&w), f.v);
+      return f;
+    }
     to_floats(a, f.v);
     if (!FULL && VEC > 1 && !whole(i)) {
 #pragma unroll
@@ -171,6 +212,15 @@ struct Rows {
     In* dst = reinterpret_cast<In*>(base) + r * cols + col(i, 0);
     if (whole(i)) {
       *reinterpret_cast<Raw<In, VEC>*>(dst) = from_floats(f.v, In());
+    } else if (!FULL && VEC > 1 && NV == 1 && pieces) {
+      const Raw<In, VEC> a = from_floats(f.v, In());
+      const uint4 w = *reinterpret_cast<const uint4*>(&a);
+      char* to = reinterpret_cast<char*>(dst);
+      auto word = [&](int o) { return o < 8 ? (o < 4 ? w.x : w.y) : (o < 12 ? w.z : w.w); };   // of byte o
+      const int at8 = (int)(pieces & 255) - 1, at4 = (int)(pieces >> 8 & 255) - 1, at2 = (int)(pieces >> 16 & 255) - 1;
+      if (at8 >= 0) *reinterpret_cast<uint2*>(to + at8) = make_uint2(word(at8), word(at8 + 4));
+      if (at4 >= 0) *reinterpret_cast<uint32_t*>(to + at4) = word(at4);
+      if (VEC == 8 && at2 >= 0) *reinterpret_cast<uint16_t*>(to + at2) = (uint16_t)(word(at2) >> 8 * (at2 & 2));
     } else {
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
@@ -185,30 +235,33 @@ struct Rows {
   }
 };
 
-// The next rows' vectors of N tensors, a thread's own.  Where a row is one vector to a thread, copied asynchronously to shared memory ahead of
-// the kRows rows that are worked on together (one's arithmetic under the other's sums); else the next row's in registers.  Copies of less than 16
+// The next rows' vectors of N tensors, a thread's own.  Where a row is one or two vectors to a thread, copied asynchronously to shared memory ahead
+// of the kRows rows that are worked on together (one's arithmetic under the other's sums); else the next row's in registers.  Copies of less than 16
 // bytes (the tensor's end, no row) fill up with zeros.
 template <typename In, int VEC, int NV, int THREADS, bool FULL, int N>
 struct Ahead {
-  static constexpr bool kAsync = VEC > 1 && NV == 1, SUB = THREADS == kSubThreads;
-  static constexpr int kRows = kAsync && THREADS <= 512 ? 2 : 1, kStages = kAsync ? (kRows == 2 ? 6 : 3) : 1;   // rows in shared memory
+  static constexpr bool kAsync = VEC > 1 && NV <= 2 && THREADS <= 512, SUB = THREADS == kSubThreads;
+  static constexpr int kRows = kAsync && NV == 1 ? 2 : 1, kStages = kAsync ? 3 * kRows : 1;   // rows in shared memory
   Raw<In, VEC> raw[N][NV];
   const void* base[N];
   int st = 0;
-  __device__ __forceinline__ uint4* slot(int stage, int n) const {
+  __device__ __forceinline__ uint4* slot(int stage, int n, int i) const {
     extern __shared__ __align__(16) uint4 ahead_rows[];
-    return ahead_rows + ((size_t)stage * N + n) * blockDim.x + threadIdx.x;
+    return ahead_rows + ((stage * N + n) * NV + i) * (int)blockDim.x + threadIdx.x;
   }
   __device__ __forceinline__ void fetch(const Rows<In, VEC, NV, SUB, FULL>& at, long long row, int stage) {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       if constexpr (kAsync) {
         if (base[n]) {
-          const bool there = row < at.rows && at.any(0);
-          const long long from = there ? row * at.cols + at.col(0, 0) : 0, left = (at.total - from) * (long long)sizeof(In);
-          const int bytes = there ? (!FULL && left < 16 ? (int)left : 16) : 0;
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(slot(stage, n))),
-                       "l"(reinterpret_cast<const In*>(base[n]) + from), "r"(bytes) : "memory");
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            const bool there = row < at.rows && at.any(i);
+            const long long from = there ? row * at.cols + at.col(i, 0) : 0, left = (at.total - from) * (long long)sizeof(In);
+            const int bytes = there ? (!FULL && left < 16 ? (int)left : 16) : 0;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(slot(stage, n, i))),
+                         "l"(reinterpret_cast<const In*>(base[n]) + from), "r"(bytes) : "memory");
+          }
         }
       } else if (base[n]) {
 #pragma unroll
@@ -234,7 +287,9 @@ struct Ahead {
       for (int p = 0; p < kRows; ++p)
 #pragma unroll
         for (int n = 0; n < N; ++n)
-          if (base[n]) use(p, n, 0, *reinterpret_cast<const Raw<In, VEC>*>(slot(st + p, n)));
+#pragma unroll
+          for (int i = 0; i < NV; ++i)
+            if (base[n]) use(p, n, i, *reinterpret_cast<const Raw<In, VEC>*>(slot(st + p, n, i)));
       st = st + kRows == kStages ? 0 : st + kRows;
     } else {
 #pragma unroll
@@ -246,8 +301,8 @@ struct Ahead {
     }
   }
 };
-constexpr size_t ahead_bytes(int vec, int nv, int threads, bool sub, int tensors) {
-  return vec > 1 && nv == 1 ? (size_t)(!sub && threads > 512 ? 3 : 6) * tensors * threads * 16 : 0;
+constexpr size_t ahead_bytes(int vec, int nv, int threads, int tensors) {
+  return vec > 1 && nv <= 2 && threads <= 512 ? (size_t)6 * tensors * threads * 16 : 0;   // (nv == 1: six rows, nv == 2: three)
 }
 
 // Sums of N values over the threads that share a row; every thread gets them.  `slot`: this call's shared memory, two used in turn
@@ -316,7 +371,7 @@ __device__ __forceinline__ void put_sums(const Rows<In, VEC, NV, SUB, FULL>& at,
 // ---------------------------------------------------------------- kernels (THREADS: kSubThreads for the short rows, else the most a CTA has)
 
 template <typename In, int VEC, int NV, int THREADS, bool FULL>
-__global__ void __launch_bounds__(THREADS) gated_norm_kernel(NormParams p) {
+__global__ void __launch_bounds__(THREADS == 257 ? 256 : THREADS) gated_norm_kernel(NormParams p) {
   constexpr bool SUB = THREADS == kSubThreads;
   __shared__ float red[2][32][1];
   const Rows<In, VEC, NV, SUB, FULL> at(p);
@@ -359,7 +414,7 @@ __global__ void __launch_bounds__(THREADS) gated_norm_kernel(NormParams p) {
 }
 
 template <typename In, int VEC, int NV, int THREADS, bool FULL>
-__global__ void __launch_bounds__(THREADS) gated_norm_back_kernel(NormParams p) {
+__global__ void __launch_bounds__(THREADS == 257 ? 256 : THREADS, THREADS <= 257 ? 2 : 1) gated_norm_back_kernel(NormParams p) {
   constexpr bool SUB = THREADS == kSubThreads;
   __shared__ float red[2][32][2 * Ahead<In, VEC, NV, THREADS, FULL, 3>::kRows];
   __shared__ float sum[SUB ? 32 * VEC : 1];
@@ -419,7 +474,7 @@ __global__ void __launch_bounds__(THREADS) gated_norm_back_kernel(NormParams p) 
 }
 
 template <typename In, int VEC, int NV, int THREADS, bool FULL, bool POST>
-__global__ void __launch_bounds__(THREADS) add_norm_kernel(NormParams p) {
+__global__ void __launch_bounds__(THREADS == 257 ? 256 : THREADS) add_norm_kernel(NormParams p) {
   constexpr bool SUB = THREADS == kSubThreads;
   __shared__ float red[2][32][1];
   const Rows<In, VEC, NV, SUB, FULL> at(p);
@@ -470,7 +525,7 @@ __global__ void __launch_bounds__(THREADS) add_norm_kernel(NormParams p) {
 }
 
 template <typename In, int VEC, int NV, int THREADS, bool FULL, bool POST>
-__global__ void __launch_bounds__(THREADS) add_norm_back_kernel(NormParams p) {
+__global__ void __launch_bounds__(THREADS == 257 ? 256 : THREADS, THREADS <= 257 ? 2 : 1) add_norm_back_kernel(NormParams p) {
   constexpr bool SUB = THREADS == kSubThreads;
   constexpr int kR = Ahead<In, VEC, NV, THREADS, FULL, 3>::kRows;
   __shared__ float red[2][32][3 * kR];
@@ -579,7 +634,7 @@ __global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const float
 struct Shape { int vec, nv, group, threads, groups; bool sub, full; };   // group: lanes of a row (sub), groups: rows of a CTA at once
 
 // `fast`: every tensor 16-byte aligned
-Shape shape_of(int cols, bool bf16, bool fast) {
+Shape shape_of(int cols, bool bf16, bool fast, bool back) {
   Shape s;
   s.vec = fast ? (bf16 ? 8 : 4) : 1;
   s.full = cols % s.vec == 0;
@@ -592,7 +647,8 @@ Shape shape_of(int cols, bool bf16, bool fast) {
     s.threads = kSubThreads;
     s.groups = kSubThreads / s.group;
   } else {
-    while (s.nv * 1024 < vectors) s.nv *= 2;
+    // backward, where a thread has more to keep: up to 256 threads with a vector each, then up to 1024 with two and more
+    while (s.nv * (back && s.nv == 1 ? 256 : 1024) < vectors) s.nv *= 2;
     s.threads = ((vectors + s.nv - 1) / s.nv + 31) / 32 * 32;
     s.groups = 1;
   }
@@ -612,7 +668,7 @@ int ctas_of(const Shape& s, long long rows, int most_threads) {
 constexpr int kBackThreads = 1024, kForwardThreads = 16384;
 
 int back_ctas(int cols, bool bf16, long long rows) {     // (of the workspace: either way of reading)
-  const int a = ctas_of(shape_of(cols, bf16, true), rows, kBackThreads), b = ctas_of(shape_of(cols, bf16, false), rows, kBackThreads);
+  const int a = ctas_of(shape_of(cols, bf16, true, true), rows, kBackThreads), b = ctas_of(shape_of(cols, bf16, false, true), rows, kBackThreads);
   return a > b ? a : b;
 }
 
@@ -633,38 +689,48 @@ cudaError_t start(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, 
 
 enum Kind { kGated, kGatedBack, kAdd, kAddBack };
 
-template <typename In, int VEC, int NV, int THREADS, bool FULL>
+template <typename In, int VEC, int NV, int THREADS, bool FULL, bool BACK>
 cudaError_t pick(Kind kind, const NormParams& p, int& ctas, int threads, cudaStream_t stream) {
   void (*k)(NormParams) = nullptr;
-  switch (kind) {
-    case kGated: k = gated_norm_kernel<In, VEC, NV, THREADS, FULL>; break;
-    case kGatedBack: k = gated_norm_back_kernel<In, VEC, NV, THREADS, FULL>; break;
-    case kAdd: k = p.w_post ? add_norm_kernel<In, VEC, NV, THREADS, FULL, true> : add_norm_kernel<In, VEC, NV, THREADS, FULL, false>; break;
-    case kAddBack: k = p.w_post ? add_norm_back_kernel<In, VEC, NV, THREADS, FULL, true> : add_norm_back_kernel<In, VEC, NV, THREADS, FULL, false>; break;
-  }
   size_t smem = 0;
-  if (kind == kGatedBack || kind == kAddBack) {
-    smem = ahead_bytes(VEC, NV, threads, THREADS == kSubThreads, kind == kAddBack && p.w_post ? 4 : 3);
+  if constexpr (BACK) {
+    if (kind == kGatedBack) k = gated_norm_back_kernel<In, VEC, NV, THREADS, FULL>;
+    else k = p.w_post ? add_norm_back_kernel<In, VEC, NV, THREADS, FULL, true> : add_norm_back_kernel<In, VEC, NV, THREADS, FULL, false>;
+    smem = ahead_bytes(VEC, NV, threads, kind == kAddBack && p.w_post ? 4 : 3);
     cudaError_t e = smem > 0 ? cudaFuncSetAttribute(reinterpret_cast<const void*>(k), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
     int resident = 1;
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, k, threads, smem);
     if (e != cudaSuccess) return e;
     const int most = (sm_count() * (resident > 0 ? resident : 1) + 7) / 8 * 8;   // (rows of a CTA stay a multiple of 8 apart)
     if (ctas > most) ctas = most;
+  } else {
+    if (kind == kGated) k = gated_norm_kernel<In, VEC, NV, THREADS, FULL>;
+    else k = p.w_post ? add_norm_kernel<In, VEC, NV, THREADS, FULL, true> : add_norm_kernel<In, VEC, NV, THREADS, FULL, false>;
   }
   return start(k, dim3((unsigned)ctas), threads, smem, stream, p);
 }
 
-template <typename In, int VEC, bool FULL>
+// (THREADS of longer rows: 257 stands for up to 256, told apart from the short rows' CTAs)
+template <typename In, int VEC, bool FULL, bool BACK>
 cudaError_t by_length(Kind kind, const NormParams& p, const Shape& s, int& ctas, cudaStream_t stream) {
-  if (s.sub) return pick<In, VEC, 1, kSubThreads, FULL>(kind, p, ctas, s.threads, stream);
-  if (s.nv == 1) return s.threads <= 512 ? pick<In, VEC, 1, 512, FULL>(kind, p, ctas, s.threads, stream) : pick<In, VEC, 1, 1024, FULL>(kind, p, ctas, s.threads, stream);
-  if (s.nv == 2) return pick<In, VEC, 2, 1024, FULL>(kind, p, ctas, s.threads, stream);
-  if (s.nv == 4) return pick<In, VEC, 4, 1024, FULL>(kind, p, ctas, s.threads, stream);   // (bf16, 16 bytes at a time: 2049 vectors are the most)
-  if constexpr (VEC <= 4) {
-    if (s.nv == 8) return pick<In, VEC, 8, 1024, FULL>(kind, p, ctas, s.threads, stream);   // (fp32: 4097)
+  if (s.sub) return pick<In, VEC, 1, kSubThreads, FULL, BACK>(kind, p, ctas, s.threads, stream);
+  if (s.nv == 1) {
+    if (s.threads <= 256) return pick<In, VEC, 1, 257, FULL, BACK>(kind, p, ctas, s.threads, stream);
+    if constexpr (!BACK)
+      return s.threads <= 512 ? pick<In, VEC, 1, 512, FULL, BACK>(kind, p, ctas, s.threads, stream) : pick<In, VEC, 1, 1024, FULL, BACK>(kind, p, ctas, s.threads, stream);
   }
-  if constexpr (VEC == 1) return pick<In, VEC, 16, 1024, FULL>(kind, p, ctas, s.threads, stream);
+  if (s.nv == 2) {
+    if constexpr (BACK) {
+      if (s.threads <= 256) return pick<In, VEC, 2, 257, FULL, BACK>(kind, p, ctas, s.threads, stream);
+      if (s.threads <= 512) return pick<In, VEC, 2, 512, FULL, BACK>(kind, p, ctas, s.threads, stream);
+    }
+    return pick<In, VEC, 2, 1024, FULL, BACK>(kind, p, ctas, s.threads, stream);
+  }
+  if (s.nv == 4) return pick<In, VEC, 4, 1024, FULL, BACK>(kind, p, ctas, s.threads, stream);   // (bf16, 16 bytes at a time: 2049 vectors are the most)
+  if constexpr (VEC <= 4) {
+    if (s.nv == 8) return pick<In, VEC, 8, 1024, FULL, BACK>(kind, p, ctas, s.threads, stream);   // (fp32: 4097)
+  }
+  if constexpr (VEC == 1) return pick<In, VEC, 16, 1024, FULL, BACK>(kind, p, ctas, s.threads, stream);
   return cudaErrorInvalidValue;
 }
 
@@ -672,14 +738,14 @@ cudaError_t by_length(Kind kind, const NormParams& p, const Shape& s, int& ctas,
 template <typename In, int VEC>
 cudaError_t by_start(Kind kind, const NormParams& p, const Shape& s, int& ctas, cudaStream_t stream) {
   if constexpr (VEC > 1) {
-    if (!s.full) return by_length<In, VEC, false>(kind, p, s, ctas, stream);
+    if (!s.full) return kind == kGated || kind == kAdd ? by_length<In, VEC, false, false>(kind, p, s, ctas, stream) : by_length<In, VEC, false, true>(kind, p, s, ctas, stream);
   }
-  return by_length<In, VEC, true>(kind, p, s, ctas, stream);
+  return kind == kGated || kind == kAdd ? by_length<In, VEC, true, false>(kind, p, s, ctas, stream) : by_length<In, VEC, true, true>(kind, p, s, ctas, stream);
 }
 
 cudaError_t run(Kind kind, NormParams& p, int dtype, uintptr_t addresses, float* dw, float* dw_post, cudaStream_t stream) {
   const bool bf16 = dtype == HA_LA_BF16, fast = !(addresses & 15), back = kind == kGatedBack || kind == kAddBack;
-  const Shape s = shape_of(p.cols, bf16, fast);
+  const Shape s = shape_of(p.cols, bf16, fast, back);
   p.group = s.group;
   int ctas = ctas_of(s, p.rows, back ? kBackThreads : kForwardThreads);
   cudaError_t e = bf16 ? (fast ? by_start<__nv_bfloat16, 8>(kind, p, s, ctas, stream) : by_start<__nv_bfloat16, 1>(kind, p, s, ctas, stream))
