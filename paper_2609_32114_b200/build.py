@@ -25,7 +25,7 @@ UNITS = [("api", "api.cu", []), ("plan", "plan.cu", []), ("tc", "tc.cu", []), ("
          ("tc_walk", "tc_walk.cu", []), ("tc_span", "tc_span.cu", []),
          ("noalloc", "noalloc.cu", []), ("decode", "decode.cu", []), ("fp32_d64", "fp32_d64.cu", []),
          ("norm", "norm.cu", []), ("gla_api", "gla/api.cu", []), ("gla_decode", "gla/decode.cu", []), ("gla_simt", "gla/simt.cu", []),
-         ("gla_tc", "gla/tc.cu", []), ("gla_tc_state", "gla/tc_state.cu", []), ("gla_tc_out", "gla/tc_out.cu", []), ("gla_tc_back", "gla/tc_back.cu", [])] + [
+         ("gla_tc", "gla/tc.cu", []), ("gla_tc_state", "gla/tc_state.cu", []), ("gla_tc_walk", "gla/tc_walk.cu", []), ("gla_tc_back", "gla/tc_back.cu", [])] + [
     (f"simt{u}", "simt.cu", [f"-DHA_LA_SIMT_UNIT={u}"]) for u in range(5)
 ] + [
     (f"fp32_{u}", "fp32.cu", [f"-DHA_LA_FP32_UNIT={u}"]) for u in range(5)

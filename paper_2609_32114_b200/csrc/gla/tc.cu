@@ -28,10 +28,10 @@ size_t tc_bytes(const Problem& p, bool back, TcWork* tw, Work* w, void* base) {
   const size_t units = (size_t)p.max_chunks * p.HV;
   const int nseg = segments(p, back);
   const size_t parts = nseg > 1 ? (size_t)p.N * p.HV * nseg : 0;
-  take(tw ? &tw->image : nullptr, units * kTileBytes * (back ? 2 : 1));
   take(tw ? &tw->part : nullptr, parts * 65536);
   take(tw ? &tw->total : nullptr, parts * 4);
   if (back) {
+    take(tw ? &tw->image : nullptr, units * kTileBytes * 2);
     const int per = heads_per_run(p);
     const size_t parts_of = p.HV / per != p.HK ? (size_t)p.T_total * (p.HV / per) * 128 * 4 : 0;
     take(tw ? &tw->image_back : nullptr, units * kTileBytes * 2);
@@ -58,15 +58,12 @@ cudaError_t make(TcCall* t, const Call& c, PlanView plan, const TcWork& w) {
   return cudaSuccess;
 }
 
-cudaError_t states(const TcCall& t, cudaStream_t stream) {
+cudaError_t sums(const TcCall& t, cudaStream_t stream) {   // the segments' start states
   const Call& c = *t.c;
-  cudaError_t e = cudaSuccess;
-  if (t.nseg > 1) {
-    e = launch_tc_states(t, true, stream);
-    if (e == cudaSuccess) e = launch_chain(t.w.total, t.w.part, c.a.h0, t.nseg, c.p.N, c.p.HV, 16384, false, stream);
-    if (e == cudaSuccess && c.back) e = launch_chain(t.w.total_back, t.w.part_back, c.a.dhT, t.nseg, c.p.N, c.p.HV, 16384, true, stream);
-  }
-  return e == cudaSuccess ? launch_tc_states(t, false, stream) : e;
+  cudaError_t e = launch_tc_states(t, true, stream);
+  if (e == cudaSuccess) e = launch_chain(t.w.total, t.w.part, c.a.h0, t.nseg, c.p.N, c.p.HV, 16384, false, stream);
+  if (e == cudaSuccess && c.back) e = launch_chain(t.w.total_back, t.w.part_back, c.a.dhT, t.nseg, c.p.N, c.p.HV, 16384, true, stream);
+  return e;
 }
 
 }  // namespace
@@ -75,15 +72,16 @@ cudaError_t launch_tc_forward(const Call& c, PlanView plan, const TcWork& w, cud
   if (c.p.T_total == 0) return launch_combine(c, false, stream);   // (no token, no tensor map: hT = h0)
   TcCall t;
   cudaError_t e = make(&t, c, plan, w);
-  if (e == cudaSuccess) e = states(t, stream);
-  return e == cudaSuccess ? launch_tc_out(t, stream) : e;
+  if (e == cudaSuccess && t.nseg > 1) e = sums(t, stream);
+  return e == cudaSuccess ? launch_tc_walk(t, stream) : e;
 }
 
 cudaError_t launch_tc_backward(const Call& c, PlanView plan, const TcWork& w, cudaStream_t stream) {
   if (c.p.T_total == 0) return launch_combine(c, true, stream);
   TcCall t;
   cudaError_t e = make(&t, c, plan, w);
-  if (e == cudaSuccess) e = states(t, stream);
+  if (e == cudaSuccess && t.nseg > 1) e = sums(t, stream);
+  if (e == cudaSuccess) e = launch_tc_states(t, false, stream);
   if (e == cudaSuccess) e = launch_tc_local_back(t, stream);
   return e == cudaSuccess ? launch_head_sums(c, c.p.HV / heads_per_run(c.p), stream) : e;
 }

@@ -185,7 +185,7 @@ size_t tc_bytes(const Problem& p, bool back, TcWork* tw, Work* w, void* base);
 cudaError_t launch_tc_forward(const Call& c, PlanView plan, const TcWork& w, cudaStream_t stream);
 cudaError_t launch_tc_backward(const Call& c, PlanView plan, const TcWork& w, cudaStream_t stream);
 cudaError_t launch_tc_states(const TcCall& t, bool sums, cudaStream_t stream);
-cudaError_t launch_tc_out(const TcCall& t, cudaStream_t stream);
+cudaError_t launch_tc_walk(const TcCall& t, cudaStream_t stream);
 size_t local_back_bytes();
 int heads_per_run(const Problem& p);
 cudaError_t launch_tc_local_back(const TcCall& t, cudaStream_t stream);

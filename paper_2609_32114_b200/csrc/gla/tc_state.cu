@@ -269,7 +269,7 @@ cudaError_t launch_tc_states(const TcCall& t, bool sums, cudaStream_t stream) {
   p.total[0] = t.w.total; p.total[1] = t.w.total_back;
   p.HK = c.p.HK; p.HV = c.p.HV; p.nseg = t.nseg; p.scale = c.p.scale; p.status = c.a.status_word;
   const dim3 grid((unsigned)((size_t)c.p.N * c.p.HV * t.nseg), c.back ? 2 : 1);
-  auto kernel = sums ? gla_tc_state_kernel<0> : c.back ? gla_tc_state_kernel<2> : gla_tc_state_kernel<1>;
+  auto kernel = sums ? gla_tc_state_kernel<0> : gla_tc_state_kernel<2>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
   return e != cudaSuccess ? e : start(kernel, grid, kThreads, kSmem, stream, t.q, t.k, t.v, t.d_o, p);
 }

@@ -11,7 +11,7 @@ from tests import test_launch_order_cpu as order
 
 CSRC = order.CSRC
 FILES = sorted(glob.glob(os.path.join(CSRC, "gla", "*.cu"))) + [os.path.join(CSRC, "norm.cu")]
-TENSOR_CORES = ["tc_back.cu", "tc_out.cu", "tc_state.cu"]
+TENSOR_CORES = ["tc_back.cu", "tc_walk.cu", "tc_state.cu"]
 
 
 def _source(path):
@@ -31,7 +31,7 @@ KERNELS = list(_kernels())
 
 def test_the_kernels_are_found():
     assert {k for _, k, _ in KERNELS} == {
-        "gla_decode_kernel", "gla_state_kernel", "gla_combine_kernel", "gla_out_kernel", "gla_back_kernel", "gla_sum_kernel", "gla_tc_state_kernel", "gla_tc_out_kernel",
+        "gla_decode_kernel", "gla_state_kernel", "gla_combine_kernel", "gla_out_kernel", "gla_back_kernel", "gla_sum_kernel", "gla_tc_state_kernel", "gla_tc_walk_kernel",
         "gla_tc_back_kernel", "gated_norm_kernel", "gated_norm_back_kernel", "add_norm_kernel", "add_norm_back_kernel", "norm_reduce_kernel"}
 
 
@@ -55,7 +55,7 @@ def test_planted_access(early):
 def test_a_wait_that_ran_out_is_reported():
     header = open(os.path.join(CSRC, "fp32_common.cuh")).read()
     copying = [(k, body) for _, k, body in KERNELS if re.search(r"\b(?:bulk_load|tma_load_4d)\(", body)]
-    assert [k for k, _ in copying] == ["gla_tc_back_kernel", "gla_tc_out_kernel", "gla_tc_state_kernel"]
+    assert [k for k, _ in copying] == ["gla_tc_back_kernel", "gla_tc_state_kernel", "gla_tc_walk_kernel"]
     assert order.unreported(copying, header) == []
     for k, body in copying:                                # ... ahead of giving tensor memory and the CTA's shared memory back
         assert body.index("report_timeout(p.status)") < body.index("tmem_dealloc(")
