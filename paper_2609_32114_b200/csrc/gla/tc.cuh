@@ -21,6 +21,23 @@ namespace gla {
 using namespace ptx;
 
 constexpr int kComputeWarps = 16;
+
+// The walk and the gradient kernel run 20 warps: 16 that compute, then producer, MMA issue, gates and one that idles.  96 registers a thread are what
+// the SM has for them; the last four hand some over, since a few bytes of spills cost 3% (with ~227 KiB of shared memory there is hardly any L1
+// left for the stack).  A launch that brought fewer than kRegs would wait for ever, so launch_split refuses it.
+constexpr int kSplitThreads = 32 * (kComputeWarps + 4), kRegs = 96, kComputeRegs = 104, kOtherRegs = 64;
+static_assert(32 * (kComputeWarps * kComputeRegs + 4 * kOtherRegs) <= kSplitThreads * kRegs && kSplitThreads * kRegs <= 65536, "register split");
+__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kComputeRegs)); }
+__device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs)); }
+
+template <typename... Args>
+cudaError_t launch_split(void (*kernel)(Args...), unsigned ctas, size_t smem, cudaStream_t stream, Args... args) {
+  cudaFuncAttributes a;
+  cudaError_t e = cudaFuncGetAttributes(&a, reinterpret_cast<const void*>(kernel));
+  if (e == cudaSuccess && a.numRegs < kRegs) e = cudaErrorInvalidKernelImage;
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  return e != cudaSuccess ? e : start(kernel, dim3(ctas), kSplitThreads, smem, stream, args...);
+}
 constexpr double kLog2e = 1.4426950408889634;
 
 // Log-gates of a step's tokens 4 lane .. 4 lane + 3 (one warp; 0 past the end), and cumulative, times log2 e, in 64 bits.

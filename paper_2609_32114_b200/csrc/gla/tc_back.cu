@@ -27,7 +27,6 @@ namespace gla {
 namespace {
 
 constexpr int kSlots = 7;
-constexpr int kThreads = 32 * (kComputeWarps + 3);
 // As StepGates, G_L = ghi + glo; and which unit these are the gates of: first token, tokens (0: no more units), V-head, V-head of the run; its run's and its q/k head
 struct BackGates { float hi[kStep], lo[kStep], er[kStep], ec[kStep], bb[64], ghi, glo; int part_head, qk_head; int4 unit; };
 constexpr uint32_t OFF_G = kSlots * kTileBytes;
@@ -67,7 +66,7 @@ __device__ __forceinline__ uint32_t fill_of(int tile, int u) {
   return (u + ((u + 3 - since) >> 2) + (tile == kV2 ? 1 : 0)) & 1;
 }
 
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kSplitThreads, 1)
 gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                    const __grid_constant__ CUtensorMap map_do, BackParams p) {
   extern __shared__ __align__(1024) uint8_t sm[];
@@ -111,180 +110,184 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   constexpr int kSums = 2 * 4 * kStep + kComputeWarps;     // [4][128] x + R - C, [4][128] y, [16] parts of <h, dh>
   float* sums = p.sums + (size_t)blockIdx.x * 2 * kSums;
 
-  if (warp == kComputeWarps) {
-    // ------------------------------------------------------------ tiles
-    if (elect_one()) {
-      Unit x{{0, 1}, 0, 0, 0};
-      for (int u = -1; x.c.L > 0 && !*abort_flag; ++u) {
-        const Unit after = unit(u + 1);                    // (its look-ups under the waits, here and below)
+  if (warp >= kComputeWarps) {
+    give_registers();
+    if (warp == kComputeWarps) {
+      // ------------------------------------------------------------ tiles
+      if (elect_one()) {
+        Unit x{{0, 1}, 0, 0, 0};
+        for (int u = -1; x.c.L > 0 && !*abort_flag; ++u) {
+          const Unit after = unit(u + 1);                    // (its look-ups under the waits, here and below)
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          if (u < 0) break;
-          const int at = slot_of(t, u);
-          wait_for(&empty[at], fill_of(t, u) ^ 1, abort_flag);
-          if (*abort_flag) break;
-          uint8_t* dst = sm + at * kTileBytes;
-          mbar_expect_tx(&full[at], kTileBytes);
-          if (t == kQ) tma_load_4d(dst, &map_q, &full[at], 0, x.j / R, x.c.tok0, 0);
-          else if (t == kK) tma_load_4d(dst, &map_k, &full[at], 0, x.j / R, x.c.tok0, 0);
-          else if (t == kDO) tma_load_4d(dst, &map_do, &full[at], 0, x.j, x.c.tok0, 0);
-          else if (t == kV || t == kV2) tma_load_4d(dst, &map_v, &full[at], 0, x.j, x.c.tok0, 0);
-          else bulk_load(dst, (t < kDH ? p.image : p.image_back) + (2 * x.sj + (t == kHL || t == kDL)) * kTileBytes, kTileBytes, &full[at]);
-        }
-        x = after;
-      }
-    }
-    __syncwarp();
-  } else if (warp == kComputeWarps + 1) {
-    // ------------------------------------------------------------ products
-    if (elect_one()) {
-      Unit x{{0, 1}, 0, 0, 0};
-      uint32_t tails = 0;
-      int last_k = 0;
-      for (int u = -1; x.c.L > 0; ++u) {
-        const Unit after = unit(u + 1);
-        if (u < 0) {
+          for (int t = 0; t < kTiles; ++t) {
+            if (u < 0) break;
+            const int at = slot_of(t, u);
+            wait_for(&empty[at], fill_of(t, u) ^ 1, abort_flag);
+            if (*abort_flag) break;
+            uint8_t* dst = sm + at * kTileBytes;
+            mbar_expect_tx(&full[at], kTileBytes);
+            if (t == kQ) tma_load_4d(dst, &map_q, &full[at], 0, x.j / R, x.c.tok0, 0);
+            else if (t == kK) tma_load_4d(dst, &map_k, &full[at], 0, x.j / R, x.c.tok0, 0);
+            else if (t == kDO) tma_load_4d(dst, &map_do, &full[at], 0, x.j, x.c.tok0, 0);
+            else if (t == kV || t == kV2) tma_load_4d(dst, &map_v, &full[at], 0, x.j, x.c.tok0, 0);
+            else bulk_load(dst, (t < kDH ? p.image : p.image_back) + (2 * x.sj + (t == kHL || t == kDL)) * kTileBytes, kTileBytes, &full[at]);
+          }
           x = after;
-          continue;
         }
-        const uint32_t ph = u & 1;
-        auto tile = [&](int t) { return smem_u32(sm + slot_of(t, u) * kTileBytes); };
-        auto wait = [&](uint64_t* b, uint32_t parity) {
-          wait_for(b, parity, abort_flag);
-          tc_fence_after_sync();
-        };
-        auto loaded = [&](int t) { wait(&full[slot_of(t, u)], fill_of(t, u)); };
-        loaded(kQ);
-        loaded(kK);
-        if (x.c.L < kStep) wait(clean, tails++ & 1);
-        if (u > 0) wait(e_v, ph ^ 1);
-        mma_cols(R0, tile(kQ), tile(kK), false);           // S
-        mma_cols(R2, tile(kK), tile(kQ), false);           // S^T
-        if (u > 0) {
-          wait(e_k, ph ^ 1);
-          mbar_arrive(&empty[last_k]);                     // (its products are complete)
+      }
+      __syncwarp();
+    } else if (warp == kComputeWarps + 1) {
+      // ------------------------------------------------------------ products
+      if (elect_one()) {
+        Unit x{{0, 1}, 0, 0, 0};
+        uint32_t tails = 0;
+        int last_k = 0;
+        for (int u = -1; x.c.L > 0; ++u) {
+          const Unit after = unit(u + 1);
+          if (u < 0) {
+            x = after;
+            continue;
+          }
+          const uint32_t ph = u & 1;
+          auto tile = [&](int t) { return smem_u32(sm + slot_of(t, u) * kTileBytes); };
+          auto wait = [&](uint64_t* b, uint32_t parity) {
+            wait_for(b, parity, abort_flag);
+            tc_fence_after_sync();
+          };
+          auto loaded = [&](int t) { wait(&full[slot_of(t, u)], fill_of(t, u)); };
+          loaded(kQ);
+          loaded(kK);
+          if (x.c.L < kStep) wait(clean, tails++ & 1);
+          if (u > 0) wait(e_v, ph ^ 1);
+          mma_cols(R0, tile(kQ), tile(kK), false);           // S
+          mma_cols(R2, tile(kK), tile(kQ), false);           // S^T
+          if (u > 0) {
+            wait(e_k, ph ^ 1);
+            mbar_arrive(&empty[last_k]);                     // (its products are complete)
+          }
+          loaded(kDO);
+          loaded(kV);
+          mma_cols(R1, tile(kDO), tile(kV), false);          // dP
+          mma_cols(R3, tile(kV), tile(kDO), false);          // dP^T
+          umma_commit(b_s);
+          umma_commit(&empty[slot_of(kV, u)]);
+          wait(e_s, ph);
+          mma_tmem_rows<16>(R1, R0, tile(kK), false);        // dS K
+          loaded(kHH);
+          mma_cols(R0, tile(kDO), tile(kHH), false);         // dO h^T
+          loaded(kHL);
+          mma_cols(R0, tile(kDO), tile(kHL), true);
+          umma_commit(b_dq);
+          wait(e_d, ph);
+          umma_commit(&empty[slot_of(kHH, u)]);
+          umma_commit(&empty[slot_of(kHL, u)]);
+          wait(e_q, ph);
+          mma_tmem_rows<16>(R1, R3, tile(kQ), false);        // dS^T Q
+          umma_commit(&empty[slot_of(kQ, u)]);
+          mma_tmem_rows<16>(R0, R2, tile(kDO), false);       // P^T dO
+          umma_commit(&empty[slot_of(kDO, u)]);
+          loaded(kDH);
+          mma_rows(R2, tile(kK), tile(kDH), false);          // K dh
+          umma_commit(b_dv);
+          loaded(kV2);
+          mma_cols(R3, tile(kV2), tile(kDH), false);         // V dh^T
+          loaded(kDL);
+          mma_cols(R3, tile(kV2), tile(kDL), true);
+          umma_commit(b_dk);
+          umma_commit(&empty[slot_of(kV2, u)]);
+          umma_commit(&empty[slot_of(kDH, u)]);
+          umma_commit(&empty[slot_of(kDL, u)]);
+          last_k = slot_of(kK, u);
+          x = after;
         }
-        loaded(kDO);
-        loaded(kV);
-        mma_cols(R1, tile(kDO), tile(kV), false);          // dP
-        mma_cols(R3, tile(kV), tile(kDO), false);          // dP^T
-        umma_commit(b_s);
-        umma_commit(&empty[slot_of(kV, u)]);
-        wait(e_s, ph);
-        mma_tmem_rows<16>(R1, R0, tile(kK), false);        // dS K
-        loaded(kHH);
-        mma_cols(R0, tile(kDO), tile(kHH), false);         // dO h^T
-        loaded(kHL);
-        mma_cols(R0, tile(kDO), tile(kHL), true);
-        umma_commit(b_dq);
-        wait(e_d, ph);
-        umma_commit(&empty[slot_of(kHH, u)]);
-        umma_commit(&empty[slot_of(kHL, u)]);
-        wait(e_q, ph);
-        mma_tmem_rows<16>(R1, R3, tile(kQ), false);        // dS^T Q
-        umma_commit(&empty[slot_of(kQ, u)]);
-        mma_tmem_rows<16>(R0, R2, tile(kDO), false);       // P^T dO
-        umma_commit(&empty[slot_of(kDO, u)]);
-        loaded(kDH);
-        mma_rows(R2, tile(kK), tile(kDH), false);          // K dh
-        umma_commit(b_dv);
-        loaded(kV2);
-        mma_cols(R3, tile(kV2), tile(kDH), false);         // V dh^T
-        loaded(kDL);
-        mma_cols(R3, tile(kV2), tile(kDL), true);
-        umma_commit(b_dk);
-        umma_commit(&empty[slot_of(kV2, u)]);
-        umma_commit(&empty[slot_of(kDH, u)]);
-        umma_commit(&empty[slot_of(kDL, u)]);
-        last_k = slot_of(kK, u);
+      }
+      __syncwarp();
+    } else if (warp == kComputeWarps + 2) {
+      // ------------------------------------------------------------ gates; dg of the unit before
+      Unit x = unit(0), before{{0, 0}, 0, 0, 0};
+      float total = 0.f;
+      float4 raw = fetch_gates(p.g, p.HV, x.j, x.c, lane);
+      for (int u = 0; x.c.L > 0 || before.c.L > 0 || u == 0; ++u) {
+        const Unit after = x.c.L > 0 ? unit(u + 1) : x;
+        float next_total = 0.f;
+        {                                                    // (behind the last unit: that there are no more)
+          double G[4];
+          scan_gates(raw, lane, G);
+          raw = fetch_gates(p.g, p.HV, after.j, after.c, lane);
+          const double Rb = __shfl_sync(0xffffffffu, G[0], lane & ~3), R1b = __shfl_sync(0xffffffffu, G[0], min((lane & ~3) + 4, 31)),
+                       GL = __shfl_sync(0xffffffffu, G[3], 31);
+          float4 hi, lo, er, ec;
+          float bb[2];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            (&hi.x)[e] = (float)G[e];
+            (&lo.x)[e] = (float)(G[e] - (double)(&hi.x)[e]);
+            (&er.x)[e] = ex2((float)(G[e] - Rb));
+            (&ec.x)[e] = ex2(fminf((float)(R1b - G[e]), 0.f));
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int I = (2 * lane + e) >> 3, J = (2 * lane + e) & 7;
+            const double rI = __shfl_sync(0xffffffffu, G[0], 4 * I), rJ = __shfl_sync(0xffffffffu, G[0], min(4 * J + 4, 31));
+            bb[e] = J < I ? ex2((float)(rI - rJ)) : 0.f;
+          }
+          next_total = ex2((float)GL);
+          if (u > 0) wait_for(g_free, (u - 1) & 1, abort_flag);
+          __syncwarp();
+          reinterpret_cast<float4*>(s->hi)[lane] = hi;
+          reinterpret_cast<float4*>(s->lo)[lane] = lo;
+          reinterpret_cast<float4*>(s->er)[lane] = er;
+          reinterpret_cast<float4*>(s->ec)[lane] = ec;
+          reinterpret_cast<float2*>(s->bb)[lane] = make_float2(bb[0], bb[1]);
+          if (lane == 0) {
+            s->ghi = (float)GL;
+            s->glo = (float)(GL - (double)(float)GL);
+            s->unit = make_int4(x.c.tok0, x.c.L, x.j, x.r);
+            s->part_head = x.j / p.per;
+            s->qk_head = x.j / R;
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(gates);
+          __syncwarp();
+        }
+        if (before.c.L > 0) {
+          wait_for(e_k, (u - 1) & 1, abort_flag);           // (the last of the unit's sums are written ahead of it)
+          __syncwarp();
+          const float* f = sums + ((u - 1) & 1) * kSums;
+          double z[4] = {0.0, 0.0, 0.0, 0.0}, y[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const float4 a = __ldcg(reinterpret_cast<const float4*>(f + g * kStep) + lane), b = __ldcg(reinterpret_cast<const float4*>(f + 4 * kStep + g * kStep) + lane);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { z[e] += (&a.x)[e]; y[e] += (&b.x)[e]; }
+          }
+          double dot = lane < kComputeWarps ? (double)__ldcg(f + 8 * kStep + lane) : 0.0;
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+          dot *= total;
+          z[2] += z[3]; z[1] += z[2]; z[0] += z[1];          // z: over this and later tokens, y: over earlier ones
+          const double y3 = y[3], y012 = y[0] + y[1] + y[2];
+          double zs = z[0], ys = y012 + y3;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const double a = __shfl_down_sync(0xffffffffu, zs, o), b = __shfl_up_sync(0xffffffffu, ys, o);
+            if (lane + o < 32) zs += a;
+            if (lane >= o) ys += b;
+          }
+          const double behind = zs - z[0], front = ys - (y012 + y3);
+          const double yy[4] = {front, front + y[0], front + y[0] + y[1], front + y012};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (4 * lane + e < before.c.L)
+              p.dg[(size_t)(before.c.tok0 + 4 * lane + e) * p.HV + before.j] = (float)(z[e] + behind + yy[e] + dot);
+        }
+        total = next_total;
+        before = x;
         x = after;
       }
-    }
-    __syncwarp();
-  } else if (warp == kComputeWarps + 2) {
-    // ------------------------------------------------------------ gates; dg of the unit before
-    Unit x = unit(0), before{{0, 0}, 0, 0, 0};
-    float total = 0.f;
-    float4 raw = fetch_gates(p.g, p.HV, x.j, x.c, lane);
-    for (int u = 0; x.c.L > 0 || before.c.L > 0 || u == 0; ++u) {
-      const Unit after = x.c.L > 0 ? unit(u + 1) : x;
-      float next_total = 0.f;
-      {                                                    // (behind the last unit: that there are no more)
-        double G[4];
-        scan_gates(raw, lane, G);
-        raw = fetch_gates(p.g, p.HV, after.j, after.c, lane);
-        const double Rb = __shfl_sync(0xffffffffu, G[0], lane & ~3), R1b = __shfl_sync(0xffffffffu, G[0], min((lane & ~3) + 4, 31)),
-                     GL = __shfl_sync(0xffffffffu, G[3], 31);
-        float4 hi, lo, er, ec;
-        float bb[2];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          (&hi.x)[e] = (float)G[e];
-          (&lo.x)[e] = (float)(G[e] - (double)(&hi.x)[e]);
-          (&er.x)[e] = ex2((float)(G[e] - Rb));
-          (&ec.x)[e] = ex2(fminf((float)(R1b - G[e]), 0.f));
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int I = (2 * lane + e) >> 3, J = (2 * lane + e) & 7;
-          const double rI = __shfl_sync(0xffffffffu, G[0], 4 * I), rJ = __shfl_sync(0xffffffffu, G[0], min(4 * J + 4, 31));
-          bb[e] = J < I ? ex2((float)(rI - rJ)) : 0.f;
-        }
-        next_total = ex2((float)GL);
-        if (u > 0) wait_for(g_free, (u - 1) & 1, abort_flag);
-        __syncwarp();
-        reinterpret_cast<float4*>(s->hi)[lane] = hi;
-        reinterpret_cast<float4*>(s->lo)[lane] = lo;
-        reinterpret_cast<float4*>(s->er)[lane] = er;
-        reinterpret_cast<float4*>(s->ec)[lane] = ec;
-        reinterpret_cast<float2*>(s->bb)[lane] = make_float2(bb[0], bb[1]);
-        if (lane == 0) {
-          s->ghi = (float)GL;
-          s->glo = (float)(GL - (double)(float)GL);
-          s->unit = make_int4(x.c.tok0, x.c.L, x.j, x.r);
-          s->part_head = x.j / p.per;
-          s->qk_head = x.j / R;
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(gates);
-        __syncwarp();
-      }
-      if (before.c.L > 0) {
-        wait_for(e_k, (u - 1) & 1, abort_flag);           // (the last of the unit's sums are written ahead of it)
-        __syncwarp();
-        const float* f = sums + ((u - 1) & 1) * kSums;
-        double z[4] = {0.0, 0.0, 0.0, 0.0}, y[4] = {0.0, 0.0, 0.0, 0.0};
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const float4 a = __ldcg(reinterpret_cast<const float4*>(f + g * kStep) + lane), b = __ldcg(reinterpret_cast<const float4*>(f + 4 * kStep + g * kStep) + lane);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) { z[e] += (&a.x)[e]; y[e] += (&b.x)[e]; }
-        }
-        double dot = lane < kComputeWarps ? (double)__ldcg(f + 8 * kStep + lane) : 0.0;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-        dot *= total;
-        z[2] += z[3]; z[1] += z[2]; z[0] += z[1];          // z: over this and later tokens, y: over earlier ones
-        const double y3 = y[3], y012 = y[0] + y[1] + y[2];
-        double zs = z[0], ys = y012 + y3;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const double a = __shfl_down_sync(0xffffffffu, zs, o), b = __shfl_up_sync(0xffffffffu, ys, o);
-          if (lane + o < 32) zs += a;
-          if (lane >= o) ys += b;
-        }
-        const double behind = zs - z[0], front = ys - (y012 + y3);
-        const double yy[4] = {front, front + y[0], front + y[0] + y[1], front + y012};
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (4 * lane + e < before.c.L)
-            p.dg[(size_t)(before.c.tok0 + 4 * lane + e) * p.HV + before.j] = (float)(z[e] + behind + yy[e] + dot);
-      }
-      total = next_total;
-      before = x;
-      x = after;
     }
   } else {
+    take_registers();
     // ------------------------------------------------------------ operands, gradients
     const int q = warp & 3, g = warp >> 2, i = 32 * q + lane;     // row (token, key), columns 32 g ..
     const uint32_t lanes = static_cast<uint32_t>(32 * q) << 16;
@@ -529,9 +532,7 @@ cudaError_t launch_tc_local_back(const TcCall& t, cudaStream_t stream) {
   p.HK = c.p.HK; p.HV = c.p.HV; p.scale = c.p.scale; p.status = c.a.status_word;
   p.units = (long long)c.p.max_chunks * (c.p.HV / p.per);
   if (p.units == 0) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(gla_tc_back_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
-  const unsigned grid = (unsigned)(p.units < sm_count() ? p.units : sm_count());
-  return e != cudaSuccess ? e : start(gla_tc_back_kernel, dim3(grid), kThreads, kSmem, stream, t.q, t.k, t.v, t.d_o, p);
+  return launch_split(gla_tc_back_kernel, (unsigned)(p.units < sm_count() ? p.units : sm_count()), kSmem, stream, t.q, t.k, t.v, t.d_o, p);
 }
 
 }  // namespace gla

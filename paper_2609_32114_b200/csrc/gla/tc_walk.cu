@@ -21,7 +21,6 @@ namespace gla {
 namespace {
 
 constexpr int kSlots = 6, kTiles = 3;                      // Q, K, V of two steps
-constexpr int kThreads = 32 * (kComputeWarps + 3);         // compute warps, producer, MMA issue, gates
 struct WalkGates { float hi[kStep], lo[kStep], er[kStep], ec[kStep], el[kStep], bb[64]; float total, pad[3]; };   // (as StepGates)
 constexpr uint32_t OFF_H = kSlots * kTileBytes;            // the state in front of the step as a tile
 constexpr uint32_t OFF_G = OFF_H + kTileBytes;
@@ -43,7 +42,7 @@ struct WalkParams {
   int32_t* status;
 };
 
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kSplitThreads, 1)
 gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, WalkParams p) {
   extern __shared__ __align__(1024) uint8_t sm[];
   WalkGates* s = reinterpret_cast<WalkGates*>(sm + OFF_G);
@@ -81,101 +80,106 @@ gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   const int s0 = min(seg * per_seg, steps), count = min(per_seg, steps - s0);
   auto geom = [&](int c) { return Geom{tok0 + (s0 + c) * kStep, min(kStep, len - (s0 + c) * kStep)}; };
 
-  if (warp == kComputeWarps) {
-    // ------------------------------------------------------------ tiles
-    if (elect_one()) {
-      int slot = 0;
-      uint32_t round = 0;
-      for (int c = 0; c < count && !*abort_flag; ++c) {
-        const int t0 = geom(c).tok0;
+  if (warp >= kComputeWarps) {
+    give_registers();
+    if (warp == kComputeWarps) {
+      // ------------------------------------------------------------ tiles
+      if (elect_one()) {
+        int slot = 0;
+        uint32_t round = 0;
+        for (int c = 0; c < count && !*abort_flag; ++c) {
+          const int t0 = geom(c).tok0;
 #pragma unroll 1
-        for (int t = 0; t < kTiles; ++t) {
-          if (round > 0) wait_for(&empty[slot], (round - 1) & 1, abort_flag);
-          if (*abort_flag) break;
-          mbar_expect_tx(&full[slot], kTileBytes);
-          tma_load_4d(sm + slot * kTileBytes, t == 0 ? &map_q : t == 1 ? &map_k : &map_v, &full[slot], 0, t == 2 ? j : jq, t0, 0);
-          if (++slot == kSlots) { slot = 0; ++round; }
+          for (int t = 0; t < kTiles; ++t) {
+            if (round > 0) wait_for(&empty[slot], (round - 1) & 1, abort_flag);
+            if (*abort_flag) break;
+            mbar_expect_tx(&full[slot], kTileBytes);
+            tma_load_4d(sm + slot * kTileBytes, t == 0 ? &map_q : t == 1 ? &map_k : &map_v, &full[slot], 0, t == 2 ? j : jq, t0, 0);
+            if (++slot == kSlots) { slot = 0; ++round; }
+          }
         }
       }
-    }
-    __syncwarp();
-  } else if (warp == kComputeWarps + 1) {
-    // ------------------------------------------------------------ products
-    if (elect_one()) {
-      const uint32_t h = smem_u32(sm + OFF_H);
-      for (int c = -1; c < count; ++c) {
-        const int at = kTiles * (c & 1), next = kTiles - at;
-        const uint32_t ph = c & 1, fill = (c >> 1) & 1, fill_next = ((c + 1) >> 1) & 1;
-        const uint32_t q = smem_u32(sm + at * kTileBytes), v = q + 2 * kTileBytes;
-        auto wait = [&](uint64_t* b, uint32_t parity) {
-          wait_for(b, parity, abort_flag);
-          tc_fence_after_sync();
-        };
-        if (c >= 0) {
-          wait(e_h, ph);
-          mma_rows(TM_O, q, h, false);                     // Q h
-          umma_commit(b_qh);
-          umma_commit(&empty[at]);
-          umma_commit(&empty[at + 1]);                     // (K: K' is there, S was complete)
-          wait(&full[at + 2], fill);
-          mma_tmem_rows(TM_D, TM_K, v, false);             // K' V
-          mma_tmem_rows(TM_D, TM_K + 64, v, true);
-          umma_commit(b_d);
-          wait(e_p, ph);
-          mma_tmem_rows<16>(TM_O, TM_S, v, true);          // + P V
-          umma_commit(b_o);
-          umma_commit(&empty[at + 2]);
-        }
-        if (c + 1 < count) {
-          wait(&full[next], fill_next);
-          wait(&full[next + 1], fill_next);
-          mma_cols(TM_S, smem_u32(sm + next * kTileBytes), smem_u32(sm + (next + 1) * kTileBytes), false);
-          umma_commit(b_s);
-          wait(e_k, (c + 1) & 1);
+      __syncwarp();
+    } else if (warp == kComputeWarps + 1) {
+      // ------------------------------------------------------------ products
+      if (elect_one()) {
+        const uint32_t h = smem_u32(sm + OFF_H);
+        for (int c = -1; c < count; ++c) {
+          const int at = kTiles * (c & 1), next = kTiles - at;
+          const uint32_t ph = c & 1, fill = (c >> 1) & 1, fill_next = ((c + 1) >> 1) & 1;
+          const uint32_t q = smem_u32(sm + at * kTileBytes), v = q + 2 * kTileBytes;
+          auto wait = [&](uint64_t* b, uint32_t parity) {
+            wait_for(b, parity, abort_flag);
+            tc_fence_after_sync();
+          };
+          if (c >= 0) {
+            wait(e_h, ph);
+            mma_rows(TM_O, q, h, false);                     // Q h
+            umma_commit(b_qh);
+            umma_commit(&empty[at]);
+            umma_commit(&empty[at + 1]);                     // (K: K' is there, S was complete)
+            wait(&full[at + 2], fill);
+            wait(e_k, ph);
+            mma_tmem_rows(TM_D, TM_K, v, false);             // K' V
+            mma_tmem_rows(TM_D, TM_K + 64, v, true);
+            umma_commit(b_d);
+            wait(e_p, ph);
+            mma_tmem_rows<16>(TM_O, TM_S, v, true);          // + P V
+            umma_commit(b_o);
+            umma_commit(&empty[at + 2]);
+          }
+          if (c + 1 < count) {
+            wait(&full[next], fill_next);
+            wait(&full[next + 1], fill_next);
+            mma_cols(TM_S, smem_u32(sm + next * kTileBytes), smem_u32(sm + (next + 1) * kTileBytes), false);
+            umma_commit(b_s);
+          }
         }
       }
-    }
-    __syncwarp();
-  } else if (warp == kComputeWarps + 2) {
-    // ------------------------------------------------------------ gates
-    float4 raw = count > 0 ? fetch_gates(p.g, p.HV, j, geom(0), lane) : make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c = 0; c < count; ++c) {
-      double G[4];
-      scan_gates(raw, lane, G);
-      if (c + 1 < count) raw = fetch_gates(p.g, p.HV, j, geom(c + 1), lane);
-      const double R = __shfl_sync(0xffffffffu, G[0], lane & ~3), R1 = __shfl_sync(0xffffffffu, G[0], min((lane & ~3) + 4, 31)),
-                   GL = __shfl_sync(0xffffffffu, G[3], 31);
-      float4 hi, lo, er, ec, el;
-      float bb[2];
+      __syncwarp();
+    } else if (warp == kComputeWarps + 2) {
+      // ------------------------------------------------------------ gates
+      float4 raw = count > 0 ? fetch_gates(p.g, p.HV, j, geom(0), lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int c = 0; c < count; ++c) {
+        double G[4];
+        scan_gates(raw, lane, G);
+        if (c + 1 < count) raw = fetch_gates(p.g, p.HV, j, geom(c + 1), lane);
+        const double R = __shfl_sync(0xffffffffu, G[0], lane & ~3), R1 = __shfl_sync(0xffffffffu, G[0], min((lane & ~3) + 4, 31)),
+                     GL = __shfl_sync(0xffffffffu, G[3], 31);
+        float4 hi, lo, er, ec, el;
+        float bb[2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        (&hi.x)[e] = (float)G[e];
-        (&lo.x)[e] = (float)(G[e] - (double)(&hi.x)[e]);
-        (&er.x)[e] = ex2((float)(G[e] - R));
-        (&ec.x)[e] = ex2(fminf((float)(R1 - G[e]), 0.f));
-        (&el.x)[e] = ex2((float)(GL - G[e]));
-      }
+        for (int e = 0; e < 4; ++e) {
+          (&hi.x)[e] = (float)G[e];
+          (&lo.x)[e] = (float)(G[e] - (double)(&hi.x)[e]);
+          (&er.x)[e] = ex2((float)(G[e] - R));
+          (&ec.x)[e] = ex2(fminf((float)(R1 - G[e]), 0.f));
+          (&el.x)[e] = ex2((float)(GL - G[e]));
+        }
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int I = (2 * lane + e) >> 3, J = (2 * lane + e) & 7;
-        const double rI = __shfl_sync(0xffffffffu, G[0], 4 * I), rJ = __shfl_sync(0xffffffffu, G[0], min(4 * J + 4, 31));
-        bb[e] = J < I ? ex2((float)(rI - rJ)) : 0.f;
+        for (int e = 0; e < 2; ++e) {
+          const int I = (2 * lane + e) >> 3, J = (2 * lane + e) & 7;
+          const double rI = __shfl_sync(0xffffffffu, G[0], 4 * I), rJ = __shfl_sync(0xffffffffu, G[0], min(4 * J + 4, 31));
+          bb[e] = J < I ? ex2((float)(rI - rJ)) : 0.f;
+        }
+        const float total = ex2((float)GL);
+        wait_for(&full[kTiles * (c & 1) + 1], (c >> 1) & 1, abort_flag);   // (K: who has waited for the gates may read it)
+        if (c > 0) wait_for(g_free, (c - 1) & 1, abort_flag);
+        __syncwarp();
+        reinterpret_cast<float4*>(s->hi)[lane] = hi;
+        reinterpret_cast<float4*>(s->lo)[lane] = lo;
+        reinterpret_cast<float4*>(s->er)[lane] = er;
+        reinterpret_cast<float4*>(s->ec)[lane] = ec;
+        reinterpret_cast<float4*>(s->el)[lane] = el;
+        reinterpret_cast<float2*>(s->bb)[lane] = make_float2(bb[0], bb[1]);
+        if (lane == 0) s->total = total;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(gates);
+        __syncwarp();
       }
-      const float total = ex2((float)GL);
-      if (c > 0) wait_for(g_free, (c - 1) & 1, abort_flag);
-      __syncwarp();
-      reinterpret_cast<float4*>(s->hi)[lane] = hi;
-      reinterpret_cast<float4*>(s->lo)[lane] = lo;
-      reinterpret_cast<float4*>(s->er)[lane] = er;
-      reinterpret_cast<float4*>(s->ec)[lane] = ec;
-      reinterpret_cast<float4*>(s->el)[lane] = el;
-      reinterpret_cast<float2*>(s->bb)[lane] = make_float2(bb[0], bb[1]);
-      if (lane == 0) s->total = total;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(gates);
-      __syncwarp();
     }
   } else {
+    take_registers();
     // ------------------------------------------------------------ decay and mask, state, scaled keys, outputs
     const int q = warp & 3, g = warp >> 2, i = 32 * q + lane;     // row i (token, key) of tensor memory; columns 32 g ..
     const uint32_t lanes = static_cast<uint32_t>(32 * q) << 16, slice = lanes + 32 * g;
@@ -207,7 +211,7 @@ gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // ---- P, 16 columns at a time: blocks 0 .. 2 q + 1 of the quarter's rows, zeros behind
         const float hi = s->hi[i], lo = s->lo[i], total = s->total;
         wait(b_s, ph);
-#pragma unroll 1
+#pragma unroll
         for (int b = g; b < 8; b += 4) {
           const uint32_t at = TM_S + lanes + 16 * b;
           uint32_t w[8] = {};
@@ -226,10 +230,10 @@ gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             } else {
               const int to = i - 16 * b;                   // the row's own column
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const float2 x = *reinterpret_cast<const float2*>(&s->hi[16 * b + 2 * k]), y = *reinterpret_cast<const float2*>(&s->lo[16 * b + 2 * k]);
-                dec[k].x = 2 * k <= to ? ex2((hi - x.x) + (lo - y.x)) : 0.f;
-                dec[k].y = 2 * k + 1 <= to ? ex2((hi - x.y) + (lo - y.y)) : 0.f;
+              for (int k = 0; k < 16; k += 4) {
+                const float4 x = *reinterpret_cast<const float4*>(&s->hi[16 * b + k]), y = *reinterpret_cast<const float4*>(&s->lo[16 * b + k]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) (&dec[(k + e) / 2].x)[e & 1] = k + e <= to ? ex2((hi - (&x.x)[e]) + (lo - (&y.x)[e])) : 0.f;
               }
               tmem_ld_wait();
 #pragma unroll
@@ -287,7 +291,6 @@ gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const uint32_t fill = ((c + 1) >> 1) & 1;
         uint8_t* tile = sm + slot * kTileBytes;
         wait_for(gates, (c + 1) & 1, abort_flag);
-        wait_for(&full[slot], fill, abort_flag);
         __syncwarp();
         if (L < kStep) {                                   // (rows behind the sequence may be NaN, which no weight of zero masks)
           wait_for(&full[slot + 1], fill, abort_flag);
@@ -361,9 +364,7 @@ cudaError_t launch_tc_walk(const TcCall& t, cudaStream_t stream) {
   WalkParams p;
   p.g = c.a.g; p.seqs = t.seqs; p.first = c.a.h0; p.part = t.w.part; p.last = c.a.hT; p.o = c.a.o;
   p.HK = c.p.HK; p.HV = c.p.HV; p.nseg = t.nseg; p.scale = c.p.scale; p.status = c.a.status_word;
-  const cudaError_t e = cudaFuncSetAttribute(gla_tc_walk_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
-  const dim3 grid((unsigned)((size_t)c.p.N * c.p.HV * t.nseg));
-  return e != cudaSuccess ? e : start(gla_tc_walk_kernel, grid, kThreads, kSmem, stream, t.q, t.k, t.v, p);
+  return launch_split(gla_tc_walk_kernel, (unsigned)((size_t)c.p.N * c.p.HV * t.nseg), kSmem, stream, t.q, t.k, t.v, p);
 }
 
 }  // namespace gla
