@@ -22,22 +22,14 @@ using namespace ptx;
 
 constexpr int kComputeWarps = 16;
 
-// The walk and the gradient kernel run 20 warps: 16 that compute, then producer, MMA issue, gates and one that idles.  96 registers a thread are what
-// the SM has for them; the last four hand some over, since a few bytes of spills cost 3% (with ~227 KiB of shared memory there is hardly any L1
-// left for the stack).  A launch that brought fewer than kRegs would wait for ever, so launch_split refuses it.
-constexpr int kSplitThreads = 32 * (kComputeWarps + 4), kRegs = 96, kComputeRegs = 104, kOtherRegs = 64;
-static_assert(32 * (kComputeWarps * kComputeRegs + 4 * kOtherRegs) <= kSplitThreads * kRegs && kSplitThreads * kRegs <= 65536, "register split");
+// The walk and the gradient kernel run 20 warps: 16 that compute, then producer, MMA issue, gates and one for dg, which idles in the walk.  96 registers a
+// thread are what an SM has for them; in the walk the last four hand some over, since a few bytes of spills cost 3% (with ~227 KiB of shared memory there is
+// hardly any L1 left for the stack).  A launch that brought fewer than kRegs would wait for ever for them, so the launcher asks.
+constexpr int kRoleThreads = 32 * (kComputeWarps + 4), kRegs = 96, kComputeRegs = 104, kOtherRegs = 64;
+static_assert(32 * (kComputeWarps * kComputeRegs + 4 * kOtherRegs) <= kRoleThreads * kRegs && kRoleThreads * kRegs <= 65536, "register split");
 __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kComputeRegs)); }
 __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs)); }
 
-template <typename... Args>
-cudaError_t launch_split(void (*kernel)(Args...), unsigned ctas, size_t smem, cudaStream_t stream, Args... args) {
-  cudaFuncAttributes a;
-  cudaError_t e = cudaFuncGetAttributes(&a, reinterpret_cast<const void*>(kernel));
-  if (e == cudaSuccess && a.numRegs < kRegs) e = cudaErrorInvalidKernelImage;
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  return e != cudaSuccess ? e : start(kernel, dim3(ctas), kSplitThreads, smem, stream, args...);
-}
 constexpr double kLog2e = 1.4426950408889634;
 
 // Log-gates of a step's tokens 4 lane .. 4 lane + 3 (one warp; 0 past the end), and cumulative, times log2 e, in 64 bits.
@@ -70,40 +62,33 @@ __device__ __forceinline__ void scan_gates(float4 x, int lane, double (&G)[4]) {
 // What e^{G_i - G_j} is made of.  Off the diagonal blocks of 16 tokens it factors through the gates at the blocks' edges, all exponents
 // <= 0: er[i] = 2^(G_i - R_I), ec[j] = 2^(R_{J+1} - G_j), bb[I][J] = 2^(R_I - R_{J+1}) (zero where J >= I), R_I = G of block I's first token.
 // Near the diagonal it is taken of the difference, G = hi + lo: sums of closed gates leave a float no bits for what comes behind.
-struct StepGates {
-  float hi[kStep], lo[kStep], er[kStep], ec[kStep];
-  float eg[kStep], el[kStep];                              // e^{G_i}, e^{G_L - G_j}
-  float bb[64];
-  float total;                                             // e^{G_L}
-  float pad[3];
-};
+struct StepGates { float hi[kStep], lo[kStep], er[kStep], ec[kStep], bb[64]; };
+struct LaneGates { float4 hi, lo, er, ec; float2 bb; };    // a lane's share of them
 
-__device__ __forceinline__ void fill_gates(StepGates* s, const double (&G)[4], int lane) {
-  const double R = __shfl_sync(0xffffffffu, G[0], lane & ~3), R1 = __shfl_sync(0xffffffffu, G[0], min((lane & ~3) + 4, 31)),
-               GL = __shfl_sync(0xffffffffu, G[3], 31);
-  float4 hi, lo, er, ec, eg, el;
+__device__ __forceinline__ LaneGates lane_gates(const double (&G)[4], int lane) {
+  const double R = __shfl_sync(0xffffffffu, G[0], lane & ~3), R1 = __shfl_sync(0xffffffffu, G[0], min((lane & ~3) + 4, 31));
+  LaneGates x;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    (&hi.x)[e] = (float)G[e];
-    (&lo.x)[e] = (float)(G[e] - (double)(&hi.x)[e]);
-    (&er.x)[e] = ex2((float)(G[e] - R));
-    (&ec.x)[e] = ex2(fminf((float)(R1 - G[e]), 0.f));      // (the last block's, which nothing uses, would be of the wrong sign)
-    (&eg.x)[e] = ex2((float)G[e]);
-    (&el.x)[e] = ex2((float)(GL - G[e]));
+    (&x.hi.x)[e] = (float)G[e];
+    (&x.lo.x)[e] = (float)(G[e] - (double)(&x.hi.x)[e]);
+    (&x.er.x)[e] = ex2((float)(G[e] - R));
+    (&x.ec.x)[e] = ex2(fminf((float)(R1 - G[e]), 0.f));    // (the last block's, which nothing uses, would be of the wrong sign)
   }
-  reinterpret_cast<float4*>(s->hi)[lane] = hi;
-  reinterpret_cast<float4*>(s->lo)[lane] = lo;
-  reinterpret_cast<float4*>(s->er)[lane] = er;
-  reinterpret_cast<float4*>(s->ec)[lane] = ec;
-  reinterpret_cast<float4*>(s->eg)[lane] = eg;
-  reinterpret_cast<float4*>(s->el)[lane] = el;
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const int I = (2 * lane + e) >> 3, J = (2 * lane + e) & 7;
     const double rI = __shfl_sync(0xffffffffu, G[0], 4 * I), rJ = __shfl_sync(0xffffffffu, G[0], min(4 * J + 4, 31));
-    s->bb[2 * lane + e] = J < I ? ex2((float)(rI - rJ)) : 0.f;
+    (&x.bb.x)[e] = J < I ? ex2((float)(rI - rJ)) : 0.f;
   }
-  if (lane == 0) s->total = ex2((float)GL);
+  return x;
+}
+__device__ __forceinline__ void put_gates(StepGates* s, const LaneGates& x, int lane) {
+  reinterpret_cast<float4*>(s->hi)[lane] = x.hi;
+  reinterpret_cast<float4*>(s->lo)[lane] = x.lo;
+  reinterpret_cast<float4*>(s->er)[lane] = x.er;
+  reinterpret_cast<float4*>(s->ec)[lane] = x.ec;
+  reinterpret_cast<float2*>(s->bb)[lane] = x.bb;
 }
 
 // Rows L .. 127 of a tile to zero, by `n` threads: what lies behind a sequence may be NaN, and zero weights would not mask that.

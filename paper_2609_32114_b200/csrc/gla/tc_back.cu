@@ -16,7 +16,7 @@
 // An operand lies over the scores that it is made of: a warp writes 16 columns of it, 8 words, over the first half of the 16 accumulator columns
 // that it alone has read, and a product's steps of 16 k go from one such place to the next.  So all four scores become operands in one phase, in which
 // the blocks of 32 x 16 on either side of the diagonal (dS below it, the transposed ones above) share out evenly: ten to the four warps of a quarter.
-// One more warp scans the next unit's gates and adds up dg of the last one; the sums over a row's columns, which four warps share, pass through a
+// One more warp scans the next unit's gates and another adds up dg; the sums over a row's columns, which four warps share, pass through a
 // few KiB of workspace that stay in L2.
 // What bounds it: 352 KiB of tiles, images and gradients a unit, and a unit's dependent phases.
 #include "tc.cuh"
@@ -27,8 +27,8 @@ namespace gla {
 namespace {
 
 constexpr int kSlots = 7;
-// As StepGates, G_L = ghi + glo; and which unit these are the gates of: first token, tokens (0: no more units), V-head, V-head of the run; its run's and its q/k head
-struct BackGates { float hi[kStep], lo[kStep], er[kStep], ec[kStep], bb[64], ghi, glo; int part_head, qk_head; int4 unit; };
+// And G_L = ghi + glo; and which unit these are the gates of: first token, tokens (0: no more units), V-head, V-head of the run; its run's and its q/k head
+struct BackGates : StepGates { float ghi, glo; int part_head, qk_head; int4 unit; };
 constexpr uint32_t OFF_G = kSlots * kTileBytes;
 constexpr uint32_t OFF_BAR = OFF_G + sizeof(BackGates);
 constexpr int kBars = 2 * kSlots + 12;
@@ -66,7 +66,7 @@ __device__ __forceinline__ uint32_t fill_of(int tile, int u) {
   return (u + ((u + 3 - since) >> 2) + (tile == kV2 ? 1 : 0)) & 1;
 }
 
-__global__ void __launch_bounds__(kSplitThreads, 1)
+__global__ void __launch_bounds__(kRoleThreads, 1)
 gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                    const __grid_constant__ CUtensorMap map_do, BackParams p) {
   extern __shared__ __align__(1024) uint8_t sm[];
@@ -81,7 +81,7 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int i = 0; i < kBars; ++i) mbar_init(&bar[i], &bar[i] >= all ? kComputeWarps : 1);
+    for (int i = 0; i < kBars; ++i) mbar_init(&bar[i], &bar[i] == g_free ? kComputeWarps + 1 : &bar[i] >= all ? kComputeWarps : 1);
     *abort_flag = 0;
     mbar_fence_init();
   }
@@ -111,7 +111,6 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   float* sums = p.sums + (size_t)blockIdx.x * 2 * kSums;
 
   if (warp >= kComputeWarps) {
-    give_registers();
     if (warp == kComputeWarps) {
       // ------------------------------------------------------------ tiles
       if (elect_one()) {
@@ -203,91 +202,75 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       }
       __syncwarp();
     } else if (warp == kComputeWarps + 2) {
-      // ------------------------------------------------------------ gates; dg of the unit before
-      Unit x = unit(0), before{{0, 0}, 0, 0, 0};
-      float total = 0.f;
+      // ------------------------------------------------------------ gates
+      Unit x = unit(0);
       float4 raw = fetch_gates(p.g, p.HV, x.j, x.c, lane);
-      for (int u = 0; x.c.L > 0 || before.c.L > 0 || u == 0; ++u) {
+#pragma unroll 1
+      for (int u = 0;; ++u) {                              // (behind the last unit: that there are no more)
         const Unit after = x.c.L > 0 ? unit(u + 1) : x;
-        float next_total = 0.f;
-        {                                                    // (behind the last unit: that there are no more)
-          double G[4];
-          scan_gates(raw, lane, G);
-          raw = fetch_gates(p.g, p.HV, after.j, after.c, lane);
-          const double Rb = __shfl_sync(0xffffffffu, G[0], lane & ~3), R1b = __shfl_sync(0xffffffffu, G[0], min((lane & ~3) + 4, 31)),
-                       GL = __shfl_sync(0xffffffffu, G[3], 31);
-          float4 hi, lo, er, ec;
-          float bb[2];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            (&hi.x)[e] = (float)G[e];
-            (&lo.x)[e] = (float)(G[e] - (double)(&hi.x)[e]);
-            (&er.x)[e] = ex2((float)(G[e] - Rb));
-            (&ec.x)[e] = ex2(fminf((float)(R1b - G[e]), 0.f));
-          }
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int I = (2 * lane + e) >> 3, J = (2 * lane + e) & 7;
-            const double rI = __shfl_sync(0xffffffffu, G[0], 4 * I), rJ = __shfl_sync(0xffffffffu, G[0], min(4 * J + 4, 31));
-            bb[e] = J < I ? ex2((float)(rI - rJ)) : 0.f;
-          }
-          next_total = ex2((float)GL);
-          if (u > 0) wait_for(g_free, (u - 1) & 1, abort_flag);
-          __syncwarp();
-          reinterpret_cast<float4*>(s->hi)[lane] = hi;
-          reinterpret_cast<float4*>(s->lo)[lane] = lo;
-          reinterpret_cast<float4*>(s->er)[lane] = er;
-          reinterpret_cast<float4*>(s->ec)[lane] = ec;
-          reinterpret_cast<float2*>(s->bb)[lane] = make_float2(bb[0], bb[1]);
-          if (lane == 0) {
-            s->ghi = (float)GL;
-            s->glo = (float)(GL - (double)(float)GL);
-            s->unit = make_int4(x.c.tok0, x.c.L, x.j, x.r);
-            s->part_head = x.j / p.per;
-            s->qk_head = x.j / R;
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(gates);
-          __syncwarp();
+        double G[4];
+        scan_gates(raw, lane, G);
+        raw = fetch_gates(p.g, p.HV, after.j, after.c, lane);
+        const LaneGates mine = lane_gates(G, lane);
+        const double GL = __shfl_sync(0xffffffffu, G[3], 31);
+        if (u > 0) wait_for(g_free, (u - 1) & 1, abort_flag);
+        __syncwarp();
+        put_gates(s, mine, lane);
+        if (lane == 0) {
+          s->ghi = (float)GL;
+          s->glo = (float)(GL - (double)(float)GL);
+          s->unit = make_int4(x.c.tok0, x.c.L, x.j, x.r);
+          s->part_head = x.j / p.per;
+          s->qk_head = x.j / R;
         }
-        if (before.c.L > 0) {
-          wait_for(e_k, (u - 1) & 1, abort_flag);           // (the last of the unit's sums are written ahead of it)
-          __syncwarp();
-          const float* f = sums + ((u - 1) & 1) * kSums;
-          double z[4] = {0.0, 0.0, 0.0, 0.0}, y[4] = {0.0, 0.0, 0.0, 0.0};
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const float4 a = __ldcg(reinterpret_cast<const float4*>(f + g * kStep) + lane), b = __ldcg(reinterpret_cast<const float4*>(f + 4 * kStep + g * kStep) + lane);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { z[e] += (&a.x)[e]; y[e] += (&b.x)[e]; }
-          }
-          double dot = lane < kComputeWarps ? (double)__ldcg(f + 8 * kStep + lane) : 0.0;
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-          dot *= total;
-          z[2] += z[3]; z[1] += z[2]; z[0] += z[1];          // z: over this and later tokens, y: over earlier ones
-          const double y3 = y[3], y012 = y[0] + y[1] + y[2];
-          double zs = z[0], ys = y012 + y3;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const double a = __shfl_down_sync(0xffffffffu, zs, o), b = __shfl_up_sync(0xffffffffu, ys, o);
-            if (lane + o < 32) zs += a;
-            if (lane >= o) ys += b;
-          }
-          const double behind = zs - z[0], front = ys - (y012 + y3);
-          const double yy[4] = {front, front + y[0], front + y[0] + y[1], front + y012};
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (4 * lane + e < before.c.L)
-              p.dg[(size_t)(before.c.tok0 + 4 * lane + e) * p.HV + before.j] = (float)(z[e] + behind + yy[e] + dot);
-        }
-        total = next_total;
-        before = x;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(gates);
+        __syncwarp();
+        if (x.c.L <= 0) break;
         x = after;
+      }
+    } else {
+      // ------------------------------------------------------------ dg
+#pragma unroll 1
+      for (int u = 0;; ++u) {
+        wait_for(gates, u & 1, abort_flag);
+        __syncwarp();
+        const int4 at = s->unit;
+        const float total = ex2(s->ghi + s->glo);
+        const bool gave_up = __any_sync(0xffffffffu, *abort_flag);
+        if (lane == 0) mbar_arrive(g_free);                // (and the sums of the unit before have been read)
+        if (at.y <= 0 || gave_up) break;
+        wait_for(e_k, u & 1, abort_flag);                  // (the last of the unit's sums are written ahead of it)
+        __syncwarp();
+        const float* f = sums + (u & 1) * kSums;
+        double z[4] = {0.0, 0.0, 0.0, 0.0}, y[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 a = __ldcg(reinterpret_cast<const float4*>(f + g * kStep) + lane), b = __ldcg(reinterpret_cast<const float4*>(f + 4 * kStep + g * kStep) + lane);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { z[e] += (&a.x)[e]; y[e] += (&b.x)[e]; }
+        }
+        double dot = lane < kComputeWarps ? (double)__ldcg(f + 8 * kStep + lane) : 0.0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+        dot *= total;
+        z[2] += z[3]; z[1] += z[2]; z[0] += z[1];          // z: over this and later tokens, y: over earlier ones
+        const double y3 = y[3], y012 = y[0] + y[1] + y[2];
+        double zs = z[0], ys = y012 + y3;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const double a = __shfl_down_sync(0xffffffffu, zs, o), b = __shfl_up_sync(0xffffffffu, ys, o);
+          if (lane + o < 32) zs += a;
+          if (lane >= o) ys += b;
+        }
+        const double behind = zs - z[0], front = ys - (y012 + y3);
+        const double yy[4] = {front, front + y[0], front + y[0] + y[1], front + y012};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (4 * lane + e < at.y) p.dg[(size_t)(at.x + 4 * lane + e) * p.HV + at.z] = (float)(z[e] + behind + yy[e] + dot);
       }
     }
   } else {
-    take_registers();
     // ------------------------------------------------------------ operands, gradients
     const int q = warp & 3, g = warp >> 2, i = 32 * q + lane;     // row (token, key), columns 32 g ..
     const uint32_t lanes = static_cast<uint32_t>(32 * q) << 16;
@@ -319,8 +302,9 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       {
         const uint32_t ph = u & 1;
         wait_for(gates, ph, abort_flag);
+        __syncwarp();
         const int4 at_unit = s->unit;
-        x = {{at_unit.x, *abort_flag ? 0 : at_unit.y}, at_unit.z, at_unit.w, by_run ? s->part_head : s->qk_head};
+        x = {{at_unit.x, __any_sync(0xffffffffu, *abort_flag) ? 0 : at_unit.y}, at_unit.z, at_unit.w, by_run ? s->part_head : s->qk_head};
         if (x.c.L <= 0) break;
         if (x.c.L < kStep) {                               // (rows behind the sequence may be NaN)
 #pragma unroll
@@ -532,7 +516,9 @@ cudaError_t launch_tc_local_back(const TcCall& t, cudaStream_t stream) {
   p.HK = c.p.HK; p.HV = c.p.HV; p.scale = c.p.scale; p.status = c.a.status_word;
   p.units = (long long)c.p.max_chunks * (c.p.HV / p.per);
   if (p.units == 0) return cudaSuccess;
-  return launch_split(gla_tc_back_kernel, (unsigned)(p.units < sm_count() ? p.units : sm_count()), kSmem, stream, t.q, t.k, t.v, t.d_o, p);
+  const cudaError_t e = cudaFuncSetAttribute(gla_tc_back_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+  const unsigned grid = (unsigned)(p.units < sm_count() ? p.units : sm_count());
+  return e != cudaSuccess ? e : start(gla_tc_back_kernel, dim3(grid), kRoleThreads, kSmem, stream, t.q, t.k, t.v, t.d_o, p);
 }
 
 }  // namespace gla

@@ -21,7 +21,7 @@ namespace gla {
 namespace {
 
 constexpr int kSlots = 6, kTiles = 3;                      // Q, K, V of two steps
-struct WalkGates { float hi[kStep], lo[kStep], er[kStep], ec[kStep], el[kStep], bb[64]; float total, pad[3]; };   // (as StepGates)
+struct WalkGates : StepGates { float el[kStep], total, pad[3]; };   // and e^{G_L - G_j}, e^{G_L}
 constexpr uint32_t OFF_H = kSlots * kTileBytes;            // the state in front of the step as a tile
 constexpr uint32_t OFF_G = OFF_H + kTileBytes;
 constexpr uint32_t OFF_BAR = OFF_G + sizeof(WalkGates);
@@ -42,7 +42,7 @@ struct WalkParams {
   int32_t* status;
 };
 
-__global__ void __launch_bounds__(kSplitThreads, 1)
+__global__ void __launch_bounds__(kRoleThreads, 1)
 gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, WalkParams p) {
   extern __shared__ __align__(1024) uint8_t sm[];
   WalkGates* s = reinterpret_cast<WalkGates*>(sm + OFF_G);
@@ -144,35 +144,16 @@ gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         double G[4];
         scan_gates(raw, lane, G);
         if (c + 1 < count) raw = fetch_gates(p.g, p.HV, j, geom(c + 1), lane);
-        const double R = __shfl_sync(0xffffffffu, G[0], lane & ~3), R1 = __shfl_sync(0xffffffffu, G[0], min((lane & ~3) + 4, 31)),
-                     GL = __shfl_sync(0xffffffffu, G[3], 31);
-        float4 hi, lo, er, ec, el;
-        float bb[2];
+        const LaneGates x = lane_gates(G, lane);
+        const double GL = __shfl_sync(0xffffffffu, G[3], 31);
+        float4 el;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          (&hi.x)[e] = (float)G[e];
-          (&lo.x)[e] = (float)(G[e] - (double)(&hi.x)[e]);
-          (&er.x)[e] = ex2((float)(G[e] - R));
-          (&ec.x)[e] = ex2(fminf((float)(R1 - G[e]), 0.f));
-          (&el.x)[e] = ex2((float)(GL - G[e]));
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int I = (2 * lane + e) >> 3, J = (2 * lane + e) & 7;
-          const double rI = __shfl_sync(0xffffffffu, G[0], 4 * I), rJ = __shfl_sync(0xffffffffu, G[0], min(4 * J + 4, 31));
-          bb[e] = J < I ? ex2((float)(rI - rJ)) : 0.f;
-        }
-        const float total = ex2((float)GL);
-        wait_for(&full[kTiles * (c & 1) + 1], (c >> 1) & 1, abort_flag);   // (K: who has waited for the gates may read it)
+        for (int e = 0; e < 4; ++e) (&el.x)[e] = ex2((float)(GL - G[e]));
         if (c > 0) wait_for(g_free, (c - 1) & 1, abort_flag);
         __syncwarp();
-        reinterpret_cast<float4*>(s->hi)[lane] = hi;
-        reinterpret_cast<float4*>(s->lo)[lane] = lo;
-        reinterpret_cast<float4*>(s->er)[lane] = er;
-        reinterpret_cast<float4*>(s->ec)[lane] = ec;
+        put_gates(s, x, lane);
         reinterpret_cast<float4*>(s->el)[lane] = el;
-        reinterpret_cast<float2*>(s->bb)[lane] = make_float2(bb[0], bb[1]);
-        if (lane == 0) s->total = total;
+        if (lane == 0) s->total = ex2((float)GL);
         __syncwarp();
         if (lane == 0) mbar_arrive(gates);
         __syncwarp();
@@ -291,6 +272,7 @@ gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const uint32_t fill = ((c + 1) >> 1) & 1;
         uint8_t* tile = sm + slot * kTileBytes;
         wait_for(gates, (c + 1) & 1, abort_flag);
+        wait_for(&full[slot], fill, abort_flag);
         __syncwarp();
         if (L < kStep) {                                   // (rows behind the sequence may be NaN, which no weight of zero masks)
           wait_for(&full[slot + 1], fill, abort_flag);
@@ -364,7 +346,12 @@ cudaError_t launch_tc_walk(const TcCall& t, cudaStream_t stream) {
   WalkParams p;
   p.g = c.a.g; p.seqs = t.seqs; p.first = c.a.h0; p.part = t.w.part; p.last = c.a.hT; p.o = c.a.o;
   p.HK = c.p.HK; p.HV = c.p.HV; p.nseg = t.nseg; p.scale = c.p.scale; p.status = c.a.status_word;
-  return launch_split(gla_tc_walk_kernel, (unsigned)((size_t)c.p.N * c.p.HV * t.nseg), kSmem, stream, t.q, t.k, t.v, p);
+  cudaFuncAttributes has;
+  cudaError_t e = cudaFuncGetAttributes(&has, gla_tc_walk_kernel);
+  if (e == cudaSuccess && has.numRegs < kRegs) e = cudaErrorInvalidKernelImage;
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(gla_tc_walk_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+  const unsigned ctas = (unsigned)((size_t)c.p.N * c.p.HV * t.nseg);
+  return e != cudaSuccess ? e : start(gla_tc_walk_kernel, dim3(ctas), kRoleThreads, kSmem, stream, t.q, t.k, t.v, p);
 }
 
 }  // namespace gla
