@@ -4,15 +4,18 @@
 namespace ha_la {
 namespace gla {
 
-// Segments that a sequence is cut into for the state kernel, which walks them at the same time: twice over, once to sum them and once from their
-// true starts, with a chain between.  `units`: CTAs without.  us: 0.9 a step, 7 for the two further launches.
+// Segments that a sequence is cut into where there are few (sequence, V-head) pairs: their sums are taken at the same time, chained, and then
+// all segments are walked at the same time.  `units`: CTAs without.  us as measured: a step of the sums 0.9, of the walk 2.8, of the states for the
+// backward pass 2.0; the two further launches 16 and 14.  16 heads, whole and in segments: 512 tokens 19 and 24 us, 1024 30 and 26, 4096 98 and 40;
+// backward 1024 tokens 43 and 45 us, 1536 63 and 59, 4096 145 and 109; four rows of 2048 (two segments at most) 55 and 63.
 int segments(const Problem& p, bool back) {
   const long long units = (long long)p.N * p.HV * (back ? 2 : 1);
   const int steps = p.max_seq_chunks, most = units > 0 ? (int)(sm_count() / units) : 0;
-  double best = 0.9 * steps;
+  const double sum = 0.9, walk = back ? 2.0 : 2.8, launches = back ? 14 : 16;
+  double best = walk * steps;
   int s = 1;
   for (int i = 2; i <= most && i <= steps; ++i) {
-    const double us = 2 * 0.9 * ((steps + i - 1) / i) + 7;
+    const double us = (sum + walk) * ((steps + i - 1) / i) + launches;
     if (us < best) { best = us; s = i; }
   }
   return s;
