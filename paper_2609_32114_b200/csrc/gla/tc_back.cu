@@ -18,7 +18,8 @@
 // the blocks of 32 x 16 on either side of the diagonal (dS below it, the transposed ones above) share out evenly: ten to the four warps of a quarter.
 // One more warp scans the next unit's gates and another adds up dg; the sums over a row's columns, which four warps share, pass through a
 // few KiB of workspace that stay in L2.
-// What bounds it: 352 KiB of tiles, images and gradients a unit, and a unit's dependent phases.
+// What bounds it: 352 KiB of tiles, images and gradients a unit, and a unit's dependent phases.  2048 units (four rows of 4096
+// tokens, 16 heads): 150 us, 10.7 us a unit of an SM; 1104 pairs of units that share a q/k head 181 us.
 #include "tc.cuh"
 
 namespace ha_la {
@@ -494,7 +495,6 @@ gla_tc_back_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 }  // namespace
 
 // V-heads of a q/k head that one CTA takes one behind the other, so that dq and dk add up on the way: as many as leave two runs to an SM.
-// (Four heads per q/k head apart and summed by a kernel of their own instead: see the figures in tc.cu.)
 int heads_per_run(const Problem& p) {
   const int R = p.HV / p.HK;
   for (int per = R; per > 1; --per)

@@ -1,5 +1,5 @@
-// States of gated linear attention on the tensor cores: the state in front of every step, and in the backward pass the gradient of the
-// state behind every step, as bf16 tiles that the output and gradient kernels take as operands.
+// States of gated linear attention on the tensor cores.  For the gradients: the state in front of every step and the gradient of the
+// state behind it, as bf16 tiles that their kernel takes as operands.  For sequences in segments, forward and backward: each segment's sum from zero.
 //
 //   forward   h  <- e^{G_L} h  + sum_j (e^{G_L - G_j} k_j) v_j^T                       in the order of the steps
 //   reverse   dh <- e^{G_L} dh + scale e^{G_0} sum_i (e^{G_i - G_0} q_i) do_i^T        against it
@@ -9,9 +9,9 @@
 // weight is one: with scale e^{G_0} in the weights dh0 had 1.5 times the error); B the values' tile as it is.  Nothing of the product waits for
 // the state, so the next step's keys are scaled under this one's product, and the chain through the steps is one multiply-add.
 //
-// What bounds it: the tiles and images through HBM when many CTAs run (96 KiB a step forward, 128 backward), else a CTA's steps, bound by the
-// scaling warps' instructions.  Few (sequence, V-head) pairs are cut into segments: a first launch sums each from zero,
-// gla_combine_kernel (simt.cu) chains the sums, and this launch walks all segments from their true starts.
+// What bounds it: the tiles and images through HBM when many CTAs run (128 KiB a step; four rows of 4096 tokens, 16 heads: 108 us, 5.0 TB/s), else
+// what an SM stores (64 KiB of images a step, some 20 bytes a cycle: 2 us), and for sums the scaling warps' instructions (0.9 us).
+// Few (sequence, V-head) pairs are cut into segments: gla_combine_kernel (simt.cu) chains the sums.
 #include "tc.cuh"
 
 namespace ha_la {
@@ -36,7 +36,7 @@ struct StateParams {
   const float* g;
   Seqs seqs;
   const float* first[2];                                   // [direction] start states, [sequence][V-head], or NULL
-  float* last[2];
+  float* last;                                             // dh0, or NULL
   uint8_t* image[2];
   float *part[2], *total[2];
   int HK, HV, nseg;
@@ -44,8 +44,8 @@ struct StateParams {
   int32_t* status;
 };
 
-// PIECES: bf16 tiles that an image has; 0: the segments' sums from zero are all that is wanted
-template <int PIECES>
+// IMAGES: the states as tiles, of two bf16 pieces each; without, the segments' sums from zero
+template <bool IMAGES>
 __global__ void __launch_bounds__(kThreads, 1)
 gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                     const __grid_constant__ CUtensorMap map_do, StateParams p) {
@@ -85,7 +85,7 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   }
   const int steps = (len + kStep - 1) / kStep, per_seg = (steps + p.nseg - 1) / p.nseg;
   const int s0 = min(seg * per_seg, steps);
-  const bool unused = PIECES == 0 && seg == (rev ? 0 : p.nseg - 1);   // (nothing starts from what the last segment adds)
+  const bool unused = !IMAGES && seg == (rev ? 0 : p.nseg - 1);   // (nothing starts from what the last segment adds)
   const int count = unused ? 0 : min(per_seg, steps - s0);
   auto index = [&](int c) { return s0 + (rev ? count - 1 - c : c); };   // step of the sequence
   auto geom = [&](int c) { return Geom{tok0 + index(c) * kStep, min(kStep, len - index(c) * kStep)}; };
@@ -151,7 +151,7 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     const size_t unit = (size_t)n * p.HV + j, part = ((size_t)n * p.nseg + seg) * p.HV + j;
     const size_t at = (size_t)key * kStep + 32 * g;
     {
-      const float* src = PIECES == 0 ? nullptr : p.nseg > 1 ? p.part[rev] + part * 16384 : p.first[rev] ? p.first[rev] + unit * 16384 : nullptr;
+      const float* src = !IMAGES ? nullptr : p.nseg > 1 ? p.part[rev] + part * 16384 : p.first[rev] ? p.first[rev] + unit * 16384 : nullptr;
 #pragma unroll
       for (int k = 0; k < 32; k += 4) {
         const float4 x = src ? *reinterpret_cast<const float4*>(src + at + k) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -197,16 +197,15 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     for (int c = 0; c < count; ++c) {
       const int b = c & 1;
       if (c + 1 < count) scale_keys(c + 1);
-      if constexpr (PIECES > 0) {
-        uint8_t* image = p.image[rev] + ((size_t)(slot0 + index(c)) * p.HV + j) * (PIECES * kTileBytes) + (g >> 1) * 16384;
+      if constexpr (IMAGES) {
+        uint8_t* image = p.image[rev] + ((size_t)(slot0 + index(c)) * p.HV + j) * (2 * kTileBytes) + (g >> 1) * 16384;
         uint4 hi[4], lo[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             const float2 x = make_float2(h[8 * k + 2 * w], h[8 * k + 2 * w + 1]);
-            if (PIECES == 2) split_bf16(x, (&hi[k].x)[w], (&lo[k].x)[w]);
-            else (&hi[k].x)[w] = pack_bf16(x);
+            split_bf16(x, (&hi[k].x)[w], (&lo[k].x)[w]);
           }
         // by way of shared memory, so that a store covers 64 bytes of eight rows: a row to a thread it takes the memory pipe four times as long
         uint8_t* mine = sm + OFF_STAGE + warp * kWarpStage;
@@ -222,7 +221,7 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
           }
         };
         put(hi, image);
-        if (PIECES == 2) put(lo, image + kTileBytes);
+        put(lo, image + kTileBytes);
       }
       const float2 f = *reinterpret_cast<const float2*>(sm + OFF_W + b * kWeightB + kStep * 4);
       wait_for(&product[b], (c >> 1) & 1, abort_flag);
@@ -242,12 +241,12 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       __syncwarp();
       if (lane == 0) mbar_arrive(&used[b]);
     }
-    float* dst = PIECES == 0 ? p.part[rev] + part * 16384 : seg == (rev ? 0 : p.nseg - 1) && p.last[rev] ? p.last[rev] + unit * 16384 : nullptr;
+    float* dst = !IMAGES ? p.part[rev] + part * 16384 : rev && seg == 0 && p.last ? p.last + unit * 16384 : nullptr;
     if (dst) {
 #pragma unroll
       for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(dst + at + k) = make_float4(h[k], h[k + 1], h[k + 2], h[k + 3]);
     }
-    if (PIECES == 0 && tid == 0) p.total[rev][part] = total;
+    if (!IMAGES && tid == 0) p.total[rev][part] = total;
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -263,13 +262,13 @@ cudaError_t launch_tc_states(const TcCall& t, bool sums, cudaStream_t stream) {
   StateParams p = {};
   p.g = c.a.g; p.seqs = t.seqs;
   p.first[0] = c.a.h0; p.first[1] = c.a.dhT;
-  p.last[0] = c.back ? nullptr : c.a.hT; p.last[1] = c.a.dh0;
+  p.last = c.a.dh0;
   p.image[0] = t.w.image; p.image[1] = t.w.image_back;
   p.part[0] = t.w.part; p.part[1] = t.w.part_back;
   p.total[0] = t.w.total; p.total[1] = t.w.total_back;
   p.HK = c.p.HK; p.HV = c.p.HV; p.nseg = t.nseg; p.scale = c.p.scale; p.status = c.a.status_word;
   const dim3 grid((unsigned)((size_t)c.p.N * c.p.HV * t.nseg), c.back ? 2 : 1);
-  auto kernel = sums ? gla_tc_state_kernel<0> : gla_tc_state_kernel<2>;
+  auto kernel = sums ? gla_tc_state_kernel<false> : gla_tc_state_kernel<true>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
   return e != cudaSuccess ? e : start(kernel, grid, kThreads, kSmem, stream, t.q, t.k, t.v, t.d_o, p);
 }
