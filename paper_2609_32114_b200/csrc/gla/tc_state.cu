@@ -9,8 +9,10 @@
 // weight is one: with scale e^{G_0} in the weights dh0 had 1.5 times the error); B the values' tile as it is.  Nothing of the product waits for
 // the state, so the next step's keys are scaled under this one's product, and the chain through the steps is one multiply-add.
 //
-// What bounds it: the tiles and images through HBM when many CTAs run (128 KiB a step; four rows of 4096 tokens, 16 heads: 108 us, 5.0 TB/s), else
-// what an SM stores (64 KiB of images a step, some 20 bytes a cycle: 2 us), and for sums the scaling warps' instructions (0.9 us).
+// A step's image goes to shared memory as it will lie in memory, and one bulk copy of 64 KiB takes it out under the next step: four rows of 4096 tokens,
+// 16 heads, gradients and all 236 us, with stores of the warps (by way of shared memory, 64 bytes of eight rows at a time) 248.
+// What bounds it: the tiles and images through HBM when many CTAs run (128 KiB a step), else for images what an SM stores, and for sums the
+// scaling warps' instructions (0.9 us a step).
 // Few (sequence, V-head) pairs are cut into segments: gla_combine_kernel (simt.cu) chains the sums.
 #include "tc.cuh"
 
@@ -19,15 +21,13 @@ namespace gla {
 
 namespace {
 
-constexpr int kStages = 3;
-constexpr uint32_t kStageB = 2 * kTileBytes;
-constexpr int kThreads = 32 * (kComputeWarps + 3);         // compute warps, producer, MMA issue, gates
-constexpr uint32_t OFF_W = kStages * kStageB;              // [2] weights of a step's tokens, its decay, its sum's factor
+constexpr int kSlots = 5;                                  // tiles of two and a half steps
+constexpr int kThreads = 32 * (kComputeWarps + 4);         // compute warps, producer, MMA issue, gates, images out
+constexpr uint32_t OFF_IMAGE = kSlots * kTileBytes;        // a step's image on its way out, two pieces
+constexpr uint32_t OFF_W = OFF_IMAGE + 2 * kTileBytes;     // [2] weights of a step's tokens, its decay, its sum's factor
 constexpr uint32_t kWeightB = (kStep + 4) * 4;
-constexpr uint32_t OFF_STAGE = OFF_W + 2 * kWeightB;       // image rows on their way out, [16 warps][32 rows][32 columns]
-constexpr uint32_t kWarpStage = 2048;
-constexpr uint32_t OFF_BAR = OFF_STAGE + kComputeWarps * kWarpStage;
-constexpr int kBars = 2 * kStages + 8;
+constexpr uint32_t OFF_BAR = OFF_W + 2 * kWeightB;
+constexpr int kBars = 2 * kSlots + 10;
 constexpr uint32_t kSmem = OFF_BAR + kBars * 8 + 16;
 static_assert(kSmem <= 227 * 1024, "shared memory budget");
 constexpr uint32_t TM_A = 0, TM_D = 256;                   // operand: [2] (hi 64 | lo 64 columns); product: [2] 128 columns
@@ -51,12 +51,14 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                     const __grid_constant__ CUtensorMap map_do, StateParams p) {
   extern __shared__ __align__(1024) uint8_t sm[];
   uint64_t* bar = reinterpret_cast<uint64_t*>(sm + OFF_BAR);
-  uint64_t* full = bar;                                    // [kStages] tiles of a step
-  uint64_t* empty = bar + kStages;                         // [kStages] its product complete
-  uint64_t* weights = bar + 2 * kStages;                   // [2] of step c in set c % 2
-  uint64_t* used = weights + 2;                            // [2] ... and done with
+  uint64_t* full = bar;                                    // [kSlots] tiles: keys, values of a step, and so on
+  uint64_t* empty = bar + kSlots;                          // [kSlots] keys scaled, product complete
+  uint64_t* weights = bar + 2 * kSlots;                    // [2] of step c in set c % 2
+  uint64_t* product = weights + 2;                         // [2]
+  uint64_t* taken = product + 2;                           // the image has been read
+  uint64_t* used = taken + 1;                              // [2] weights done with
   uint64_t* operand = used + 2;                            // [2] scaled keys in tensor memory
-  uint64_t* product = operand + 2;                         // [2]
+  uint64_t* put = operand + 2;                             // the image is there
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -64,7 +66,7 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   const int seg = blockIdx.x % p.nseg, nj = blockIdx.x / p.nseg, j = nj % p.HV, jq = j / (p.HV / p.HK);
 
   if (tid == 0) {
-    for (int i = 0; i < kBars; ++i) mbar_init(&bar[i], &bar[i] >= used && &bar[i] < product ? kComputeWarps : 1);
+    for (int i = 0; i < kBars; ++i) mbar_init(&bar[i], &bar[i] >= used ? kComputeWarps : 1);
     *abort_flag = 0;
     mbar_fence_init();
   }
@@ -93,13 +95,14 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   if (warp == kComputeWarps) {
     // ------------------------------------------------------------ tiles
     if (elect_one()) {
-      for (int c = 0; c < count; ++c) {
-        const int st = c % kStages, t0 = geom(c).tok0;
-        if (c >= kStages) wait_for(&empty[st], (c / kStages - 1) & 1, abort_flag);
+      int slot = 0;
+      uint32_t round = 0;
+      for (int x = 0; x < 2 * count; ++x) {
+        if (round > 0) wait_for(&empty[slot], (round - 1) & 1, abort_flag);
         if (*abort_flag) break;
-        mbar_expect_tx(&full[st], kStageB);
-        tma_load_4d(sm + st * kStageB, rev ? &map_q : &map_k, &full[st], 0, jq, t0, 0);
-        tma_load_4d(sm + st * kStageB + kTileBytes, rev ? &map_do : &map_v, &full[st], 0, j, t0, 0);
+        mbar_expect_tx(&full[slot], kTileBytes);
+        tma_load_4d(sm + slot * kTileBytes, x & 1 ? (rev ? &map_do : &map_v) : (rev ? &map_q : &map_k), &full[slot], 0, x & 1 ? j : jq, geom(x >> 1).tok0, 0);
+        if (++slot == kSlots) { slot = 0; ++round; }
       }
     }
     __syncwarp();
@@ -107,16 +110,30 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     // ------------------------------------------------------------ products
     if (elect_one()) {
       for (int c = 0; c < count; ++c) {
-        const int st = c % kStages, b = c & 1;
-        wait_for(&full[st], (c / kStages) & 1, abort_flag);
+        const int b = c & 1, sk = 2 * c % kSlots, sv = (2 * c + 1) % kSlots;
+        wait_for(&full[sv], ((2 * c + 1) / kSlots) & 1, abort_flag);
         wait_for(&operand[b], (c >> 1) & 1, abort_flag);
+        mbar_arrive(&empty[sk]);
         tc_fence_after_sync();
-        const uint32_t tile = smem_u32(sm + st * kStageB + kTileBytes);
+        const uint32_t tile = smem_u32(sm + sv * kTileBytes);
         mma_tmem_rows(TM_D + 128 * b, TM_A + 128 * b, tile, false);
         mma_tmem_rows(TM_D + 128 * b, TM_A + 128 * b + 64, tile, true);
         umma_commit(&product[b]);
-        umma_commit(&empty[st]);
+        umma_commit(&empty[sv]);
       }
+    }
+    __syncwarp();
+  } else if (warp == kComputeWarps + 3) {
+    // ------------------------------------------------------------ images out
+    if (IMAGES && elect_one()) {
+      for (int c = 0; c < count; ++c) {
+        wait_for(put, c & 1, abort_flag);
+        if (*abort_flag) break;
+        bulk_store(p.image[rev] + ((size_t)(slot0 + index(c)) * p.HV + j) * (2 * kTileBytes), sm + OFF_IMAGE, 2 * kTileBytes);
+        bulk_store_read();
+        mbar_arrive(taken);
+      }
+      bulk_store_done();
     }
     __syncwarp();
   } else if (warp == kComputeWarps + 2) {
@@ -160,15 +177,17 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     }
     float total = 1.f;
     auto scale_keys = [&](int c) {
-      const int st = c % kStages, b = c & 1, L = geom(c).L;
-      uint8_t* tile = sm + st * kStageB;
+      const int b = c & 1, L = geom(c).L, sk = 2 * c % kSlots, sv = (2 * c + 1) % kSlots;
+      uint8_t* tile = sm + sk * kTileBytes;
       wait_for(&weights[b], (c >> 1) & 1, abort_flag);
-      wait_for(&full[st], (c / kStages) & 1, abort_flag);
+      wait_for(&full[sk], (2 * c / kSlots) & 1, abort_flag);
       __syncwarp();
       if (L < kStep) {                                     // (rows behind the sequence may be NaN, which no weight of zero masks)
+        wait_for(&full[sv], ((2 * c + 1) / kSlots) & 1, abort_flag);
         clear_rows(tile, L, tid, 32 * kComputeWarps);
-        clear_rows(tile + kTileBytes, L, tid, 32 * kComputeWarps);
+        clear_rows(sm + sv * kTileBytes, L, tid, 32 * kComputeWarps);
         fence_proxy_async_smem();
+        __syncwarp();
         asm volatile("bar.sync 1, %0;" ::"n"(32 * kComputeWarps) : "memory");
       }
       // 16 keys x 16 tokens at a time, transposed by ldmatrix; this lane's tokens are 2 (lane % 4), + 1 of each eight
@@ -198,30 +217,20 @@ gla_tc_state_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
       const int b = c & 1;
       if (c + 1 < count) scale_keys(c + 1);
       if constexpr (IMAGES) {
-        uint8_t* image = p.image[rev] + ((size_t)(slot0 + index(c)) * p.HV + j) * (2 * kTileBytes) + (g >> 1) * 16384;
-        uint4 hi[4], lo[4];
+        if (c > 0) wait_for(taken, (c - 1) & 1, abort_flag);
+        uint8_t* row = sm + OFF_IMAGE + (g >> 1) * 16384 + key * 128;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 4; ++k) {
+          uint4 hi, lo;
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const float2 x = make_float2(h[8 * k + 2 * w], h[8 * k + 2 * w + 1]);
-            split_bf16(x, (&hi[k].x)[w], (&lo[k].x)[w]);
-          }
-        // by way of shared memory, so that a store covers 64 bytes of eight rows: a row to a thread it takes the memory pipe four times as long
-        uint8_t* mine = sm + OFF_STAGE + warp * kWarpStage;
-        auto put = [&](const uint4 (&x)[4], uint8_t* dst) {
-          __syncwarp();
-#pragma unroll
-          for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(mine + sw64_offset(lane, k)) = x[k];
-          __syncwarp();
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int r = 8 * k + (lane >> 2), row = 32 * q + r;
-            *reinterpret_cast<uint4*>(dst + row * 128 + (((4 * (g & 1) + (lane & 3)) ^ (row & 7)) << 4)) = *reinterpret_cast<const uint4*>(mine + sw64_offset(r, lane & 3));
-          }
-        };
-        put(hi, image);
-        put(lo, image + kTileBytes);
+          for (int w = 0; w < 4; ++w) split_bf16(make_float2(h[8 * k + 2 * w], h[8 * k + 2 * w + 1]), (&hi.x)[w], (&lo.x)[w]);
+          const int at = ((4 * (g & 1) + k) ^ (key & 7)) << 4;
+          *reinterpret_cast<uint4*>(row + at) = hi;
+          *reinterpret_cast<uint4*>(row + kTileBytes + at) = lo;
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(put);
       }
       const float2 f = *reinterpret_cast<const float2*>(sm + OFF_W + b * kWeightB + kStep * 4);
       wait_for(&product[b], (c >> 1) & 1, abort_flag);
