@@ -43,8 +43,8 @@ int make_problem(const ha_la_gla_args* a, Problem* p) {
     chunks = (long long)a->batch * ((a->seqlen + step - 1) / step);
   }
   p->max_seq_chunks = (int)((p->max_len + step - 1) / step);
-  // CTAs are counted in 31 bits: chunks x V-heads, sequences x V-heads x pieces of a state, pieces of dq
-  if (chunks * p->HV > 0x7fffffffLL || (long long)p->N * p->HV > 0x7fffffffLL / (p->dk * p->dv / 1024)) return HA_LA_ERR_UNSUPPORTED;
+  // CTAs are counted in 31 bits: chunks x V-heads (x parts of a chunk), sequences x V-heads x pieces of a state, pieces of dq
+  if (chunks * p->HV > 0x7fffffffLL / (on_tensor_cores(*p) ? 1 : 2) || (long long)p->N * p->HV > 0x7fffffffLL / (p->dk * p->dv / 1024)) return HA_LA_ERR_UNSUPPORTED;
   if (rows * p->HK > 0x7fffffffLL * 8) return HA_LA_ERR_UNSUPPORTED;
   p->max_chunks = (int)chunks;
   p->planned_runs = p->runs = p->segments = 1;
@@ -55,7 +55,7 @@ size_t plan_part(const Problem& p) { return p.varlen ? plan_bytes(p) : 0; }
 
 size_t bytes_of(const Problem& p, bool back) {
   const size_t n = on_tensor_cores(p) ? gla::tc_bytes(p, back, nullptr, nullptr, nullptr) : gla::simt_bytes(p, back, nullptr, nullptr);
-  return align_up(plan_part(p) + n, 256);
+  return align_up(plan_part(p) + (n > 0 ? n : 1), 256);
 }
 
 template <typename... P> uintptr_t any_of(P... p) { return (... | (uintptr_t)p); }

@@ -32,10 +32,11 @@ struct SimtParams {
 
 // ---------------------------------------------------------------- pieces
 
-// rows of 64 tokens x D, zeros past the chunk's end
+// `rows` (64) tokens x D, zeros past the chunk's end
 template <typename In, int D>
-__device__ __forceinline__ void load_rows(float* dst, const void* src, int tok0, int L, int heads, int head) {
-  for (int i = threadIdx.x; i < kTok * (D / 4); i += kThreads) {
+__device__ __forceinline__ void load_rows(float* dst, const void* src, int tok0, int L, int heads, int head, int rows = kTok) {
+#pragma unroll 4
+  for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
     const int t = i / (D / 4), c = i % (D / 4) * 4;
     const float4 x = t < L ? load4(reinterpret_cast<const In*>(src) + ((size_t)(tok0 + t) * heads + head) * D + c) : make_float4(0.f, 0.f, 0.f, 0.f);
     *reinterpret_cast<float4*>(dst + t * (D + kPad) + c) = x;
@@ -67,95 +68,105 @@ __device__ __forceinline__ float decay(const Gates& s, int to, int from) {   // 
 }
 __device__ __forceinline__ float decay0(const Gates& s, int to) { return expf(s.hi[to] + s.lo[to]); }
 
-// acc[r][m] += rows 4 ty + r, columns tx + 16 m of A B (nn), A B^T (nt), A^T B (tn), over n
-template <int M>
-__device__ __forceinline__ void nn(float (&acc)[4][M], const float* A, int lda, const float* B, int ldb, int n) {
+// acc[r][m] += rows R ty + r, columns tx + 16 m of A B (nn), A B^T (nt), A^T B (tn), over n
+template <int R, int M>
+__device__ __forceinline__ void nn(float (&acc)[R][M], const float* A, int lda, const float* B, int ldb, int n) {
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
   for (int k = 0; k < n; k += 4) {
-    float4 a[4];
+    float4 a[R];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) a[r] = *reinterpret_cast<const float4*>(A + (4 * ty + r) * lda + k);
+    for (int r = 0; r < R; ++r) a[r] = *reinterpret_cast<const float4*>(A + (R * ty + r) * lda + k);
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
       for (int m = 0; m < M; ++m) {
         const float b = B[(k + kk) * ldb + tx + 16 * m];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[r][m] = fmaf((&a[r].x)[kk], b, acc[r][m]);
+        for (int r = 0; r < R; ++r) acc[r][m] = fmaf((&a[r].x)[kk], b, acc[r][m]);
       }
   }
 }
-template <int M>
-__device__ __forceinline__ void nt(float (&acc)[4][M], const float* A, int lda, const float* B, int ldb, int n) {
+template <int R, int M>
+__device__ __forceinline__ void nt(float (&acc)[R][M], const float* A, int lda, const float* B, int ldb, int n) {
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
   for (int k = 0; k < n; k += 4) {
-    float4 a[4];
+    float4 a[R];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) a[r] = *reinterpret_cast<const float4*>(A + (4 * ty + r) * lda + k);
+    for (int r = 0; r < R; ++r) a[r] = *reinterpret_cast<const float4*>(A + (R * ty + r) * lda + k);
 #pragma unroll
     for (int m = 0; m < M; ++m) {
       const float4 b = *reinterpret_cast<const float4*>(B + (tx + 16 * m) * ldb + k);
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+      for (int r = 0; r < R; ++r)
         acc[r][m] = fmaf(a[r].x, b.x, fmaf(a[r].y, b.y, fmaf(a[r].z, b.z, fmaf(a[r].w, b.w, acc[r][m]))));
     }
   }
 }
-template <int M>
-__device__ __forceinline__ void tn(float (&acc)[4][M], const float* A, int lda, const float* B, int ldb, int n) {
+template <int R, int M>
+__device__ __forceinline__ void tn(float (&acc)[R][M], const float* A, int lda, const float* B, int ldb, int n) {
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll 4
   for (int k = 0; k < n; ++k) {
-    const float4 a = *reinterpret_cast<const float4*>(A + k * lda + 4 * ty);
+    float a[R];
+    if constexpr (R == 4) *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(A + k * lda + 4 * ty);
+    else a[0] = A[k * lda + ty];
 #pragma unroll
     for (int m = 0; m < M; ++m) {
       const float b = B[k * ldb + tx + 16 * m];
-      acc[0][m] = fmaf(a.x, b, acc[0][m]); acc[1][m] = fmaf(a.y, b, acc[1][m]);
-      acc[2][m] = fmaf(a.z, b, acc[2][m]); acc[3][m] = fmaf(a.w, b, acc[3][m]);
+#pragma unroll
+      for (int r = 0; r < R; ++r) acc[r][m] = fmaf(a[r], b, acc[r][m]);
     }
   }
 }
-template <int M> __device__ __forceinline__ void zero(float (&acc)[4][M]) {
+template <int R, int M> __device__ __forceinline__ void zero(float (&acc)[R][M]) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
+  for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int m = 0; m < M; ++m) acc[r][m] = 0.f;
 }
 
 // ---------------------------------------------------------------- a chunk's addition to the state
 
-template <typename In, int D, bool REV>
+// (16 R of its rows to a CTA: R = 1 in calls of few chunks, see `few`)
+template <typename In, int D, int R, bool REV>
 __global__ void __launch_bounds__(kThreads) gla_state_kernel(SimtParams p) {
+  constexpr int LD = D + kPad, ROWS = 16 * R, LA = ROWS + kPad;
   extern __shared__ __align__(16) float sm[];
   __shared__ Gates G;
-  __shared__ float weight[kTok];
-  float *a = sm, *b = sm + kTok * (D + kPad);
-  const int slot = blockIdx.x / p.HV, j = blockIdx.x % p.HV, jq = j / (p.HV / p.HK);
+  float *a = sm, *b = sm + kTok * LA;
+  const int part = blockIdx.x % (D / ROWS), unit = blockIdx.x / (D / ROWS), slot = unit / p.HV, j = unit % p.HV, jq = j / (p.HV / p.HK);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const Geom c = geom_of(p.chunks, slot);
   if (c.L <= 0) return;
   load_gates(G, p.g, c.tok0, c.L, p.HV, j);
-  load_rows<In, D>(a, REV ? p.q : p.k, c.tok0, c.L, p.HK, jq);
   load_rows<In, D>(b, REV ? p.d_o : p.v, c.tok0, c.L, p.HV, j);
-  __syncthreads();
-  if (threadIdx.x < kTok) weight[threadIdx.x] = REV ? p.scale * decay0(G, threadIdx.x) : decay(G, kTok - 1, threadIdx.x);
-  if (!REV && threadIdx.x == 0) p.w.total[(size_t)slot * p.HV + j] = decay0(G, kTok - 1);
-  __syncthreads();
-  for (int i = threadIdx.x; i < kTok * D; i += kThreads) b[i / D * (D + kPad) + i % D] *= weight[i / D];
-  __syncthreads();
-  float* out = (REV ? p.w.dh : p.w.h) + ((size_t)slot * p.HV + j) * D * D;
-  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-#pragma unroll 1
-  for (int half = 0; half < D / 64; ++half) {
-    float acc[4][D / 16];
-    zero(acc);
-    tn(acc, a + 64 * half, D + kPad, b, D + kPad, kTok);
+  const In* src = reinterpret_cast<const In*>(REV ? p.q : p.k) + part * ROWS;
+  constexpr int kMine = kTok * (ROWS / 4) / kThreads;      // float4 of this CTA's rows to a thread
+  float4 x[kMine];
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int m = 0; m < D / 16; ++m) out[(size_t)(64 * half + 4 * ty + r) * D + tx + 16 * m] = acc[r][m];
+  for (int i = 0; i < kMine; ++i) {
+    const int at = threadIdx.x + kThreads * i, t = at / (ROWS / 4), cc = at % (ROWS / 4) * 4;
+    x[i] = t < c.L ? load4(src + ((size_t)(c.tok0 + t) * p.HK + jq) * D + cc) : make_float4(0.f, 0.f, 0.f, 0.f);
   }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {                        // times their tokens' weights
+    const int at = threadIdx.x + kThreads * i, t = at / (ROWS / 4), cc = at % (ROWS / 4) * 4;
+    const float w = REV ? p.scale * decay0(G, t) : decay(G, kTok - 1, t);
+    *reinterpret_cast<float4*>(a + t * LA + cc) = make_float4(x[i].x * w, x[i].y * w, x[i].z * w, x[i].w * w);
+  }
+  if (!REV && part == 0 && threadIdx.x == 0) p.w.total[(size_t)slot * p.HV + j] = decay0(G, kTok - 1);
+  __syncthreads();
+  float acc[R][D / 16];
+  zero(acc);
+  tn(acc, a, LA, b, LD, kTok);
+  float* out = (REV ? p.w.dh : p.w.h) + ((size_t)slot * p.HV + j) * D * D + (size_t)part * ROWS * D;
+  const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int m = 0; m < D / 16; ++m) out[(size_t)(R * ty + r) * D + tx + 16 * m] = acc[r][m];
 }
 
 // ---------------------------------------------------------------- the scan
@@ -206,59 +217,75 @@ __global__ void __launch_bounds__(kThreads) gla_combine_kernel(CombineParams p) 
 
 // ---------------------------------------------------------------- outputs
 
-template <typename In, int D>
+// (16 R tokens to a CTA.  R = 4: keys, state and values in turn in one place, so that several CTAs share an SM; R = 1: all at once, read ahead)
+template <typename In, int D, int R>
 __global__ void __launch_bounds__(kThreads) gla_out_kernel(SimtParams p) {
-  constexpr int LD = D + kPad, LP = kTok + kPad, M = D / 16;
+  constexpr int LD = D + kPad, LP = kTok + kPad, M = D / 16, ROWS = 16 * R;
   extern __shared__ __align__(16) float sm[];
   __shared__ Gates G;
-  float *q = sm, *kv = q + kTok * LD, *P = kv + kTok * LD;
-  const int slot = blockIdx.x / p.HV, j = blockIdx.x % p.HV, jq = j / (p.HV / p.HK), ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
+  float *q = sm, *P = q + ROWS * LD, *k = P + ROWS * LP, *v = R == 1 ? k + kTok * LD : k, *hs = R == 1 ? v + kTok * LD : k;
+  const int part = blockIdx.x % (kTok / ROWS), unit = blockIdx.x / (kTok / ROWS), r0 = part * ROWS, upto = r0 + ROWS;
+  const int slot = unit / p.HV, j = unit % p.HV, jq = j / (p.HV / p.HK), ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const Geom c = geom_of(p.chunks, slot);
-  if (c.L <= 0) return;
+  if (c.L <= r0) return;
+  const float* h = p.w.h + ((size_t)slot * p.HV + j) * D * D;
+  auto load_state = [&](int at, int rows) {
+#pragma unroll 8
+    for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
+      const int t = i / (D / 4), cc = i % (D / 4) * 4;
+      *reinterpret_cast<float4*>(hs + t * LD + cc) = *reinterpret_cast<const float4*>(h + (size_t)(at + t) * D + cc);
+    }
+  };
   load_gates(G, p.g, c.tok0, c.L, p.HV, j);
-  load_rows<In, D>(q, p.q, c.tok0, c.L, p.HK, jq);
-  load_rows<In, D>(kv, p.k, c.tok0, c.L, p.HK, jq);
+  load_rows<In, D>(q, p.q, c.tok0 + r0, c.L - r0, p.HK, jq, ROWS);
+  load_rows<In, D>(k, p.k, c.tok0, c.L, p.HK, jq, upto);
+  if (R == 1) {
+    load_state(0, D);
+    load_rows<In, D>(v, p.v, c.tok0, c.L, p.HV, j, upto);
+  }
   __syncthreads();
-  float s[4][4];
+  float s[R][4];
   zero(s);
-  nt(s, q, LD, kv, LD, D);
+  nt(s, q, LD, k, LD, D);                                  // (R = 1: beyond this CTA's rows of whatever lies there, which the mask leaves out)
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
+  for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-      const int i = 4 * ty + r, jj = tx + 16 * m;
-      P[i * LP + jj] = i >= jj ? s[r][m] * decay(G, i, jj) : 0.f;
+      const int i = r0 + R * ty + r, jj = tx + 16 * m;
+      P[(R * ty + r) * LP + jj] = i >= jj ? s[r][m] * decay(G, i, jj) : 0.f;
     }
-  // q h first, the state's rows by 64, times e^{G_i}; then P v on top
-  float acc[4][M];
+  // q h first, times e^{G_i}; then P v on top
+  float acc[R][M];
   zero(acc);
-  const float* h = p.w.h + ((size_t)slot * p.HV + j) * D * D;
+  if (R == 1) {
+    nn(acc, q, LD, hs, LD, D);
+  } else {
 #pragma unroll 1
-  for (int half = 0; half < D / 64; ++half) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < 64 * (D / 4); i += kThreads) {
-      const int t = i / (D / 4), cc = i % (D / 4) * 4;
-      *reinterpret_cast<float4*>(kv + t * LD + cc) = *reinterpret_cast<const float4*>(h + (size_t)(64 * half + t) * D + cc);
+    for (int half = 0; half < D / 64; ++half) {
+      __syncthreads();
+      load_state(64 * half, 64);
+      __syncthreads();
+      nn(acc, q + 64 * half, LD, hs, LD, 64);
     }
-    __syncthreads();
-    nn(acc, q + 64 * half, LD, kv, LD, 64);
   }
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const float e = decay0(G, 4 * ty + r);
+  for (int r = 0; r < R; ++r) {
+    const float e = decay0(G, r0 + R * ty + r);
 #pragma unroll
     for (int m = 0; m < M; ++m) acc[r][m] *= e;
   }
   __syncthreads();
-  load_rows<In, D>(kv, p.v, c.tok0, c.L, p.HV, j);
-  __syncthreads();
-  nn(acc, P, LP, kv, LD, kTok);
+  if (R != 1) {
+    load_rows<In, D>(v, p.v, c.tok0, c.L, p.HV, j);
+    __syncthreads();
+  }
+  nn(acc, P, LP, v, LD, upto);
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
-    if (4 * ty + r < c.L) {
-      In* o = reinterpret_cast<In*>(p.o) + ((size_t)(c.tok0 + 4 * ty + r) * p.HV + j) * D;
+  for (int r = 0; r < R; ++r)
+    if (r0 + R * ty + r < c.L) {
+      In* o = reinterpret_cast<In*>(p.o) + ((size_t)(c.tok0 + r0 + R * ty + r) * p.HV + j) * D;
 #pragma unroll
       for (int m = 0; m < M; ++m) o[tx + 16 * m] = from_f32<In>(p.scale * acc[r][m]);
     }
@@ -448,8 +475,8 @@ __global__ void __launch_bounds__(kThreads) gla_sum_kernel(SumParams p) {
 
 // ---------------------------------------------------------------- host
 
-constexpr size_t smem_state(int D) { return 2u * kTok * (D + kPad) * 4; }
-constexpr size_t smem_out(int D) { return (2u * kTok * (D + kPad) + kTok * (kTok + kPad)) * 4; }
+constexpr size_t smem_state(int D, int R) { return kTok * (D + 16 * R + 2 * kPad) * 4u; }
+constexpr size_t smem_out(int D, int R) { return (16 * R * (D + kTok + 2 * kPad) + (R == 1 ? 2 * kTok + D : kTok) * (D + kPad)) * 4u; }
 constexpr size_t smem_back(int D) { return (4u * kTok * (D + kPad) + 2 * kTok * (kTok + kPad) + kStage * (D + kPad)) * 4; }
 static_assert(smem_back(128) + 8192 <= 227 * 1024, "shared memory budget");
 
@@ -462,34 +489,44 @@ SimtParams params_of(const Call& c) {
   return s;
 }
 
-cudaError_t launch(void (*kernel)(SimtParams), size_t smem, const Call& c, cudaStream_t stream) {
+// `parts` CTAs to a (chunk, V-head)
+cudaError_t launch(void (*kernel)(SimtParams), int parts, size_t smem, const Call& c, cudaStream_t stream) {
   const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  return start(kernel, dim3((unsigned)((size_t)c.p.max_chunks * c.p.HV)), kThreads, smem, stream, params_of(c));
+  return start(kernel, dim3((unsigned)((size_t)c.p.max_chunks * c.p.HV * parts)), kThreads, smem, stream, params_of(c));
 }
+
+// Rows of a thread in the chunks' additions and outputs: 1, with four times the CTAs, where all of these run at once (three to an SM at d = 64, one at 128:
+// 61 and 143 KiB).  us with 4 and with 1, fp32: one chunk at d = 64 22 and 13, 40 chunks x V-heads 22 and 21, 160 34 and 45; d = 128, 4 of them 42 and 22, 80 45 and 57.
+bool few(const Call& c) { return (long long)c.p.max_chunks * c.p.HV * 4 <= sm_count() * (c.p.dk == 64 ? 3 : 1); }
+
+template <typename In, int D, int R>
+cudaError_t chunks_forward(const Call& c, cudaStream_t stream) { return launch(gla_state_kernel<In, D, R, false>, D / (16 * R), smem_state(D, R), c, stream); }
+template <typename In, int D, int R>
+cudaError_t chunks_reverse(const Call& c, cudaStream_t stream) { return launch(gla_state_kernel<In, D, R, true>, D / (16 * R), smem_state(D, R), c, stream); }
 
 template <typename In, int D>
 cudaError_t forward(const Call& c, cudaStream_t stream) {
   if (c.p.max_chunks > 0) {
-    const cudaError_t e = launch(gla_state_kernel<In, D, false>, smem_state(D), c, stream);
+    const cudaError_t e = few(c) ? chunks_forward<In, D, 1>(c, stream) : chunks_forward<In, D, 4>(c, stream);
     if (e != cudaSuccess) return e;
   }
   const cudaError_t e = launch_combine(c, false, stream);
   if (e != cudaSuccess || c.p.max_chunks == 0) return e;
-  return launch(gla_out_kernel<In, D>, smem_out(D), c, stream);
+  return few(c) ? launch(gla_out_kernel<In, D, 1>, kTok / 16, smem_out(D, 1), c, stream) : launch(gla_out_kernel<In, D, 4>, 1, smem_out(D, 4), c, stream);
 }
 
 template <typename In, int D>
 cudaError_t backward(const Call& c, cudaStream_t stream) {
   cudaError_t e = cudaSuccess;
   if (c.p.max_chunks > 0) {
-    e = launch(gla_state_kernel<In, D, false>, smem_state(D), c, stream);
-    if (e == cudaSuccess) e = launch(gla_state_kernel<In, D, true>, smem_state(D), c, stream);
+    e = few(c) ? chunks_forward<In, D, 1>(c, stream) : chunks_forward<In, D, 4>(c, stream);
+    if (e == cudaSuccess) e = few(c) ? chunks_reverse<In, D, 1>(c, stream) : chunks_reverse<In, D, 4>(c, stream);
     if (e == cudaSuccess) e = launch_combine(c, false, stream);
   }
   if (e == cudaSuccess) e = launch_combine(c, true, stream);
   if (e != cudaSuccess || c.p.max_chunks == 0) return e;
-  e = launch(gla_back_kernel<In, D>, smem_back(D), c, stream);
+  e = launch(gla_back_kernel<In, D>, 1, smem_back(D), c, stream);
   return e == cudaSuccess ? launch_head_sums(c, c.p.HV, stream) : e;
 }
 
