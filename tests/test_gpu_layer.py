@@ -12,6 +12,14 @@ from tests.test_gpu_gla import check, close, cuda, inputs
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(scope="module", autouse=True)
+def memory_given_back():
+    """The large tensors' segments, which other tests' small ones would be put into."""
+    yield
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+
+
 def _ha():
     import paper_2609_32114_b200 as ha
 

@@ -11,6 +11,14 @@ from tests import layer_reference as ref
 
 pytestmark = pytest.mark.gpu
 
+
+@pytest.fixture(scope="module", autouse=True)
+def memory_given_back():
+    """The large tensors' segments, which other tests' small ones would be put into."""
+    yield
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+
 COLS = [1, 2, 7, 8, 9, 40, 64, 100, 127, 128, 129, 248, 249, 256, 257, 1000, 2048, 2049, 4096, 4100, 8192, 8200, 16383, 16384]
 
 
