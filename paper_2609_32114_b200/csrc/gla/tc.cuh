@@ -98,9 +98,8 @@ __device__ __forceinline__ void clear_rows(uint8_t* tile, int L, int tid, int n)
     *reinterpret_cast<uint4*>(tile + (i & 1) * 16384 + (L + (i >> 4)) * 128 + ((i >> 1) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// Two (four) lanes that hold two (four) 16-byte pieces of a row each exchange them: v[i] becomes this lane's piece of the row of lane i of the
-// two (four).  A warp's store of v[i] then covers 32 (64) bytes of sixteen (eight) rows instead of 16 of thirty-two: a store takes the memory pipe
-// a cycle for every 128-byte line it touches.
+// Four lanes that hold four 16-byte pieces of a row each exchange them: v[i] becomes this lane's piece of the row of lane i of the four.  A warp's
+// store of v[i] then covers 64 bytes of eight rows instead of 16 of thirty-two: a store takes the memory pipe a cycle for every 128-byte line it touches.
 __device__ __forceinline__ void exchange(uint4& first, uint4& second, bool keep_second, int with) {
   const uint4 send = keep_second ? first : second;
   uint4 got;
@@ -111,7 +110,6 @@ __device__ __forceinline__ void exchange(uint4& first, uint4& second, bool keep_
   if (keep_second) first = got;
   else second = got;
 }
-__device__ __forceinline__ void exchange2(uint4 (&v)[2], int lane) { exchange(v[0], v[1], lane & 1, 1); }
 __device__ __forceinline__ void exchange4(uint4 (&v)[4], int lane) {
   exchange(v[0], v[1], lane & 1, 1);
   exchange(v[2], v[3], lane & 1, 1);

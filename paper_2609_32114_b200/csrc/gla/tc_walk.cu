@@ -13,7 +13,8 @@
 // What bounds it: a step's phases, 2.8 to 3.0 us; of 5700 cycles P takes 1200, K' 1200, o 1200, the state and its tile 600, and looking at seven barriers
 // 1400 (time stamps of one warp).  HBM would allow 2.6 us with 128 CTAs (128 KiB a step): eight sequences of 7914 to 15654 tokens, 16 heads
 // 368 us, 4.2 TB/s on the average.  Outputs as a kernel of their own over stored states took 573 us; eight more warps for o 388, the state's and the outputs'
-// phases in different warps 500 (seven warps to a scheduler, spills); 96 registers with 16 bytes of spills instead of 104 without 378.
+// phases in different warps 500 (seven warps to a scheduler, spills); 96 registers with 16 bytes of spills instead of 104 without 378; o by way
+// of Q's slot and a tensor store 486 (the slot comes free a step later).
 // Few (sequence, V-head) pairs are cut into segments: gla_tc_state_kernel sums each from zero, gla_combine_kernel (simt.cu) chains the sums, and this
 // kernel walks all segments from their true starts.
 #include "tc.cuh"
