@@ -56,7 +56,8 @@ cudaError_t make(TcCall* t, const Call& c, PlanView plan, const TcWork& w) {
   t->nseg = segments(c.p, c.back);
   t->seqs = {plan.seq_tok0, plan.seq_len, plan.seq_chunk0, plan.seq_order, c.p.T_row, c.p.max_seq_chunks};
   if (!make_map_tile(&t->q, c.a.q, c.p.T_total, c.p.HK) || !make_map_tile(&t->k, c.a.k, c.p.T_total, c.p.HK) ||
-      !make_map_tile(&t->v, c.a.v, c.p.T_total, c.p.HV) || !make_map_tile(&t->d_o, c.back ? c.a.do_ : c.a.v, c.p.T_total, c.p.HV))
+      !make_map_tile(&t->v, c.a.v, c.p.T_total, c.p.HV) || !make_map_tile(&t->d_o, c.back ? c.a.do_ : c.a.v, c.p.T_total, c.p.HV) ||
+      !make_map_tile(&t->o, c.back ? c.a.v : c.a.o, c.p.T_total, c.p.HV))
     return cudaErrorInvalidValue;
   return cudaSuccess;
 }

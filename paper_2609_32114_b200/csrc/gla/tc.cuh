@@ -22,7 +22,7 @@ using namespace ptx;
 
 constexpr int kComputeWarps = 16;
 
-// The walk and the gradient kernel run 20 warps: 16 that compute, then producer, MMA issue, gates and one for dg, which idles in the walk.  96 registers a
+// The walk and the gradient kernel run 20 warps: 16 that compute, then producer, MMA issue, gates and one for dg or, in the walk, for o.  96 registers a
 // thread are what an SM has for them; in the walk the last four hand some over, since a few bytes of spills cost 3% (with ~227 KiB of shared memory there is
 // hardly any L1 left for the stack).  A launch that brought fewer than kRegs would wait for ever for them, so the launcher asks.
 constexpr int kRoleThreads = 32 * (kComputeWarps + 4), kRegs = 96, kComputeRegs = 104, kOtherRegs = 64;
@@ -174,7 +174,7 @@ struct TcWork {
 
 struct TcCall {
   const Call* c;
-  CUtensorMap q, k, v, d_o;
+  CUtensorMap q, k, v, d_o, o;                             // d_o: backward, o: forward
   Seqs seqs;
   TcWork w;
   int nseg;

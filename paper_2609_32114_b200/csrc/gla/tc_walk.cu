@@ -10,11 +10,12 @@
 //   threads   P(c)   scale Q h(c)   h(c + 1) and its tile   K'(c + 1)   o(c) out
 //   products  ...    K' V(c)        P V(c)  S(c + 1)        Q h(c + 1)  K' V(c + 1)
 // so each product runs under what the threads do next, and nothing but q, k, v and o goes through HBM.
-// What bounds it: a step's phases, 2.8 to 3.0 us; of 5700 cycles P takes 1200, K' 1200, o 1200, the state and its tile 600, and looking at seven barriers
-// 1400 (time stamps of one warp).  HBM would allow 2.6 us with 128 CTAs (128 KiB a step): eight sequences of 7914 to 15654 tokens, 16 heads
-// 368 us, 4.2 TB/s on the average.  Outputs as a kernel of their own over stored states took 573 us; eight more warps for o 388, the state's and the outputs'
-// phases in different warps 500 (seven warps to a scheduler, spills); 96 registers with 16 bytes of spills instead of 104 without 378; o by way
-// of Q's slot and a tensor store 486 (the slot comes free a step later).
+// o goes out by a tensor store from where V lay, which is of no more use then; a last step of fewer tokens by plain stores.
+// What bounds it: a step's phases, 2.6 to 2.9 us: 12000 instructions of a warp, four at a time, and looking at seven barriers, some 200 cycles each.
+// HBM would allow 2.6 us with 128 CTAs (128 KiB a step): eight sequences of 7914 to 15654 tokens, 16 heads 355 us, 4.3 TB/s on the average.
+// Outputs as a kernel of their own over stored states took 573 us; eight more warps for o 388, the state's and the outputs' phases in different
+// warps 500 (seven warps to a scheduler, spills); 96 registers with 16 bytes of spills instead of 104 without + 10; o by exchanges between lanes and stores of
+// 64 bytes a row 376; o from where Q lay 486 (that slot is wanted a step sooner).
 // Few (sequence, V-head) pairs are cut into segments: gla_tc_state_kernel sums each from zero, gla_combine_kernel (simt.cu) chains the sums, and this
 // kernel walks all segments from their true starts.
 #include "tc.cuh"
@@ -29,7 +30,7 @@ struct WalkGates : StepGates { float el[kStep], total, pad[3]; };   // and e^{G_
 constexpr uint32_t OFF_H = kSlots * kTileBytes;            // the state in front of the step as a tile
 constexpr uint32_t OFF_G = OFF_H + kTileBytes;
 constexpr uint32_t OFF_BAR = OFF_G + sizeof(WalkGates);
-constexpr int kBars = 2 * kSlots + 9;
+constexpr int kBars = 2 * kSlots + 10;
 constexpr uint32_t kSmem = OFF_BAR + kBars * 8 + 16;
 static_assert(kSmem <= 227 * 1024 && sizeof(WalkGates) % 16 == 0, "shared memory budget");
 constexpr uint32_t TM_S = 0, TM_O = 128, TM_K = 256, TM_D = 384;
@@ -47,15 +48,16 @@ struct WalkParams {
 };
 
 __global__ void __launch_bounds__(kRoleThreads, 1)
-gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, WalkParams p) {
+gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                   const __grid_constant__ CUtensorMap map_o, WalkParams p) {
   extern __shared__ __align__(1024) uint8_t sm[];
   WalkGates* s = reinterpret_cast<WalkGates*>(sm + OFF_G);
   uint64_t* bar = reinterpret_cast<uint64_t*>(sm + OFF_BAR);
   uint64_t *full = bar, *empty = bar + kSlots;             // [kSlots]
   uint64_t* one = bar + 2 * kSlots;                        // by one thread or by the tensor cores: gates; products complete: S, Q h, K' V, P V
   uint64_t *gates = one, *b_s = one + 1, *b_qh = one + 2, *b_d = one + 3, *b_o = one + 4;
-  uint64_t* all = one + 5;                                 // by the compute warps: gates done with; P there and Q h scaled; K' there; O read and the state's tile written
-  uint64_t *g_free = all, *e_p = all + 1, *e_k = all + 2, *e_h = all + 3;
+  uint64_t* all = one + 5;                                 // by the compute warps: gates done with; P there and Q h scaled; K' there; O read and the state's tile written; o there
+  uint64_t *g_free = all, *e_p = all + 1, *e_k = all + 2, *e_h = all + 3, *put = all + 4;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -121,7 +123,7 @@ gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             mma_rows(TM_O, q, h, false);                     // Q h
             umma_commit(b_qh);
             umma_commit(&empty[at]);
-            umma_commit(&empty[at + 1]);                     // (K: K' is there, S was complete)
+            umma_commit(&empty[at + 1]);                   // (K: K' is there, S was complete)
             wait(&full[at + 2], fill);
             wait(e_k, ph);
             mma_tmem_rows(TM_D, TM_K, v, false);             // K' V
@@ -130,7 +132,6 @@ gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             wait(e_p, ph);
             mma_tmem_rows<16>(TM_O, TM_S, v, true);          // + P V
             umma_commit(b_o);
-            umma_commit(&empty[at + 2]);
           }
           if (c + 1 < count) {
             wait(&full[next], fill_next);
@@ -162,6 +163,31 @@ gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         if (lane == 0) mbar_arrive(gates);
         __syncwarp();
       }
+    } else {
+      // ------------------------------------------------------------ outputs, out of where V was
+#pragma unroll 1
+      for (int c = 0; c < count; ++c) {
+        wait_for(put, c & 1, abort_flag);
+        if (__any_sync(0xffffffffu, *abort_flag)) break;
+        const Geom at = geom(c);
+        const uint8_t* tile = sm + (kTiles * (c & 1) + 2) * kTileBytes;
+        if (at.L == kStep) {
+          if (lane == 0) {
+            tma_store_4d(&map_o, tile, 0, j, at.tok0, 0);
+            bulk_store_read();
+          }
+        } else {                                           // (not over the next sequence's rows)
+          uint4* dst = reinterpret_cast<uint4*>(p.o) + ((size_t)at.tok0 * p.HV + j) * 16;
+#pragma unroll 4
+          for (int x = lane; x < at.L * 16; x += 32)
+            dst[(size_t)(x >> 4) * p.HV * 16 + (x & 15)] = *reinterpret_cast<const uint4*>(tile + (x & 8) * 2048 + (x >> 4) * 128 + (((x ^ (x >> 4)) & 7) << 4));
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&empty[kTiles * (c & 1) + 2]);
+        __syncwarp();
+      }
+      if (lane == 0) bulk_store_done();
+      __syncwarp();
     }
   } else {
     take_registers();
@@ -241,7 +267,11 @@ gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           tmem_ld16(TM_O + slice + k, r);
           tmem_ld_wait();
 #pragma unroll
-          for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(eg * __uint_as_float(r[e]));
+          for (int e = 0; e < 16; e += 2) {
+            const float2 x = mul2(make_float2(eg, eg), as_f2(r[e], r[e + 1]));
+            r[e] = __float_as_uint(x.x);
+            r[e + 1] = __float_as_uint(x.y);
+          }
           tmem_st16(TM_O + slice + k, r);
         }
         tmem_st_wait();
@@ -321,13 +351,12 @@ gla_tc_walk_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       }
       if (c + 1 < count) arrive(e_h);
       if (c >= 0) {
-        exchange4(o, lane);
-        const Geom at = geom(c);
-        const int row = 32 * q + (lane & ~3);
-        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.o) + ((size_t)(at.tok0 + row) * p.HV + j) * 128 + 32 * g + 8 * (lane & 3);
+        uint8_t* row = sm + (kTiles * (c & 1) + 2) * kTileBytes + (g >> 1) * 16384 + i * 128;   // (P V is complete, and V of no more use)
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (row + k < at.L) *reinterpret_cast<uint4*>(dst + (size_t)k * p.HV * 128) = o[k];
+        for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(row + (((4 * (g & 1) + k) ^ (i & 7)) << 4)) = o[k];
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(put);
       }
     }
     float* dst = seg == p.nseg - 1 && p.last ? p.last + unit * 16384 : nullptr;
@@ -355,7 +384,7 @@ cudaError_t launch_tc_walk(const TcCall& t, cudaStream_t stream) {
   if (e == cudaSuccess && has.numRegs < kRegs) e = cudaErrorInvalidKernelImage;
   if (e == cudaSuccess) e = cudaFuncSetAttribute(gla_tc_walk_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
   const unsigned ctas = (unsigned)((size_t)c.p.N * c.p.HV * t.nseg);
-  return e != cudaSuccess ? e : start(gla_tc_walk_kernel, dim3(ctas), kRoleThreads, kSmem, stream, t.q, t.k, t.v, p);
+  return e != cudaSuccess ? e : start(gla_tc_walk_kernel, dim3(ctas), kRoleThreads, kSmem, stream, t.q, t.k, t.v, t.o, p);
 }
 
 }  // namespace gla
