@@ -175,6 +175,9 @@ struct Rows {
   __device__ __forceinline__ bool on(long long r) const {
     return SUB ? r - threadIdx.x / threads < rows : r < rows;
   }
+  // Is there such a row?  Of the `together` rows that are worked on at once the first always is, but in CTAs of short rows, which have places left over:
+  // all zeros, so that their scale is infinite with eps = 0, and zero times that must not get into a sum over rows.
+  __device__ __forceinline__ bool there(long long r, int together) const { return (!SUB && together == 1) || r < rows; }
   __device__ __forceinline__ int col(int i, int e) const { return VEC * (t + i * threads) - (FULL ? 0 : shift) + e; }
   __device__ __forceinline__ bool in(int i, int e) const { return FULL ? col(i, 0) < cols : (unsigned)col(i, e) < (unsigned)cols; }
   __device__ __forceinline__ bool any(int i) const { return FULL ? col(i, 0) < cols : col(i, VEC - 1) >= 0 && col(i, 0) < cols; }
@@ -465,7 +468,7 @@ __global__ void __launch_bounds__(THREADS == 257 ? 256 : THREADS, THREADS <= 257
       for (int i = 0; i < NV; ++i) {
         const Vec<VEC> t = mul(d[q][i], rs);
         at.store(p.dx, row + q * at.step, i, fma(t, w[i], mul(x[q][i], m)));
-        if (P == 1 || row + q * at.step < at.rows) dw[i] = fma(t, x[q][i], dw[i]);
+        if (at.there(row + q * at.step, P)) dw[i] = fma(t, x[q][i], dw[i]);
         if (p.z) at.store(p.dz, row + q * at.step, i, mul(slope[q][i], mul(x[q][i], rs)));
       }
     }
@@ -574,7 +577,7 @@ __global__ void __launch_bounds__(THREADS == 257 ? 256 : THREADS, THREADS <= 257
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const Vec<VEC> t = mul(d[q][i], rs);
-        if (P == 1 || row + q * at.step < at.rows) dw[i] = fma(t, r[q][i], dw[i]);
+        if (at.there(row + q * at.step, P)) dw[i] = fma(t, r[q][i], dw[i]);
         r[q][i] = fma(t, w[i], fma(r[q][i], m, g[q][i]));              // dr
         if (POST) u[q] = dot(mul(r[q][i], wp[i]), x[q][i], u[q]);
         at.store(p.dr, row + q * at.step, i, r[q][i]);
@@ -590,7 +593,7 @@ __global__ void __launch_bounds__(THREADS == 257 ? 256 : THREADS, THREADS <= 257
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           const Vec<VEC> t = mul(r[q][i], rx);
-          if (P == 1 || row + q * at.step < at.rows) dwp[i] = fma(t, x[q][i], dwp[i]);
+          if (at.there(row + q * at.step, P)) dwp[i] = fma(t, x[q][i], dwp[i]);
           at.store(p.dx, row + q * at.step, i, fma(t, wp[i], mul(x[q][i], mx)));
         }
       }
