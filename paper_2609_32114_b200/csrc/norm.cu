@@ -5,6 +5,8 @@
 //   add_norm     r' = r + s f,  f = x or x rx w_post;  y = r' rs w
 //     backward   with dn = dy w:  dr = dr' + rs (dn - r' rs^2 mean(dn r')),  dw = sum dy r' rs;  df = s dr, and with a norm behind the block
 //                dw_post = sum df x rx,  dx = rx (dm - x rx^2 mean(dm x)) with dm = df w_post
+// Grouped so that no value is of a higher power of the row's size than the first: dx = rs dn + (x rs) m with m = -(rs mean(dn x)) rs.  (rs^3 alone
+// leaves fp32 for rows of 1e13 and of 1e-13.)
 // Nothing is kept from the forward pass: the row is there anyway, so its norm costs no traffic.  The sums that do not wait for one another
 // go through one reduction (mean(dn x) is taken of x, not of x rs), so a row needs one, two with w_post.
 //
@@ -463,13 +465,13 @@ __global__ void __launch_bounds__(THREADS == 257 ? 256 : THREADS, THREADS <= 257
     turn ^= 1;
 #pragma unroll
     for (int q = 0; q < P; ++q) {
-      const float rs = rsqrtf(s[2 * q] / at.cols + p.eps), m = -rs * rs * rs * (s[2 * q + 1] / at.cols);
+      const float rs = rsqrtf(s[2 * q] / at.cols + p.eps), m = -(rs * (s[2 * q + 1] / at.cols)) * rs;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const Vec<VEC> t = mul(d[q][i], rs);
-        at.store(p.dx, row + q * at.step, i, fma(t, w[i], mul(x[q][i], m)));
+        const Vec<VEC> t = mul(d[q][i], rs), n = mul(x[q][i], rs);
+        at.store(p.dx, row + q * at.step, i, fma(t, w[i], mul(n, m)));
         if (at.there(row + q * at.step, P)) dw[i] = fma(t, x[q][i], dw[i]);
-        if (p.z) at.store(p.dz, row + q * at.step, i, mul(slope[q][i], mul(x[q][i], rs)));
+        if (p.z) at.store(p.dz, row + q * at.step, i, mul(slope[q][i], n));
       }
     }
   }
@@ -573,12 +575,12 @@ __global__ void __launch_bounds__(THREADS == 257 ? 256 : THREADS, THREADS <= 257
     row_sum<3 * P, SUB>(s, p.group, red[turn]);
 #pragma unroll
     for (int q = 0; q < P; ++q) {
-      const float rs = rsqrtf(s[3 * q] / at.cols + p.eps), m = -rs * rs * rs * (s[3 * q + 1] / at.cols);
+      const float rs = rsqrtf(s[3 * q] / at.cols + p.eps), m = -(rs * (s[3 * q + 1] / at.cols)) * rs;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const Vec<VEC> t = mul(d[q][i], rs);
         if (at.there(row + q * at.step, P)) dw[i] = fma(t, r[q][i], dw[i]);
-        r[q][i] = fma(t, w[i], fma(r[q][i], m, g[q][i]));              // dr
+        r[q][i] = fma(t, w[i], fma(mul(r[q][i], rs), m, g[q][i]));     // dr
         if (POST) u[q] = dot(mul(r[q][i], wp[i]), x[q][i], u[q]);
         at.store(p.dr, row + q * at.step, i, r[q][i]);
         r[q][i] = mul(r[q][i], p.scale);                               // df
@@ -589,12 +591,12 @@ __global__ void __launch_bounds__(THREADS == 257 ? 256 : THREADS, THREADS <= 257
       row_sum<P, SUB>(u, p.group, red1[turn]);
 #pragma unroll
       for (int q = 0; q < P; ++q) {
-        const float rx = rsqrtf(s[3 * q + 2] / at.cols + p.eps), mx = -rx * rx * rx * (p.scale * u[q] / at.cols);
+        const float rx = rsqrtf(s[3 * q + 2] / at.cols + p.eps), mx = -(rx * (p.scale * u[q] / at.cols)) * rx;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           const Vec<VEC> t = mul(r[q][i], rx);
           if (at.there(row + q * at.step, P)) dwp[i] = fma(t, x[q][i], dwp[i]);
-          at.store(p.dx, row + q * at.step, i, fma(t, wp[i], mul(x[q][i], mx)));
+          at.store(p.dx, row + q * at.step, i, fma(t, wp[i], mul(mul(x[q][i], rx), mx)));
         }
       }
     }
