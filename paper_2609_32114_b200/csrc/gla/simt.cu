@@ -567,7 +567,7 @@ cudaError_t launch_chain(const float* total, float* s, const float* first, int c
 }
 
 cudaError_t launch_head_sums(const Call& c, int parts, cudaStream_t stream) {
-  if (parts == c.p.HK) return cudaSuccess;
+  if (parts == c.p.HK || c.p.T_total == 0) return cudaSuccess;   // (empty sequences have chunk slots, but no token)
   SumParams p;
   p.dq = c.w.dq; p.dk = c.w.dk; p.out_q = c.a.dq; p.out_k = c.a.dk;
   p.n = (size_t)c.p.T_total * c.p.HK * c.p.dk; p.R = parts / c.p.HK; p.per_head = c.p.dk;
