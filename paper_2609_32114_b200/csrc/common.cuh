@@ -17,7 +17,7 @@ constexpr int kChunk = 64;
 struct PlanView {
   int32_t* hdr;         // [8]: hdr[0] = chunk slots in use, hdr[1] = sequences
   int32_t* seq_tok0;    // [N]   first token row of sequence n
-  int32_t* seq_len;     // [N]   tokens in sequence n (0 if the sequence failed a check)
+  int32_t* seq_len;     // [N]   tokens in sequence n (0 if it failed a check, or others did and the rest overlap)
   int32_t* seq_chunk0;  // [N+1] first chunk slot of sequence n (prefix sum)
   int32_t* seq_order;   // [N]   sequences by descending length (longest first), for launch order
   int32_t* chunk_seq;   // [MC]  sequence of chunk slot s

@@ -22,6 +22,7 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(PlanParams p, const int3
                                                    int32_t* status) {
   __shared__ int s_warp[kThreads / 32];
   __shared__ int s_carry;
+  __shared__ unsigned long long s_tokens;
   __shared__ int s_tok0[kOnChip], s_len[kOnChip], s_chunk0[kOnChip];
   const int tid = threadIdx.x;
   const bool on_chip = p.N <= kOnChip;
@@ -32,6 +33,7 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(PlanParams p, const int3
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // 1. per-sequence start and length, checked
+  bool bad = false;
   for (int n = tid; n < p.N; n += blockDim.x) {
     int t0, len;
     if (cu) {
@@ -40,6 +42,7 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(PlanParams p, const int3
       if (n == 0 && a != 0) ok = false;
       if (n == p.N - 1 && b != p.T_total) ok = false;
       if (!ok) report_status(status, HA_LA_ERR_DEVICE_CHECK);
+      bad |= !ok;
       t0 = ok ? a : 0;
       len = ok ? (b - a) : 0;
     } else {
@@ -53,8 +56,25 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(PlanParams p, const int3
       s_len[n] = len;
     }
   }
-  if (tid == 0) s_carry = 0;
-  __syncthreads();
+  if (tid == 0) {
+    s_carry = 0;
+    s_tokens = 0;
+  }
+  // Sequences that all pass lie one behind the other.  Where one does not, those that do may overlap, and hold more tokens than there are; then none
+  // is taken.  (So chunks and slots are as many as the callers' bound (T_total + (step - 1) N) / step says, and all tables agree.)
+  if (__syncthreads_or(bad)) {
+    unsigned long long mine = 0;
+    for (int n = tid; n < p.N; n += blockDim.x) mine += lens[n];
+    atomicAdd(&s_tokens, mine);
+    __syncthreads();
+    if (s_tokens > (unsigned long long)p.T_total) {
+      for (int n = tid; n < p.N; n += blockDim.x) {
+        v.seq_tok0[n] = v.seq_len[n] = 0;
+        if (on_chip) s_tok0[n] = s_len[n] = 0;
+      }
+    }
+    __syncthreads();
+  }
 
   // 1b. sequences by descending length (ties: by index), so that a kernel with one CTA per sequence can start
   // the longest ones first.  Rank by counting; beyond a few thousand sequences the order is left as it is
@@ -94,11 +114,7 @@ __global__ void __launch_bounds__(kThreads) plan_kernel(PlanParams p, const int3
     if (tid == blockDim.x - 1) s_carry = incl;
     __syncthreads();
   }
-  int total = s_carry;
-  if (total > p.max_chunks) {   // cannot happen for checked lengths; guard the table anyway
-    if (tid == 0) report_status(status, HA_LA_ERR_DEVICE_CHECK);
-    total = 0;
-  }
+  const int total = s_carry;
   if (tid == 0) {
     v.seq_chunk0[p.N] = total;
     v.hdr[0] = total;
