@@ -701,8 +701,11 @@ cudaError_t pick(Kind kind, const NormParams& p, int& ctas, int threads, cudaStr
   if constexpr (BACK) {
     if (kind == kGatedBack) k = gated_norm_back_kernel<In, VEC, NV, THREADS, FULL>;
     else k = p.w_post ? add_norm_back_kernel<In, VEC, NV, THREADS, FULL, true> : add_norm_back_kernel<In, VEC, NV, THREADS, FULL, false>;
-    smem = ahead_bytes(VEC, NV, threads, kind == kAddBack && p.w_post ? 4 : 3);
-    cudaError_t e = smem > 0 ? cudaFuncSetAttribute(reinterpret_cast<const void*>(k), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+    const int tensors = kind == kAddBack && p.w_post ? 4 : 3;
+    smem = ahead_bytes(VEC, NV, threads, tensors);
+    // (the kernel's most, whatever this call takes: another thread's call of another width may be between this and its launch)
+    const size_t most_smem = ahead_bytes(VEC, NV, THREADS == 257 ? 256 : THREADS, tensors);
+    cudaError_t e = smem > 0 ? cudaFuncSetAttribute(reinterpret_cast<const void*>(k), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most_smem) : cudaSuccess;
     int resident = 1;
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, k, threads, smem);
     if (e != cudaSuccess) return e;
