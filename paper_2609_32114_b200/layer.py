@@ -170,6 +170,19 @@ def _as(t, like, name, shape, dtype=None):
                          f"contiguous, on {like.device}")
 
 
+_INT32_MAX = 2 ** 31 - 1                                     # the structs' sizes are 32-bit; ctypes would cut a larger one down to its low bits
+
+
+def _sizes(t, name):
+    if any(n > _INT32_MAX for n in t.shape):
+        raise ValueError(f"{name}: {tuple(t.shape)}; a dimension has at most {_INT32_MAX}")
+
+
+def _bound(v):
+    """A bound on lengths: no sequence is longer than 32 bits count, so a larger one is that one."""
+    return max(-_INT32_MAX - 1, min(int(v), _INT32_MAX))
+
+
 def _float(v, name):
     v = float(v)
     if v != v:
@@ -234,6 +247,8 @@ def _gla_args(what, q, k, v, g, h0, cu_seqlens, max_seqlen, scale):
     if q.dim() not in (3, 4) or v.dim() != q.dim():
         raise ValueError(f"q: {tuple(q.shape)}, v: {tuple(v.shape)}; wanted are [B, T, heads, d] or [T, heads, d]")
     dtype = _element(q, "q")
+    _sizes(q, "q")
+    _sizes(v, "v")
     lead, (HK, d), HV = tuple(q.shape[:-2]), q.shape[-2:], v.shape[-2]
     B, T = lead if len(lead) == 2 else (1, lead[0])
     _as(q, q, "q", q.shape)
@@ -245,11 +260,12 @@ def _gla_args(what, q, k, v, g, h0, cu_seqlens, max_seqlen, scale):
         if B != 1 or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
             raise ValueError(f"cu_seqlens: {tuple(cu_seqlens.shape)} with q {tuple(q.shape)}; wanted are [N + 1], N >= 1, and a batch of one")
         _as(cu_seqlens, q, "cu_seqlens", cu_seqlens.shape, torch.int32)
+        _sizes(cu_seqlens, "cu_seqlens")
         N = cu_seqlens.numel() - 1
     _check_room("h0", h0, q, torch.float32, N * HV * d * d)
     args = ha_la_gla_args(dtype=dtype, batch=B, seqlen=T, num_qk_heads=HK, num_v_heads=HV, d_k=d, d_v=d, scale=_float(scale, "scale"),
                           q=_ptr(q), k=_ptr(k), v=_ptr(v), g=_ptr(g), h0=_ptr(h0), cu_seqlens=_ptr(cu_seqlens),
-                          num_seqs=0 if cu_seqlens is None else N, max_seqlen=int(max_seqlen))
+                          num_seqs=0 if cu_seqlens is None else N, max_seqlen=_bound(max_seqlen))
     return args, HV, d, N
 
 
@@ -344,6 +360,8 @@ def ha_la_gla_decode(q, k, v, g, state, *, scale=1.0, o=None, state_out=None, st
     _cuda(q, "ha_la_gla_decode")
     if q.dim() != 3 or v.dim() != 3:
         raise ValueError(f"q: {tuple(q.shape)}, v: {tuple(v.shape)}; wanted are [N, heads, d]")
+    _sizes(q, "q")
+    _sizes(v, "v")
     dtype, (N, HK, d), HV = _element(q, "q"), q.shape, v.shape[1]
     _as(q, q, "q", q.shape)
     _as(k, q, "k", (N, HK, d))
@@ -372,6 +390,8 @@ def _rows_of(what, x, w):
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError(f"x: {tuple(x.shape)}; wanted are rows of at least one value")
     dtype = _element(x, "x")
+    if x.shape[-1] > _INT32_MAX:
+        raise ValueError(f"x: {tuple(x.shape)}; a row has at most {_INT32_MAX} values")
     _as(x, x, "x", x.shape)
     _as(w, x, "w", (x.shape[-1],), torch.float32)
     return dtype, x.numel() // x.shape[-1], x.shape[-1]
