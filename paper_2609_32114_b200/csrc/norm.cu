@@ -734,11 +734,14 @@ cudaError_t by_length(Kind kind, const NormParams& p, const Shape& s, int& ctas,
     }
     return pick<In, VEC, 2, 1024, FULL, BACK>(kind, p, ctas, s.threads, stream);
   }
-  if (s.nv == 4) return pick<In, VEC, 4, 1024, FULL, BACK>(kind, p, ctas, s.threads, stream);   // (bf16, 16 bytes at a time: 2049 vectors are the most)
-  if constexpr (VEC <= 4) {
-    if (s.nv == 8) return pick<In, VEC, 8, 1024, FULL, BACK>(kind, p, ctas, s.threads, stream);   // (fp32: 4097)
+  constexpr int kMostVectors = kMaxCols / VEC + (FULL ? 0 : 1);
+  if constexpr (kMostVectors > 2 * 1024) {
+    if (s.nv == 4) return pick<In, VEC, 4, 1024, FULL, BACK>(kind, p, ctas, s.threads, stream);
   }
-  if constexpr (VEC == 1) return pick<In, VEC, 16, 1024, FULL, BACK>(kind, p, ctas, s.threads, stream);
+  if constexpr (kMostVectors > 4 * 1024) {
+    if (s.nv == 8) return pick<In, VEC, 8, 1024, FULL, BACK>(kind, p, ctas, s.threads, stream);
+  }
+  if constexpr (kMostVectors > 8 * 1024) return pick<In, VEC, 16, 1024, FULL, BACK>(kind, p, ctas, s.threads, stream);
   return cudaErrorInvalidValue;
 }
 
