@@ -250,9 +250,11 @@ int ha_la_decode(const ha_la_decode_args* args, void* cuda_stream);
  * prints no equations for them.)
  *
  * Evaluated by chunks: 64 tokens in fp32 (fp32 inputs, or d = 64), 128 on the tensor cores (bf16, d = 128).  Cumulative
- * log-gates are held in 64 bits.  States, dg and dh0 have fp32 accuracy on both paths (operands that go into a state are
- * split into two bf16 pieces); o, dq, dk and dv of the tensor-core path come of bf16 operands with fp32 sums.  Results are
- * the same bits from run to run: nothing is added atomically.
+ * log-gates are held in 64 bits.  States and dh0 have fp32 accuracy on both paths (operands that go into a state are
+ * split into two bf16 pieces); o, dq, dk and dv of the tensor-core path come of bf16 operands with fp32 sums.  dg has fp32
+ * accuracy but for what pairs of tokens inside a chunk add to it, which is a difference of sums over all of the chunk's
+ * pairs: up to 2^-18 of their magnitudes, however small dg itself is (where exp(g) = 0 that is what comes back for zero).
+ * Results are the same bits from run to run: nothing is added atomically.
  *
  * Conventions as for ha_la_prefill (device pointers, caller's stream, no allocation, no synchronisation, may be captured,
  * a workspace belongs to one call at a time).  The same log-gates: finite, <= 0 (very negative ones, that make exp(g)

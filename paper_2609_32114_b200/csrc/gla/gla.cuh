@@ -10,7 +10,9 @@
 //   dg_t = sum_{i >= t} x_i + sum_{j < t} y_j + e^{G_L} <h, dh> + sum_{i >= t > j} E_ij
 //     x_i = scale e^{G_i} q_i . (h do_i),  y_j = e^{G_L - G_j} k_j . (dh v_j),  E = scale S dS: all that goes from before token t to it or behind it
 // so that the states in front of (behind) all chunks are a scan of small matrices that each chunk makes by itself, and everything else is
-// chunk-local.  No term of dg is a difference of large ones but the sums over E, which are taken of the same fp32 values.
+// chunk-local.  No term of dg is a difference of large ones but the sums over E: sum over i >= t of (row i's sum - column i's sum), which
+// leaves the roundings of all of the chunk's pairs behind, up to 2^-18 of their magnitudes.  (On the tensor cores rows and columns are
+// sums of scores that were made separately.)
 #pragma once
 
 #include "common.cuh"

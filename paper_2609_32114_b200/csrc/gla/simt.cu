@@ -7,8 +7,10 @@
 //   gla_sum_kernel      dq, dk of q/k heads that several V-heads share, from their parts in order
 //
 // A product of a chunk is 64 rows by d (or 64) columns, 4 rows and every sixteenth column to a thread; the operands lie in shared memory with
-// rows padded by 4 floats, so that 16-byte reads of neighbouring rows hit different banks.  The fp32 multiply-adds and their shared-memory
-// reads bound it; the calls that come here are short.
+// rows padded by 4 floats, so that 16-byte reads of neighbouring rows hit different banks.  In calls of few chunks (`few`) the first and third kernel
+// give a CTA 16 rows, one to a thread, and four times the CTAs.  Reads of operands from shared memory and the fp32 multiply-adds bound it: eight rows of 600
+// tokens, 16 heads, d = 128: additions 83 us (shared memory's pipe 74 % busy, fp32 52 %), outputs 194 (60 %, 43 %), gradients 720 (one CTA of 256
+// threads to an SM: 50 %, 30 %).
 #include "gla.cuh"
 
 namespace ha_la {

@@ -2,8 +2,8 @@
 //
 // Steps of 128 tokens.  Tiles are [2][128 rows][64 columns] bf16, 32 KiB, rows of 128 bytes with the 128-byte swizzle: as TMA brings q, k, v and do
 // (rows = tokens), and as the state kernel writes the images of a state (rows = keys, columns = value channels).  Such a tile
-// is an operand either way round: K-major over its columns, MN-major over its rows.  What threads make (P, the scaled keys) goes to
-// tensor memory as A operand, so no thread writes shared memory that the tensor cores read, but for the rows behind the end of a sequence.
+// is an operand either way round: K-major over its columns, MN-major over its rows.  What threads make of P, dS and the scaled keys goes to
+// tensor memory as A operand; what they write to shared memory for the tensor cores is the walk's tile of the state, and zeros behind the end of a sequence.
 #pragma once
 
 #include <cuda.h>
@@ -164,12 +164,12 @@ struct Seqs {
 };
 
 struct TcWork {
-  uint8_t* image;                                          // [slot][V-head] states in front of the steps as tiles: bf16, backward two pieces
+  uint8_t* image;                                          // backward: [slot][V-head] states in front of the steps as tiles, two bf16 pieces
   uint8_t* image_back;                                     // ... gradients behind them
   float *part, *part_back;                                 // [sequence][segment][V-head] fp32 states
   float *total, *total_back;                               // ... and decays
-  float4* shared;                                          // ... and add up over V-heads
-  float* sums;                                             // backward: what the gradient kernel's CTAs pass on
+  float4* shared;                                          // backward: dq and dk that the gradient kernel's CTAs add up over a run's V-heads
+  float* sums;                                             // ... and what their warps pass on for dg
 };
 
 struct TcCall {

@@ -6,12 +6,13 @@
 //   dq: dS K, dO h^T    dk: dS^T Q, V dh^T    dv: P^T dO, K dh
 // The parts by the states are products of their own, for their rows are scaled by e^{G_i} (e^{G_L - G_j}) behind them, and because x_i and y_j, what
 // dg is a sum of, come of them alone: with h and dh as two bf16 pieces they keep the accuracy of fp32.  E = S dS is taken of the fp32
-// accumulators.  P and dS are rounded to bf16 for the products that give dq, dk and dv, which are rounded to bf16 anyway.
+// accumulators.  P and dS are rounded to bf16 for the products that give dq, dk and dv, and dv takes the first piece of dh alone, 2^-8 of it left out:
+// all three are rounded to bf16 anyway.
 //
 // Shared memory has seven slots for a unit's tiles: K, Q, dO, V, two pieces of h, two of dh.  V makes room for the second piece of dh once the scores are
 // made and is loaded again, out of L2, where the first piece of h was: so all pieces are there for <h, dh> while the products for dq run, and the slots come free
 // over the length of a unit, each for what is needed next.  (An SM gets some 32 bytes a cycle when all load, 1000 cycles for a tile.  With <h, dh> at the
-// end the last piece of dh and the next unit's K came 4000 cycles late each, of 25000 a unit.)  Tensor memory: four regions of 128 columns,
+// end the last piece of dh and the next unit's K came 4000 cycles late each, of 25000 a unit then; 20000 now.)  Tensor memory: four regions of 128 columns,
 //   R0: S, then dS | dq by h | dv by P      R1: dP | dq by dS | dk by dS      R2: S^T, then P^T | dv by dh      R3: dP^T, then dS^T | dk by dh
 // An operand lies over the scores that it is made of: a warp writes 16 columns of it, 8 words, over the first half of the 16 accumulator columns
 // that it alone has read, and a product's steps of 16 k go from one such place to the next.  So all four scores become operands in one phase, in which
@@ -19,7 +20,7 @@
 // One more warp scans the next unit's gates and another adds up dg; the sums over a row's columns, which four warps share, pass through a
 // few KiB of workspace that stay in L2.
 // What bounds it: 352 KiB of tiles, images and gradients a unit, and a unit's dependent phases.  2048 units (four rows of 4096
-// tokens, 16 heads): 150 us, 10.7 us a unit of an SM; 1104 pairs of units that share a q/k head 181 us.
+// tokens, 16 heads): 148 us, 10.7 us a unit of an SM; 1104 pairs of units that share a q/k head 181 us.
 #include "tc.cuh"
 
 namespace ha_la {

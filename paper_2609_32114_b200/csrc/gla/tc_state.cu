@@ -10,7 +10,7 @@
 // the state, so the next step's keys are scaled under this one's product, and the chain through the steps is one multiply-add.
 //
 // A step's image goes to shared memory as it will lie in memory, and one bulk copy of 64 KiB takes it out under the next step: four rows of 4096 tokens,
-// 16 heads, gradients and all 236 us, with stores of the warps (by way of shared memory, 64 bytes of eight rows at a time) 248.
+// 16 heads, 88 us, and 148 of the gradient kernel behind it; with stores of the warps (by way of shared memory, 64 bytes of eight rows at a time) 12 us more.
 // What bounds it: the tiles and images through HBM when many CTAs run (128 KiB a step), else for images what an SM stores, and for sums the
 // scaling warps' instructions (0.9 us a step).
 // Few (sequence, V-head) pairs are cut into segments: gla_combine_kernel (simt.cu) chains the sums.

@@ -12,7 +12,7 @@
 // so each product runs under what the threads do next, and nothing but q, k, v and o goes through HBM.
 // o goes out by a tensor store from where V lay, which is of no more use then; a last step of fewer tokens by plain stores.
 // What bounds it: a step's phases, 2.6 to 2.9 us: 12000 instructions of a warp, four at a time, and looking at seven barriers, some 200 cycles each.
-// HBM would allow 2.6 us with 128 CTAs (128 KiB a step): eight sequences of 7914 to 15654 tokens, 16 heads 355 us, 4.3 TB/s on the average.
+// HBM would allow 2.6 us with 128 CTAs (128 KiB a step): eight sequences of 7914 to 15654 tokens, 16 heads 365 us, 4.2 TB/s on the average.
 // Outputs as a kernel of their own over stored states took 573 us; eight more warps for o 388, the state's and the outputs' phases in different
 // warps 500 (seven warps to a scheduler, spills); 96 registers with 16 bytes of spills instead of 104 without + 10; o by exchanges between lanes and stores of
 // 64 bytes a row 376; o from where Q lay 486 (that slot is wanted a step sooner).

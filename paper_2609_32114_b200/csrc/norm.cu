@@ -10,7 +10,10 @@
 // Nothing is kept from the forward pass: the row is there anyway, so its norm costs no traffic.  The sums that do not wait for one another
 // go through one reduction (mean(dn x) is taken of x, not of x rs), so a row needs one, two with w_post.
 //
-// What bounds them is HBM, and latency in small calls.  A row lies in registers, 16 bytes of each tensor to a thread: rows of up to 32
+// What bounds them is HBM, and latency in small calls; in large bf16 ones HBM is busy for half of its cycles only.  Counters, 262144 rows of 128 and 16384 of 2048 with both norms:
+// forward 46 us (issue slots 68 % used, the pipe of exponentials and quotients 50 %) and 76 (the pipe of shared memory and exchanges 72 %, the sums of two
+// norms); backward 73 (issue 66 %) and 91 (61 %), by 16 warps of 122 to 128 registers on an SM, which wait for their own arithmetic more
+// than for loads.  fp32 moves twice the bytes by much the same instructions: 5.1 to 6.2 TB/s.  A row lies in registers, 16 bytes of each tensor to a thread: rows of up to 32
 // vectors are shared by 1, 2, 4 .. 32 neighbouring lanes, longer ones by a CTA.  A row that does not start on a 16-byte boundary is
 // read in aligned vectors all the same, with the neighbours' values at its ends masked: a group's rows are a multiple of 8 apart, so the
 // column that an element of a thread holds is the same in every row, weights stay in registers and so do the sums for dw, which
