@@ -320,7 +320,7 @@ int ha_la_gla_decode(const ha_la_decode_args* args, void* cuda_stream);
  * Otherwise outputs must not overlap inputs or each other.
  * The backward passes sum the weights' gradients over rows in a fixed order (the same bits from run to run) and need a
  * workspace; the forward passes need none and ignore it.                                          */
-typedef enum { HA_LA_ACT_SILU = 0, HA_LA_ACT_SIGMOID = 1 } ha_la_activation;
+typedef enum { HA_LA_ACT_SILU = 0, HA_LA_ACT_SIGMOID = 1, HA_LA_ACT_NONE = 2 /* ha_la_conv only */ } ha_la_activation;
 
 typedef struct {
   int32_t dtype;          /* ha_la_dtype of x, z, y, dy, dx, dz                              */
@@ -368,6 +368,108 @@ int ha_la_gated_norm_backward(const ha_la_gated_norm_args* args, void* cuda_stre
 int ha_la_add_norm_workspace_bytes(const ha_la_add_norm_args* args, size_t* out_bytes);       /* host only */
 int ha_la_add_norm(const ha_la_add_norm_args* args, void* cuda_stream);
 int ha_la_add_norm_backward(const ha_la_add_norm_args* args, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * The layers that alternate with the recurrences above in a hybrid model.  What holds for all of them:
+ *   - Conventions as for ha_la_prefill (device pointers, caller's stream, no allocation, no synchronisation, may be captured,
+ *     a workspace belongs to one call at a time, a status word that the caller zeroes).
+ *   - Sequences: B rows of `seqlen` tokens (cu_seqlens NULL), or num_seqs of them end to end with B = 1, as in
+ *     ha_la_prefill_args.  A sequence whose offsets do not fit is reported through the status word and its outputs are
+ *     unspecified; nothing is read or written out of range.  Sequences without a token are legal.
+ *   - A `*_stride` is the number of elements from a token to the next (rows of a wider tensor, such as a fused projection's
+ *     output); 0 stands for a contiguous tensor.  Inside a token everything is contiguous.
+ *   - Results are the same bits from run to run: nothing is added atomically.
+ *   - What a sequence holds never reaches another, NaN and infinities included.
+ *   - Outputs must not overlap inputs or each other unless it is said that they may.
+ *
+ * ha_la_conv: short causal convolution of every channel by itself, in front of a recurrence,
+ *     y_t = act(bias + sum_j w[j] x_{t - taps + 1 + j})            act = silu or none
+ *   with the taps - 1 inputs in front of a sequence from h0 (oldest first; NULL: zeros); hT: the last taps - 1 inputs, h0's
+ *   where the sequence is shorter than that.  ha_la_conv_backward: dx, dw, db (with bias), dh0 from dy and dhT; needs a
+ *   workspace (its size: ha_la_conv_workspace_bytes).  ha_la_conv_decode: one token for each of `batch` sequences (seqlen = 1);
+ *   hT may be exactly h0.
+ * All arithmetic fp32, rounded once at the end.  Tensors that are 16-byte aligned, with channels and strides that keep every
+ * token so, are read and written 16 bytes at a time, others element by element.                    */
+typedef struct {
+  int32_t dtype;          /* ha_la_dtype of x, y, h0, hT and their gradients                 */
+  int32_t batch;          /* B (ha_la_conv_decode: sequences)                                */
+  int32_t seqlen;
+  int32_t channels;       /* C >= 1                                                          */
+  int32_t taps;           /* 2, 3 or 4                                                       */
+  int32_t activation;     /* HA_LA_ACT_SILU or HA_LA_ACT_NONE                                */
+  int64_t x_stride;       /* 0 or >= C                                                       */
+  const void*  x;         /* [B, T, C]                                                       */
+  const float* w;         /* [C, taps]; the last one is the current token's                  */
+  const float* bias;      /* [C] or NULL                                                     */
+  const void*  h0;        /* [N, taps - 1, C] or NULL (zeros)                                */
+  const int32_t* cu_seqlens;
+  int32_t num_seqs;
+  int32_t max_seqlen;
+  void*   y;              /* forward: [B, T, C]                                              */
+  void*   hT;             /* forward: [N, taps - 1, C] or NULL (not wanted)                  */
+  const void*  dy;        /* backward: [B, T, C]                                             */
+  const void*  dhT;       /* backward: gradient of hT, or NULL (zeros)                       */
+  void*   dx;             /* backward: [B, T, C]                                             */
+  float*  dw;             /* backward: [C, taps]                                             */
+  float*  db;             /* backward: [C] or NULL (not wanted)                              */
+  void*   dh0;            /* backward: [N, taps - 1, C] or NULL (not wanted)                 */
+  void*   workspace;      /* backward: >= ha_la_conv_workspace_bytes(), 256-byte aligned     */
+  size_t  workspace_bytes;
+  int32_t* status_word;   /* optional                                                        */
+} ha_la_conv_args;
+
+int ha_la_conv_workspace_bytes(const ha_la_conv_args* args, size_t* out_bytes);   /* of the backward pass; host only */
+int ha_la_conv(const ha_la_conv_args* args, void* cuda_stream);
+int ha_la_conv_backward(const ha_la_conv_args* args, void* cuda_stream);
+int ha_la_conv_decode(const ha_la_conv_args* args, void* cuda_stream);
+
+/* Selective state space scan.  Per sequence and channel c (group j = c / (C / G)), with h (S states) starting at h0 or zero:
+ *     delta_t = softplus(dt_t + dt_bias)   (softplus = 0: dt_t + dt_bias)
+ *     h <- e^{delta_t A} h + delta_t B_t[j] x_t        y_t = (<C_t[j], h> + D x_t) silu(z_t)      hT = h after the last token
+ * D, z and dt_bias may be NULL (no such term).  All arithmetic fp32, y rounded once at the end, states fp32.
+ * ha_la_scan_backward: gradients of everything from dy and dhT; the forward pass's states are computed again.  dB and dC are
+ * sums over a group's channels, dA, dD and ddt_bias over all tokens.
+ * ha_la_scan_decode: one token for each of `batch` sequences (seqlen = 1), no workspace; hT may be exactly h0.
+ * hT may be exactly h0 in ha_la_scan too, and dh0 exactly dhT.
+ * What the inputs must satisfy: finite values, A <= 0, delta >= 0 (so with softplus = 0 dt + dt_bias >= 0).    */
+typedef struct {
+  int32_t dtype;          /* ha_la_dtype of x, dt, B, C, z, y and their gradients            */
+  int32_t batch;
+  int32_t seqlen;
+  int32_t channels;       /* >= 1                                                            */
+  int32_t states;         /* S, 1 .. 64                                                      */
+  int32_t groups;         /* G, divides channels                                             */
+  int32_t softplus;       /* 0 or 1                                                          */
+  int32_t num_seqs;
+  int32_t max_seqlen;
+  const int32_t* cu_seqlens;
+  int64_t x_stride, dt_stride, b_stride, c_stride, z_stride;
+  const void*  x;         /* [B, T, channels]                                                */
+  const void*  dt;        /* [B, T, channels]                                                */
+  const void*  B;         /* [B, T, G, S]                                                    */
+  const void*  C;         /* [B, T, G, S]                                                    */
+  const void*  z;         /* [B, T, channels] or NULL                                        */
+  const float* A;         /* [channels, S]                                                   */
+  const float* D;         /* [channels] or NULL                                              */
+  const float* dt_bias;   /* [channels] or NULL                                              */
+  const float* h0;        /* [N, channels, S] or NULL (zeros)                                */
+  void*   y;              /* forward: [B, T, channels]                                       */
+  float*  hT;             /* forward: [N, channels, S] or NULL (not wanted)                  */
+  const void*  dy;        /* backward: [B, T, channels]                                      */
+  const float* dhT;       /* backward: gradient of hT, or NULL (zeros)                       */
+  void   *dx, *ddt, *dB, *dC;   /* backward, contiguous                                      */
+  void*   dz;             /* backward, with z                                                */
+  float  *dA, *dD, *ddt_bias;   /* backward; dD with D, ddt_bias with dt_bias                */
+  float*  dh0;            /* backward: [N, channels, S] or NULL (not wanted)                 */
+  void*   workspace;      /* >= ha_la_scan_workspace_bytes(), 256-byte aligned               */
+  size_t  workspace_bytes;
+  int32_t* status_word;   /* optional                                                        */
+} ha_la_scan_args;
+
+int ha_la_scan_workspace_bytes(const ha_la_scan_args* args, int backward, size_t* out_bytes);   /* host only */
+int ha_la_scan(const ha_la_scan_args* args, void* cuda_stream);
+int ha_la_scan_backward(const ha_la_scan_args* args, void* cuda_stream);
+int ha_la_scan_decode(const ha_la_scan_args* args, void* cuda_stream);
 
 /* Test hook for the device-side bounded waits (the paper has no counterpart).  Every wait inside the
  * kernels is on an mbarrier; it gives up after a fixed number of polls, records HA_LA_ERR_TIMEOUT in

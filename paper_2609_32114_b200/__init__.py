@@ -47,3 +47,15 @@ from .layer import (  # noqa: F401
     ha_la_gla_prefill,
     ha_la_gla_workspace_bytes,
 )
+from .mixer import (  # noqa: F401
+    ha_la_conv,
+    ha_la_conv_args,
+    ha_la_conv_backward,
+    ha_la_conv_decode,
+    ha_la_conv_workspace_bytes,
+    ha_la_scan,
+    ha_la_scan_args,
+    ha_la_scan_backward,
+    ha_la_scan_decode,
+    ha_la_scan_workspace_bytes,
+)

@@ -46,6 +46,14 @@ EXPORTS = (
     "ha_la_add_norm_workspace_bytes",
     "ha_la_add_norm",
     "ha_la_add_norm_backward",
+    "ha_la_conv_workspace_bytes",
+    "ha_la_conv",
+    "ha_la_conv_backward",
+    "ha_la_conv_decode",
+    "ha_la_scan_workspace_bytes",
+    "ha_la_scan",
+    "ha_la_scan_backward",
+    "ha_la_scan_decode",
     "ha_la_debug_wait_timeout",
     "ha_la_status_string",
     "ha_la_version",
@@ -154,9 +162,10 @@ def load_library(path: Optional[str] = None):
     lib.ha_la_status_string.restype = ctypes.c_char_p
     lib.ha_la_version.argtypes = []
     lib.ha_la_version.restype = ctypes.c_int
-    from . import layer
+    from . import layer, mixer
 
     layer.declare(lib)
+    mixer.declare(lib)
     if path is None:
         _lib = lib
     return lib

@@ -25,7 +25,8 @@ UNITS = [("api", "api.cu", []), ("plan", "plan.cu", []), ("tc", "tc.cu", []), ("
          ("tc_walk", "tc_walk.cu", []), ("tc_span", "tc_span.cu", []),
          ("noalloc", "noalloc.cu", []), ("decode", "decode.cu", []), ("fp32_d64", "fp32_d64.cu", []),
          ("norm", "norm.cu", []), ("gla_api", "gla/api.cu", []), ("gla_decode", "gla/decode.cu", []), ("gla_simt", "gla/simt.cu", []),
-         ("gla_tc", "gla/tc.cu", []), ("gla_tc_state", "gla/tc_state.cu", []), ("gla_tc_walk", "gla/tc_walk.cu", []), ("gla_tc_back", "gla/tc_back.cu", [])] + [
+         ("gla_tc", "gla/tc.cu", []), ("gla_tc_state", "gla/tc_state.cu", []), ("gla_tc_walk", "gla/tc_walk.cu", []), ("gla_tc_back", "gla/tc_back.cu", []),
+         ("conv", "mix/conv.cu", []), ("scan", "mix/scan.cu", []), ("scan_back", "mix/scan_back.cu", [])] + [
     (f"simt{u}", "simt.cu", [f"-DHA_LA_SIMT_UNIT={u}"]) for u in range(5)
 ] + [
     (f"fp32_{u}", "fp32.cu", [f"-DHA_LA_FP32_UNIT={u}"]) for u in range(5)
@@ -39,7 +40,7 @@ def _nvcc() -> str:
 
 def _headers_mtime() -> float:
     t = os.path.getmtime(os.path.abspath(__file__))
-    for d in (CSRC, os.path.join(CSRC, "gla"), INCLUDE):
+    for d in (CSRC, os.path.join(CSRC, "gla"), os.path.join(CSRC, "mix"), INCLUDE):
         for f in os.listdir(d):
             if f.endswith((".cuh", ".h")):
                 t = max(t, os.path.getmtime(os.path.join(d, f)))

@@ -1,0 +1,521 @@
+// Selective scan forward and for one token; see scan.cuh for the formulas.
+//
+// A CTA has CH channels of a sequence (or of a segment of one) and goes through its tokens in order, 32 at a time.  Four warps hold the states, SP of them
+// and 32 / LS channels to a warp's lanes, and do nothing but the recurrence; four others make delta and delta x of the next 32 tokens (once a channel,
+// not once a state), bring B and C, and finish the outputs of the last 32.  What bounds it is the exponentials: 16 states are 16 of the 20
+// special-function results of a (token, channel).  So few channels are spread over all SMs by giving a thread fewer states (SP 4, 2, 1) first, and only then are
+// sequences cut into segments, whose states are made first, by all at once, at the price of every exponential twice.
+#include <algorithm>
+
+#include "scan.cuh"
+
+namespace ha_la {
+namespace mix {
+namespace {
+
+constexpr int kThreads = 256, kTile = 32;
+enum Mode { kOut, kEnds, kKeep };                          // outputs; states behind segments; states in front of every 8 tokens
+
+template <typename In, int SP, int LS, Mode M>
+__global__ void __launch_bounds__(kThreads, 2) scan_kernel(ScanParams p) {
+  constexpr int LC = 32 / LS, CH = 4 * LC, NP = SP * LS, E = CH / 4;      // channels of a warp, of the CTA; states; channels of a helping thread
+  constexpr int BC = kTile * NP / 128;                     // values of B (and C) that a helping thread brings
+  __shared__ __align__(16) float2 s_du[2][kTile][CH];
+  __shared__ __align__(16) float s_b[2][kTile][NP], s_c[2][M == kOut ? kTile : 1][NP];
+  __shared__ float s_y[M == kOut ? 2 : 1][M == kOut ? kTile : 1][CH];
+  __shared__ int s_n;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int nb = p.blocks * p.G, unit = blockIdx.x / nb, cb = blockIdx.x - unit * nb, group = cb / p.blocks;
+  const int c_in = (cb - group * p.blocks) * CH, left = min(CH, p.per_group - c_in), c0 = group * p.per_group + c_in;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (blockIdx.x == 0) check_seqs(p.seqs, p.status);
+  // which sequence, and which tokens of it
+  int n = unit, k = 0;
+  if (p.seg_log < 31) {
+    if (p.seqs.cu) {
+      if (warp == 0) {
+        const int f = find_seq(p.seqs, unit, p.seg_log, 1);
+        if (lane == 0) s_n = f;
+      }
+      __syncthreads();
+      n = s_n;
+    } else {
+      n = unit / p.segs;
+    }
+  }
+  const Seq q = seq_of(p.seqs, n);
+  if (q.len < 0) return;
+  const int slot0 = p.seg_log < 31 ? slot_of(p.seqs, n, q.tok0, p.seg_log, p.segs) : 0;
+  if (p.seg_log < 31) k = unit - slot0;
+  const int L = p.seg_log < 31 ? 1 << p.seg_log : q.len;
+  if (k < 0 || (k > 0 && (k > (q.len - 1) >> p.seg_log || p.seg_log == 31))) return;       // (a slot that no token falls to)
+  const int start = k * (p.seg_log < 31 ? L : 0), len = min(L, q.len - start), tok0 = q.tok0 + start;
+  if (M == kEnds && start + len >= q.len) {                // nobody asks for the state behind the last segment
+    if (k > 0 || !p.first) return;
+  }
+  const int tiles = (len + kTile - 1) / kTile;
+
+  if (warp < 4) {
+    const int c = warp * LC + lane % LC, s0 = lane / LC * SP, ch = c0 + c;
+    const bool mine = c < left;
+    float A[SP], h[SP];
+#pragma unroll
+    for (int s = 0; s < SP; ++s) {
+      A[s] = mine && s0 + s < p.S ? p.A[(size_t)ch * p.S + s0 + s] * kLog2e : 0.f;
+      h[s] = 0.f;
+    }
+    const size_t at = (size_t)ch * p.S + s0, state = (size_t)p.C * p.S;
+    const bool moved = M == kOut && p.first;               // (in place, and in segments: hT may be written already)
+    if (mine && k == 0) {
+      if (moved) {
+#pragma unroll
+        for (int s = 0; s < SP; ++s) h[s] = p.first[((size_t)n * p.C + ch) * NP + s0 + s];
+      } else if (p.h0) {
+#pragma unroll
+        for (int s = 0; s < SP; ++s)
+          if (s0 + s < p.S) h[s] = p.h0[n * state + at + s];
+      }
+      if (M == kEnds && p.first) {
+#pragma unroll
+        for (int s = 0; s < SP; ++s) p.first[((size_t)n * p.C + ch) * NP + s0 + s] = h[s];
+      }
+    } else if (mine && M == kOut) {                        // through the segments in front; segment 0's end has h0 in it
+#pragma unroll 4
+      for (int j = 0; j < k; ++j) {
+        const size_t sl = (size_t)(slot0 + j) * p.C + ch;
+        const float total = p.seg_delta[sl];
+        const Vec<SP> end = load_v<SP>(p.seg_h + sl * NP + s0);
+#pragma unroll
+        for (int s = 0; s < SP; ++s) h[s] = fmaf(ex2(A[s] * total), h[s], end.v[s]);
+      }
+    }
+    if (M == kEnds && start + len >= q.len) return;
+    float total = 0.f;
+    const int ck0 = M == kKeep ? slot_of(p.seqs, n, q.tok0, kCkptLog, (p.seqs.T_row + kCkpt - 1) / kCkpt) : 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i < tiles; ++i) {
+      const int b = i & 1;
+      float part = 0.f;
+#pragma unroll(LS >= 8 ? 1 : 2)
+      for (int t0 = 0; t0 < kTile; t0 += LS) {
+        float yv[LS];
+#pragma unroll
+        for (int j = 0; j < LS; ++j) {
+          if (M == kKeep && (LS <= kCkpt ? j == 0 && t0 % kCkpt == 0 : j % kCkpt == 0)) {
+            const int tk = i * kTile + t0 + j;
+            if (mine && tk < len) {
+              Vec<SP> now;
+#pragma unroll
+              for (int s = 0; s < SP; ++s) now.v[s] = h[s];
+              store_v<SP>(p.ckpt + ((size_t)(ck0 + (tk >> kCkptLog)) * p.C + ch) * NP + s0, now);
+            }
+          }
+          const float2 du = s_du[b][t0 + j][c];
+          const Vec<SP> bv = load_v<SP>(&s_b[b][t0 + j][s0]);
+          if (M == kEnds) part += du.x;
+          Vec<SP> cv;
+          if (M == kOut) cv = load_v<SP>(&s_c[b][t0 + j][s0]);
+          float y = 0.f;
+#pragma unroll
+          for (int s = 0; s < SP; ++s) {
+            h[s] = fmaf(ex2(du.x * A[s]), h[s], du.y * bv.v[s]);
+            if (M == kOut) y = fmaf(h[s], cv.v[s], y);
+          }
+          yv[j] = y;
+        }
+        if (M == kOut) {
+          spread_sum<LS, ilog2(LS)>(yv, 16);
+          s_y[b][t0 + lane / LC][c] = yv[0];
+        }
+      }
+      total += part;
+      __syncthreads();
+    }
+    if (mine) {
+      if (M == kEnds) {
+        const size_t sl = (size_t)(slot0 + k) * p.C + ch;
+#pragma unroll
+        for (int s = 0; s < SP; ++s) p.seg_h[sl * NP + s0 + s] = h[s];
+        if (s0 == 0) p.seg_delta[sl] = total;
+      } else if (M == kOut && p.hT && start + len >= q.len) {
+#pragma unroll
+        for (int s = 0; s < SP; ++s)
+          if (s0 + s < p.S) p.hT[n * state + at + s] = h[s];
+      }
+    }
+    return;
+  }
+
+  // ---- the helping warps
+  if (M == kEnds && start + len >= q.len) return;
+  const int ht = tid - 128, row = ht / 4, c = ht % 4 * E, have = left - c;     // a token and E channels
+  const bool vec = p.vec;
+  const In *x = reinterpret_cast<const In*>(p.x) + c0 + c, *dt = reinterpret_cast<const In*>(p.dt) + c0 + c;
+  const In *B = reinterpret_cast<const In*>(p.B) + (size_t)group * p.S, *C = reinterpret_cast<const In*>(p.C_) + (size_t)group * p.S;
+  const In* z = reinterpret_cast<const In*>(p.z) + c0 + c;
+  Vec<E> bias = {}, skip = {};
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (p.dt_bias && e < have) bias.v[e] = p.dt_bias[c0 + c + e];
+    if (M == kOut && p.D && e < have) skip.v[e] = p.D[c0 + c + e];
+  }
+  Vec<E> vx = {}, vd = {};
+  float vb[BC], vc[M == kOut ? BC : 1];
+  auto fetch = [&](int i) {                                // tile i's rows on their way
+    const int t = i * kTile + row;
+    if (t < len) {
+      vx = load_row<In, E>(x + (size_t)(tok0 + t) * p.xs, vec, have);
+      vd = load_row<In, E>(dt + (size_t)(tok0 + t) * p.dts, vec, have);
+    }
+#pragma unroll
+    for (int j = 0; j < BC; ++j) {
+      const int f = j * 128 + ht, r = i * kTile + f / NP, s = f % NP;
+      const bool ok = r < len && s < p.S;
+      vb[j] = ok ? to_f32(B[(size_t)(tok0 + r) * p.bs + s]) : 0.f;
+      if (M == kOut) vc[j] = ok ? to_f32(C[(size_t)(tok0 + r) * p.cs + s]) : 0.f;
+    }
+  };
+  auto put = [&](int i) {                                  // ... in shared memory, as the other warps take them
+    const int b = i & 1;
+    const bool ok = i * kTile + row < len;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float v = vd.v[e] + bias.v[e], delta = ok && e < have ? (p.softplus ? softplus(v) : v) : 0.f;
+      s_du[b][row][c + e] = make_float2(delta, ok && e < have ? delta * vx.v[e] : 0.f);
+    }
+#pragma unroll
+    for (int j = 0; j < BC; ++j) {
+      const int f = j * 128 + ht;
+      s_b[b][f / NP][f % NP] = vb[j];
+      if (M == kOut) s_c[b][f / NP][f % NP] = vc[j];
+    }
+  };
+  auto finish = [&](int i, const Vec<E>& xi, const Vec<E>& zi) {
+    const int t = i * kTile + row;
+    if (t >= len) return;
+    Vec<E> y;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      y.v[e] = fmaf(skip.v[e], xi.v[e], s_y[i & 1][row][c + e]);
+      if (p.z) y.v[e] *= zi.v[e] * sigmoid(zi.v[e]);
+    }
+    store_row<In, E>(reinterpret_cast<In*>(p.y) + (size_t)(tok0 + t) * p.C + c0 + c, vec, have, y);
+  };
+  if (tiles > 0) {
+    fetch(0);
+    put(0);
+    if (tiles > 1) fetch(1);
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int i = 0; i <= tiles; ++i) {
+    Vec<E> xi = {}, zi = {};
+    if (M == kOut && i > 0) {
+      const int t = (i - 1) * kTile + row;
+      if (t < len) {
+        if (p.D) xi = load_row<In, E>(x + (size_t)(tok0 + t) * p.xs, vec, have);
+        if (p.z) zi = load_row<In, E>(z + (size_t)(tok0 + t) * p.zs, vec, have);
+      }
+    }
+    if (i + 1 < tiles) {
+      put(i + 1);
+      if (i + 2 < tiles) fetch(i + 2);
+    }
+    if (M == kOut && i > 0) finish(i - 1, xi, zi);
+    if (i < tiles) __syncthreads();
+  }
+}
+
+// One token: a state is read and written once, so HBM bounds it (8 S bytes a channel).  LS lanes to a channel, four states each; a thread
+// takes its channel of several sequences, whose states are on their way together, with one look at A.
+template <typename In, int LS, bool VEC>
+__global__ void __launch_bounds__(128) scan_decode_kernel(ScanParams p) {
+  constexpr int LC = 32 / LS, U = 4;
+  const int lane = threadIdx.x & 31, s0 = lane / LC * 4;
+  const int c = (blockIdx.x * 4 + (threadIdx.x >> 5)) * LC + lane % LC, ch = min(c, p.C - 1), group = ch / p.per_group;
+  const bool mine = c < p.C;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const size_t state = (size_t)p.C * p.S, at = (size_t)ch * p.S + s0;
+  auto four = [&](const float* a) {
+    Vec<4> r = {};
+    if (VEC) {
+      const float4 w = __ldcs(reinterpret_cast<const float4*>(a));
+      r.v[0] = w.x; r.v[1] = w.y; r.v[2] = w.z; r.v[3] = w.w;
+    } else {
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        if (s0 + s < p.S) r.v[s] = a[s];
+    }
+    return r;
+  };
+  const Vec<4> A = VEC ? load_v<4>(p.A + at) : four(p.A + at);
+  const float bias = p.dt_bias ? p.dt_bias[ch] : 0.f, skip = p.D ? p.D[ch] : 0.f;
+  for (int n0 = blockIdx.y * U; n0 < p.seqs.N; n0 += gridDim.y * U) {
+    Vec<4> h[U] = {};
+    float x[U], dt[U], z[U];
+    Vec<4> b[U], cc[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (n0 + i < p.seqs.N && p.h0) h[i] = four(p.h0 + (n0 + i) * state + at);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int n = min(n0 + i, p.seqs.N - 1);
+      x[i] = to_f32(reinterpret_cast<const In*>(p.x)[n * p.xs + ch]);
+      dt[i] = to_f32(reinterpret_cast<const In*>(p.dt)[n * p.dts + ch]);
+      z[i] = p.z ? to_f32(reinterpret_cast<const In*>(p.z)[n * p.zs + ch]) : 0.f;
+      const In *B = reinterpret_cast<const In*>(p.B) + n * p.bs + (size_t)group * p.S + s0, *C = reinterpret_cast<const In*>(p.C_) + n * p.cs + (size_t)group * p.S + s0;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        b[i].v[s] = s0 + s < p.S ? to_f32(B[s]) : 0.f;
+        cc[i].v[s] = s0 + s < p.S ? to_f32(C[s]) : 0.f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const float v = dt[i] + bias, delta = p.softplus ? softplus(v) : v, u = delta * x[i];
+      float y = 0.f;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        h[i].v[s] = fmaf(ex2(delta * A.v[s] * kLog2e), h[i].v[s], u * b[i].v[s]);
+        y = fmaf(h[i].v[s], cc[i].v[s], y);
+      }
+#pragma unroll
+      for (int off = 16; off >= LC; off >>= 1) y += __shfl_xor_sync(0xffffffffu, y, off);
+      if (!mine || n0 + i >= p.seqs.N) continue;
+      float* o = p.hT + (n0 + i) * state + at;
+      if (VEC) {
+        __stcs(reinterpret_cast<float4*>(o), make_float4(h[i].v[0], h[i].v[1], h[i].v[2], h[i].v[3]));
+      } else {
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+          if (s0 + s < p.S) o[s] = h[i].v[s];
+      }
+      if (s0 == 0) {
+        y = fmaf(skip, x[i], y);
+        if (p.z) y *= z[i] * sigmoid(z[i]);
+        reinterpret_cast<In*>(p.y)[(size_t)(n0 + i) * p.C + ch] = from_f32<In>(y);
+      }
+    }
+  }
+}
+
+int padded(int S) { return S <= 16 ? 16 : S <= 32 ? 32 : 64; }
+
+struct Shape { int sp, ls, ch; };
+
+// States to a thread.  A CTA's four recurrence warps take one scheduler each, so what counts is how many CTAs there are to an SM: the most
+// states to a thread (the fewest shared-memory reads and sums a value) that still gives every SM one.
+Shape shape_of(int S, long long rows, int per_group, int G) {
+  const int np = padded(S);
+  Shape last = {};
+  for (int sp = np == 64 ? 8 : np == 32 ? 8 : 4; sp >= np / 16; sp /= 2) {
+    const int ls = np / sp, ch = 128 / ls;
+    last = {sp, ls, ch};
+    if (rows * ((per_group + ch - 1) / ch) * G >= sm_count()) break;
+  }
+  return last;
+}
+
+// Segments: tokens to one, by its logarithm, or 31.  Two passes over the tokens and a launch more have to pay.
+int segment_log(const ScanParams& p, const Shape& s) {
+  const long long ctas = (long long)p.seqs.N * ((p.per_group + s.ch - 1) / s.ch) * p.G;
+  const int longest = p.seqs.max_len;
+  if (ctas * 4 > sm_count() || longest < 512) return 31;
+  int log = 7;
+  while (((long long)1 << log) * sm_count() < ctas * longest && log < 30) ++log;
+  return ((long long)2 << log) * 2 <= longest ? log : 31;
+}
+
+template <typename In, int SP, int LS> cudaError_t launch(Mode m, const ScanParams& p, long long units, cudaStream_t stream) {
+  const long long grid = units * p.blocks * p.G;
+  if (grid == 0) return cudaSuccess;
+  void (*k)(ScanParams) = m == kOut ? scan_kernel<In, SP, LS, kOut> : m == kEnds ? scan_kernel<In, SP, LS, kEnds> : scan_kernel<In, SP, LS, kKeep>;
+  return start(k, dim3((unsigned)grid), kThreads, 0, stream, p);
+}
+
+template <typename In> cudaError_t launch_shape(Mode m, const Shape& s, const ScanParams& p, long long units, cudaStream_t stream) {
+  switch (s.sp * 100 + s.ls) {
+    case 404: return launch<In, 4, 4>(m, p, units, stream);
+    case 208: return launch<In, 2, 8>(m, p, units, stream);
+    case 116: return launch<In, 1, 16>(m, p, units, stream);
+    case 804: return launch<In, 8, 4>(m, p, units, stream);
+    case 408: return launch<In, 4, 8>(m, p, units, stream);
+    case 216: return launch<In, 2, 16>(m, p, units, stream);
+    case 808: return launch<In, 8, 8>(m, p, units, stream);
+    default: return launch<In, 4, 16>(m, p, units, stream);
+  }
+}
+
+int check(const ha_la_scan_args* a, ScanParams* p, bool token) {
+  if (!a) return HA_LA_ERR_INVALID_ARG;
+  if (a->dtype != HA_LA_BF16 && a->dtype != HA_LA_FP32) return HA_LA_ERR_INVALID_ARG;
+  if (a->batch < (token ? 0 : 1) || a->channels < 1 || a->groups < 1 || a->states < 1 || a->channels % a->groups) return HA_LA_ERR_INVALID_ARG;
+  if (a->softplus != 0 && a->softplus != 1) return HA_LA_ERR_INVALID_ARG;
+  if (a->states > 64 || a->channels > (1 << 24)) return HA_LA_ERR_UNSUPPORTED;
+  *p = ScanParams{};
+  if (!make_seqs(&p->seqs, a->cu_seqlens, a->batch, a->seqlen, token ? 0 : a->num_seqs, a->max_seqlen)) return HA_LA_ERR_INVALID_ARG;
+  if ((long long)a->batch * a->seqlen > 0x7fffffffLL - 256) return HA_LA_ERR_UNSUPPORTED;
+  const long long gs = (long long)a->groups * a->states;
+  p->C = a->channels; p->S = a->states; p->G = a->groups; p->per_group = a->channels / a->groups;
+  p->softplus = a->softplus;
+  p->packed = !token && (a->cu_seqlens || a->num_seqs > 0);
+  auto stride = [&](int64_t given, long long own, long long* out) {
+    *out = given ? given : own;
+    return given == 0 || given >= own;
+  };
+  if (!stride(a->x_stride, p->C, &p->xs) || !stride(a->dt_stride, p->C, &p->dts) || !stride(a->z_stride, p->C, &p->zs) ||
+      !stride(a->b_stride, gs, &p->bs) || !stride(a->c_stride, gs, &p->cs))
+    return HA_LA_ERR_INVALID_ARG;
+  p->x = a->x; p->dt = a->dt; p->B = a->B; p->C_ = a->C; p->z = a->z; p->dy = a->dy;
+  p->A = a->A; p->D = a->D; p->dt_bias = a->dt_bias; p->h0 = a->h0; p->dhT = a->dhT;
+  p->y = a->y; p->dx = a->dx; p->ddt = a->ddt; p->dz = a->dz; p->hT = a->hT; p->dh0 = a->dh0;
+  p->status = a->status_word;
+  p->seg_log = 31;
+  return HA_LA_OK;
+}
+
+// Sizes of a forward call: shape, segments, slots.
+struct Plan { Shape s; long long units; size_t bytes; };
+
+Plan forward_plan(ScanParams* p) {
+  Plan f = {};
+  f.s = shape_of(p->S, p->seqs.N, p->per_group, p->G);
+  p->blocks = (p->per_group + f.s.ch - 1) / f.s.ch;
+  p->seg_log = segment_log(*p, f.s);
+  p->segs = 1;
+  f.units = p->seqs.N;
+  if (p->seg_log < 31) {
+    const int L = 1 << p->seg_log;
+    p->segs = (p->seqs.T_row + L - 1) / L;
+    f.units = p->packed ? (long long)(p->seqs.T_total >> p->seg_log) + p->seqs.N : (long long)p->seqs.N * p->segs;
+    const size_t np = padded(p->S);
+    f.bytes = align_up((size_t)f.units * p->C * (np + 1) * 4, 256) + align_up((size_t)p->seqs.N * p->C * np * 4, 256);
+  }
+  if (f.bytes == 0) f.bytes = 256;
+  return f;
+}
+
+bool aligned_rows(const ha_la_scan_args* a, const ScanParams& p, bool back) {
+  const int e = a->dtype == HA_LA_BF16 ? 2 : 4;
+  uintptr_t at = any_of(a->x, a->dt, a->z);
+  at |= back ? any_of(a->dy, a->dx, a->ddt, a->dz) : any_of(a->y);
+  const long long steps = p.xs | p.dts | p.C | (a->z ? p.zs : 0) | (p.G > 1 ? p.per_group : 0);
+  return at % 16 == 0 && steps * e % 16 == 0;
+}
+
+}  // namespace
+
+// What the backward pass takes of the forward one: states in front of every eight tokens.
+cudaError_t launch_scan_keep(bool bf16, ScanParams p, cudaStream_t stream) {
+  p.seg_log = 31;
+  const Shape s = shape_of(p.S, p.seqs.N, p.per_group, p.G);
+  p.blocks = (p.per_group + s.ch - 1) / s.ch;
+  return bf16 ? launch_shape<__nv_bfloat16>(kKeep, s, p, p.seqs.N, stream) : launch_shape<float>(kKeep, s, p, p.seqs.N, stream);
+}
+cudaError_t launch_scan_back(bool bf16, ScanParams p, int padded_states, const ha_la_scan_args& a, cudaStream_t stream);   // scan_back.cu
+int scan_back_channels(int padded_states);
+
+namespace {
+
+size_t backward_bytes(ScanParams* p) {
+  const size_t np = padded(p->S), ch = scan_back_channels((int)np), blocks = (p->per_group + ch - 1) / ch * p->G, T = p->seqs.T_total;
+  const size_t slots = (T >> kCkptLog) + p->seqs.N + 1;
+  p->blocks = (int)(blocks / p->G);
+  return align_up(slots * p->C * np * 4, 256) + align_up(blocks * T * 2 * np * 4, 256) + align_up((size_t)p->seqs.N * p->C * p->S * 4, 256) +
+         align_up((size_t)p->seqs.N * p->C * 2 * 4, 256) + 256;
+}
+
+int run(const ha_la_scan_args* a, bool back, cudaStream_t stream) {
+  ScanParams p;
+  const int rc = check(a, &p, false);
+  if (rc != HA_LA_OK) return rc;
+  if (a->num_seqs > 0 && !a->cu_seqlens) return HA_LA_ERR_INVALID_ARG;
+  const bool bf16 = a->dtype == HA_LA_BF16;
+  if (any_of(a->x, a->dt, a->B, a->C, a->z, a->y, a->dy, a->dx, a->ddt, a->dB, a->dC, a->dz) & (bf16 ? 1 : 3)) return HA_LA_ERR_INVALID_ARG;
+  if (any_of(a->A, a->D, a->dt_bias, a->h0, a->hT, a->dhT, a->dA, a->dD, a->ddt_bias, a->dh0, a->cu_seqlens, a->status_word) & 3) return HA_LA_ERR_INVALID_ARG;
+  if (!a->A) return HA_LA_ERR_INVALID_ARG;
+  if (p.seqs.T_total > 0 && (!a->x || !a->dt || !a->B || !a->C)) return HA_LA_ERR_INVALID_ARG;
+  if (p.seqs.T_total > 0 && (back ? !a->dy || !a->dx || !a->ddt || !a->dB || !a->dC || (a->z && !a->dz) : !a->y)) return HA_LA_ERR_INVALID_ARG;
+  if (back && (!a->dA || (a->D && !a->dD) || (a->dt_bias && !a->ddt_bias))) return HA_LA_ERR_INVALID_ARG;
+  p.vec = aligned_rows(a, p, back);
+  if (!a->workspace || ((uintptr_t)a->workspace & 255)) return HA_LA_ERR_WORKSPACE;
+  char* ws = reinterpret_cast<char*>(a->workspace);
+  if (back) {
+    if (a->workspace_bytes < backward_bytes(&p)) return HA_LA_ERR_WORKSPACE;
+    const size_t np = padded(p.S), T = p.seqs.T_total, slots = (T >> kCkptLog) + p.seqs.N + 1;
+    // (rows: a row's first slot is its number times the slots of a row, at most one more than its tokens / 8)
+    const int back_blocks = p.blocks;
+    p.ckpt = reinterpret_cast<float*>(ws); ws += align_up(slots * p.C * np * 4, 256);
+    p.part_bc = reinterpret_cast<float*>(ws); ws += align_up((size_t)back_blocks * p.G * T * 2 * np * 4, 256);
+    p.part_a = reinterpret_cast<float*>(ws); ws += align_up((size_t)p.seqs.N * p.C * p.S * 4, 256);
+    p.part_d = reinterpret_cast<float*>(ws);
+    if ((long long)p.seqs.N * p.C > 0x7fffffffLL || (long long)T * p.G > 0x7fffffffLL / 2) return HA_LA_ERR_UNSUPPORTED;
+    cudaError_t e = launch_scan_keep(bf16, p, stream);
+    p.blocks = back_blocks;
+    if (e == cudaSuccess) e = launch_scan_back(bf16, p, (int)np, *a, stream);
+    return e == cudaSuccess ? HA_LA_OK : HA_LA_ERR_CUDA;
+  }
+  const Plan f = forward_plan(&p);
+  if (a->workspace_bytes < f.bytes) return HA_LA_ERR_WORKSPACE;
+  if (f.units * p.blocks * p.G > 0x7fffffffLL) return HA_LA_ERR_UNSUPPORTED;
+  cudaError_t e = cudaSuccess;
+  if (p.seg_log < 31) {
+    const size_t np = padded(p.S);
+    p.seg_h = reinterpret_cast<float*>(ws);
+    p.seg_delta = p.seg_h + (size_t)f.units * p.C * np;
+    if (p.hT && p.hT == p.h0) p.first = reinterpret_cast<float*>(ws + align_up((size_t)f.units * p.C * (np + 1) * 4, 256));
+    e = bf16 ? launch_shape<__nv_bfloat16>(kEnds, f.s, p, f.units, stream) : launch_shape<float>(kEnds, f.s, p, f.units, stream);
+  }
+  if (e == cudaSuccess) e = bf16 ? launch_shape<__nv_bfloat16>(kOut, f.s, p, f.units, stream) : launch_shape<float>(kOut, f.s, p, f.units, stream);
+  return e == cudaSuccess ? HA_LA_OK : HA_LA_ERR_CUDA;
+}
+
+template <typename In> cudaError_t launch_decode(const ScanParams& p, bool vec, cudaStream_t stream) {
+  const int ls = padded(p.S) / 4, per_cta = 4 * (32 / ls);
+  const int gx = (p.C + per_cta - 1) / per_cta, n4 = (p.seqs.N + 3) / 4;
+  const int gy = std::min(n4, std::max(1, sm_count() * 16 / gx));          // (16 CTAs of 128 threads an SM)
+  void (*k)(ScanParams) = ls == 4 ? (vec ? scan_decode_kernel<In, 4, true> : scan_decode_kernel<In, 4, false>)
+                        : ls == 8 ? (vec ? scan_decode_kernel<In, 8, true> : scan_decode_kernel<In, 8, false>)
+                                  : (vec ? scan_decode_kernel<In, 16, true> : scan_decode_kernel<In, 16, false>);
+  return start(k, dim3((unsigned)gx, (unsigned)std::min(gy, 65535)), 128, 0, stream, p);
+}
+
+}  // namespace
+}  // namespace mix
+}  // namespace ha_la
+
+using namespace ha_la;
+
+extern "C" {
+
+int ha_la_scan_workspace_bytes(const ha_la_scan_args* a, int backward, size_t* out_bytes) {
+  if (!out_bytes) return HA_LA_ERR_INVALID_ARG;
+  mix::ScanParams p;
+  const int rc = mix::check(a, &p, false);
+  if (rc != HA_LA_OK) return rc;
+  *out_bytes = backward ? mix::backward_bytes(&p) : mix::forward_plan(&p).bytes;
+  return HA_LA_OK;
+}
+int ha_la_scan(const ha_la_scan_args* a, void* s) { return mix::run(a, false, reinterpret_cast<cudaStream_t>(s)); }
+int ha_la_scan_backward(const ha_la_scan_args* a, void* s) { return mix::run(a, true, reinterpret_cast<cudaStream_t>(s)); }
+
+int ha_la_scan_decode(const ha_la_scan_args* a, void* cuda_stream) {
+  mix::ScanParams p;
+  const int rc = mix::check(a, &p, true);
+  if (rc != HA_LA_OK) return rc;
+  if (a->seqlen != 1 || a->cu_seqlens || a->num_seqs) return HA_LA_ERR_INVALID_ARG;
+  if (p.seqs.N == 0) return HA_LA_OK;
+  const bool bf16 = a->dtype == HA_LA_BF16;
+  if (!a->x || !a->dt || !a->A || !a->B || !a->C || !a->y || !a->hT) return HA_LA_ERR_INVALID_ARG;
+  if (mix::any_of(a->x, a->dt, a->B, a->C, a->z, a->y) & (bf16 ? 1 : 3)) return HA_LA_ERR_INVALID_ARG;
+  if (mix::any_of(a->A, a->D, a->dt_bias, a->h0, a->hT) & 3) return HA_LA_ERR_INVALID_ARG;
+  const bool vec = p.S == mix::padded(p.S) && mix::any_of(a->A, a->h0, a->hT) % 16 == 0;
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = bf16 ? mix::launch_decode<__nv_bfloat16>(p, vec, stream) : mix::launch_decode<float>(p, vec, stream);
+  return e == cudaSuccess ? HA_LA_OK : HA_LA_ERR_CUDA;
+}
+
+}  // extern "C"
