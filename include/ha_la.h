@@ -471,6 +471,77 @@ int ha_la_scan(const ha_la_scan_args* args, void* cuda_stream);
 int ha_la_scan_backward(const ha_la_scan_args* args, void* cuda_stream);
 int ha_la_scan_decode(const ha_la_scan_args* args, void* cuda_stream);
 
+/* Attention whose keys and values come of one latent vector a token, for the layers of a hybrid model that look at every token.
+ *
+ * ha_la_latent_prefill, for prompts, on expanded keys and values.  Head h of token i of a sequence:
+ *     s_ij = scale (q_i[h][0 .. d_nope) . kn_j[h] + q_i[h][d_nope ..] . kr_j)      o_i[h] = sum_j softmax_j(s_ij) v_j[h]
+ *   over the keys j <= i + (keys - queries) of the sequence: the queries are its last tokens.  kr is shared by all heads.
+ * ha_la_latent_decode, for one or a few new tokens a sequence, absorbed: the expanding products are in q already and what the
+ *   output still needs of them is applied to o, so all heads attend to the cached rows c_j [d_latent + d_rope] themselves,
+ *     s_ij = scale q_i[h] . c_j        o_i[h] = sum_j softmax_j(s_ij) c_j[0 .. d_latent)
+ *   The cache is in pages; row j of sequence n is row j % page_size of page page_table[n][j / page_size].  lengths[n] counts the
+ *   sequence's cached rows, those of the new tokens, its last ones, among them; a new token sees the rows up to its own.
+ * lse = log sum_j e^{s_ij} (natural), for joining results over parts of the keys; NULL: not wanted.  A row that sees no key has
+ * o = 0 and lse = -infinity.  What no row of a sequence sees (the rest of its last page, other pages) may hold anything, NaN included.
+ * A length that is negative or longer than its row of the table counts as zero and is reported through the status word, as is a
+ * page that does not exist, whose sequence's results are unspecified.
+ * Scores, their sums and o's sums are fp32; with bf16 tensors the weights are rounded to bf16 for the product with the values.
+ * Tensor cores: bf16 with d_nope = 128, d_rope = 64, d_v = 128, 16-byte aligned with strides that are multiples of 8;
+ * decode bf16 with d_latent = 512, d_rope = 64, 16-byte aligned.  Everything else runs on the CUDA cores, much slower.    */
+typedef struct {
+  int32_t dtype;          /* ha_la_dtype of q, kn, kr, v, o                                  */
+  int32_t batch;          /* B; must be 1 when cu_seqlens != NULL                            */
+  int32_t seqlen;         /* queries per row (packed: in all)                                */
+  int32_t seqlen_k;       /* keys per row (packed: in all)                                   */
+  int32_t num_heads;
+  int32_t d_nope;         /* 1 .. 256                                                        */
+  int32_t d_rope;         /* 0 .. 128                                                        */
+  int32_t d_v;            /* 1 .. 256                                                        */
+  float   scale;
+  int32_t num_seqs;       /* packed sequences, or 0                                          */
+  int32_t max_seqlen;     /* packed: bound on a sequence's queries (sizes the launch); 0: seqlen */
+  const int32_t* cu_seqlens;     /* [N + 1] offsets of queries, or NULL                      */
+  const int32_t* cu_seqlens_k;   /* [N + 1] offsets of keys; with cu_seqlens                 */
+  int64_t q_stride, kn_stride, kr_stride, v_stride;   /* elements from a token to the next   */
+  int64_t kn_head_stride, v_head_stride;              /* ... from a head to the next; tokens and heads may lie either way round */
+  const void*  q;         /* [B, T, H, d_nope + d_rope], contiguous in a token               */
+  const void*  kn;        /* [B, Tk, H, d_nope]                                              */
+  const void*  kr;        /* [B, Tk, d_rope] (d_rope = 0: not read)                          */
+  const void*  v;         /* [B, Tk, H, d_v]                                                 */
+  void*   o;              /* [B, T, H, d_v] contiguous                                       */
+  float*  lse;            /* [B, T, H] or NULL                                               */
+  int32_t* status_word;   /* optional                                                        */
+} ha_la_latent_prefill_args;
+
+typedef struct {
+  int32_t dtype;          /* ha_la_dtype of q, cache, o                                      */
+  int32_t num_seqs;       /* N >= 0                                                          */
+  int32_t new_tokens;     /* per sequence, >= 1                                              */
+  int32_t num_heads;
+  int32_t d_latent;       /* 1 .. 512                                                        */
+  int32_t d_rope;         /* 0 .. 128                                                        */
+  int32_t page_size;      /* rows of a page: a power of two                                  */
+  int32_t num_pages;
+  int32_t max_pages;      /* row length of the table                                         */
+  float   scale;
+  const void*  q;         /* [N, new_tokens, H, d_latent + d_rope] contiguous                */
+  const void*  cache;     /* [num_pages, page_size, d_latent + d_rope] contiguous            */
+  const int32_t* page_table;  /* [N, max_pages]; entries behind a sequence's rows are not read */
+  const int32_t* lengths; /* [N]                                                             */
+  void*   o;              /* [N, new_tokens, H, d_latent]                                    */
+  float*  lse;            /* [N, new_tokens, H] or NULL                                      */
+  void*   workspace;      /* >= ha_la_latent_decode_workspace_bytes(), 256-byte aligned      */
+  size_t  workspace_bytes;
+  int32_t* status_word;   /* optional                                                        */
+} ha_la_latent_decode_args;
+
+/* "tc", "simt" or NULL if the sizes are not supported; by sizes and types (tensors aligned).  Host only. */
+const char* ha_la_latent_prefill_path(const ha_la_latent_prefill_args* args);
+const char* ha_la_latent_decode_path(const ha_la_latent_decode_args* args);
+int ha_la_latent_prefill(const ha_la_latent_prefill_args* args, void* cuda_stream);
+int ha_la_latent_decode_workspace_bytes(const ha_la_latent_decode_args* args, size_t* out_bytes);   /* host only */
+int ha_la_latent_decode(const ha_la_latent_decode_args* args, void* cuda_stream);
+
 /* Test hook for the device-side bounded waits (the paper has no counterpart).  Every wait inside the
  * kernels is on an mbarrier; it gives up after a fixed number of polls, records HA_LA_ERR_TIMEOUT in
  * *status_word and lets the kernel run to a normal exit with unspecified outputs.  This call makes such

@@ -53,6 +53,13 @@ from .mixer import (  # noqa: F401
     ha_la_conv_backward,
     ha_la_conv_decode,
     ha_la_conv_workspace_bytes,
+    ha_la_latent_decode,
+    ha_la_latent_decode_args,
+    ha_la_latent_decode_path,
+    ha_la_latent_decode_workspace_bytes,
+    ha_la_latent_prefill,
+    ha_la_latent_prefill_args,
+    ha_la_latent_prefill_path,
     ha_la_scan,
     ha_la_scan_args,
     ha_la_scan_backward,

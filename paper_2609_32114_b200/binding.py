@@ -54,6 +54,11 @@ EXPORTS = (
     "ha_la_scan",
     "ha_la_scan_backward",
     "ha_la_scan_decode",
+    "ha_la_latent_prefill_path",
+    "ha_la_latent_prefill",
+    "ha_la_latent_decode_path",
+    "ha_la_latent_decode_workspace_bytes",
+    "ha_la_latent_decode",
     "ha_la_debug_wait_timeout",
     "ha_la_status_string",
     "ha_la_version",

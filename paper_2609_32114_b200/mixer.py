@@ -1,5 +1,5 @@
 """Binding of the layers that alternate with the recurrences in a hybrid model (include/ha_la.h): short causal convolution, selective
-state space scan, forward, backward and one token.
+state space scan, forward, backward and one token; attention over latent rows, for prompts and for single tokens.
 
 As in `layer`: marshalling only, torch CUDA tensors in and out, everything is computed by the library's kernels on the caller's
 stream, nothing is synchronised, tensors whose type, layout, size or device does not fit raise ValueError before anything is launched,
@@ -12,7 +12,7 @@ import ctypes
 
 from . import binding
 from .binding import HA_LA_OK, HaLaError, _aligned_part, _check_room, _reachable
-from .layer import _INT32_MAX, _On, _as, _bound, _cuda, _element, _ptr, _sizes
+from .layer import _On, _as, _bound, _cuda, _element, _float, _ptr, _sizes
 
 HA_LA_ACT_SILU, HA_LA_ACT_NONE = 0, 2
 _ACTIVATIONS = {"silu": HA_LA_ACT_SILU, None: HA_LA_ACT_NONE}
@@ -37,8 +37,26 @@ class ha_la_scan_args(ctypes.Structure):
     ]
 
 
+class ha_la_latent_prefill_args(ctypes.Structure):
+    _fields_ = [
+        *((n, _i) for n in ("dtype", "batch", "seqlen", "seqlen_k", "num_heads", "d_nope", "d_rope", "d_v")), ("scale", ctypes.c_float),
+        ("num_seqs", _i), ("max_seqlen", _i), ("cu_seqlens", _p), ("cu_seqlens_k", _p),
+        *((n, _l) for n in ("q_stride", "kn_stride", "kr_stride", "v_stride", "kn_head_stride", "v_head_stride")),
+        *((n, _p) for n in ("q", "kn", "kr", "v", "o", "lse", "status_word")),
+    ]
+
+
+class ha_la_latent_decode_args(ctypes.Structure):
+    _fields_ = [
+        *((n, _i) for n in ("dtype", "num_seqs", "new_tokens", "num_heads", "d_latent", "d_rope", "page_size", "num_pages", "max_pages")),
+        ("scale", ctypes.c_float), *((n, _p) for n in ("q", "cache", "page_table", "lengths", "o", "lse", "workspace")),
+        ("workspace_bytes", ctypes.c_size_t), ("status_word", _p),
+    ]
+
+
 _STRUCTS = {"ha_la_conv": ha_la_conv_args, "ha_la_conv_backward": ha_la_conv_args, "ha_la_conv_decode": ha_la_conv_args,
-            "ha_la_scan": ha_la_scan_args, "ha_la_scan_backward": ha_la_scan_args, "ha_la_scan_decode": ha_la_scan_args}
+            "ha_la_scan": ha_la_scan_args, "ha_la_scan_backward": ha_la_scan_args, "ha_la_scan_decode": ha_la_scan_args,
+            "ha_la_latent_prefill": ha_la_latent_prefill_args, "ha_la_latent_decode": ha_la_latent_decode_args}
 
 
 def declare(lib) -> None:
@@ -49,8 +67,12 @@ def declare(lib) -> None:
     size = ctypes.POINTER(ctypes.c_size_t)
     lib.ha_la_conv_workspace_bytes.argtypes = [ctypes.POINTER(ha_la_conv_args), size]
     lib.ha_la_scan_workspace_bytes.argtypes = [ctypes.POINTER(ha_la_scan_args), ctypes.c_int, size]
-    for name in ("conv", "scan"):
+    lib.ha_la_latent_decode_workspace_bytes.argtypes = [ctypes.POINTER(ha_la_latent_decode_args), size]
+    for name in ("conv", "scan", "latent_decode"):
         getattr(lib, f"ha_la_{name}_workspace_bytes").restype = ctypes.c_int
+    for name in ("prefill", "decode"):
+        f = getattr(lib, f"ha_la_latent_{name}_path")
+        f.argtypes, f.restype = [ctypes.POINTER(_STRUCTS[f"ha_la_latent_{name}"])], ctypes.c_char_p
 
 
 # ---------------------------------------------------------------- calls
@@ -70,6 +92,24 @@ def ha_la_scan_workspace_bytes(args: ha_la_scan_args, backward: bool = False) ->
     if rc != HA_LA_OK:
         raise HaLaError(rc, "ha_la_scan_workspace_bytes")
     return n.value
+
+
+def ha_la_latent_decode_workspace_bytes(args: ha_la_latent_decode_args) -> int:
+    n = ctypes.c_size_t(0)
+    rc = binding.load_library().ha_la_latent_decode_workspace_bytes(ctypes.byref(args), ctypes.byref(n))
+    if rc != HA_LA_OK:
+        raise HaLaError(rc, "ha_la_latent_decode_workspace_bytes")
+    return n.value
+
+
+def ha_la_latent_prefill_path(args: ha_la_latent_prefill_args):
+    r = binding.load_library().ha_la_latent_prefill_path(ctypes.byref(args))
+    return None if r is None else r.decode()
+
+
+def ha_la_latent_decode_path(args: ha_la_latent_decode_args):
+    r = binding.load_library().ha_la_latent_decode_path(ctypes.byref(args))
+    return None if r is None else r.decode()
 
 
 def _rows(t, like, name, lead, inner):
@@ -335,3 +375,123 @@ def ha_la_scan_decode(x, dt, A, B, C, state, *, D=None, z=None, dt_bias=None, so
         args.h0, args.y, args.hT = _ptr(state), _ptr(y), _ptr(state_out)
         on.call("ha_la_scan_decode", args)
     return y, state_out
+
+
+# ---------------------------------------------------------------- attention over latent rows
+
+def _heads(t, like, name, lead, H):
+    """(elements from a token to the next, from a head to the next, head size) of [*lead, H, d]: contiguous within a head, else at any distances."""
+    if t.dim() != len(lead) + 2:
+        raise ValueError(f"{name}: {tuple(t.shape)}; wanted are {(*lead, H, 'd')}")
+    d = t.shape[-1]
+    ok = _reachable(t, like) and t.dtype == like.dtype and tuple(t.shape) == (*lead, H, d) and d >= 1
+    if ok and t.numel() == 0:
+        return H * d, d, d
+    head = t.stride(-2) if H > 1 else d
+    step, tokens = H * d, 1
+    if ok:
+        ok = (d == 1 or t.stride(-1) == 1) and head >= d
+        for n, s in zip(reversed(lead), reversed(t.stride()[:len(lead)])):
+            if n > 1:
+                if tokens == 1:
+                    step = s
+                ok = ok and s == step * tokens
+            tokens *= n
+    if not ok or step < d:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, strides {tuple(t.stride())}, on {t.device}; wanted is {like.dtype} {(*lead, H, 'd')} "
+                         f"on {like.device}, contiguous within a head, with one distance from token to token and one from head to head")
+    return step, head, d
+
+
+def ha_la_latent_prefill(q, kn, kr, v, *, scale=1.0, cu_seqlens=None, cu_seqlens_k=None, max_seqlen=0, o=None, lse=None, status_word=None, stream=None):
+    """Causal attention of a prompt on expanded keys and values: s_ij = scale (q_i[..d_nope] . kn_j + q_i[d_nope..] . kr_j) per head, kr shared by
+    all heads.  A sequence's queries are its last tokens: query i sees the keys up to i + (keys - queries).
+
+    q  : [B, T, H, d_nope + d_rope] (or [T, H, ..]) bf16 or fp32, may be rows of a wider tensor    kn : [B, Tk, H, d_nope]    kr : [B, Tk, d_rope]
+    v  : [B, Tk, H, d_v]; kn and v may be slices of one tensor    cu_seqlens : int32 [N+1] or None (packed, B = 1), cu_seqlens_k the same of the keys
+    (None: the queries')    max_seqlen : bound on a sequence's queries, 0 = T
+    Returns (o, lse, status_word): o [B, T, H, d_v], lse fp32 [B, T, H], the logarithm of the sum of e^s; a query without a key has 0 and -infinity.
+    """
+    import torch
+
+    _cuda(q, "ha_la_latent_prefill")
+    if q.dim() not in (3, 4):
+        raise ValueError(f"q: {tuple(q.shape)}; wanted are [B, T, heads, d] or [T, heads, d]")
+    _sizes(q, "q")
+    dtype, lead, H, dq = _element(q, "q"), tuple(q.shape[:-2]), q.shape[-2], q.shape[-1]
+    if kr.dim() != len(lead) + 1 or kr.shape[-1] >= dq or H < 1:
+        raise ValueError(f"kr: {tuple(kr.shape)}; wanted are {len(lead) + 1} dimensions and less than q's {dq} channels")
+    _sizes(kr, "kr")
+    keys, dr = (*lead[:-1], kr.shape[-2]), kr.shape[-1]
+    B, T = lead if len(lead) == 2 else (1, lead[0])
+    N = 0
+    if cu_seqlens is None and cu_seqlens_k is not None:
+        raise ValueError("cu_seqlens_k without cu_seqlens")
+    if cu_seqlens is not None:
+        _, _, _, N = _sequences(q.flatten(-2) if q.is_contiguous() else q[..., 0], cu_seqlens, "q")
+        if cu_seqlens_k is None:
+            if keys != lead:
+                raise ValueError(f"kr: {tuple(kr.shape)} for {T} queries; cu_seqlens_k is wanted")
+            cu_seqlens_k = cu_seqlens
+        _as(cu_seqlens_k, q, "cu_seqlens_k", (N + 1,), torch.int32)
+    q_stride = _rows(q, q, "q", lead, (H, dq))
+    kr_stride = _rows(kr, q, "kr", keys, (dr,))
+    kn_stride, kn_head, dn = _heads(kn, q, "kn", keys, H)
+    v_stride, v_head, dv = _heads(v, q, "v", keys, H)
+    if dn + dr != dq:
+        raise ValueError(f"q: {tuple(q.shape)}; wanted are kn's {dn} and kr's {dr} channels together")
+    for name, t, dt, n in (("o", o, q.dtype, B * T * H * dv), ("lse", lse, torch.float32, B * T * H), ("status_word", status_word, torch.int32, 1)):
+        _check_room(name, t, q, dt, n)
+    args = ha_la_latent_prefill_args(dtype=dtype, batch=B, seqlen=T, seqlen_k=keys[-1], num_heads=H, d_nope=dn, d_rope=dr, d_v=dv, scale=_float(scale, "scale"),
+                                     num_seqs=N, max_seqlen=_bound(max_seqlen), cu_seqlens=_ptr(cu_seqlens), cu_seqlens_k=_ptr(cu_seqlens_k),
+                                     q_stride=q_stride, kn_stride=kn_stride, kr_stride=kr_stride, v_stride=v_stride, kn_head_stride=kn_head,
+                                     v_head_stride=v_head, q=_ptr(q), kn=_ptr(kn), kr=_ptr(kr), v=_ptr(v))
+    with _On(stream, q) as on:
+        o, lse = on.new(o, (*lead, H, dv), q.dtype), on.new(lse, (*lead, H), torch.float32)
+        args.o, args.lse = _ptr(o), _ptr(lse)
+        status_word = _status(on, args, status_word)
+        on.call("ha_la_latent_prefill", args)
+    return o, lse, status_word
+
+
+def ha_la_latent_decode(q, cache, page_table, lengths, *, scale=1.0, o=None, lse=None, d_latent=None, workspace=None, status_word=None, stream=None):
+    """Attention of one or a few new tokens a sequence to the cached latent rows themselves (absorbed form): s_ij = scale q_i . c_j per head,
+    o_i = sum of softmax weights times c_j[..d_latent].
+
+    q : [N, new, H, d_latent + d_rope] bf16 or fp32    cache : [pages, page_size, d_latent + d_rope], q's type, page_size a power of two
+    page_table : int32 [N, max_pages]    lengths : int32 [N], cached rows of each sequence, the new tokens' among them; token i of the new ones sees
+    the rows up to its own    d_latent : default the row size - 64
+    Returns (o, lse, status_word, workspace): o [N, new, H, d_latent], lse fp32 [N, new, H]; a token without a row has 0 and -infinity.
+    A status word other than 0 reports a length or a page that does not exist.
+    """
+    import torch
+
+    _cuda(q, "ha_la_latent_decode")
+    if q.dim() != 4 or cache.dim() != 3 or page_table.dim() != 2:
+        raise ValueError(f"q: {tuple(q.shape)}, cache: {tuple(cache.shape)}, page_table: {tuple(page_table.shape)}; wanted are [N, new, heads, d], "
+                         "[pages, page_size, d] and [N, max_pages]")
+    for t, name in ((q, "q"), (cache, "cache"), (page_table, "page_table")):
+        _sizes(t, name)
+    dtype, (N, new, H, d) = _element(q, "q"), q.shape
+    dl = d - 64 if d_latent is None else int(d_latent)
+    if not 1 <= dl <= d:
+        raise ValueError(f"d_latent: {dl} of {d} channels")
+    if new < 1 or H < 1 or cache.shape[1] < 1 or cache.shape[1] & (cache.shape[1] - 1):
+        raise ValueError(f"q: {tuple(q.shape)}, cache: {tuple(cache.shape)}; wanted are at least one token and head, and pages of a power of two")
+    _as(q, q, "q", q.shape)
+    _as(cache, q, "cache", (*cache.shape[:2], d))
+    _as(page_table, q, "page_table", (N, page_table.shape[1]), torch.int32)
+    _as(lengths, q, "lengths", (N,), torch.int32)
+    for name, t, dt, n in (("o", o, q.dtype, N * new * H * dl), ("lse", lse, torch.float32, N * new * H), ("workspace", workspace, None, 0),
+                           ("status_word", status_word, torch.int32, 1)):
+        _check_room(name, t, q, dt, n)
+    args = ha_la_latent_decode_args(dtype=dtype, num_seqs=N, new_tokens=new, num_heads=H, d_latent=dl, d_rope=d - dl, page_size=cache.shape[1],
+                                    num_pages=cache.shape[0], max_pages=page_table.shape[1], scale=_float(scale, "scale"), q=_ptr(q), cache=_ptr(cache),
+                                    page_table=_ptr(page_table), lengths=_ptr(lengths))
+    with _On(stream, q) as on:
+        o, lse = on.new(o, (N, new, H, dl), q.dtype), on.new(lse, (N, new, H), torch.float32)
+        args.o, args.lse = _ptr(o), _ptr(lse)
+        workspace = _workspace(on, args, workspace, ha_la_latent_decode_workspace_bytes(args))
+        status_word = _status(on, args, status_word)
+        on.call("ha_la_latent_decode", args)
+    return o, lse, status_word, workspace
