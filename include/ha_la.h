@@ -486,7 +486,7 @@ int ha_la_scan_decode(const ha_la_scan_args* args, void* cuda_stream);
  * A length that is negative or longer than its row of the table counts as zero and is reported through the status word, as is a
  * page that does not exist, whose sequence's results are unspecified.
  * Scores, their sums and o's sums are fp32; with bf16 tensors the weights are rounded to bf16 for the product with the values.
- * Tensor cores: bf16 with d_nope = 128, d_rope = 64, d_v = 128, 16-byte aligned with strides that are multiples of 8;
+ * Tensor cores: bf16 with d_nope = 128, d_rope = 64, d_v = 128, 16-byte aligned with strides that are multiples of 8, scale > 0;
  * decode bf16 with d_latent = 512, d_rope = 64, 16-byte aligned.  Everything else runs on the CUDA cores, much slower.    */
 typedef struct {
   int32_t dtype;          /* ha_la_dtype of q, kn, kr, v, o                                  */

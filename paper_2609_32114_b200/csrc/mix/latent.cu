@@ -29,6 +29,12 @@ int check(const ha_la_latent_prefill_args* a, mix::PromptParams* p) {
   return HA_LA_OK;
 }
 
+// (a scale that is not positive would turn the largest score around, or mask with 0 * infinity)
+bool on_tensor_cores(const ha_la_latent_prefill_args* a, const mix::PromptParams& p) {
+  return a->dtype == HA_LA_BF16 && p.dn == 128 && p.dr == 64 && p.dv == 128 && p.scale > 0.f && mix::any_of(a->q, a->kn, a->kr, a->v, a->o) % 16 == 0 &&
+         ((p.qs | p.kns | p.krs | p.vs | p.kn_hs | p.v_hs) & 7) == 0;
+}
+
 int check(const ha_la_latent_decode_args* a, mix::TokenParams* p) {
   if (!a) return HA_LA_ERR_INVALID_ARG;
   if (a->dtype != HA_LA_BF16 && a->dtype != HA_LA_FP32) return HA_LA_ERR_INVALID_ARG;
@@ -53,7 +59,7 @@ extern "C" {
 
 const char* ha_la_latent_prefill_path(const ha_la_latent_prefill_args* a) {
   mix::PromptParams p;
-  return check(a, &p) == HA_LA_OK ? "simt" : nullptr;
+  return check(a, &p) != HA_LA_OK ? nullptr : on_tensor_cores(a, p) ? "tc" : "simt";
 }
 
 int ha_la_latent_prefill(const ha_la_latent_prefill_args* a, void* cuda_stream) {
@@ -67,7 +73,8 @@ int ha_la_latent_prefill(const ha_la_latent_prefill_args* a, void* cuda_stream) 
   if (p.q_seqs.T_total == 0) return HA_LA_OK;
   if (!a->q || !a->o) return HA_LA_ERR_INVALID_ARG;
   if (p.k_seqs.T_total > 0 && (!a->kn || !a->v || (a->d_rope > 0 && !a->kr))) return HA_LA_ERR_INVALID_ARG;
-  const cudaError_t e = mix::launch_prompt_simt(bf16, p, reinterpret_cast<cudaStream_t>(cuda_stream));
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = on_tensor_cores(a, p) ? mix::launch_prompt_tc(p, stream) : mix::launch_prompt_simt(bf16, p, stream);
   return e == cudaSuccess ? HA_LA_OK : HA_LA_ERR_CUDA;
 }
 

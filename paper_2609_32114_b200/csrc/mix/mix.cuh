@@ -2,6 +2,8 @@
 // token strides, launches.
 #pragma once
 
+#include <atomic>
+
 #include "../common.cuh"
 
 namespace ha_la {
@@ -67,6 +69,17 @@ cudaError_t start(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, 
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// A kernel's shared memory limit, raised once per device.
+template <auto kern> cudaError_t allow_smem(size_t smem) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
+  if (dev < 64 && (done.load() >> dev & 1)) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev);
+  return e;
 }
 
 template <typename... P> uintptr_t any_of(P... p) { return (... | (uintptr_t)p); }
