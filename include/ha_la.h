@@ -487,7 +487,7 @@ int ha_la_scan_decode(const ha_la_scan_args* args, void* cuda_stream);
  * page that does not exist, whose sequence's results are unspecified.
  * Scores, their sums and o's sums are fp32; with bf16 tensors the weights are rounded to bf16 for the product with the values.
  * Tensor cores: bf16 with d_nope = 128, d_rope = 64, d_v = 128, 16-byte aligned with strides that are multiples of 8, scale > 0;
- * decode bf16 with d_latent = 512, d_rope = 64, 16-byte aligned.  Everything else runs on the CUDA cores, much slower.    */
+ * decode bf16 with d_latent = 512, d_rope = 64, pages of 16 rows or more, 16-byte aligned, scale > 0.  Everything else runs on the CUDA cores, much slower.    */
 typedef struct {
   int32_t dtype;          /* ha_la_dtype of q, kn, kr, v, o                                  */
   int32_t batch;          /* B; must be 1 when cu_seqlens != NULL                            */

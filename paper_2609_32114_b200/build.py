@@ -27,7 +27,8 @@ UNITS = [("api", "api.cu", []), ("plan", "plan.cu", []), ("tc", "tc.cu", []), ("
          ("norm", "norm.cu", []), ("gla_api", "gla/api.cu", []), ("gla_decode", "gla/decode.cu", []), ("gla_simt", "gla/simt.cu", []),
          ("gla_tc", "gla/tc.cu", []), ("gla_tc_state", "gla/tc_state.cu", []), ("gla_tc_walk", "gla/tc_walk.cu", []), ("gla_tc_back", "gla/tc_back.cu", []),
          ("conv", "mix/conv.cu", []), ("scan", "mix/scan.cu", []), ("scan_back", "mix/scan_back.cu", []),
-         ("latent", "mix/latent.cu", []), ("latent_simt", "mix/latent_simt.cu", []), ("latent_prompt", "mix/latent_prompt.cu", [])] + [
+         ("latent", "mix/latent.cu", []), ("latent_simt", "mix/latent_simt.cu", []), ("latent_prompt", "mix/latent_prompt.cu", []),
+         ("latent_decode", "mix/latent_decode.cu", [])] + [
     (f"simt{u}", "simt.cu", [f"-DHA_LA_SIMT_UNIT={u}"]) for u in range(5)
 ] + [
     (f"fp32_{u}", "fp32.cu", [f"-DHA_LA_FP32_UNIT={u}"]) for u in range(5)

@@ -53,6 +53,11 @@ int check(const ha_la_latent_decode_args* a, mix::TokenParams* p) {
   return HA_LA_OK;
 }
 
+// By sizes; a tensor that is not aligned goes the other way, which needs less room.
+bool on_tensor_cores(const ha_la_latent_decode_args* a, const mix::TokenParams& p) {
+  return a->dtype == HA_LA_BF16 && p.dl == 512 && p.dr == 64 && p.page_log >= 4 && p.scale > 0.f && (long long)p.N * p.T * p.H <= 0x7fffffffLL / 4;
+}
+
 }  // namespace
 
 extern "C" {
@@ -80,14 +85,14 @@ int ha_la_latent_prefill(const ha_la_latent_prefill_args* a, void* cuda_stream) 
 
 const char* ha_la_latent_decode_path(const ha_la_latent_decode_args* a) {
   mix::TokenParams p;
-  return check(a, &p) == HA_LA_OK ? "simt" : nullptr;
+  return check(a, &p) != HA_LA_OK ? nullptr : on_tensor_cores(a, p) && mix::any_of(a->q, a->cache, a->o) % 16 == 0 ? "tc" : "simt";
 }
 
 int ha_la_latent_decode_workspace_bytes(const ha_la_latent_decode_args* a, size_t* out_bytes) {
   if (!out_bytes) return HA_LA_ERR_INVALID_ARG;
   mix::TokenParams p;
   const int rc = check(a, &p);
-  if (rc == HA_LA_OK) *out_bytes = 256;
+  if (rc == HA_LA_OK) *out_bytes = on_tensor_cores(a, p) ? mix::token_tc_bytes(p) : 256;
   return rc;
 }
 
@@ -103,7 +108,9 @@ int ha_la_latent_decode(const ha_la_latent_decode_args* a, void* cuda_stream) {
   size_t need = 0;
   ha_la_latent_decode_workspace_bytes(a, &need);
   if (!a->workspace || ((uintptr_t)a->workspace & 255) || a->workspace_bytes < need) return HA_LA_ERR_WORKSPACE;
-  const cudaError_t e = mix::launch_token_simt(bf16, p, reinterpret_cast<cudaStream_t>(cuda_stream));
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const bool tc = on_tensor_cores(a, p) && mix::any_of(a->q, a->cache, a->o) % 16 == 0;
+  const cudaError_t e = tc ? mix::launch_token_tc(p, a->workspace, stream) : mix::launch_token_simt(bf16, p, stream);
   return e == cudaSuccess ? HA_LA_OK : HA_LA_ERR_CUDA;
 }
 

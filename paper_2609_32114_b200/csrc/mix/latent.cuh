@@ -67,6 +67,8 @@ __device__ __forceinline__ long long cache_row(const TokenParams& p, int n, int 
 
 cudaError_t launch_prompt_simt(bool bf16, const PromptParams& p, cudaStream_t stream);
 cudaError_t launch_prompt_tc(const PromptParams& p, cudaStream_t stream);
+size_t token_tc_bytes(const TokenParams& p);
+cudaError_t launch_token_tc(const TokenParams& p, void* workspace, cudaStream_t stream);
 cudaError_t launch_token_simt(bool bf16, const TokenParams& p, cudaStream_t stream);
 
 }  // namespace mix
