@@ -197,7 +197,10 @@ def _torch_call():
                      for f in (lib.ha_la_prefill, lib.ha_la_prefill_workspace_bytes, lib.ha_la_decode,
                                lib.ha_la_gla_prefill, lib.ha_la_gla_backward, lib.ha_la_gla_workspace_bytes, lib.ha_la_gla_decode,
                                lib.ha_la_gated_norm, lib.ha_la_gated_norm_backward, lib.ha_la_gated_norm_workspace_bytes,
-                               lib.ha_la_add_norm, lib.ha_la_add_norm_backward, lib.ha_la_add_norm_workspace_bytes)))
+                               lib.ha_la_add_norm, lib.ha_la_add_norm_backward, lib.ha_la_add_norm_workspace_bytes,
+                               lib.ha_la_conv, lib.ha_la_conv_backward, lib.ha_la_conv_workspace_bytes, lib.ha_la_conv_decode,
+                               lib.ha_la_scan, lib.ha_la_scan_backward, lib.ha_la_scan_workspace_bytes, lib.ha_la_scan_decode,
+                               lib.ha_la_latent_prefill, lib.ha_la_latent_decode, lib.ha_la_latent_decode_workspace_bytes)))
         _call_lib = lib
     return _call
 

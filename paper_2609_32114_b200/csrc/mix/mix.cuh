@@ -71,13 +71,17 @@ cudaError_t start(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, 
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// A kernel's shared memory limit, raised once per device.
-template <auto kern> cudaError_t allow_smem(size_t smem) {
+// A kernel's shared memory limit, raised once per device.  `regs`: registers of a thread that its roles share out among themselves; with fewer at launch
+// they would wait for ever.
+template <auto kern> cudaError_t allow_smem(size_t smem, int regs = 0) {
   static std::atomic<uint64_t> done{0};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return cudaErrorInvalidDevice;
   if (dev < 64 && (done.load() >> dev & 1)) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  cudaFuncAttributes has;
+  cudaError_t e = cudaFuncGetAttributes(&has, kern);
+  if (e == cudaSuccess && has.numRegs < regs) e = cudaErrorInvalidKernelImage;
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev);
   return e;
 }
@@ -140,7 +144,18 @@ template <int V> __device__ __forceinline__ void store_v(float* p, const Vec<V>&
   else *p = r.v[0];
 }
 
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float ex2(float x) {            // 2^x, zero for very negative x
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float sigmoid(float z) { return reciprocal(1.f + ex2(-z * kLog2e)); }
 
 }  // namespace mix
 }  // namespace ha_la

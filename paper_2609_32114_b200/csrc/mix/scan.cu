@@ -13,16 +13,48 @@ namespace ha_la {
 namespace mix {
 namespace {
 
-constexpr int kThreads = 256, kTile = 32;
+constexpr int kThreads = 384, kTile = 32;
+constexpr int kRegs = 80, kScanRegs = 128, kHelpRegs = 56; // a thread's at launch, and as the roles share them out
+static_assert(128 * kScanRegs + 256 * kHelpRegs <= kThreads * kRegs && 2 * kThreads * kRegs <= 65536, "register split");
 enum Mode { kOut, kEnds, kKeep };                          // outputs; states behind segments; states in front of every 8 tokens
+
+// Dynamic shared memory: what the recurrence takes, two tiles; rows on their way, as they are in memory (a thread's own pieces side by side).
+template <typename In, int SP, int LS> struct Stage {
+  static constexpr int CH = 128 / LS, NP = SP * LS, E = CH >= 16 ? CH / 8 : 2, BC = kTile * NP / 4 / 128;
+  static constexpr uint32_t kRowB = E * sizeof(In), kQuadB = 4 * sizeof(In);
+  static constexpr uint32_t OFF_B = 2 * kTile * CH * 8, OFF_C = OFF_B + 2 * kTile * NP * 4, OFF_X = OFF_C + 2 * kTile * NP * 4;
+  static constexpr uint32_t OFF_DT = OFF_X + 4 * 256 * kRowB, OFF_Z = OFF_DT + 2 * 256 * kRowB, OFF_BC = OFF_Z + 2 * 256 * kRowB;
+  static constexpr size_t bytes = OFF_BC + 2 * 256 * BC * kQuadB;
+};
+
+// Pieces of 16 bytes in a row of what one side writes and the other reads: exchanged within their neighbourhood, so that eight threads that are neighbours meet all
+// banks on both sides (without that, reads of the sums took four times as long and bounded the kernel).
+__device__ __forceinline__ int sum_piece(int u) { return u ^ ((u >> 3) & 3); }        // four lanes' sums
+__device__ __forceinline__ int step_piece(int u) { return u ^ ((u >> 3) & 1); }       // delta and delta x of two channels
+
+// `bytes` from global to shared memory in the background, if that can be (`fast`: aligned and whole), else by way of registers.
+template <typename In, int V> __device__ __forceinline__ void stage_row(uint8_t* to, const In* from, bool fast, int left) {
+  if (fast && left >= V) {
+    const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(to));
+    if constexpr (V * sizeof(In) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(from), "n"(V * sizeof(In)) : "memory");
+  } else {
+    *reinterpret_cast<Raw<In, V>*>(to) = load_row<In, V>(from, false, left);
+  }
+}
 
 template <typename In, int SP, int LS, Mode M>
 __global__ void __launch_bounds__(kThreads, 2) scan_kernel(ScanParams p) {
-  constexpr int LC = 32 / LS, CH = 4 * LC, NP = SP * LS, E = CH / 4;      // channels of a warp, of the CTA; states; channels of a helping thread
-  constexpr int BC = kTile * NP / 128;                     // values of B (and C) that a helping thread brings
-  __shared__ __align__(16) float2 s_du[2][kTile][CH];
-  __shared__ __align__(16) float s_b[2][kTile][NP], s_c[2][M == kOut ? kTile : 1][NP];
-  __shared__ float s_y[M == kOut ? 2 : 1][M == kOut ? kTile : 1][CH];
+  constexpr int LC = 32 / LS, CH = 4 * LC, NP = SP * LS;   // channels of a warp, of the CTA; states
+  constexpr int E = CH >= 16 ? CH / 8 : 2, TPR = CH / E;   // channels of a helping thread, threads to a token
+  constexpr int BC = kTile * NP / 4 / 128;                 // quads of B (or C) that a helping thread brings
+  using St = Stage<In, SP, LS>;
+  extern __shared__ __align__(16) uint8_t dyn[];
+  float4(*const s_du)[kTile][CH / 2] = reinterpret_cast<float4(*)[kTile][CH / 2]>(dyn);
+  float(*const s_b)[kTile][NP] = reinterpret_cast<float(*)[kTile][NP]>(dyn + St::OFF_B);
+  float(*const s_c)[kTile][NP] = reinterpret_cast<float(*)[kTile][NP]>(dyn + St::OFF_C);
+  // (an object of its own, so that the compiler may move reads of the others ahead of what is written here)
+  __shared__ __align__(16) float s_y[M == kOut ? 2 : 1][M == kOut ? kTile : 1][CH * LS];
   __shared__ int s_n;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int nb = p.blocks * p.G, unit = blockIdx.x / nb, cb = blockIdx.x - unit * nb, group = cb / p.blocks;
@@ -57,6 +89,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_kernel(ScanParams p) {
   const int tiles = (len + kTile - 1) / kTile;
 
   if (warp < 4) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kScanRegs));
     const int c = warp * LC + lane % LC, s0 = lane / LC * SP, ch = c0 + c;
     const bool mine = c < left;
     float A[SP], h[SP];
@@ -91,6 +124,8 @@ __global__ void __launch_bounds__(kThreads, 2) scan_kernel(ScanParams p) {
       }
     }
     if (M == kEnds && start + len >= q.len) return;
+    constexpr int U = kCkpt;
+    const int du_at = step_piece(c / 2) * 2 + c % 2, sum = c * LS + lane / LC, y_at = sum_piece(sum / 4) * 4 + sum % 4;
     float total = 0.f;
     const int ck0 = M == kKeep ? slot_of(p.seqs, n, q.tok0, kCkptLog, (p.seqs.T_row + kCkpt - 1) / kCkpt) : 0;
     __syncthreads();
@@ -98,12 +133,12 @@ __global__ void __launch_bounds__(kThreads, 2) scan_kernel(ScanParams p) {
     for (int i = 0; i < tiles; ++i) {
       const int b = i & 1;
       float part = 0.f;
-#pragma unroll(LS >= 8 ? 1 : 2)
-      for (int t0 = 0; t0 < kTile; t0 += LS) {
-        float yv[LS];
+#pragma unroll 2
+      for (int t0 = 0; t0 < kTile; t0 += U) {
+        float yv[U];
 #pragma unroll
-        for (int j = 0; j < LS; ++j) {
-          if (M == kKeep && (LS <= kCkpt ? j == 0 && t0 % kCkpt == 0 : j % kCkpt == 0)) {
+        for (int j = 0; j < U; ++j) {
+          if (M == kKeep && j == 0) {
             const int tk = i * kTile + t0 + j;
             if (mine && tk < len) {
               Vec<SP> now;
@@ -112,22 +147,33 @@ __global__ void __launch_bounds__(kThreads, 2) scan_kernel(ScanParams p) {
               store_v<SP>(p.ckpt + ((size_t)(ck0 + (tk >> kCkptLog)) * p.C + ch) * NP + s0, now);
             }
           }
-          const float2 du = s_du[b][t0 + j][c];
+          const float2 du = reinterpret_cast<const float2*>(&s_du[b][t0 + j][0])[du_at];
           const Vec<SP> bv = load_v<SP>(&s_b[b][t0 + j][s0]);
           if (M == kEnds) part += du.x;
           Vec<SP> cv;
           if (M == kOut) cv = load_v<SP>(&s_c[b][t0 + j][s0]);
           float y = 0.f;
+          if constexpr (SP == 1) {
+            h[0] = fmaf(ex2(du.x * A[0]), h[0], du.y * bv.v[0]);
+            if (M == kOut) y = h[0] * cv.v[0];
+          } else {                                         // (two states to an instruction)
+            float2 y2 = make_float2(0.f, 0.f);
 #pragma unroll
-          for (int s = 0; s < SP; ++s) {
-            h[s] = fmaf(ex2(du.x * A[s]), h[s], du.y * bv.v[s]);
-            if (M == kOut) y = fmaf(h[s], cv.v[s], y);
+            for (int s = 0; s < SP; s += 2) {
+              const float2 g = ptx::mul2(make_float2(du.x, du.x), make_float2(A[s], A[s + 1]));
+              const float2 hn = ptx::fma2(make_float2(ex2(g.x), ex2(g.y)), make_float2(h[s], h[s + 1]),
+                                          ptx::mul2(make_float2(du.y, du.y), make_float2(bv.v[s], bv.v[s + 1])));
+              h[s] = hn.x;
+              h[s + 1] = hn.y;
+              if (M == kOut) y2 = s ? ptx::fma2(hn, make_float2(cv.v[s], cv.v[s + 1]), y2) : ptx::mul2(hn, make_float2(cv.v[s], cv.v[s + 1]));
+            }
+            y = y2.x + y2.y;
           }
           yv[j] = y;
         }
         if (M == kOut) {
-          spread_sum<LS, ilog2(LS)>(yv, 16);
-          s_y[b][t0 + lane / LC][c] = yv[0];
+#pragma unroll
+          for (int j = 0; j < U; ++j) s_y[b][t0 + j][y_at] = yv[j];
         }
       }
       total += part;
@@ -148,9 +194,10 @@ __global__ void __launch_bounds__(kThreads, 2) scan_kernel(ScanParams p) {
     return;
   }
 
-  // ---- the helping warps
+  // ---- the helping warps: E channels of a token to a thread
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHelpRegs));
   if (M == kEnds && start + len >= q.len) return;
-  const int ht = tid - 128, row = ht / 4, c = ht % 4 * E, have = left - c;     // a token and E channels
+  const int ht = tid - 128, row = ht / TPR, c = ht % TPR * E, have = row < kTile ? left - c : 0;
   const bool vec = p.vec;
   const In *x = reinterpret_cast<const In*>(p.x) + c0 + c, *dt = reinterpret_cast<const In*>(p.dt) + c0 + c;
   const In *B = reinterpret_cast<const In*>(p.B) + (size_t)group * p.S, *C = reinterpret_cast<const In*>(p.C_) + (size_t)group * p.S;
@@ -161,69 +208,95 @@ __global__ void __launch_bounds__(kThreads, 2) scan_kernel(ScanParams p) {
     if (p.dt_bias && e < have) bias.v[e] = p.dt_bias[c0 + c + e];
     if (M == kOut && p.D && e < have) skip.v[e] = p.D[c0 + c + e];
   }
-  Vec<E> vx = {}, vd = {};
-  float vb[BC], vc[M == kOut ? BC : 1];
-  auto fetch = [&](int i) {                                // tile i's rows on their way
+  // A thread's pieces, which nobody else looks at: x of tile i in place i % 4 (it is wanted again for the outputs), the others in place i % 2
+  uint8_t* const own = dyn + ht * St::kRowB;
+  auto x_at = [&](int i) { return own + St::OFF_X + (i & 3) * 256 * St::kRowB; };
+  auto dt_at = [&](int i) { return own + St::OFF_DT + (i & 1) * 256 * St::kRowB; };
+  auto z_at = [&](int i) { return own + St::OFF_Z + (i & 1) * 256 * St::kRowB; };
+  auto bc_at = [&](int i, int j) { return dyn + St::OFF_BC + (((i & 1) * BC + j) * 256 + ht) * St::kQuadB; };
+  const In* const bc = ht < 128 ? B : C;                   // the first 128 threads bring B, the others C
+  const long long bc_step = ht < 128 ? p.bs : p.cs;
+  const bool bc_mine = ht < 128 || M == kOut;
+  auto fetch = [&](int i) {
     const int t = i * kTile + row;
-    if (t < len) {
-      vx = load_row<In, E>(x + (size_t)(tok0 + t) * p.xs, vec, have);
-      vd = load_row<In, E>(dt + (size_t)(tok0 + t) * p.dts, vec, have);
+    if (t < len && have > 0) {
+      stage_row<In, E>(x_at(i), x + (size_t)(tok0 + t) * p.xs, vec, have);
+      stage_row<In, E>(dt_at(i), dt + (size_t)(tok0 + t) * p.dts, vec, have);
     }
 #pragma unroll
     for (int j = 0; j < BC; ++j) {
-      const int f = j * 128 + ht, r = i * kTile + f / NP, s = f % NP;
-      const bool ok = r < len && s < p.S;
-      vb[j] = ok ? to_f32(B[(size_t)(tok0 + r) * p.bs + s]) : 0.f;
-      if (M == kOut) vc[j] = ok ? to_f32(C[(size_t)(tok0 + r) * p.cs + s]) : 0.f;
+      const int f = (j * 128 + (ht & 127)) * 4, r = i * kTile + f / NP, s = f % NP;
+      if (bc_mine && r < len) stage_row<In, 4>(bc_at(i, j), bc + (size_t)(tok0 + r) * bc_step + s, p.bc_vec, p.S - s);
     }
   };
-  auto put = [&](int i) {                                  // ... in shared memory, as the other warps take them
+  auto fetch_z = [&](int i) {
+    const int t = i * kTile + row;
+    if (M == kOut && p.z && t < len && have > 0) stage_row<In, E>(z_at(i), z + (size_t)(tok0 + t) * p.zs, vec, have);
+  };
+  auto put = [&](int i) {                                  // ... as the other warps take them
     const int b = i & 1;
-    const bool ok = i * kTile + row < len;
+    if (row < kTile) {
+      const bool ok = i * kTile + row < len;
+      const Vec<E> vx = unpack_row<In, E>(*reinterpret_cast<const Raw<In, E>*>(x_at(i))), vd = unpack_row<In, E>(*reinterpret_cast<const Raw<In, E>*>(dt_at(i)));
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float v = vd.v[e] + bias.v[e], delta = ok && e < have ? (p.softplus ? softplus(v) : v) : 0.f;
-      s_du[b][row][c + e] = make_float2(delta, ok && e < have ? delta * vx.v[e] : 0.f);
+      for (int e = 0; e < E; e += 2) {
+        float4 w;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float u = vd.v[e + k] + bias.v[e + k], delta = ok && e + k < have ? (p.softplus ? softplus(u) : u) : 0.f;
+          (&w.x)[2 * k] = delta;
+          (&w.x)[2 * k + 1] = ok && e + k < have ? delta * vx.v[e + k] : 0.f;
+        }
+        s_du[b][row][step_piece((c + e) / 2)] = w;
+      }
     }
 #pragma unroll
     for (int j = 0; j < BC; ++j) {
-      const int f = j * 128 + ht;
-      s_b[b][f / NP][f % NP] = vb[j];
-      if (M == kOut) s_c[b][f / NP][f % NP] = vc[j];
+      const int f = (j * 128 + (ht & 127)) * 4, r = f / NP, s = f % NP;
+      Vec<4> w = {};
+      if (i * kTile + r < len) w = unpack_row<In, 4>(*reinterpret_cast<const Raw<In, 4>*>(bc_at(i, j)));
+      if (bc_mine) store_v<4>(ht < 128 ? &s_b[b][r][s] : &s_c[b][r][s], w);
     }
   };
-  auto finish = [&](int i, const Vec<E>& xi, const Vec<E>& zi) {
+  auto finish = [&](int i) {
     const int t = i * kTile + row;
-    if (t >= len) return;
-    Vec<E> y;
+    if (t >= len || have <= 0) return;
+    const Vec<E> xi = unpack_row<In, E>(*reinterpret_cast<const Raw<In, E>*>(x_at(i))), zi = unpack_row<In, E>(*reinterpret_cast<const Raw<In, E>*>(z_at(i)));
+    Vec<E> y = {};
+#pragma unroll
+    for (int k = 0; k < E * LS / 4; ++k) {
+      const float4 part = *reinterpret_cast<const float4*>(&s_y[i & 1][M == kOut ? row : 0][sum_piece(c * LS / 4 + k) * 4]);
+      y.v[k / (LS / 4)] += (part.x + part.y) + (part.z + part.w);
+    }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      y.v[e] = fmaf(skip.v[e], xi.v[e], s_y[i & 1][row][c + e]);
+      if (p.D) y.v[e] = fmaf(skip.v[e], xi.v[e], y.v[e]);
       if (p.z) y.v[e] *= zi.v[e] * sigmoid(zi.v[e]);
     }
     store_row<In, E>(reinterpret_cast<In*>(p.y) + (size_t)(tok0 + t) * p.C + c0 + c, vec, have, y);
   };
+  auto sent = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
+  // What is wanted while tile i is gone through has been sent for two tiles before.
   if (tiles > 0) {
     fetch(0);
-    put(0);
-    if (tiles > 1) fetch(1);
+    fetch_z(0);
   }
+  sent();
+  if (tiles > 1) fetch(1);
+  sent();
+  asm volatile("cp.async.wait_group 1;" ::: "memory");
+  if (tiles > 0) put(0);
+  if (tiles > 2) fetch(2);                                 // (its place was tile 0's)
+  sent();
   __syncthreads();
 #pragma unroll 1
   for (int i = 0; i <= tiles; ++i) {
-    Vec<E> xi = {}, zi = {};
-    if (M == kOut && i > 0) {
-      const int t = (i - 1) * kTile + row;
-      if (t < len) {
-        if (p.D) xi = load_row<In, E>(x + (size_t)(tok0 + t) * p.xs, vec, have);
-        if (p.z) zi = load_row<In, E>(z + (size_t)(tok0 + t) * p.zs, vec, have);
-      }
-    }
-    if (i + 1 < tiles) {
-      put(i + 1);
-      if (i + 2 < tiles) fetch(i + 2);
-    }
-    if (M == kOut && i > 0) finish(i - 1, xi, zi);
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    if (i + 1 < tiles) put(i + 1);
+    if (M == kOut && i > 0) finish(i - 1);
+    if (i + 3 < tiles) fetch(i + 3);
+    if (i + 1 < tiles) fetch_z(i + 1);
+    sent();
     if (i < tiles) __syncthreads();
   }
 }
@@ -306,15 +379,16 @@ int padded(int S) { return S <= 16 ? 16 : S <= 32 ? 32 : 64; }
 
 struct Shape { int sp, ls, ch; };
 
-// States to a thread.  A CTA's four recurrence warps take one scheduler each, so what counts is how many CTAs there are to an SM: the most
-// states to a thread (the fewest shared-memory reads and sums a value) that still gives every SM one.
+// States to a thread: the most (the fewest shared-memory reads and sums a value) that still gives three SMs of four a CTA.  1024 tokens, 16 states, us, four, two
+// and one to a thread: 128, 256, 512 CTAs 42, 48, 82; 64, 128, 256 42, 30, 42; 32, 64, 128 35, 29, 30; 512, 1024, 2048 131, 158, 285.  (Eight, two lanes to a channel: 68 for 64
+// CTAs, and 998 instead of 848 for eight sequences of 100 to 8000 tokens and 4096 channels.)
 Shape shape_of(int S, long long rows, int per_group, int G) {
   const int np = padded(S);
   Shape last = {};
-  for (int sp = np == 64 ? 8 : np == 32 ? 8 : 4; sp >= np / 16; sp /= 2) {
+  for (int sp = np == 16 ? 4 : 8; sp >= np / 16; sp /= 2) {
     const int ls = np / sp, ch = 128 / ls;
     last = {sp, ls, ch};
-    if (rows * ((per_group + ch - 1) / ch) * G >= sm_count()) break;
+    if (rows * ((per_group + ch - 1) / ch) * G >= sm_count() * 3 / 4) break;
   }
   return last;
 }
@@ -332,8 +406,11 @@ int segment_log(const ScanParams& p, const Shape& s) {
 template <typename In, int SP, int LS> cudaError_t launch(Mode m, const ScanParams& p, long long units, cudaStream_t stream) {
   const long long grid = units * p.blocks * p.G;
   if (grid == 0) return cudaSuccess;
+  constexpr size_t smem = Stage<In, SP, LS>::bytes;
   void (*k)(ScanParams) = m == kOut ? scan_kernel<In, SP, LS, kOut> : m == kEnds ? scan_kernel<In, SP, LS, kEnds> : scan_kernel<In, SP, LS, kKeep>;
-  return start(k, dim3((unsigned)grid), kThreads, 0, stream, p);
+  const cudaError_t e = m == kOut ? allow_smem<scan_kernel<In, SP, LS, kOut>>(smem, kRegs) : m == kEnds ? allow_smem<scan_kernel<In, SP, LS, kEnds>>(smem, kRegs)
+                                                                                                  : allow_smem<scan_kernel<In, SP, LS, kKeep>>(smem, kRegs);
+  return e == cudaSuccess ? start(k, dim3((unsigned)grid), kThreads, smem, stream, p) : e;
 }
 
 template <typename In> cudaError_t launch_shape(Mode m, const Shape& s, const ScanParams& p, long long units, cudaStream_t stream) {
@@ -398,6 +475,11 @@ Plan forward_plan(ScanParams* p) {
   return f;
 }
 
+bool aligned_states(const ha_la_scan_args* a, const ScanParams& p) {
+  const int e = a->dtype == HA_LA_BF16 ? 2 : 4;
+  return any_of(a->B, a->C) % (4 * e) == 0 && ((p.bs | p.cs | p.S) & 3) == 0;
+}
+
 bool aligned_rows(const ha_la_scan_args* a, const ScanParams& p, bool back) {
   const int e = a->dtype == HA_LA_BF16 ? 2 : 4;
   uintptr_t at = any_of(a->x, a->dt, a->z);
@@ -441,6 +523,7 @@ int run(const ha_la_scan_args* a, bool back, cudaStream_t stream) {
   if (p.seqs.T_total > 0 && (back ? !a->dy || !a->dx || !a->ddt || !a->dB || !a->dC || (a->z && !a->dz) : !a->y)) return HA_LA_ERR_INVALID_ARG;
   if (back && (!a->dA || (a->D && !a->dD) || (a->dt_bias && !a->ddt_bias))) return HA_LA_ERR_INVALID_ARG;
   p.vec = aligned_rows(a, p, back);
+  p.bc_vec = aligned_states(a, p);
   if (!a->workspace || ((uintptr_t)a->workspace & 255)) return HA_LA_ERR_WORKSPACE;
   char* ws = reinterpret_cast<char*>(a->workspace);
   if (back) {

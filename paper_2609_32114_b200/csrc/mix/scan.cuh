@@ -9,6 +9,7 @@
 #pragma once
 
 #include "mix.cuh"
+#include "../tc_mma.cuh"
 
 namespace ha_la {
 namespace mix {
@@ -17,7 +18,7 @@ struct ScanParams {
   Seqs seqs;
   int C, S, G, per_group;                                  // channels; states; groups; channels to a group
   int blocks;                                              // channel blocks of a group
-  int softplus, packed, vec;                               // vec: rows can be read and written several channels at a time
+  int softplus, packed, vec, bc_vec;                       // vec: rows can be read and written several channels at a time; bc_vec: B and C four states
   int seg_log, segs;                                       // tokens to a segment (a power of two) and segments of a row; 31: sequences whole
   long long xs, dts, bs, cs, zs;
   const void *x, *dt, *B, *C_, *z, *dy;
@@ -33,32 +34,56 @@ struct ScanParams {
 
 constexpr int kCkpt = 8, kCkptLog = 3;                     // tokens from one kept state to the next
 
-// softplus(v) = max(v, 0) + log1p(e^-|v|), with log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3, by its power series (s^15 / 15 < 5e-9):
-// small steps keep all of their bits, where a logarithm of 1 + e would have lost them.
+constexpr float kLn2 = 0.6931471805599453f;
+
+// softplus(v) = max(v, 0) + log1p(e^-|v|), with log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3: small steps keep all of their bits, where a logarithm of 1 + e
+// would have lost them.  artanh(s) / s as a polynomial in s^2 through its Chebyshev points on [0, 1/9], off by 4e-9.
 __device__ __forceinline__ float softplus(float v) {
-  const float e = __expf(-fabsf(v)), s = __fdividef(e, 2.f + e), q = s * s;
-  float r = 1.f / 13.f;
-  r = fmaf(r, q, 1.f / 11.f); r = fmaf(r, q, 1.f / 9.f); r = fmaf(r, q, 1.f / 7.f); r = fmaf(r, q, 1.f / 5.f); r = fmaf(r, q, 1.f / 3.f);
-  r = fmaf(r, q, 1.f);
+  const float e = ex2(-fabsf(v) * kLog2e), s = e * reciprocal(2.f + e), q = s * s;
+  float r = fmaf(0.14078889f, q, 0.13982579f);
+  r = fmaf(r, q, 0.20012298f); r = fmaf(r, q, 0.33333161f); r = fmaf(r, q, 1.f);
   return fmaf(2.f * s, r, fmaxf(v, 0.f));
 }
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // What a slot of 2^log tokens stands for: sequence n has those from (tok0 >> log) + n on (packed) or n * per_row on.
 __device__ __forceinline__ int slot_of(const Seqs& s, int n, int tok0, int log, int per_row) { return s.cu ? (tok0 >> log) + n : n * per_row; }
 
-// V values of a row that may not be aligned, or end (channels from `left` on are zero).
-template <typename In, int V> __device__ __forceinline__ Vec<V> load_row(const In* p, bool vec, int left) {
-  if (vec && left >= V) return load_v<V>(p);
-  Vec<V> r;
+// V values of a row that may not be aligned, or end (channels from `left` on are zero), as they are in memory: nothing waits for them until they are unpacked.
+template <typename In, int V> struct Raw { uint32_t w[V * sizeof(In) / 4]; };
+template <typename In, int V> __device__ __forceinline__ Raw<In, V> load_row(const In* p, bool vec, int left) {
+  constexpr int W = V * sizeof(In) / 4;
+  Raw<In, V> r;
+  if (vec && left >= V) {
+    if constexpr (W >= 4) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) r.v[i] = i < left ? to_f32(p[i]) : 0.f;
+      for (int i = 0; i < W; i += 4) {
+        const uint4 x = reinterpret_cast<const uint4*>(p)[i / 4];
+        r.w[i] = x.x; r.w[i + 1] = x.y; r.w[i + 2] = x.z; r.w[i + 3] = x.w;
+      }
+    } else if constexpr (W == 2) {
+      const uint2 x = *reinterpret_cast<const uint2*>(p);
+      r.w[0] = x.x; r.w[1] = x.y;
+    } else {
+      r.w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+    return r;
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    if constexpr (sizeof(In) == 4) r.w[i] = i < left ? __float_as_uint(p[i]) : 0u;
+    else r.w[i] = (2 * i < left ? (uint32_t)reinterpret_cast<const uint16_t*>(p)[2 * i] : 0u) |
+                  (2 * i + 1 < left ? (uint32_t)reinterpret_cast<const uint16_t*>(p)[2 * i + 1] << 16 : 0u);
+  }
   return r;
+}
+template <typename In, int V> __device__ __forceinline__ Vec<V> unpack_row(const Raw<In, V>& r) {
+  Vec<V> v;
+#pragma unroll
+  for (int i = 0; i < V * (int)sizeof(In) / 4; ++i) {
+    if constexpr (sizeof(In) == 4) v.v[i] = __uint_as_float(r.w[i]);
+    else unpack2(r.w[i], v.v + 2 * i);
+  }
+  return v;
 }
 template <typename In, int V> __device__ __forceinline__ void store_row(In* p, bool vec, int left, const Vec<V>& r) {
   if (vec && left >= V) return store_v<V>(p, r);

@@ -157,9 +157,10 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
     if (p.dt_bias && e < have) bias.v[e] = p.dt_bias[c0 + c + e];
     if (p.D && e < have) skip.v[e] = p.D[c0 + c + e];
   }
-  Vec<E> vx = {}, vd = {}, vz = {}, vg = {};
-  float vb[BC], vc[BC];
-  auto rows = [&](int tile, Vec<E>& ax, Vec<E>& ad, Vec<E>& az, Vec<E>& ag) {
+  using Row = Raw<In, E>;
+  Row rx = {}, rd = {}, rz = {}, rg = {};
+  In rb[BC], rc[BC];
+  auto rows = [&](int tile, Row& ax, Row& ad, Row& az, Row& ag) {
     const int t = tile * kTile + row;
     if (t >= len) return;
     ax = load_row<In, E>(x + (size_t)(tok0 + t) * p.xs, vec, have);
@@ -168,17 +169,18 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
     ag = load_row<In, E>(dy + (size_t)(tok0 + t) * p.C, vec, have);
   };
   auto fetch = [&](int tile) {
-    rows(tile, vx, vd, vz, vg);
+    rows(tile, rx, rd, rz, rg);
 #pragma unroll
     for (int j = 0; j < BC; ++j) {
       const int f = j * 128 + ht, r = tile * kTile + f / NP, s = f % NP;
       const bool ok = r < len && s < p.S;
-      vb[j] = ok ? to_f32(B[(size_t)(tok0 + r) * p.bs + s]) : 0.f;
-      vc[j] = ok ? to_f32(C[(size_t)(tok0 + r) * p.cs + s]) : 0.f;
+      rb[j] = ok ? B[(size_t)(tok0 + r) * p.bs + s] : from_f32<In>(0.f);
+      rc[j] = ok ? C[(size_t)(tok0 + r) * p.cs + s] : from_f32<In>(0.f);
     }
   };
   auto put = [&](int tile, int buf) {
     const bool in = tile * kTile + row < len;
+    const Vec<E> vx = unpack_row<In, E>(rx), vd = unpack_row<In, E>(rd), vz = unpack_row<In, E>(rz), vg = unpack_row<In, E>(rg);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const bool ok = in && e < have;
@@ -191,13 +193,14 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
 #pragma unroll
     for (int j = 0; j < BC; ++j) {
       const int f = j * 128 + ht;
-      s_b[(buf * kTile + f / NP) * NP + f % NP] = vb[j];
-      s_c[(buf * kTile + f / NP) * NP + f % NP] = vc[j];
+      s_b[(buf * kTile + f / NP) * NP + f % NP] = to_f32(rb[j]);
+      s_c[(buf * kTile + f / NP) * NP + f % NP] = to_f32(rc[j]);
     }
   };
-  auto finish = [&](int tile, int buf, const Vec<E>& ax, const Vec<E>& ad, const Vec<E>& az, const Vec<E>& ag) {
+  auto finish = [&](int tile, int buf, const Row& x_in, const Row& d_in, const Row& z_in, const Row& g_in) {
     const int t = tile * kTile + row;
     if (t < len) {
+      const Vec<E> ax = unpack_row<In, E>(x_in), ad = unpack_row<In, E>(d_in), az = unpack_row<In, E>(z_in), ag = unpack_row<In, E>(g_in);
       Vec<E> dx, ddt, dz;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -235,16 +238,18 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
     if (tiles > 1) fetch(tiles - 2);
   }
   __syncthreads();
+  Row ax = {}, ad = {}, az = {}, ag = {};                  // of the tile that is gone through now
 #pragma unroll 1
   for (int i = 0; i <= tiles; ++i) {
-    Vec<E> ax = {}, ad = {}, az = {}, ag = {};
-    if (i > 0) rows(tiles - i, ax, ad, az, ag);
     if (i + 1 < tiles) {
       put(tiles - 2 - i, (i + 1) & 1);
       if (i + 2 < tiles) fetch(tiles - 3 - i);
     }
     if (i > 0) finish(tiles - i, (i - 1) & 1, ax, ad, az, ag);
-    if (i < tiles) __syncthreads();
+    if (i < tiles) {
+      rows(tiles - 1 - i, ax, ad, az, ag);
+      __syncthreads();
+    }
   }
   // over the rows: through the places of the results, which nobody reads any more but the helping warps themselves
   __syncthreads();

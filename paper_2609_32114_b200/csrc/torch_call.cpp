@@ -33,6 +33,18 @@ int (*g_add_norm)(const ha_la_add_norm_args*, void*) = nullptr;
 int (*g_add_norm_backward)(const ha_la_add_norm_args*, void*) = nullptr;
 int (*g_add_norm_bytes)(const ha_la_add_norm_args*, size_t*) = nullptr;
 
+int (*g_conv)(const ha_la_conv_args*, void*) = nullptr;
+int (*g_conv_backward)(const ha_la_conv_args*, void*) = nullptr;
+int (*g_conv_bytes)(const ha_la_conv_args*, size_t*) = nullptr;
+int (*g_conv_decode)(const ha_la_conv_args*, void*) = nullptr;
+int (*g_scan)(const ha_la_scan_args*, void*) = nullptr;
+int (*g_scan_backward)(const ha_la_scan_args*, void*) = nullptr;
+int (*g_scan_bytes)(const ha_la_scan_args*, int, size_t*) = nullptr;
+int (*g_scan_decode)(const ha_la_scan_args*, void*) = nullptr;
+int (*g_latent_prefill)(const ha_la_latent_prefill_args*, void*) = nullptr;
+int (*g_latent_decode)(const ha_la_latent_decode_args*, void*) = nullptr;
+int (*g_latent_decode_bytes)(const ha_la_latent_decode_args*, size_t*) = nullptr;
+
 // a tensor, or nullptr for None; anything else is not ordinary
 bool unpack(PyObject* o, const at::Tensor** t) {
   *t = nullptr;
@@ -100,7 +112,7 @@ struct CallStream {
 
 // The library's entry points, as addresses
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 13) { PyErr_SetString(PyExc_TypeError, "thirteen addresses"); return nullptr; }
+  if (n != 24) { PyErr_SetString(PyExc_TypeError, "twenty-four addresses"); return nullptr; }
   int i = 0;
   auto take = [&](auto& f) { f = reinterpret_cast<std::remove_reference_t<decltype(f)>>(PyLong_AsVoidPtr(a[i++])); };
   take(g_prefill);
@@ -116,6 +128,17 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   take(g_add_norm);
   take(g_add_norm_backward);
   take(g_add_norm_bytes);
+  take(g_conv);
+  take(g_conv_backward);
+  take(g_conv_bytes);
+  take(g_conv_decode);
+  take(g_scan);
+  take(g_scan_backward);
+  take(g_scan_bytes);
+  take(g_scan_decode);
+  take(g_latent_prefill);
+  take(g_latent_decode);
+  take(g_latent_decode_bytes);
   if (PyErr_Occurred()) return nullptr;
   Py_RETURN_NONE;
 }
@@ -250,7 +273,7 @@ bool number(PyObject* o, double* v) {                     // false: not an ordin
 
 // Outputs, scratch and status word of a call: what the caller did not bring is allocated on the call's stream.
 struct Outputs {
-  static constexpr int kMax = 8;
+  static constexpr int kMax = 12;
   c10::cuda::CUDAGuard device;
   CallStream on;
   PyObject* stream;
@@ -562,6 +585,359 @@ PyObject* add_norm_backward_call(PyObject* const* a, Py_ssize_t n) {
   return pack({out.wrap(dx, a[8]), out.wrap(dr, a[9]), out.wrap(dw, a[10]), wp ? out.wrap(dwp, a[11]) : Py_NewRef(Py_None)});
 }
 
+// ---------------------------------------------------------------- mixer.py: short convolution, selective scan, attention over latent rows
+//
+// As above; inputs with a row to a token may be rows of a wider tensor.
+
+// t is [*lead, *inner] of like's type and device, contiguous within a token, tokens at one distance: that distance, in elements
+bool token_rows(const at::Tensor* t, const at::Tensor& like, at::IntArrayRef lead, std::initializer_list<int64_t> inner, int64_t* step) {
+  if (!t || t->scalar_type() != like.scalar_type() || t->device() != like.device() || t->dim() != (int64_t)(lead.size() + inner.size())) return false;
+  const auto size = t->sizes(), stride = t->strides();
+  int64_t d = t->dim() - 1, width = 1;
+  for (auto i = inner.end(); i != inner.begin(); --d) {
+    const int64_t n = *--i;
+    if (size[d] != n || (n != 1 && stride[d] != width)) return false;
+    width *= n;
+  }
+  *step = width;
+  int64_t tokens = 1;
+  for (; d >= 0; --d) {
+    if (size[d] != lead[d]) return false;
+    if (lead[d] > 1) {
+      if (tokens == 1) *step = stride[d];
+      if (stride[d] != *step * tokens) return false;
+    }
+    tokens *= lead[d];
+  }
+  if (tokens == 0) *step = width;
+  return *step >= width;
+}
+// ... [*lead, H, d], contiguous within a head, heads at one distance too
+bool head_rows(const at::Tensor* t, const at::Tensor& like, at::IntArrayRef lead, int64_t H, int64_t* step, int64_t* head, int64_t* d) {
+  if (!t || t->scalar_type() != like.scalar_type() || t->device() != like.device() || t->dim() != (int64_t)lead.size() + 2) return false;
+  const auto size = t->sizes(), stride = t->strides();
+  const int64_t k = lead.size();
+  *d = size[k + 1];
+  if (size[k] != H || *d < 1 || (*d > 1 && stride[k + 1] != 1)) return false;
+  *head = H > 1 ? stride[k] : *d;
+  *step = H * *d;
+  int64_t tokens = 1;
+  for (int64_t i = k - 1; i >= 0; --i) {
+    if (size[i] != lead[i]) return false;
+    if (lead[i] > 1) {
+      if (tokens == 1) *step = stride[i];
+      if (stride[i] != *step * tokens) return false;
+    }
+    tokens *= lead[i];
+  }
+  return tokens > 0 && *head >= *d && *step >= *d;
+}
+bool vector(const at::Tensor* t, const at::Tensor& like, at::IntArrayRef shape) { return !t || same(t, like, at::kFloat, shape); }
+bool offsets(const at::Tensor* cu, const at::Tensor& like, int64_t batch) {
+  return !cu || (plain(cu, at::kInt, 1) && cu->device() == like.device() && batch == 1 && cu->numel() >= 2 && cu->numel() <= INT32_MAX);
+}
+template <typename F, typename A> int without_lock(F f, const A* args, void* stream) {
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = f(args, stream);
+  Py_END_ALLOW_THREADS
+  return rc;
+}
+
+// x [B, T, C] (`token`: [N, C]), w, bias, activation, cu_seqlens
+bool conv_inputs(const at::Tensor* x, const at::Tensor* w, const at::Tensor* bias, PyObject* act, const at::Tensor* cu, bool token, ha_la_conv_args* d, int64_t* N) {
+  if (!element(x) || x->dim() != (token ? 2 : 3) || !w || w->dim() != 2) return false;
+  const auto s = x->sizes();
+  const int64_t B = s[0], T = token ? 1 : s[1], C = s[token ? 1 : 2], K = w->size(1);
+  if (B > INT32_MAX || T > INT32_MAX || C > INT32_MAX || C < 1 || K < 2 || K > 4) return false;
+  if (!same(w, *x, at::kFloat, {C, K}) || !vector(bias, *x, {C}) || !activation_of(act, &d->activation) || !offsets(cu, *x, B)) return false;
+  if (!token_rows(x, *x, s.slice(0, token ? 1 : 2), {C}, &d->x_stride)) return false;
+  d->dtype = x->scalar_type() == at::kFloat;
+  d->batch = (int32_t)B; d->seqlen = (int32_t)T; d->channels = (int32_t)C; d->taps = (int32_t)K;
+  *N = cu ? cu->numel() - 1 : B;
+  d->num_seqs = cu ? (int32_t)*N : 0;
+  d->x = ptr(x); d->w = (const float*)ptr(w); d->bias = (const float*)ptr(bias); d->cu_seqlens = (const int32_t*)ptr(cu);
+  return true;
+}
+
+// conv(x, w, bias, activation, h0, cu_seqlens, max_seqlen, y, hT, want_hT, status_word, stream) -> (y, hT, status_word) | status | None
+PyObject* conv_call(PyObject* const* a, Py_ssize_t n) {
+  if (n != 12 || !g_conv) { PyErr_SetString(PyExc_TypeError, "twelve arguments"); return nullptr; }
+  const at::Tensor *x, *w, *bias, *h0, *cu, *y, *hT, *sw;
+  ha_la_conv_args d{};
+  int64_t N;
+  if (!unpack(a[0], &x) || !unpack(a[1], &w) || !unpack(a[2], &bias) || !unpack(a[4], &h0) || !unpack(a[5], &cu) || !unpack(a[7], &y) || !unpack(a[8], &hT) ||
+      !unpack(a[10], &sw) || !conv_inputs(x, w, bias, a[3], cu, false, &d, &N) || !length(a[6], &d.max_seqlen))
+    Py_RETURN_NONE;
+  const at::ScalarType type = x->scalar_type();
+  const int64_t C = d.channels, K = d.taps - 1;
+  if (!room(h0, *x, type, N * K * C) || !room(y, *x, type, x->numel()) || !room(hT, *x, type, N * K * C) || !room(sw, *x, at::kInt, 1)) Py_RETURN_NONE;
+  const int want = hT ? 0 : PyObject_IsTrue(a[9]);
+  if (want < 0) return nullptr;
+  Outputs out(a[11], *x);
+  if (!out.set()) return nullptr;
+  y = out.take(y, x->sizes(), type);
+  if (want) hT = out.take(hT, {N, K, C}, type);
+  sw = out.take(sw, {1}, at::kInt, true);
+  d.h0 = ptr(h0); d.y = ptr(y); d.hT = ptr(hT); d.status_word = (int32_t*)ptr(sw);
+  const int rc = without_lock(g_conv, &d, out.on.handle);
+  if (rc != HA_LA_OK) return PyLong_FromLong(rc);
+  return pack({out.wrap(y, a[7]), out.wrap(hT, a[8]), out.wrap(sw, a[10])});
+}
+
+// conv_backward(dy, x, w, bias, activation, h0, dhT, cu_seqlens, max_seqlen, dx, dw, db, dh0, want_dh0, workspace, status_word, stream)
+//   -> (dx, dw, db, dh0, status_word, workspace) | status | None
+PyObject* conv_backward_call(PyObject* const* a, Py_ssize_t n) {
+  if (n != 17 || !g_conv_backward) { PyErr_SetString(PyExc_TypeError, "seventeen arguments"); return nullptr; }
+  const at::Tensor *dy, *x, *w, *bias, *h0, *dhT, *cu, *dx, *dw, *db, *dh0, *ws, *sw;
+  ha_la_conv_args d{};
+  int64_t N;
+  if (!unpack(a[0], &dy) || !unpack(a[1], &x) || !unpack(a[2], &w) || !unpack(a[3], &bias) || !unpack(a[5], &h0) || !unpack(a[6], &dhT) || !unpack(a[7], &cu) ||
+      !unpack(a[9], &dx) || !unpack(a[10], &dw) || !unpack(a[11], &db) || !unpack(a[12], &dh0) || !unpack(a[14], &ws) || !unpack(a[15], &sw) ||
+      !conv_inputs(x, w, bias, a[4], cu, false, &d, &N) || !length(a[8], &d.max_seqlen))
+    Py_RETURN_NONE;
+  const at::ScalarType type = x->scalar_type();
+  const int64_t C = d.channels, K = d.taps - 1;
+  if (!same(dy, *x, type, x->sizes()) || !room(h0, *x, type, N * K * C) || !room(dhT, *x, type, N * K * C) || !room(dx, *x, type, x->numel()) ||
+      !room(dw, *x, at::kFloat, C * (K + 1)) || !room(db, *x, at::kFloat, C) || !room(dh0, *x, type, N * K * C) || !scratch_ok(ws, *x) || !room(sw, *x, at::kInt, 1))
+    Py_RETURN_NONE;
+  size_t need = 0;
+  if (g_conv_bytes(&d, &need) != HA_LA_OK) Py_RETURN_NONE;
+  const int want = dh0 ? 0 : PyObject_IsTrue(a[13]);
+  if (want < 0) return nullptr;
+  Outputs out(a[16], *x);
+  if (!out.set()) return nullptr;
+  dx = out.take(dx, x->sizes(), type);
+  dw = out.take(dw, {C, K + 1}, at::kFloat);
+  db = bias ? out.take(db, {C}, at::kFloat) : nullptr;
+  if (want) dh0 = out.take(dh0, {N, K, C}, type);
+  ws = out.scratch(ws, need, &d.workspace, &d.workspace_bytes);
+  sw = out.take(sw, {1}, at::kInt, true);
+  d.h0 = ptr(h0); d.dy = ptr(dy); d.dhT = ptr(dhT); d.dx = ptr(dx); d.dw = (float*)ptr(dw); d.db = (float*)ptr(db); d.dh0 = ptr(dh0);
+  d.status_word = (int32_t*)ptr(sw);
+  const int rc = without_lock(g_conv_backward, &d, out.on.handle);
+  if (rc != HA_LA_OK) return PyLong_FromLong(rc);
+  return pack({out.wrap(dx, a[9]), out.wrap(dw, a[10]), db ? out.wrap(db, a[11]) : Py_NewRef(Py_None), out.wrap(dh0, a[12]), out.wrap(sw, a[15]), out.wrap(ws, a[14])});
+}
+
+// conv_decode(x, w, state, bias, activation, y, state_out, stream) -> (y, state) | status | None
+PyObject* conv_decode_call(PyObject* const* a, Py_ssize_t n) {
+  if (n != 8 || !g_conv_decode) { PyErr_SetString(PyExc_TypeError, "eight arguments"); return nullptr; }
+  const at::Tensor *x, *w, *st, *bias, *y, *so;
+  ha_la_conv_args d{};
+  int64_t N;
+  if (!unpack(a[0], &x) || !unpack(a[1], &w) || !unpack(a[2], &st) || !unpack(a[3], &bias) || !unpack(a[5], &y) || !unpack(a[6], &so) ||
+      !conv_inputs(x, w, bias, a[4], nullptr, true, &d, &N))
+    Py_RETURN_NONE;
+  const at::ScalarType type = x->scalar_type();
+  const int64_t C = d.channels, K = d.taps - 1;
+  if (!room(st, *x, type, N * K * C) || !room(so, *x, type, N * K * C) || !room(y, *x, type, x->numel())) Py_RETURN_NONE;
+  Outputs out(a[7], *x);
+  if (!out.set()) return nullptr;
+  y = out.take(y, x->sizes(), type);
+  const bool in_place = !so && st;
+  if (!so) so = st ? st : out.take(nullptr, {N, K, C}, type);
+  d.h0 = ptr(st); d.y = ptr(y); d.hT = ptr(so);
+  const int rc = without_lock(g_conv_decode, &d, out.on.handle);
+  if (rc != HA_LA_OK) return PyLong_FromLong(rc);
+  return pack({out.wrap(y, a[5]), out.wrap(so, in_place ? a[2] : a[6])});
+}
+
+// x, dt, z [B, T, channels] (`token`: [N, channels]), A, B, C, D, dt_bias, cu_seqlens
+bool scan_inputs(const at::Tensor* x, const at::Tensor* dt, const at::Tensor* A, const at::Tensor* B, const at::Tensor* C, const at::Tensor* D, const at::Tensor* z,
+                 const at::Tensor* bias, PyObject* softplus, const at::Tensor* cu, bool token, ha_la_scan_args* d, int64_t* N) {
+  const int64_t k = token ? 1 : 2;
+  if (!element(x) || x->dim() != k + 1 || !A || A->dim() != 2 || !B || B->dim() != k + 2 || (softplus != Py_True && softplus != Py_False)) return false;
+  const auto s = x->sizes(), lead = s.slice(0, k);
+  const int64_t batch = s[0], T = token ? 1 : s[1], ch = s[k], G = B->size(k), S = B->size(k + 1);
+  if (batch > INT32_MAX || T > INT32_MAX || ch > INT32_MAX || ch < 1 || G < 1 || S < 1 || S > 64 || ch % G) return false;
+  if (!same(A, *x, at::kFloat, {ch, S}) || !vector(D, *x, {ch}) || !vector(bias, *x, {ch}) || !offsets(cu, *x, batch)) return false;
+  if (!token_rows(x, *x, lead, {ch}, &d->x_stride) || !token_rows(dt, *x, lead, {ch}, &d->dt_stride) || !token_rows(B, *x, lead, {G, S}, &d->b_stride) ||
+      !token_rows(C, *x, lead, {G, S}, &d->c_stride) || (z && !token_rows(z, *x, lead, {ch}, &d->z_stride)))
+    return false;
+  d->dtype = x->scalar_type() == at::kFloat;
+  d->batch = (int32_t)batch; d->seqlen = (int32_t)T; d->channels = (int32_t)ch; d->states = (int32_t)S; d->groups = (int32_t)G;
+  d->softplus = softplus == Py_True;
+  *N = cu ? cu->numel() - 1 : batch;
+  d->num_seqs = cu ? (int32_t)*N : 0;
+  d->cu_seqlens = (const int32_t*)ptr(cu);
+  d->x = ptr(x); d->dt = ptr(dt); d->B = ptr(B); d->C = ptr(C); d->z = ptr(z);
+  d->A = (const float*)ptr(A); d->D = (const float*)ptr(D); d->dt_bias = (const float*)ptr(bias);
+  return true;
+}
+
+// scan(x, dt, A, B, C, D, z, dt_bias, softplus, h0, cu_seqlens, max_seqlen, y, hT, want_hT, workspace, status_word, stream) -> (y, hT, status_word, workspace) | status | None
+PyObject* scan_call(PyObject* const* a, Py_ssize_t n) {
+  if (n != 18 || !g_scan) { PyErr_SetString(PyExc_TypeError, "eighteen arguments"); return nullptr; }
+  const at::Tensor *x, *dt, *A, *B, *C, *D, *z, *bias, *h0, *cu, *y, *hT, *ws, *sw;
+  ha_la_scan_args d{};
+  int64_t N;
+  if (!unpack(a[0], &x) || !unpack(a[1], &dt) || !unpack(a[2], &A) || !unpack(a[3], &B) || !unpack(a[4], &C) || !unpack(a[5], &D) || !unpack(a[6], &z) ||
+      !unpack(a[7], &bias) || !unpack(a[9], &h0) || !unpack(a[10], &cu) || !unpack(a[12], &y) || !unpack(a[13], &hT) || !unpack(a[15], &ws) || !unpack(a[16], &sw) ||
+      !scan_inputs(x, dt, A, B, C, D, z, bias, a[8], cu, false, &d, &N) || !length(a[11], &d.max_seqlen))
+    Py_RETURN_NONE;
+  const int64_t ch = d.channels, S = d.states, state = N * ch * S;
+  if (!room(h0, *x, at::kFloat, state) || !room(y, *x, x->scalar_type(), x->numel()) || !room(hT, *x, at::kFloat, state) || !scratch_ok(ws, *x) || !room(sw, *x, at::kInt, 1))
+    Py_RETURN_NONE;
+  size_t need = 0;
+  if (g_scan_bytes(&d, 0, &need) != HA_LA_OK) Py_RETURN_NONE;
+  const int want = hT ? 0 : PyObject_IsTrue(a[14]);
+  if (want < 0) return nullptr;
+  Outputs out(a[17], *x);
+  if (!out.set()) return nullptr;
+  y = out.take(y, x->sizes(), x->scalar_type());
+  if (want) hT = out.take(hT, {N, ch, S}, at::kFloat);
+  ws = out.scratch(ws, need, &d.workspace, &d.workspace_bytes);
+  sw = out.take(sw, {1}, at::kInt, true);
+  d.h0 = (const float*)ptr(h0); d.y = ptr(y); d.hT = (float*)ptr(hT); d.status_word = (int32_t*)ptr(sw);
+  const int rc = without_lock(g_scan, &d, out.on.handle);
+  if (rc != HA_LA_OK) return PyLong_FromLong(rc);
+  return pack({out.wrap(y, a[12]), out.wrap(hT, a[13]), out.wrap(sw, a[16]), out.wrap(ws, a[15])});
+}
+
+// scan_backward(dy, x, dt, A, B, C, D, z, dt_bias, softplus, h0, dhT, cu_seqlens, max_seqlen, dx, ddt, dA, dB, dC, dD, dz, ddt_bias, dh0, want_dh0, workspace,
+//   status_word, stream) -> (dx, ddt, dA, dB, dC, dD, dz, ddt_bias, dh0, status_word, workspace) | status | None
+PyObject* scan_backward_call(PyObject* const* a, Py_ssize_t n) {
+  if (n != 27 || !g_scan_backward) { PyErr_SetString(PyExc_TypeError, "twenty-seven arguments"); return nullptr; }
+  const at::Tensor *dy, *x, *dt, *A, *B, *C, *D, *z, *bias, *h0, *dhT, *cu, *dx, *ddt, *dA, *dB, *dC, *dD, *dz, *dbias, *dh0, *ws, *sw;
+  ha_la_scan_args d{};
+  int64_t N;
+  if (!unpack(a[0], &dy) || !unpack(a[1], &x) || !unpack(a[2], &dt) || !unpack(a[3], &A) || !unpack(a[4], &B) || !unpack(a[5], &C) || !unpack(a[6], &D) ||
+      !unpack(a[7], &z) || !unpack(a[8], &bias) || !unpack(a[10], &h0) || !unpack(a[11], &dhT) || !unpack(a[12], &cu) || !unpack(a[14], &dx) || !unpack(a[15], &ddt) ||
+      !unpack(a[16], &dA) || !unpack(a[17], &dB) || !unpack(a[18], &dC) || !unpack(a[19], &dD) || !unpack(a[20], &dz) || !unpack(a[21], &dbias) || !unpack(a[22], &dh0) ||
+      !unpack(a[24], &ws) || !unpack(a[25], &sw) || !scan_inputs(x, dt, A, B, C, D, z, bias, a[9], cu, false, &d, &N) || !length(a[13], &d.max_seqlen))
+    Py_RETURN_NONE;
+  const at::ScalarType type = x->scalar_type(), f32 = at::kFloat;
+  const int64_t ch = d.channels, S = d.states, state = N * ch * S;
+  if (!same(dy, *x, type, x->sizes()) || !room(h0, *x, f32, state) || !room(dhT, *x, f32, state) || !room(dx, *x, type, x->numel()) || !room(ddt, *x, type, x->numel()) ||
+      !room(dA, *x, f32, ch * S) || !room(dB, *x, type, B->numel()) || !room(dC, *x, type, B->numel()) || !room(dD, *x, f32, ch) || !room(dz, *x, type, x->numel()) ||
+      !room(dbias, *x, f32, ch) || !room(dh0, *x, f32, state) || !scratch_ok(ws, *x) || !room(sw, *x, at::kInt, 1))
+    Py_RETURN_NONE;
+  size_t need = 0;
+  if (g_scan_bytes(&d, 1, &need) != HA_LA_OK) Py_RETURN_NONE;
+  const int want = dh0 ? 0 : PyObject_IsTrue(a[23]);
+  if (want < 0) return nullptr;
+  Outputs out(a[26], *x);
+  if (!out.set()) return nullptr;
+  dx = out.take(dx, x->sizes(), type);
+  ddt = out.take(ddt, x->sizes(), type);
+  dA = out.take(dA, {ch, S}, f32);
+  dB = out.take(dB, B->sizes(), type);
+  dC = out.take(dC, B->sizes(), type);
+  dD = D ? out.take(dD, {ch}, f32) : nullptr;
+  dz = z ? out.take(dz, x->sizes(), type) : nullptr;
+  dbias = bias ? out.take(dbias, {ch}, f32) : nullptr;
+  if (want) dh0 = out.take(dh0, {N, ch, S}, f32);
+  ws = out.scratch(ws, need, &d.workspace, &d.workspace_bytes);
+  sw = out.take(sw, {1}, at::kInt, true);
+  d.h0 = (const float*)ptr(h0); d.dy = ptr(dy); d.dhT = (const float*)ptr(dhT); d.dx = ptr(dx); d.ddt = ptr(ddt); d.dA = (float*)ptr(dA); d.dB = ptr(dB); d.dC = ptr(dC);
+  d.dD = (float*)ptr(dD); d.dz = ptr(dz); d.ddt_bias = (float*)ptr(dbias); d.dh0 = (float*)ptr(dh0); d.status_word = (int32_t*)ptr(sw);
+  const int rc = without_lock(g_scan_backward, &d, out.on.handle);
+  if (rc != HA_LA_OK) return PyLong_FromLong(rc);
+  auto given = [&](const at::Tensor* t, PyObject* o) { return t ? out.wrap(t, o) : Py_NewRef(Py_None); };
+  return pack({out.wrap(dx, a[14]), out.wrap(ddt, a[15]), out.wrap(dA, a[16]), out.wrap(dB, a[17]), out.wrap(dC, a[18]), given(dD, a[19]), given(dz, a[20]),
+               given(dbias, a[21]), out.wrap(dh0, a[22]), out.wrap(sw, a[25]), out.wrap(ws, a[24])});
+}
+
+// scan_decode(x, dt, A, B, C, state, D, z, dt_bias, softplus, y, state_out, stream) -> (y, state) | status | None
+PyObject* scan_decode_call(PyObject* const* a, Py_ssize_t n) {
+  if (n != 13 || !g_scan_decode) { PyErr_SetString(PyExc_TypeError, "thirteen arguments"); return nullptr; }
+  const at::Tensor *x, *dt, *A, *B, *C, *st, *D, *z, *bias, *y, *so;
+  ha_la_scan_args d{};
+  int64_t N;
+  if (!unpack(a[0], &x) || !unpack(a[1], &dt) || !unpack(a[2], &A) || !unpack(a[3], &B) || !unpack(a[4], &C) || !unpack(a[5], &st) || !unpack(a[6], &D) ||
+      !unpack(a[7], &z) || !unpack(a[8], &bias) || !unpack(a[10], &y) || !unpack(a[11], &so) || !scan_inputs(x, dt, A, B, C, D, z, bias, a[9], nullptr, true, &d, &N))
+    Py_RETURN_NONE;
+  const int64_t ch = d.channels, S = d.states, state = N * ch * S;
+  if (!room(st, *x, at::kFloat, state) || !room(so, *x, at::kFloat, state) || !room(y, *x, x->scalar_type(), x->numel())) Py_RETURN_NONE;
+  Outputs out(a[12], *x);
+  if (!out.set()) return nullptr;
+  y = out.take(y, x->sizes(), x->scalar_type());
+  const bool in_place = !so && st;
+  if (!so) so = st ? st : out.take(nullptr, {N, ch, S}, at::kFloat);
+  d.h0 = (const float*)ptr(st); d.y = ptr(y); d.hT = (float*)ptr(so);
+  const int rc = without_lock(g_scan_decode, &d, out.on.handle);
+  if (rc != HA_LA_OK) return PyLong_FromLong(rc);
+  return pack({out.wrap(y, a[10]), out.wrap(so, in_place ? a[5] : a[11])});
+}
+
+// latent_prefill(q, kn, kr, v, scale, cu_seqlens, cu_seqlens_k, max_seqlen, o, lse, status_word, stream) -> (o, lse, status_word) | status | None
+PyObject* latent_prefill_call(PyObject* const* a, Py_ssize_t n) {
+  if (n != 12 || !g_latent_prefill) { PyErr_SetString(PyExc_TypeError, "twelve arguments"); return nullptr; }
+  const at::Tensor *q, *kn, *kr, *v, *cu, *cuk, *o, *lse, *sw;
+  ha_la_latent_prefill_args d{};
+  double scale;
+  if (!unpack(a[0], &q) || !unpack(a[1], &kn) || !unpack(a[2], &kr) || !unpack(a[3], &v) || !unpack(a[5], &cu) || !unpack(a[6], &cuk) || !unpack(a[8], &o) ||
+      !unpack(a[9], &lse) || !unpack(a[10], &sw) || !number(a[4], &scale) || !length(a[7], &d.max_seqlen) || !element(q) || q->dim() != 4 || !kr || kr->dim() != 3 ||
+      (!cu && cuk))
+    Py_RETURN_NONE;
+  const auto qs = q->sizes();
+  const int64_t B = qs[0], T = qs[1], H = qs[2], dq = qs[3], Tk = kr->size(1), dr = kr->size(2), keys[2] = {B, Tk};
+  if (B > INT32_MAX || T > INT32_MAX || Tk > INT32_MAX || H > INT32_MAX || H < 1 || dr >= dq || dq > 4096 || !offsets(cu, *q, B)) Py_RETURN_NONE;
+  if (cu && !cuk) {
+    if (Tk != T) Py_RETURN_NONE;
+    cuk = cu;
+  }
+  int64_t dn, dv;
+  const at::IntArrayRef lead_k(keys, 2);
+  if (!token_rows(q, *q, qs.slice(0, 2), {H, dq}, &d.q_stride) || !token_rows(kr, *q, lead_k, {dr}, &d.kr_stride) ||
+      !head_rows(kn, *q, lead_k, H, &d.kn_stride, &d.kn_head_stride, &dn) || !head_rows(v, *q, lead_k, H, &d.v_stride, &d.v_head_stride, &dv) || dn + dr != dq ||
+      (cuk && !same(cuk, *q, at::kInt, cu->sizes())) || dv > 4096 || !room(o, *q, q->scalar_type(), B * T * H * dv) || !room(lse, *q, at::kFloat, B * T * H) ||
+      !room(sw, *q, at::kInt, 1))
+    Py_RETURN_NONE;
+  d.dtype = q->scalar_type() == at::kFloat;
+  d.batch = (int32_t)B; d.seqlen = (int32_t)T; d.seqlen_k = (int32_t)Tk; d.num_heads = (int32_t)H;
+  d.d_nope = (int32_t)dn; d.d_rope = (int32_t)dr; d.d_v = (int32_t)dv; d.scale = (float)scale;
+  d.num_seqs = cu ? (int32_t)(cu->numel() - 1) : 0;
+  Outputs out(a[11], *q);
+  if (!out.set()) return nullptr;
+  o = out.take(o, {B, T, H, dv}, q->scalar_type());
+  lse = out.take(lse, {B, T, H}, at::kFloat);
+  sw = out.take(sw, {1}, at::kInt, true);
+  d.cu_seqlens = (const int32_t*)ptr(cu); d.cu_seqlens_k = (const int32_t*)ptr(cuk);
+  d.q = ptr(q); d.kn = ptr(kn); d.kr = ptr(kr); d.v = ptr(v); d.o = ptr(o); d.lse = (float*)ptr(lse); d.status_word = (int32_t*)ptr(sw);
+  const int rc = without_lock(g_latent_prefill, &d, out.on.handle);
+  if (rc != HA_LA_OK) return PyLong_FromLong(rc);
+  return pack({out.wrap(o, a[8]), out.wrap(lse, a[9]), out.wrap(sw, a[10])});
+}
+
+// latent_decode(q, cache, page_table, lengths, scale, o, lse, d_latent, workspace, status_word, stream) -> (o, lse, status_word, workspace) | status | None
+PyObject* latent_decode_call(PyObject* const* a, Py_ssize_t n) {
+  if (n != 11 || !g_latent_decode) { PyErr_SetString(PyExc_TypeError, "eleven arguments"); return nullptr; }
+  const at::Tensor *q, *cache, *table, *lengths, *o, *lse, *ws, *sw;
+  ha_la_latent_decode_args d{};
+  double scale;
+  if (!unpack(a[0], &q) || !unpack(a[1], &cache) || !unpack(a[2], &table) || !unpack(a[3], &lengths) || !unpack(a[5], &o) || !unpack(a[6], &lse) ||
+      !unpack(a[8], &ws) || !unpack(a[9], &sw) || !number(a[4], &scale) || !element(q) || q->dim() != 4 || !q->is_contiguous() || !cache || cache->dim() != 3 ||
+      !table || table->dim() != 2 || (a[7] != Py_None && !length(a[7], &d.d_latent)))
+    Py_RETURN_NONE;
+  const int64_t N = q->size(0), T = q->size(1), H = q->size(2), D = q->size(3), P = cache->size(0), page = cache->size(1), M = table->size(1);
+  if (N > INT32_MAX || T > INT32_MAX || H > INT32_MAX || D > 4096 || P > INT32_MAX || page > INT32_MAX || M > INT32_MAX || T < 1 || H < 1 || page < 1 || (page & (page - 1)))
+    Py_RETURN_NONE;
+  if (a[7] == Py_None) d.d_latent = (int32_t)D - 64;
+  if (d.d_latent < 1 || d.d_latent > D) Py_RETURN_NONE;
+  const int64_t dl = d.d_latent;
+  if (!same(cache, *q, q->scalar_type(), {P, page, D}) || !same(table, *q, at::kInt, {N, M}) || !same(lengths, *q, at::kInt, {N}) ||
+      !room(o, *q, q->scalar_type(), N * T * H * dl) || !room(lse, *q, at::kFloat, N * T * H) || !scratch_ok(ws, *q) || !room(sw, *q, at::kInt, 1))
+    Py_RETURN_NONE;
+  d.dtype = q->scalar_type() == at::kFloat;
+  d.num_seqs = (int32_t)N; d.new_tokens = (int32_t)T; d.num_heads = (int32_t)H; d.d_rope = (int32_t)(D - dl);
+  d.page_size = (int32_t)page; d.num_pages = (int32_t)P; d.max_pages = (int32_t)M; d.scale = (float)scale;
+  size_t need = 0;
+  Outputs out(a[10], *q);                                  // (the workspace is for the device's SMs)
+  if (!out.set()) return nullptr;
+  if (g_latent_decode_bytes(&d, &need) != HA_LA_OK) Py_RETURN_NONE;
+  o = out.take(o, {N, T, H, dl}, q->scalar_type());
+  lse = out.take(lse, {N, T, H}, at::kFloat);
+  ws = out.scratch(ws, need, &d.workspace, &d.workspace_bytes);
+  sw = out.take(sw, {1}, at::kInt, true);
+  d.q = ptr(q); d.cache = ptr(cache); d.page_table = (const int32_t*)ptr(table); d.lengths = (const int32_t*)ptr(lengths);
+  d.o = ptr(o); d.lse = (float*)ptr(lse); d.status_word = (int32_t*)ptr(sw);
+  const int rc = without_lock(g_latent_decode, &d, out.on.handle);
+  if (rc != HA_LA_OK) return PyLong_FromLong(rc);
+  return pack({out.wrap(o, a[5]), out.wrap(lse, a[6]), out.wrap(sw, a[9]), out.wrap(ws, a[8])});
+}
+
 // torch's C++ calls throw (no memory, no driver, a tensor without storage).  An exception that left these functions would go
 // through the interpreter's C frames and end the process; torch's own translation gives the caller the type that the same
 // call raises in Python.
@@ -583,6 +959,14 @@ PyMethodDef kMethods[] = {
     {"gated_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&guarded<gated_norm_backward_call>)), METH_FASTCALL, nullptr},
     {"add_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&guarded<add_norm_call>)), METH_FASTCALL, nullptr},
     {"add_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&guarded<add_norm_backward_call>)), METH_FASTCALL, nullptr},
+    {"conv", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&guarded<conv_call>)), METH_FASTCALL, nullptr},
+    {"conv_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&guarded<conv_backward_call>)), METH_FASTCALL, nullptr},
+    {"conv_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&guarded<conv_decode_call>)), METH_FASTCALL, nullptr},
+    {"scan", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&guarded<scan_call>)), METH_FASTCALL, nullptr},
+    {"scan_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&guarded<scan_backward_call>)), METH_FASTCALL, nullptr},
+    {"scan_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&guarded<scan_decode_call>)), METH_FASTCALL, nullptr},
+    {"latent_prefill", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&guarded<latent_prefill_call>)), METH_FASTCALL, nullptr},
+    {"latent_decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&guarded<latent_decode_call>)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "ha_la_torch_call", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -211,6 +211,11 @@ def ha_la_conv(x, w, *, bias=None, activation="silu", h0=None, cu_seqlens=None, 
     Returns (y, hT, status_word): hT the last taps - 1 inputs of each sequence (None if not wanted); a status word other than 0 reports lengths
     that do not fit.
     """
+    r = binding._native().conv(x, w, bias, _ACTIVATIONS.get(activation), h0, cu_seqlens, max_seqlen, y, hT, want_hT, status_word, stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        raise HaLaError(r, "ha_la_conv")
     import torch
 
     args, N, C, K = _conv_args("ha_la_conv", x, w, bias, activation, cu_seqlens, max_seqlen)
@@ -232,6 +237,12 @@ def ha_la_conv_backward(dy, x, w, *, bias=None, activation="silu", h0=None, dhT=
 
     Returns (dx, dw, db, dh0, status_word, workspace); db is None without a bias, dh0 if it is not wanted.
     """
+    r = binding._native().conv_backward(dy, x, w, bias, _ACTIVATIONS.get(activation), h0, dhT, cu_seqlens, max_seqlen, dx, dw, db, dh0, want_dh0,
+                                        workspace, status_word, stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        raise HaLaError(r, "ha_la_conv_backward")
     import torch
 
     args, N, C, K = _conv_args("ha_la_conv_backward", x, w, bias, activation, cu_seqlens, max_seqlen)
@@ -258,6 +269,11 @@ def ha_la_conv_decode(x, w, state, *, bias=None, activation="silu", y=None, stat
     x : [N, C]    state : [N, taps - 1, C], the last inputs, oldest first, or None (zeros)
     The new state goes to state_out (default: in place into state; allocated when that is None).  Returns (y, new state).
     """
+    r = binding._native().conv_decode(x, w, state, bias, _ACTIVATIONS.get(activation), y, state_out, stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        raise HaLaError(r, "ha_la_conv_decode")
     args, _, C, K = _conv_args("ha_la_conv_decode", x, w, bias, activation, None, 0, (2,))
     N = x.shape[0]
     for name, t, n in (("state", state, N * K * C), ("state_out", state_out, N * K * C), ("y", y, x.numel())):
@@ -302,6 +318,11 @@ def ha_la_scan(x, dt, A, B, C, *, D=None, z=None, dt_bias=None, softplus=True, h
     which has to be >= 0    h0 : fp32 [N, channels, S] or None (zeros)    cu_seqlens, max_seqlen : as in ha_la_conv
     Returns (y, hT, status_word, workspace); hT is None if not wanted.  workspace and status_word may be handed in again, for one call at a time.
     """
+    r = binding._native().scan(x, dt, A, B, C, D, z, dt_bias, softplus, h0, cu_seqlens, max_seqlen, y, hT, want_hT, workspace, status_word, stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        raise HaLaError(r, "ha_la_scan")
     import torch
 
     args, N, ch, S = _scan_args("ha_la_scan", x, dt, A, B, C, D, z, dt_bias, softplus, cu_seqlens, max_seqlen)
@@ -327,6 +348,12 @@ def ha_la_scan_backward(dy, x, dt, A, B, C, *, D=None, z=None, dt_bias=None, sof
     Returns (dx, ddt, dA, dB, dC, dD, dz, ddt_bias, dh0, status_word, workspace); dD, dz and ddt_bias are None without D, z and dt_bias, dh0 if it is
     not wanted.
     """
+    r = binding._native().scan_backward(dy, x, dt, A, B, C, D, z, dt_bias, softplus, h0, dhT, cu_seqlens, max_seqlen, dx, ddt, dA, dB, dC, dD, dz,
+                                        ddt_bias, dh0, want_dh0, workspace, status_word, stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        raise HaLaError(r, "ha_la_scan_backward")
     import torch
 
     args, N, ch, S = _scan_args("ha_la_scan_backward", x, dt, A, B, C, D, z, dt_bias, softplus, cu_seqlens, max_seqlen)
@@ -361,6 +388,11 @@ def ha_la_scan_decode(x, dt, A, B, C, state, *, D=None, z=None, dt_bias=None, so
     x, dt, z : [N, channels]    B, C : [N, groups, S]    state : fp32 [N, channels, S] or None (zeros)
     The new state goes to state_out (default: in place into state; allocated when that is None).  Returns (y, new state).
     """
+    r = binding._native().scan_decode(x, dt, A, B, C, state, D, z, dt_bias, softplus, y, state_out, stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        raise HaLaError(r, "ha_la_scan_decode")
     import torch
 
     args, _, ch, S = _scan_args("ha_la_scan_decode", x, dt, A, B, C, D, z, dt_bias, softplus, None, 0, (2,))
@@ -412,6 +444,11 @@ def ha_la_latent_prefill(q, kn, kr, v, *, scale=1.0, cu_seqlens=None, cu_seqlens
     (None: the queries')    max_seqlen : bound on a sequence's queries, 0 = T
     Returns (o, lse, status_word): o [B, T, H, d_v], lse fp32 [B, T, H], the logarithm of the sum of e^s; a query without a key has 0 and -infinity.
     """
+    r = binding._native().latent_prefill(q, kn, kr, v, scale, cu_seqlens, cu_seqlens_k, max_seqlen, o, lse, status_word, stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        raise HaLaError(r, "ha_la_latent_prefill")
     import torch
 
     _cuda(q, "ha_la_latent_prefill")
@@ -464,6 +501,11 @@ def ha_la_latent_decode(q, cache, page_table, lengths, *, scale=1.0, o=None, lse
     Returns (o, lse, status_word, workspace): o [N, new, H, d_latent], lse fp32 [N, new, H]; a token without a row has 0 and -infinity.
     A status word other than 0 reports a length or a page that does not exist.
     """
+    r = binding._native().latent_decode(q, cache, page_table, lengths, scale, o, lse, d_latent, workspace, status_word, stream)
+    if r.__class__ is tuple:
+        return r
+    if r is not None:
+        raise HaLaError(r, "ha_la_latent_decode")
     import torch
 
     _cuda(q, "ha_la_latent_decode")
