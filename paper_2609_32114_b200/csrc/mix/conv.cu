@@ -1,8 +1,7 @@
 // Short causal convolution per channel (ha_la_conv* in ha_la.h): y_t = act(bias + sum_j w[j] x_{t-K+1+j}), K = 2, 3 or 4.
 //
 // One read of x and one write of y are all that has to move, and 2 K operations a value are nothing beside it, so HBM bounds it.  A thread
-// has V channels (16 bytes forward, 8 backward, where registers for the sums of dw take the room) of a run of consecutive tokens: the K - 1
-// inputs in front stay in registers from token to token, only a run's first ones are read twice.  A run is taken apart at sequence
+// has V channels (8 bytes) of a run of consecutive tokens: the K - 1 inputs in front stay in registers from token to token, only a run's first ones are read twice.  A run is taken apart at sequence
 // starts, in front of which h0's inputs stand, so the inner loops know no boundaries.
 //
 // Backwards, with p_t the sum ahead of the activation (made again), e_t = dy_t act'(p_t):
@@ -10,8 +9,10 @@
 // the K - 1 tokens behind a run are read again for their e.  Sums over tokens: a run in registers, runs by a second kernel in 64 bits and
 // in order, so the same bits every time.
 #include <algorithm>
+#include <type_traits>
 
 #include "mix.cuh"
+#include "../tc_mma.cuh"
 
 namespace ha_la {
 namespace mix {
@@ -29,8 +30,51 @@ struct ConvParams {
 };
 
 constexpr int kThreads = 128;
+constexpr int kBytes = 8;                                  // of a token to a thread: with 16 the taps' registers leave too few warps (prompts 261 us for 223)
 
-template <int K, int V> struct Taps { float w[K][V], b[V]; };
+// A thread's values of a token as they are in memory: nothing waits for them until they are unpacked.
+template <typename In, int V> struct Piece { In v[V]; };
+template <typename In, int V> __device__ __forceinline__ Piece<In, V> fetch(const In* p) {
+  constexpr int B = V * sizeof(In);
+  Piece<In, V> r;
+  if constexpr (B == kBytes) *reinterpret_cast<uint2*>(&r) = *reinterpret_cast<const uint2*>(p);
+  else r.v[0] = *p;
+  return r;
+}
+template <typename In, int V> __device__ __forceinline__ Vec<V> unpack(const Piece<In, V>& r) {
+  Vec<V> x;
+#pragma unroll
+  for (int v = 0; v < V; ++v) x.v[v] = to_f32(r.v[v]);
+  return x;
+}
+
+// A thread's pieces of the tokens ahead, in shared memory by asynchronous copies: kRing batches of U tokens, whose places nobody else looks at.  In registers they
+// would take so many that too few warps were left to wait for them (16384 tokens x 4096 channels: 140 us, and 107 this way with a branch-free loop).
+constexpr int kRing = 4;
+__device__ __forceinline__ void copy8(uint8_t* to, const void* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to))), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 2) : "memory"); }
+
+// a b + c, two values to an instruction
+template <int V> __device__ __forceinline__ Vec<V> fma_v(const Vec<V>& a, const Vec<V>& b, const Vec<V>& c) {
+  Vec<V> r;
+  if constexpr (V % 2 == 0) {
+#pragma unroll
+    for (int v = 0; v < V; v += 2) {
+      const float2 x = ptx::fma2(make_float2(a.v[v], a.v[v + 1]), make_float2(b.v[v], b.v[v + 1]), make_float2(c.v[v], c.v[v + 1]));
+      r.v[v] = x.x;
+      r.v[v + 1] = x.y;
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) r.v[v] = fmaf(a.v[v], b.v[v], c.v[v]);
+  }
+  return r;
+}
+
+template <int K, int V> struct Taps { Vec<V> w[K], b; };
 
 template <int K, int V> __device__ __forceinline__ void load_taps(Taps<K, V>& t, const ConvParams& p, int c) {
   constexpr int L = V >= 4 ? 4 : V;                        // (a thread's K V weights lie together)
@@ -41,14 +85,13 @@ template <int K, int V> __device__ __forceinline__ void load_taps(Taps<K, V>& t,
 #pragma unroll
     for (int l = 0; l < L; ++l) flat[i + l] = w.v[l];
   }
-  Vec<V> b = {};
-  if (p.bias) b = load_v<V>(p.bias + c);
+  Vec<V> none = {};
+  t.b = none;
+  if (p.bias) t.b = load_v<V>(p.bias + c);
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
+  for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int j = 0; j < K; ++j) t.w[j][v] = flat[v * K + j];
-    t.b[v] = b.v[v];
-  }
+    for (int j = 0; j < K; ++j) t.w[j].v[v] = flat[v * K + j];
 }
 
 // The input at position `pos` of the sequence, which may lie in front of it.
@@ -60,15 +103,10 @@ template <typename In, int K, int V> __device__ __forceinline__ Vec<V> input_at(
 }
 
 template <int K, int V> __device__ __forceinline__ Vec<V> sum_of(const Taps<K, V>& t, const Vec<V> (&win)[K - 1], const Vec<V>& x) {
-  Vec<V> s;
+  Vec<V> s = t.b;
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    s.v[v] = t.b[v];
-#pragma unroll
-    for (int j = 0; j < K - 1; ++j) s.v[v] = fmaf(t.w[j][v], win[j].v[v], s.v[v]);
-    s.v[v] = fmaf(t.w[K - 1][v], x.v[v], s.v[v]);
-  }
-  return s;
+  for (int j = 0; j < K - 1; ++j) s = fma_v<V>(t.w[j], win[j], s);
+  return fma_v<V>(t.w[K - 1], x, s);
 }
 
 template <int K, int V> __device__ __forceinline__ void push(Vec<V> (&win)[K - 1], const Vec<V>& x) {
@@ -100,7 +138,7 @@ template <typename In, int K, int V> __device__ __forceinline__ void last_inputs
 
 template <typename In, int K, int V, bool SILU>
 __global__ void __launch_bounds__(kThreads) conv_kernel(ConvParams p) {
-  constexpr int U = 4;                                     // tokens whose loads are in flight together
+  constexpr int U = 8;                                     // tokens whose loads are in flight together (four: 266 us for 223, sixteen: 255)
   const int row = blockIdx.x / p.groups, c = ((blockIdx.x - row * p.groups) * kThreads + threadIdx.x) * V;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -135,11 +173,11 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(ConvParams p) {
       push<K, V>(win, now);
     };
     for (; t + U <= end; t += U) {
-      Vec<V> in[U];
+      Piece<In, V> in[U];
 #pragma unroll
-      for (int i = 0; i < U; ++i) in[i] = load_v<V>(x + (size_t)(t + i) * p.stride);
+      for (int i = 0; i < U; ++i) in[i] = fetch<In, V>(x + (size_t)(t + i) * p.stride);
 #pragma unroll
-      for (int i = 0; i < U; ++i) token(t + i, in[i]);
+      for (int i = 0; i < U; ++i) token(t + i, unpack<In, V>(in[i]));
     }
     for (; t < end; ++t) token(t, load_v<V>(x + (size_t)t * p.stride));
   }
@@ -175,7 +213,7 @@ template <typename In, int K, int V, bool SILU> __device__ __forceinline__ void 
     for (int j = 0; j < K - 1; ++j)                        // tap j of token u reads place u + j of what lies in front
       if (u + j < K - 1) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) d[u + j].v[v] = fmaf(taps.w[j][v], e.v[v], d[u + j].v[v]);
+        for (int v = 0; v < V; ++v) d[u + j].v[v] = fmaf(taps.w[j].v[v], e.v[v], d[u + j].v[v]);
       }
   }
 #pragma unroll
@@ -208,7 +246,7 @@ __global__ void __launch_bounds__(kThreads) conv_back_kernel(ConvParams p) {
   load_taps<K, V>(taps, p, c);
   const In *x = reinterpret_cast<const In*>(p.x) + c, *dy = reinterpret_cast<const In*>(p.dy) + c;
   In* dx = reinterpret_cast<In*>(p.dx) + c;
-  float dw[K][V] = {}, db[V] = {};
+  Vec<V> dw[K] = {}, db = {};
   while (t < t1) {
     Seq q = seq_of(p.seqs, n);
     while (n + 1 < p.seqs.N && q.len >= 0 && q.tok0 + q.len <= t) q = seq_of(p.seqs, ++n);
@@ -226,37 +264,58 @@ __global__ void __launch_bounds__(kThreads) conv_back_kernel(ConvParams p) {
       store_v<V>(dx + (size_t)at * p.C, a);
     };
     const int first = t;
-    auto token = [&](int u, const Vec<V>& now, Vec<V> e) {
+    // (`inside`: one of the run's own tokens with K - 1 of the run in front of it, which is most of them, without a branch)
+    auto token = [&](auto inside, int u, const Vec<V>& now, Vec<V> e) {
       through_act<V, SILU>(e, sum_of<K, V>(taps, win, now));
-      if (u < mine) {
+      if (inside.value || u < mine) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          db[v] += e.v[v];
+        for (int j = 0; j < K - 1; ++j) dw[j] = fma_v<V>(e, win[j], dw[j]);
+        dw[K - 1] = fma_v<V>(e, now, dw[K - 1]);
 #pragma unroll
-          for (int j = 0; j < K - 1; ++j) dw[j][v] = fmaf(e.v[v], win[j].v[v], dw[j][v]);
-          dw[K - 1][v] = fmaf(e.v[v], now.v[v], dw[K - 1][v]);
-        }
+        for (int v = 0; v < V; ++v) db.v[v] += e.v[v];
       }
       push<K, V>(win, now);
 #pragma unroll
-      for (int j = K - 1; j >= 0; --j) {
+      for (int j = K - 1; j > 0; --j) acc[j] = fma_v<V>(taps.w[K - 1 - j], e, acc[j - 1]);
 #pragma unroll
-        for (int v = 0; v < V; ++v) acc[j].v[v] = fmaf(taps.w[K - 1 - j][v], e.v[v], j ? acc[j - 1].v[v] : 0.f);
-      }
-      if (u - (K - 1) >= first) emit(u - (K - 1), acc[K - 1]);
+      for (int v = 0; v < V; ++v) acc[0].v[v] = taps.w[K - 1].v[v] * e.v[v];
+      if (inside.value || u - (K - 1) >= first) store_v<V>(dx + (size_t)(u - (K - 1)) * p.C, acc[K - 1]);
     };
     int u = t;
-    for (; u + U <= last; u += U) {
-      Vec<V> in[U], d[U];
+    if constexpr (V * sizeof(In) == kBytes) {
+      __shared__ __align__(16) uint8_t ring[kRing * U * 2][kThreads][8];
+      auto send = [&](int b) {
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        in[i] = load_v<V>(x + (size_t)(u + i) * p.stride);
-        d[i] = load_v<V>(dy + (size_t)(u + i) * p.C);
+        for (int i = 0; i < U; ++i) {
+          const int at = first + b * U + i, place = (b % kRing * U + i) * 2;
+          if (at < last) {
+            copy8(ring[place][threadIdx.x], x + (size_t)at * p.stride);
+            copy8(ring[place + 1][threadIdx.x], dy + (size_t)at * p.C);
+          }
+        }
+        copies_sent();
+      };
+      for (int b = 0; b < kRing - 1; ++b) send(b);
+#pragma unroll 1
+      for (int b = 0; u < last; ++b) {
+        copies_wait();
+        auto from_ring = [&](auto inside, int i) {
+          const int place = (b % kRing * U + i) * 2;
+          token(inside, u + i, unpack<In, V>(fetch<In, V>(reinterpret_cast<const In*>(ring[place][threadIdx.x]))),
+                unpack<In, V>(fetch<In, V>(reinterpret_cast<const In*>(ring[place + 1][threadIdx.x]))));
+        };
+        if (b > 0 && u + U <= mine) {
+#pragma unroll
+          for (int i = 0; i < U; ++i) from_ring(std::true_type(), i);
+        } else {
+#pragma unroll 1
+          for (int i = 0; i < U && u + i < last; ++i) from_ring(std::false_type(), i);
+        }
+        u += U;
+        send(b + kRing - 1);
       }
-#pragma unroll
-      for (int i = 0; i < U; ++i) token(u + i, in[i], d[i]);
     }
-    for (; u < last; ++u) token(u, load_v<V>(x + (size_t)u * p.stride), load_v<V>(dy + (size_t)u * p.C));
+    for (; u < last; ++u) token(std::false_type(), u, load_v<V>(x + (size_t)u * p.stride), load_v<V>(dy + (size_t)u * p.C));
 #pragma unroll
     for (int j = K - 2; j >= 0; --j)                       // (the tokens that no later one of the sequence follows K - 1 behind)
       if (last - 1 - j >= first && last - 1 - j < mine) emit(last - 1 - j, acc[j]);
@@ -266,8 +325,8 @@ __global__ void __launch_bounds__(kThreads) conv_back_kernel(ConvParams p) {
 #pragma unroll
   for (int v = 0; v < V; ++v) {
 #pragma unroll
-    for (int j = 0; j < K; ++j) part[(size_t)j * p.C + v] = dw[j][v];
-    part[(size_t)K * p.C + v] = db[v];
+    for (int j = 0; j < K; ++j) part[(size_t)j * p.C + v] = dw[j].v[v];
+    part[(size_t)K * p.C + v] = db.v[v];
   }
 }
 
@@ -311,8 +370,7 @@ __global__ void __launch_bounds__(kThreads) conv_decode_kernel(ConvParams p) {
 enum Form { kForward, kBackward, kToken };
 
 template <typename In, int K, int V, bool SILU> cudaError_t launch(Form f, const ConvParams& p, long long grid, cudaStream_t stream) {
-  constexpr int VB = V > 1 ? V / 2 : 1;
-  void (*k)(ConvParams) = f == kForward ? conv_kernel<In, K, V, SILU> : f == kBackward ? conv_back_kernel<In, K, VB, SILU> : conv_decode_kernel<In, K, V, SILU>;
+  void (*k)(ConvParams) = f == kForward ? conv_kernel<In, K, V, SILU> : f == kBackward ? conv_back_kernel<In, K, V, SILU> : conv_decode_kernel<In, K, V, SILU>;
   return start(k, dim3((unsigned)grid), kThreads, 0, stream, p);
 }
 template <typename In, int V> cudaError_t launch_taps(Form f, int K, bool silu, const ConvParams& p, long long grid, cudaStream_t stream) {
@@ -323,11 +381,12 @@ template <typename In, int V> cudaError_t launch_taps(Form f, int K, bool silu, 
   }
 }
 
-// Tokens to a run.  Long ones read less twice and leave fewer sums, short ones give the SMs something to do: aim at 8 (forward) and 12 warps an SM.
+// Tokens to a run.  Short ones give the SMs something to do; long ones read less twice and, backward, leave fewer sums, all of them at once on the SMs
+// (4 CTAs each: 107 us; 1.4 rounds of them 137).
 int run_of(long long tokens, int C, int V, bool back) {
-  const long long warps = (C + 32 * V - 1) / (32 * V), want = (long long)sm_count() * (back ? 12 : 16);
-  long long run = tokens * warps / want;
-  return (int)std::min<long long>(std::max<long long>(run, back ? 8 : 4), back ? 128 : 32);
+  const long long warps = (C + 32 * V - 1) / (32 * V), want = (long long)sm_count() * (back ? 16 : 32);
+  const long long run = tokens * warps / want + back;
+  return (int)std::min<long long>(std::max<long long>(run, back ? 8 : 4), back ? 512 : 32);
 }
 
 int check(const ha_la_conv_args* a, ConvParams* p, bool packed_ok) {
@@ -348,11 +407,11 @@ int check(const ha_la_conv_args* a, ConvParams* p, bool packed_ok) {
   return HA_LA_OK;
 }
 
-// Values to a thread: 16 bytes forward and 8 backward, if every token of every tensor starts so aligned, else one.
+// Values to a thread: kBytes, if every token of every tensor starts on a 16-byte boundary, else one.
 int width_of(const ha_la_conv_args* a, const ConvParams& p, bool back) {
-  const int e = a->dtype == HA_LA_BF16 ? 2 : 4, V = a->dtype == HA_LA_BF16 ? (back ? 4 : 8) : (back ? 2 : 4);
-  const uintptr_t at = any_of(a->x, a->h0, back ? a->dy : nullptr, back ? a->dhT : nullptr, back ? a->dx : a->y, back ? a->dh0 : a->hT);
-  return at % (V * e) == 0 && any_of(a->w, a->bias) % 16 == 0 && p.C % V == 0 && p.stride % V == 0 ? V : 1;
+  const int e = a->dtype == HA_LA_BF16 ? 2 : 4;
+  const uintptr_t at = any_of(a->x, a->h0, a->w, a->bias, back ? a->dy : nullptr, back ? a->dhT : nullptr, back ? a->dx : a->y, back ? a->dh0 : a->hT);
+  return at % 16 == 0 && (p.C | p.stride) * e % 16 == 0 ? kBytes / e : 1;
 }
 
 void shape(ConvParams* p, int V, bool back) {
@@ -364,7 +423,7 @@ void shape(ConvParams* p, int V, bool back) {
 // The workspace is for the narrow threads too, whatever the pointers are: the most runs that either has.
 size_t part_bytes(const ha_la_conv_args* a, ConvParams p) {
   int most = 0;
-  for (int V : {a->dtype == HA_LA_BF16 ? 4 : 2, 1}) {
+  for (int V : {kBytes / (a->dtype == HA_LA_BF16 ? 2 : 4), 1}) {
     shape(&p, V, true);
     most = std::max(most, p.runs);
   }
@@ -397,9 +456,9 @@ int run(const ha_la_conv_args* a, Form f, cudaStream_t stream) {
   const bool silu = a->activation == HA_LA_ACT_SILU;
   if (grid > 0) {
     if (a->dtype == HA_LA_BF16)
-      e = V > 1 ? launch_taps<__nv_bfloat16, 8>(f, a->taps, silu, p, grid, stream) : launch_taps<__nv_bfloat16, 1>(f, a->taps, silu, p, grid, stream);
+      e = V > 1 ? launch_taps<__nv_bfloat16, 4>(f, a->taps, silu, p, grid, stream) : launch_taps<__nv_bfloat16, 1>(f, a->taps, silu, p, grid, stream);
     else
-      e = V > 1 ? launch_taps<float, 4>(f, a->taps, silu, p, grid, stream) : launch_taps<float, 1>(f, a->taps, silu, p, grid, stream);
+      e = V > 1 ? launch_taps<float, 2>(f, a->taps, silu, p, grid, stream) : launch_taps<float, 1>(f, a->taps, silu, p, grid, stream);
   }
   if (e == cudaSuccess && back) {
     const long long per = (long long)p.C * (a->taps + 1);
