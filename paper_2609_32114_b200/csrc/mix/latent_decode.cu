@@ -9,7 +9,8 @@
 // query's maximum is spread over 64 threads: they take the exact one for a segment's first rows and whenever a score exceeds it by 2^8 (one vote), and
 // each adds up its own weights until the end.
 // The scores of the next 64 rows are made ahead of the products with these rows' values, and shared memory holds two to two and a half such tiles: copies are
-// under way all the time.  (128 rows at a time, of which shared memory holds one and a quarter: 124 us for the 64 contexts below instead of NEW_US.)
+// under way all the time.  (64 contexts of 500 to 16000 rows, 32 heads: 122 us a call; 128 rows at a time, of which shared memory holds one and a quarter, 156.)
+// What bounds it there is the rate at which the copy engine takes its 128-byte pieces: 2800 cycles a tile with nothing else going on (6 TB/s), 3500 beside the products.
 //
 // Work is cut into units of 64 rows of all sequences one behind the other, in equal parts for the CTAs, one an SM: long and short contexts, few or many,
 // load all of them evenly.  A sequence that several CTAs share leaves unnormalised parts, joined by a second kernel in order.
@@ -29,6 +30,7 @@ using namespace ptx;
 using gla::wait_for;
 
 constexpr int kThreads = 192, kTile = 64, kLatent = 512, kRow = 576;      // threads: softmax, copies, products
+constexpr int kAhead = 2;                                  // tiles on their way to L2 or further (one: 130 us a call, three 125, four 132: the copy engine does this too)
 constexpr uint32_t kChunkB = 8192, kPairB = 2 * kChunkB;   // 64 rows x 64 channels; two of them
 
 template <int NR> struct Cfg {
@@ -219,9 +221,19 @@ latent_token_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         const int j = t * kTile + lane % boxes * box;
         return t < walk.t1 && j < len ? (int)cache_row(p, walk.n, j) : -1;
       };
-      int row = row_at(walk.t0);
+      // A tile's rows lie together (page by page), its copies take 128 bytes of each at a time: brought to L2 as they lie, some tiles ahead.
+      auto ahead = [&](int row) {
+        if (lane < boxes && row >= 0)
+          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<const uint8_t*>(p.cache) + (size_t)row * (kRow * 2)), "r"(box * kRow * 2) : "memory");
+      };
+      int rows_ahead[kAhead];                              // of tiles t, t + 1, ..
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        rows_ahead[i] = row_at(walk.t0 + i);
+        if (i > 0) ahead(rows_ahead[i]);
+      }
       for (int t = walk.t0; t < walk.t1; ++t, ++tile) {
-        const int next = row_at(t + 1), have = min(boxes, (min(len - t * kTile, kTile) + box - 1) / box), r = tile % kRopes;
+        const int row = rows_ahead[0], next = row_at(t + kAhead), have = min(boxes, (min(len - t * kTile, kTile) + box - 1) / box), r = tile % kRopes;
         if (tile >= kRopes) wait_for(&rope_free[r], (tile / kRopes - 1) & 1, abort_flag);
         __syncwarp();
         if (*abort_flag) break;
@@ -241,7 +253,10 @@ latent_token_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             tma_load_4d(sm + slot * kPairB + half * kChunkB + lane % boxes * box * 128, &map_c, &pair_full[slot], 0, row, 2 * b + half, 0);
           __syncwarp();
         }
-        row = next;
+        ahead(next);
+#pragma unroll
+        for (int i = 1; i < kAhead; ++i) rows_ahead[i - 1] = rows_ahead[i];
+        rows_ahead[kAhead - 1] = next;
       }
       ++seg;
       if (*abort_flag) break;
