@@ -27,22 +27,6 @@ template <typename In, int SP, int LS> struct Stage {
   static constexpr size_t bytes = OFF_BC + 2 * 256 * BC * kQuadB;
 };
 
-// Pieces of 16 bytes in a row of what one side writes and the other reads: exchanged within their neighbourhood, so that eight threads that are neighbours meet all
-// banks on both sides (without that, reads of the sums took four times as long and bounded the kernel).
-__device__ __forceinline__ int sum_piece(int u) { return u ^ ((u >> 3) & 3); }        // four lanes' sums
-__device__ __forceinline__ int step_piece(int u) { return u ^ ((u >> 3) & 1); }       // delta and delta x of two channels
-
-// `bytes` from global to shared memory in the background, if that can be (`fast`: aligned and whole), else by way of registers.
-template <typename In, int V> __device__ __forceinline__ void stage_row(uint8_t* to, const In* from, bool fast, int left) {
-  if (fast && left >= V) {
-    const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(to));
-    if constexpr (V * sizeof(In) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(from) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(from), "n"(V * sizeof(In)) : "memory");
-  } else {
-    *reinterpret_cast<Raw<In, V>*>(to) = load_row<In, V>(from, false, left);
-  }
-}
-
 template <typename In, int SP, int LS, Mode M>
 __global__ void __launch_bounds__(kThreads, 2) scan_kernel(ScanParams p) {
   constexpr int LC = 32 / LS, CH = 4 * LC, NP = SP * LS;   // channels of a warp, of the CTA; states
@@ -124,7 +108,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_kernel(ScanParams p) {
       }
     }
     if (M == kEnds && start + len >= q.len) return;
-    constexpr int U = kCkpt;
+    constexpr int U = 8;
     const int du_at = step_piece(c / 2) * 2 + c % 2, sum = c * LS + lane / LC, y_at = sum_piece(sum / 4) * 4 + sum % 4;
     float total = 0.f;
     const int ck0 = M == kKeep ? slot_of(p.seqs, n, q.tok0, kCkptLog, (p.seqs.T_row + kCkpt - 1) / kCkpt) : 0;
@@ -138,7 +122,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_kernel(ScanParams p) {
         float yv[U];
 #pragma unroll
         for (int j = 0; j < U; ++j) {
-          if (M == kKeep && j == 0) {
+          if (M == kKeep && j % kCkpt == 0) {
             const int tk = i * kTile + t0 + j;
             if (mine && tk < len) {
               Vec<SP> now;

@@ -92,6 +92,22 @@ template <typename In, int V> __device__ __forceinline__ void store_row(In* p, b
     if (i < left) p[i] = from_f32<In>(r.v[i]);
 }
 
+// Pieces of 16 bytes in a row of what one side writes and the other reads: exchanged within their neighbourhood, so that eight threads that are neighbours meet all
+// banks on both sides (without that, reads of the sums took four times as long and bounded the kernel).
+__device__ __forceinline__ int sum_piece(int u) { return u ^ ((u >> 3) & 3); }        // four lanes' sums
+__device__ __forceinline__ int step_piece(int u) { return u ^ ((u >> 3) & 1); }       // delta and delta x of two channels
+
+// `bytes` from global to shared memory in the background, if that can be (`fast`: aligned and whole), else by way of registers.
+template <typename In, int V> __device__ __forceinline__ void stage_row(uint8_t* to, const In* from, bool fast, int left) {
+  if (fast && left >= V) {
+    const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(to));
+    if constexpr (V * sizeof(In) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(from), "n"(V * sizeof(In)) : "memory");
+  } else {
+    *reinterpret_cast<Raw<In, V>*>(to) = load_row<In, V>(from, false, left);
+  }
+}
+
 // Sums of v[0 .. n) over the lanes that differ in bits `top`, top / 2, .. (`bits` of them), spread out: a lane keeps the sums of the places whose
 // index it spells with those bits, n >> bits of them (one, if there are fewer places than lanes).
 template <int n, int bits> __device__ __forceinline__ void spread_sum(float (&v)[n], int top) {

@@ -1,30 +1,35 @@
 // Selective scan backward; see scan.cuh for the formulas.
 //
 // The states in front of every eight tokens come from a run of the forward recurrence (scan.cu).  Here a CTA goes through a sequence's tokens from the
-// last to the first, 16 at a time, for CH channels: four warps make the eight tokens' states and decays from the kept one, hold them in registers
-// (128 of them) and come back through them, so that a value costs two exponentials in all and the states never go through memory one by one.  Four
-// other warps bring the next 16 tokens and finish the last ones.  Sums over states (dx, ddelta, p) and over channels (dB, dC) cross the lanes of a warp: with
-// two channels and four states to a thread both are short (6 and 7 shuffles a token for 256 values); dB and dC then go over the warps in shared memory and
-// over the channel blocks in a second kernel, in order.  What bounds it is the issue slots: some 150 instructions a token and warp.
+// last to the first, 16 at a time, for CH channels: eight warps make eight tokens' states from the kept one, hold them in registers and come back
+// through them, so that the states never go through memory one by one; a decay is made three times in all, which is cheaper than the registers that would keep
+// it (622 us a call of two rows of 2048 tokens and 4096 channels, 667 with decays kept).  Eight other warps bring the next 16 tokens and finish the last ones.  Sums over states (dx,
+// ddelta, p) and over channels (dB, dC) cross the lanes of a warp, 10 shuffles a token; dB and dC then go over the warps in shared memory and over the channel blocks in a second kernel,
+// in order.  What bounds it is the length of a token's own chain, products, two sums across lanes, results, with two such warps to a scheduler: issue slots are 40 % used.  (Four
+// warps with two channels to a thread: 706 us; kept states sent for one part ahead instead of a tile: 758.)
 #include "scan.cuh"
 
 namespace ha_la {
 namespace mix {
 namespace {
 
-constexpr int kThreads = 256, kTile = 16, SP = 4, CP = 2;
+constexpr int kWarps = 8, kScan = 32 * kWarps, kThreads = kScan + 256, kTile = 16, SP = 4;   // recurrence warps and threads
 
-template <int LS> struct BackShape {
-  static constexpr int LC = 32 / LS, WC = CP * LC, CH = 4 * WC, NP = SP * LS;
-  // shared memory, in floats
+template <typename In, int LS> struct BackShape {
+  static constexpr int LC = 32 / LS, CH = kWarps * LC, NP = SP * LS;
+  static constexpr int E = CH >= 32 ? CH / 16 : 2, TPR = CH / E;           // channels of a helping thread, threads to a token
+  static constexpr int RES = kTile * CH + 8;                             // (three kinds that a warp writes at once, in banks of their own)
+  // shared memory, in floats; then rows on their way, as they are in memory: x, dt, z, dy of four tiles, B and C of two
   static constexpr int du = 0, g = du + 2 * kTile * CH * 2, b = g + 2 * kTile * CH, c = b + 2 * kTile * NP, res = c + 2 * kTile * NP,
-                       bc = res + 2 * 3 * kTile * CH, floats = bc + 2 * 4 * kTile * 2 * NP;
+                       bc = res + 2 * 3 * RES, floats = bc + 2 * kWarps * kTile * 2 * NP;
+  static constexpr int kRowB = E * sizeof(In), kQuadB = 4 * sizeof(In), QUADS = 2 * kTile * NP / 4, BC = (QUADS + 255) / 256;
+  static constexpr size_t OFF_ROWS = floats * 4, OFF_BC = OFF_ROWS + 4 * 4 * 256 * kRowB, bytes = OFF_BC + 2 * BC * 256 * kQuadB;
 };
 
 template <typename In, int LS, bool GATE>
 __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
-  using S = BackShape<LS>;
-  constexpr int LC = S::LC, CH = S::CH, NP = S::NP, E = CH / 8, BC = kTile * NP / 128;
+  using S = BackShape<In, LS>;
+  constexpr int LC = S::LC, CH = S::CH, NP = S::NP, E = S::E, BC = S::BC;
   extern __shared__ __align__(16) float sm[];
   float* const s_du = sm + S::du;
   float* const s_g = sm + S::g;
@@ -41,111 +46,101 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
   const int len = max(q.len, 0), tok0 = q.tok0, tiles = (len + kTile - 1) / kTile;
   const size_t state = (size_t)p.C * p.S;
 
-  if (warp < 4) {
-    const int cl = lane % LC, s0 = lane / LC * SP, g = lane / LC;
-    int c[CP];
-    bool mine[CP];
-    float A[CP][SP], dh[CP][SP], dA[CP][SP] = {};
+  if (warp < kWarps) {
+    const int cl = lane % LC, g = lane / LC, s0 = g * SP, c = warp * LC + cl, du_at = step_piece(c / 2) * 4 + c % 2 * 2;
+    const bool mine = c < left;
+    float2 A[SP / 2], dh[SP / 2], dA[SP / 2] = {};         // (two states to an instruction)
 #pragma unroll
-    for (int i = 0; i < CP; ++i) {
-      c[i] = warp * S::WC + i * LC + cl;
-      mine[i] = c[i] < left;
-#pragma unroll
-      for (int s = 0; s < SP; ++s) {
-        const bool ok = mine[i] && s0 + s < p.S;
-        const size_t at = (size_t)(c0 + c[i]) * p.S + s0 + s;
-        A[i][s] = ok ? p.A[at] * kLog2e : 0.f;
-        dh[i][s] = ok && p.dhT && q.len >= 0 ? p.dhT[n * state + at] : 0.f;
-      }
+    for (int s = 0; s < SP; ++s) {
+      const bool ok = mine && s0 + s < p.S;
+      const size_t at = (size_t)(c0 + c) * p.S + s0 + s;
+      (&A[s / 2].x)[s % 2] = ok ? p.A[at] * kLog2e : 0.f;
+      (&dh[s / 2].x)[s % 2] = ok && p.dhT && q.len >= 0 ? p.dhT[n * state + at] : 0.f;
     }
     const int ck0 = slot_of(p.seqs, n, tok0, kCkptLog, (p.seqs.T_row + kCkpt - 1) / kCkpt);
-    Vec<SP> kept[CP] = {};
-    auto fetch = [&](int chunk) {                          // the states in front of it
-#pragma unroll
-      for (int i = 0; i < CP; ++i)
-        if (mine[i] && chunk >= 0 && chunk * kCkpt < len) kept[i] = load_v<SP>(p.ckpt + ((size_t)(ck0 + chunk) * p.C + c0 + c[i]) * NP + s0);
+    constexpr int PARTS = kTile / kCkpt;
+    Vec<SP> kept[PARTS] = {};                              // the states in front of a tile's parts, sent for a tile ahead
+    auto fetch = [&](int tile, int part) {
+      const int chunk = tile * PARTS + part;
+      if (mine && chunk >= 0 && chunk * kCkpt < len) kept[part] = load_v<SP>(p.ckpt + ((size_t)(ck0 + chunk) * p.C + c0 + c) * NP + s0);
     };
-    fetch((len - 1) >> kCkptLog);
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) fetch(tiles - 1, part);
     __syncthreads();
 #pragma unroll 1
     for (int i = 0; i < tiles; ++i) {
       const int tile = tiles - 1 - i, buf = i & 1;
-#pragma unroll 1
-      for (int half = kTile / kCkpt - 1; half >= 0; --half) {
-        const int chunk = tile * (kTile / kCkpt) + half, r0 = half * kCkpt;
-        if (chunk * kCkpt >= len) continue;
-        float first[CP][SP], h[kCkpt][CP][SP], a[kCkpt][CP][SP];
 #pragma unroll
-        for (int u = 0; u < CP; ++u)
+      for (int part = PARTS - 1; part >= 0; --part) {
+        const int r0 = part * kCkpt;
+        if (tile * kTile + r0 >= len) {
+          fetch(tile - 1, part);
+          continue;
+        }
+        float2 first[SP / 2], h[kCkpt][SP / 2];
 #pragma unroll
-          for (int s = 0; s < SP; ++s) first[u][s] = kept[u].v[s];
-        fetch(chunk - 1);
+        for (int s = 0; s < SP / 2; ++s) first[s] = make_float2(kept[part].v[2 * s], kept[part].v[2 * s + 1]);
+        fetch(tile - 1, part);
+        const float *const du0 = s_du + (buf * kTile + r0) * CH * 2 + du_at, *const g0 = s_g + (buf * kTile + r0) * CH + c;
+        const float *const b0 = s_b + (buf * kTile + r0) * NP + s0, *const cc0 = s_c + (buf * kTile + r0) * NP + s0;
 #pragma unroll
         for (int j = 0; j < kCkpt; ++j) {
-          const Vec<SP> bv = load_v<SP>(s_b + (buf * kTile + r0 + j) * NP + s0);
+          const Vec<SP> bv = load_v<SP>(b0 + j * NP);
+          const float2 du = *reinterpret_cast<const float2*>(du0 + j * CH * 2);
 #pragma unroll
-          for (int u = 0; u < CP; ++u) {
-            const float2 du = *reinterpret_cast<const float2*>(s_du + ((buf * kTile + r0 + j) * CH + c[u]) * 2);
-#pragma unroll
-            for (int s = 0; s < SP; ++s) {
-              a[j][u][s] = ex2(du.x * A[u][s]);
-              h[j][u][s] = fmaf(a[j][u][s], j ? h[j - 1][u][s] : first[u][s], du.y * bv.v[s]);
-            }
+          for (int s = 0; s < SP / 2; ++s) {
+            const float2 x = ptx::mul2(make_float2(du.x, du.x), A[s]);
+            h[j][s] = ptx::fma2(make_float2(ex2(x.x), ex2(x.y)), j ? h[j - 1][s] : first[s], ptx::mul2(make_float2(du.y, du.y), make_float2(bv.v[2 * s], bv.v[2 * s + 1])));
           }
         }
 #pragma unroll
         for (int j = kCkpt - 1; j >= 0; --j) {
-          const int r = r0 + j;
-          const Vec<SP> bv = load_v<SP>(s_b + (buf * kTile + r) * NP + s0), cv = load_v<SP>(s_c + (buf * kTile + r) * NP + s0);
-          float to_x[8] = {}, to_b[8] = {};                // by kind and channel; dB, dC
+          const Vec<SP> bv = load_v<SP>(b0 + j * NP), cv = load_v<SP>(cc0 + j * NP);
+          const float2 du = *reinterpret_cast<const float2*>(du0 + j * CH * 2);
+          const float gy = g0[j * CH];
+          const float2 g2 = make_float2(gy, gy), u2 = make_float2(du.y, du.y);
+          float to_x[4], to_b[8];                          // <dh, B>, <f, A>, <C, h>; dB, dC
+          float2 from_b, from_a, out = make_float2(0.f, 0.f);
 #pragma unroll
-          for (int u = 0; u < CP; ++u) {
-            const float2 du = *reinterpret_cast<const float2*>(s_du + ((buf * kTile + r) * CH + c[u]) * 2);
-            const float gy = s_g[(buf * kTile + r) * CH + c[u]];
-#pragma unroll
-            for (int s = 0; s < SP; ++s) {
-              dh[u][s] = fmaf(gy, cv.v[s], dh[u][s]);
-              to_x[u] = fmaf(dh[u][s], bv.v[s], to_x[u]);
-              if (GATE) to_x[4 + u] = fmaf(h[j][u][s], cv.v[s], to_x[4 + u]);
-              to_b[s] = fmaf(dh[u][s], du.y, to_b[s]);
-              to_b[4 + s] = fmaf(h[j][u][s], gy, to_b[4 + s]);
-              dh[u][s] *= a[j][u][s];
-              const float f = dh[u][s] * (j ? h[j - 1][u][s] : first[u][s]);
-              to_x[2 + u] = fmaf(f, A[u][s], to_x[2 + u]);
-              dA[u][s] = fmaf(f, du.x, dA[u][s]);
-            }
+          for (int s = 0; s < SP / 2; ++s) {
+            const float2 b2 = make_float2(bv.v[2 * s], bv.v[2 * s + 1]), c2 = make_float2(cv.v[2 * s], cv.v[2 * s + 1]);
+            dh[s] = ptx::fma2(g2, c2, dh[s]);
+            from_b = s ? ptx::fma2(dh[s], b2, from_b) : ptx::mul2(dh[s], b2);
+            if (GATE) out = s ? ptx::fma2(h[j][s], c2, out) : ptx::mul2(h[j][s], c2);
+            const float2 db = ptx::mul2(dh[s], u2), dc = ptx::mul2(h[j][s], g2);
+            const float2 x = ptx::mul2(make_float2(du.x, du.x), A[s]);   // (made again: kept, decays take as many registers as the states)
+            dh[s] = ptx::mul2(dh[s], make_float2(ex2(x.x), ex2(x.y)));
+            const float2 f = ptx::mul2(dh[s], j ? h[j - 1][s] : first[s]);
+            from_a = s ? ptx::fma2(f, A[s], from_a) : ptx::mul2(f, A[s]);
+            dA[s] = ptx::fma2(f, make_float2(du.x, du.x), dA[s]);
+            to_b[2 * s] = db.x; to_b[2 * s + 1] = db.y;
+            to_b[SP + 2 * s] = dc.x; to_b[SP + 2 * s + 1] = dc.y;
           }
-          spread_sum<8, ilog2(LS)>(to_x, 16);              // a lane's places: the top bits of g
-          spread_sum<8, ilog2(LC)>(to_b, LC / 2);          // ... of cl
-          constexpr int nx = LS >= 8 ? 1 : 8 / LS, nbc = LC >= 8 ? 1 : 8 / LC;
-          const int px = LS >= 8 ? g / (LS / 8) : g * nx, pb = LC >= 8 ? cl / (LC / 8) : cl * nbc;
+          to_x[0] = from_b.x + from_b.y; to_x[1] = from_a.x + from_a.y; to_x[2] = out.x + out.y; to_x[3] = 0.f;
+          spread_sum<4, ilog2(LS)>(to_x, 16);              // a lane's kind: the top two bits of g
+          spread_sum<8, ilog2(LC)>(to_b, LC / 2);          // ... its places: the top bits of cl
+          constexpr int nbc = LC >= 8 ? 1 : 8 / LC;
+          const int kind = g / (LS / 4), pb = LC >= 8 ? cl / (LC / 8) : cl * nbc, r = r0 + j;
+          if (kind < (GATE ? 3 : 2) && g % (LS / 4) == 0) s_res[(buf * 3 + kind) * S::RES + r * CH + c] = to_x[0];
 #pragma unroll
-          for (int e = 0; e < nx; ++e) {
-            const int kind = (px + e) / CP, u = (px + e) % CP;
-            if (kind < (GATE ? 3 : 2) && (LS < 16 || g % 2 == 0)) s_res[((buf * 3 + kind) * kTile + r) * CH + warp * S::WC + u * LC + cl] = to_x[e];
-          }
-#pragma unroll
-          for (int e = 0; e < nbc; ++e)
-            s_bc[((((buf * 4 + warp) * kTile + r) * 2) + (pb + e) / SP) * NP + s0 + (pb + e) % SP] = to_b[e];
+          for (int e = 0; e < nbc; ++e) s_bc[((buf * kWarps + warp) * kTile + r) * 2 * NP + (pb + e) / SP * NP + s0 + (pb + e) % SP] = to_b[e];
         }
       }
       __syncthreads();
     }
 #pragma unroll
-    for (int i = 0; i < CP; ++i)
-#pragma unroll
-      for (int s = 0; s < SP; ++s)
-        if (mine[i] && s0 + s < p.S) {
-          const size_t at = n * state + (size_t)(c0 + c[i]) * p.S + s0 + s;
-          p.part_a[at] = dA[i][s];
-          if (p.dh0 && q.len >= 0) p.dh0[at] = dh[i][s];
-        }
+    for (int s = 0; s < SP; ++s)
+      if (mine && s0 + s < p.S) {
+        const size_t at = n * state + (size_t)(c0 + c) * p.S + s0 + s;
+        p.part_a[at] = (&dA[s / 2].x)[s % 2];
+        if (p.dh0 && q.len >= 0) p.dh0[at] = (&dh[s / 2].x)[s % 2];
+      }
     __syncthreads();
     return;
   }
 
-  // ---- the helping warps: a token and E channels to a thread
-  const int ht = tid - 128, row = ht / 8, c = ht % 8 * E, have = left - c;
+  // ---- the helping warps: E channels of a token to a thread
+  const int ht = tid - kScan, row = ht / S::TPR, c = ht % S::TPR * E, have = row < kTile ? left - c : 0;
   const bool vec = p.vec;
   const In *x = reinterpret_cast<const In*>(p.x) + c0 + c, *dt = reinterpret_cast<const In*>(p.dt) + c0 + c, *z = reinterpret_cast<const In*>(p.z) + c0 + c,
            *dy = reinterpret_cast<const In*>(p.dy) + c0 + c;
@@ -157,67 +152,90 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
     if (p.dt_bias && e < have) bias.v[e] = p.dt_bias[c0 + c + e];
     if (p.D && e < have) skip.v[e] = p.D[c0 + c + e];
   }
-  using Row = Raw<In, E>;
-  Row rx = {}, rd = {}, rz = {}, rg = {};
-  In rb[BC], rc[BC];
-  auto rows = [&](int tile, Row& ax, Row& ad, Row& az, Row& ag) {
-    const int t = tile * kTile + row;
-    if (t >= len) return;
-    ax = load_row<In, E>(x + (size_t)(tok0 + t) * p.xs, vec, have);
-    ad = load_row<In, E>(dt + (size_t)(tok0 + t) * p.dts, vec, have);
-    if (GATE) az = load_row<In, E>(z + (size_t)(tok0 + t) * p.zs, vec, have);
-    ag = load_row<In, E>(dy + (size_t)(tok0 + t) * p.C, vec, have);
+  // A thread's pieces, which nobody else looks at: rows of the i-th tile from the end in place i % 4 (they are wanted again for the results), B and C in place i % 2
+  uint8_t* const own = reinterpret_cast<uint8_t*>(sm) + S::OFF_ROWS + ht * S::kRowB;
+  auto row_at = [&](int i, int kind) { return own + ((i & 3) * 4 + kind) * 256 * S::kRowB; };
+  auto row_of = [&](int i, int kind) { return unpack_row<In, E>(*reinterpret_cast<const Raw<In, E>*>(row_at(i, kind))); };
+  auto bc_at = [&](int i, int j) { return reinterpret_cast<uint8_t*>(sm) + S::OFF_BC + (((i & 1) * BC + j) * 256 + ht) * S::kQuadB; };
+  auto tile_of = [&](int i) { return tiles - 1 - i; };
+  auto quad = [&](int j, int& which, int& r, int& s) {      // of B or C: its token and first state; false: there is none
+    const int f = j * 256 + ht, in = f % (S::QUADS / 2) * 4;
+    which = f / (S::QUADS / 2);
+    r = in / NP;
+    s = in % NP;
+    return f < S::QUADS;
   };
-  auto fetch = [&](int tile) {
-    rows(tile, rx, rd, rz, rg);
-#pragma unroll
-    for (int j = 0; j < BC; ++j) {
-      const int f = j * 128 + ht, r = tile * kTile + f / NP, s = f % NP;
-      const bool ok = r < len && s < p.S;
-      rb[j] = ok ? B[(size_t)(tok0 + r) * p.bs + s] : from_f32<In>(0.f);
-      rc[j] = ok ? C[(size_t)(tok0 + r) * p.cs + s] : from_f32<In>(0.f);
-    }
-  };
-  auto put = [&](int tile, int buf) {
-    const bool in = tile * kTile + row < len;
-    const Vec<E> vx = unpack_row<In, E>(rx), vd = unpack_row<In, E>(rd), vz = unpack_row<In, E>(rz), vg = unpack_row<In, E>(rg);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const bool ok = in && e < have;
-      const float v = vd.v[e] + bias.v[e], delta = ok ? (p.softplus ? softplus(v) : v) : 0.f;
-      *reinterpret_cast<float2*>(s_du + ((buf * kTile + row) * CH + c + e) * 2) = make_float2(delta, ok ? delta * vx.v[e] : 0.f);
-      float gy = ok ? vg.v[e] : 0.f;
-      if (GATE && ok) gy *= vz.v[e] * sigmoid(vz.v[e]);
-      s_g[(buf * kTile + row) * CH + c + e] = gy;
+  auto fetch = [&](int i) {
+    const int t = tile_of(i) * kTile + row;
+    if (t < len && have > 0) {
+      stage_row<In, E>(row_at(i, 0), x + (size_t)(tok0 + t) * p.xs, vec, have);
+      stage_row<In, E>(row_at(i, 1), dt + (size_t)(tok0 + t) * p.dts, vec, have);
+      if (GATE) stage_row<In, E>(row_at(i, 2), z + (size_t)(tok0 + t) * p.zs, vec, have);
+      stage_row<In, E>(row_at(i, 3), dy + (size_t)(tok0 + t) * p.C, vec, have);
     }
 #pragma unroll
     for (int j = 0; j < BC; ++j) {
-      const int f = j * 128 + ht;
-      s_b[(buf * kTile + f / NP) * NP + f % NP] = to_f32(rb[j]);
-      s_c[(buf * kTile + f / NP) * NP + f % NP] = to_f32(rc[j]);
+      int which, r, s;
+      const bool ok = quad(j, which, r, s);
+      const int tq = tile_of(i) * kTile + r;
+      if (ok && tq < len) stage_row<In, 4>(bc_at(i, j), which ? C + (size_t)(tok0 + tq) * p.cs + s : B + (size_t)(tok0 + tq) * p.bs + s, p.bc_vec, p.S - s);
     }
   };
-  auto finish = [&](int tile, int buf, const Row& x_in, const Row& d_in, const Row& z_in, const Row& g_in) {
-    const int t = tile * kTile + row;
-    if (t < len) {
-      const Vec<E> ax = unpack_row<In, E>(x_in), ad = unpack_row<In, E>(d_in), az = unpack_row<In, E>(z_in), ag = unpack_row<In, E>(g_in);
+  auto put = [&](int i) {
+    const int buf = i & 1;
+    if (row < kTile) {
+      const bool in = tile_of(i) * kTile + row < len;
+      const Vec<E> vx = row_of(i, 0), vd = row_of(i, 1), vz = row_of(i, 2), vg = row_of(i, 3);
+      Vec<E> gy;
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        float4 w;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const bool ok = in && e + k < have;
+          const float v = vd.v[e + k] + bias.v[e + k], delta = ok ? (p.softplus ? softplus(v) : v) : 0.f;
+          (&w.x)[2 * k] = delta;
+          (&w.x)[2 * k + 1] = ok ? delta * vx.v[e + k] : 0.f;
+          gy.v[e + k] = ok ? (GATE ? vg.v[e + k] * (vz.v[e + k] * sigmoid(vz.v[e + k])) : vg.v[e + k]) : 0.f;
+        }
+        *reinterpret_cast<float4*>(s_du + (buf * kTile + row) * CH * 2 + step_piece((c + e) / 2) * 4) = w;
+      }
+      store_v<E>(s_g + (buf * kTile + row) * CH + c, gy);
+    }
+#pragma unroll
+    for (int j = 0; j < BC; ++j) {
+      int which, r, s;
+      if (!quad(j, which, r, s)) continue;
+      Vec<4> w = {};
+      if (tile_of(i) * kTile + r < len) w = unpack_row<In, 4>(*reinterpret_cast<const Raw<In, 4>*>(bc_at(i, j)));
+      store_v<4>((which ? s_c : s_b) + (buf * kTile + r) * NP + s, w);
+    }
+  };
+  auto finish = [&](int i) {
+    const int buf = i & 1, t = tile_of(i) * kTile + row;
+    if (t < len && have > 0) {
+      const Vec<E> ax = row_of(i, 0), ad = row_of(i, 1), az = row_of(i, 2), ag = row_of(i, 3);
+      const float* const res = s_res + buf * 3 * S::RES + row * CH + c;
+      const Vec<E> from_b = load_v<E>(res), from_a = load_v<E>(res + S::RES);
+      Vec<E> out = {};
+      if (GATE) out = load_v<E>(res + 2 * S::RES);
       Vec<E> dx, ddt, dz;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const int at = row * CH + c + e;
-        const float from_b = s_res[buf * 3 * kTile * CH + at], from_a = s_res[(buf * 3 + 1) * kTile * CH + at];
         const float v = ad.v[e] + bias.v[e], delta = p.softplus ? softplus(v) : v;
         float gy = ag.v[e];
         if (GATE) {
-          const float sg = sigmoid(az.v[e]), out = fmaf(skip.v[e], ax.v[e], s_res[(buf * 3 + 2) * kTile * CH + at]);
-          dz.v[e] = gy * out * sg * fmaf(az.v[e], 1.f - sg, 1.f);
+          const float sg = sigmoid(az.v[e]);
+          dz.v[e] = gy * fmaf(skip.v[e], ax.v[e], out.v[e]) * sg * fmaf(az.v[e], 1.f - sg, 1.f);
           gy *= az.v[e] * sg;
         }
-        dx.v[e] = fmaf(delta, from_b, skip.v[e] * gy);
-        ddt.v[e] = fmaf(from_a, kLn2, ax.v[e] * from_b);
+        dx.v[e] = fmaf(delta, from_b.v[e], skip.v[e] * gy);
+        ddt.v[e] = fmaf(from_a.v[e], kLn2, ax.v[e] * from_b.v[e]);
         if (p.softplus) ddt.v[e] *= sigmoid(v);
-        dD[e] = fmaf(gy, ax.v[e], dD[e]);
-        dbias[e] += ddt.v[e];
+        if (e < have) {
+          dD[e] = fmaf(gy, ax.v[e], dD[e]);
+          dbias[e] += ddt.v[e];
+        }
       }
       const size_t at = (size_t)(tok0 + t) * p.C + c0 + c;
       store_row<In, E>(reinterpret_cast<In*>(p.dx) + at, vec, have, dx);
@@ -225,41 +243,48 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
       if (GATE) store_row<In, E>(reinterpret_cast<In*>(p.dz) + at, vec, have, dz);
     }
     constexpr int per = 2 * NP;
-    for (int f = ht; f < kTile * per; f += 128) {
-      const int r = f / per, t2 = tile * kTile + r;
+#pragma unroll
+    for (int f = ht; f < kTile * per; f += 256) {
+      const int r = f / per, t2 = tile_of(i) * kTile + r;
       if (t2 >= len) break;
-      const float* o = s_bc + (buf * 4 * kTile + r) * per + f % per;
-      p.part_bc[((size_t)cb * p.seqs.T_total + tok0 + t2) * per + f % per] = (o[0] + o[kTile * per]) + (o[2 * kTile * per] + o[3 * kTile * per]);
+      const float* o = s_bc + (buf * kWarps * kTile + r) * per + f % per;
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) sum += o[w * kTile * per];
+      p.part_bc[((size_t)cb * p.seqs.T_total + tok0 + t2) * per + f % per] = sum;
     }
   };
-  if (tiles > 0) {
-    fetch(tiles - 1);
-    put(tiles - 1, 0);
-    if (tiles > 1) fetch(tiles - 2);
-  }
+  auto sent = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
+  // What is wanted for the next tile has been sent for two tiles before.
+  if (tiles > 0) fetch(0);
+  sent();
+  if (tiles > 1) fetch(1);
+  sent();
+  asm volatile("cp.async.wait_group 1;" ::: "memory");
+  if (tiles > 0) put(0);
+  if (tiles > 2) fetch(2);
+  sent();
   __syncthreads();
-  Row ax = {}, ad = {}, az = {}, ag = {};                  // of the tile that is gone through now
 #pragma unroll 1
   for (int i = 0; i <= tiles; ++i) {
-    if (i + 1 < tiles) {
-      put(tiles - 2 - i, (i + 1) & 1);
-      if (i + 2 < tiles) fetch(tiles - 3 - i);
-    }
-    if (i > 0) finish(tiles - i, (i - 1) & 1, ax, ad, az, ag);
-    if (i < tiles) {
-      rows(tiles - 1 - i, ax, ad, az, ag);
-      __syncthreads();
-    }
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    if (i + 1 < tiles) put(i + 1);
+    if (i > 0) finish(i - 1);
+    if (i + 3 < tiles) fetch(i + 3);
+    sent();
+    if (i < tiles) __syncthreads();
   }
   // over the rows: through the places of the results, which nobody reads any more but the helping warps themselves
   __syncthreads();
   float* const s_sum = s_res;                              // [row][dD, dbias][channel]
+  if (row < kTile) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    s_sum[(row * 2) * CH + c + e] = dD[e];
-    s_sum[(row * 2 + 1) * CH + c + e] = dbias[e];
+    for (int e = 0; e < E; ++e) {
+      s_sum[(row * 2) * CH + c + e] = dD[e];
+      s_sum[(row * 2 + 1) * CH + c + e] = dbias[e];
+    }
   }
-  asm volatile("bar.sync 1, 128;" ::: "memory");
+  asm volatile("bar.sync 1, 256;" ::: "memory");
   if (ht < 2 * CH) {
     float sum = 0.f;
 #pragma unroll
@@ -304,9 +329,9 @@ __global__ void __launch_bounds__(128) scan_bc_kernel(ScanParams p, int np, In* 
 }
 
 template <typename In, int LS> cudaError_t launch(const ScanParams& p, cudaStream_t stream) {
-  const size_t smem = BackShape<LS>::floats * sizeof(float);
+  constexpr size_t smem = BackShape<In, LS>::bytes;
   void (*k)(ScanParams) = p.z ? scan_back_kernel<In, LS, true> : scan_back_kernel<In, LS, false>;
-  cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(k), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  const cudaError_t e = p.z ? allow_smem<scan_back_kernel<In, LS, true>>(smem) : allow_smem<scan_back_kernel<In, LS, false>>(smem);
   if (e != cudaSuccess) return e;
   const long long grid = (long long)p.seqs.N * p.blocks * p.G;
   if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
@@ -324,7 +349,7 @@ template <typename In> cudaError_t launch_all(const ScanParams& p, int np, const
 
 }  // namespace
 
-int scan_back_channels(int padded_states) { return padded_states == 16 ? BackShape<4>::CH : padded_states == 32 ? BackShape<8>::CH : BackShape<16>::CH; }
+int scan_back_channels(int padded_states) { return padded_states == 16 ? BackShape<float, 4>::CH : padded_states == 32 ? BackShape<float, 8>::CH : BackShape<float, 16>::CH; }
 
 cudaError_t launch_scan_back(bool bf16, ScanParams p, int padded_states, const ha_la_scan_args& a, cudaStream_t stream) {
   return bf16 ? launch_all<__nv_bfloat16>(p, padded_states, a, stream) : launch_all<float>(p, padded_states, a, stream);
