@@ -3,7 +3,8 @@
 // A CTA has 128 TILES queries of a head and goes through the keys 128 at a time: S = Q K^T (128 x 128, twelve steps of 16 channels, the last four of
 // them on the positional key that all heads share), P = 2^(S - m) in bf16 over S's place in tensor memory, O += P V with P as the operand from there.
 // With two tiles of queries the tensor cores work on one while the softmax warps, a thread to a query, are on the other's scores: the products of
-// both are 2560 cycles a round, their exponentials 2048, and K and V are read once for 256 queries.
+// both are 2560 cycles a round, their exponentials 2048, and K and V are read once for 256 queries.  A round takes some 4200: a tile's own chain of scores, softmax (2000 beside
+// the other tile's) and values.  8192 tokens, 32 heads: 590 us, 1165 TFLOP/s of the causal half.
 // m need not be the largest score, only near it: O and l are rescaled when a score exceeds m by 2^8, which after the first keys is rare, so O is hardly
 // ever read back.  P <= 2^8 loses nothing in bf16, and l adds up the weights as they are before that rounding, in fp32.
 #include <algorithm>
@@ -132,7 +133,7 @@ latent_prompt_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       if (most > 0) umma_commit(&k_free[0]);
       for (int i = 0; i < most; ++i) {
         wait_for(&v_full[i % VS], (i / VS) & 1, abort_flag);
-        if (i + 1 < most) wait_for(&k_full[(i + 1) & 1], ((i + 1) >> 1) & 1, abort_flag);
+        bool keys_there = false;
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
           if (i >= steps[t]) continue;
@@ -141,10 +142,14 @@ latent_prompt_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
           tc_fence_after_sync();
           gla::mma_tmem_rows(tm + kTmO + 128 * t, tm + kTmS + 128 * t, smem_u32(sm + C::OFF_V + (i % VS) * kVB), i > 0);
           umma_commit(&added[t]);
-          // (behind the product that reads the weights there, in the tensor cores' order)
-          if (i + 1 < steps[t]) make_scores(t, i + 1);
+          if (t == TILES - 1 || i >= steps[TILES - 1]) umma_commit(&v_free[i % VS]);   // (the last that reads these values, and ahead of the next scores)
+          if (i + 1 < steps[t]) {
+            if (!keys_there) wait_for(&k_full[(i + 1) & 1], ((i + 1) >> 1) & 1, abort_flag);
+            keys_there = true;
+            tc_fence_after_sync();
+            make_scores(t, i + 1);                         // behind the product that reads the weights there, in the tensor cores' order
+          }
         }
-        umma_commit(&v_free[i % VS]);
         if (i + 1 < most) umma_commit(&k_free[(i + 1) & 1]);
         if (*abort_flag) break;
       }
@@ -172,16 +177,40 @@ latent_prompt_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
 #pragma unroll
           for (int e = 0; e < 32; ++e) raw[c][e] = 32 * c + e < lim ? raw[c][e] : 0xff800000u;
       }
-      float top[4];
+      // Weights by the m of before, the scores' maximum on the side; where that m will not do any more, which after the first keys is rare, once more by the new one.
+      float2 sum;
+      float top;
+      auto weigh = [&](float base) {
+        float2 part[2] = {};
+        float tops[2] = {kNegInf, kNegInf};
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        top[c] = __uint_as_float(raw[c][0]);
+        for (int c = 0; c < 4; ++c) {
+          uint32_t w[16];
 #pragma unroll
-        for (int e = 1; e < 32; ++e) top[c] = fmaxf(top[c], __uint_as_float(raw[c][e]));
+          for (int e = 0; e < 32; e += 2) {
+            const float2 s = as_f2(raw[c][e], raw[c][e + 1]);
+            tops[(e >> 1) & 1] = fmaxf(tops[(e >> 1) & 1], fmaxf(s.x, s.y));
+            const float2 x = fma2(s, make_float2(to_log2, to_log2), make_float2(-base, -base));
+            const float2 y = make_float2(ex2(x.x), ex2(x.y));
+            part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], y);
+            w[e / 2] = pack_bf16(y);
+          }
+          tmem_st16(S + 16 * c, w);
+        }
+        sum = add2(part[0], part[1]);
+        top = fmaxf(tops[0], tops[1]) * to_log2;
+      };
+      if (i == 0) {
+        float tops[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) tops[e & 3] = fmaxf(tops[e & 3], __uint_as_float(raw[c][e]));
+        m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * to_log2;
       }
-      const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * to_log2;
-      if (__any_sync(0xffffffffu, now > m + 8.f)) {
-        const float next = fmaxf(m, now), f = m == kNegInf ? 0.f : ex2(m - next);
+      weigh(m == kNegInf ? 0.f : m);
+      if (__any_sync(0xffffffffu, top > m + 8.f)) {
+        const float next = fmaxf(m, top), f = m == kNegInf ? 0.f : ex2(m - next);
         m = next;
         l *= f;
         if (i > 0) {
@@ -197,24 +226,10 @@ latent_prompt_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
             tmem_st16(O + 16 * c, o);
           }
-          tmem_st_wait();
         }
+        weigh(m == kNegInf ? 0.f : m);
       }
-      const float base = m == kNegInf ? 0.f : m;
-      float2 sum[2] = {};
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t w[16];
-#pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-          const float2 x = fma2(as_f2(raw[c][e], raw[c][e + 1]), make_float2(to_log2, to_log2), make_float2(-base, -base));
-          const float2 y = make_float2(ex2(x.x), ex2(x.y));
-          sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], y);
-          w[e / 2] = pack_bf16(y);
-        }
-        tmem_st16(S + 16 * c, w);
-      }
-      l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+      l += sum.x + sum.y;
       tmem_st_wait();
       const int keys = g.k - 128 * i;                      // what lies behind the sequence may be NaN, which no weight of zero masks
       if (keys < 128) {
