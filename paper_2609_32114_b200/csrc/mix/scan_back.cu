@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
           fetch(tile - 1, part);
           continue;
         }
-        float2 first[SP / 2], h[kCkpt][SP / 2];
+        float2 first[SP / 2], h[kCkpt][SP / 2], sum_A[SP / 2];
 #pragma unroll
         for (int s = 0; s < SP / 2; ++s) first[s] = make_float2(kept[part].v[2 * s], kept[part].v[2 * s + 1]);
         fetch(tile - 1, part);
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
             dh[s] = ptx::mul2(dh[s], make_float2(ex2(x.x), ex2(x.y)));
             const float2 f = ptx::mul2(dh[s], j ? h[j - 1][s] : first[s]);
             from_a = s ? ptx::fma2(f, A[s], from_a) : ptx::mul2(f, A[s]);
-            dA[s] = ptx::fma2(f, make_float2(du.x, du.x), dA[s]);
+            sum_A[s] = j == kCkpt - 1 ? ptx::mul2(f, make_float2(du.x, du.x)) : ptx::fma2(f, make_float2(du.x, du.x), sum_A[s]);
             to_b[2 * s] = db.x; to_b[2 * s + 1] = db.y;
             to_b[SP + 2 * s] = dc.x; to_b[SP + 2 * s + 1] = dc.y;
           }
@@ -125,6 +125,8 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
 #pragma unroll
           for (int e = 0; e < nbc; ++e) s_bc[((buf * kWarps + warp) * kTile + r) * 2 * NP + (pb + e) / SP * NP + s0 + (pb + e) % SP] = to_b[e];
         }
+#pragma unroll
+        for (int s = 0; s < SP / 2; ++s) dA[s] = ptx::add2(dA[s], sum_A[s]);   // (eight tokens at a time: token by token it is off by a third more; in 64 bits by no less)
       }
       __syncthreads();
     }
