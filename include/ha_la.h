@@ -5,7 +5,9 @@
  * (scalar log-gate per head per token) or its Kimi-Delta-Attention (KDA)
  * variant (log-gate per key channel), with its decoding step; further down what
  * stands next to it in a hybrid model: gated linear attention (forward, backward,
- * one token) and the norms on both sides of a block (forward, backward).
+ * one token), the norms on both sides of a block (forward, backward), the short
+ * convolution and the selective scan (forward, backward, one token) and attention
+ * over latent rows (prompts and new tokens; no backward).
  *
  * Paper passages that define the operation:
  *   - Section 2.1, "Architecture of Linear-Attention Hybrids": a fixed-size
@@ -389,7 +391,7 @@ int ha_la_add_norm_backward(const ha_la_add_norm_args* args, void* cuda_stream);
  *   workspace (its size: ha_la_conv_workspace_bytes).  ha_la_conv_decode: one token for each of `batch` sequences (seqlen = 1);
  *   hT may be exactly h0.
  * All arithmetic fp32, rounded once at the end.  Tensors that are 16-byte aligned, with channels and strides that keep every
- * token so, are read and written 16 bytes at a time, others element by element.                    */
+ * token so, are read and written 8 bytes to a thread, others element by element.                    */
 typedef struct {
   int32_t dtype;          /* ha_la_dtype of x, y, h0, hT and their gradients                 */
   int32_t batch;          /* B (ha_la_conv_decode: sequences)                                */
@@ -483,6 +485,7 @@ int ha_la_scan_decode(const ha_la_scan_args* args, void* cuda_stream);
  *   sequence's cached rows, those of the new tokens, its last ones, among them; a new token sees the rows up to its own.
  * lse = log sum_j e^{s_ij} (natural), for joining results over parts of the keys; NULL: not wanted.  A row that sees no key has
  * o = 0 and lse = -infinity.  What no row of a sequence sees (the rest of its last page, other pages) may hold anything, NaN included.
+ * What one of its rows sees has to be finite: a NaN there may reach the rows ahead of it too.
  * A length that is negative or longer than its row of the table counts as zero and is reported through the status word, as is a
  * page that does not exist, whose sequence's results are unspecified.
  * Scores, their sums and o's sums are fp32; with bf16 tensors the weights are rounded to bf16 for the product with the values.

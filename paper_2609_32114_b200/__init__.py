@@ -1,7 +1,8 @@
 """B200 (sm_100a) linear attention for hybrid models behind a C ABI: the chunkwise prefill of the delta rule (GDN and KDA) and its
-decoding step, gated linear attention with its backward pass, and the norms on both sides of a block.
+decoding step, gated linear attention with its backward pass, the norms on both sides of a block, and what such layers alternate with:
+the short convolution, the selective scan and attention over latent rows.
 
-`layer` has the latter two; `binding` marshals torch CUDA tensors into the C struct of include/ha_la.h and calls
+`layer` has gated linear attention and the norms, `mixer` the last three; `binding` marshals torch CUDA tensors into the C struct of include/ha_la.h and calls
 libha_la.so; `synth` draws the seeded synthetic workloads; `build` compiles the library.
 Importing the package loads nothing native; the first call does, and raises if the
 library has not been built.

@@ -1,8 +1,9 @@
 // Short causal convolution per channel (ha_la_conv* in ha_la.h): y_t = act(bias + sum_j w[j] x_{t-K+1+j}), K = 2, 3 or 4.
 //
 // One read of x and one write of y are all that has to move, and 2 K operations a value are nothing beside it, so HBM bounds it.  A thread
-// has V channels (8 bytes) of a run of consecutive tokens: the K - 1 inputs in front stay in registers from token to token, only a run's first ones are read twice.  A run is taken apart at sequence
-// starts, in front of which h0's inputs stand, so the inner loops know no boundaries.
+// has V channels (8 bytes) of a run of consecutive tokens: the K - 1 inputs in front stay in registers from token to token, only a run's first ones are
+// read twice.  A run is taken apart at sequence starts, in front of which h0's inputs stand, so the inner loops know no boundaries.  (35 k tokens of 8192
+// channels 223 us; gradients of 16384 tokens of 4096 channels 107.)
 //
 // Backwards, with p_t the sum ahead of the activation (made again), e_t = dy_t act'(p_t):
 //   dx_t = sum_j w[K-1-j] e_{t+j}  (+ dhT's part for the last K - 1 tokens)    dw[j] = sum_t e_t x_{t-K+1+j}    db = sum_t e_t
