@@ -143,6 +143,27 @@ def test_tokens_one_by_one(N, ch, S, G, dtype):
 
 
 @TYPES
+@pytest.mark.parametrize("N,ch,S,G", [(1, 64, 16, 1), (7, 70, 32, 2), (130, 24, 64, 3)])
+def test_token_wherever_b_and_c_lie(N, ch, S, G, dtype):
+    ha = _ha()
+    t, names = inputs(N, 1, ch, S, G, dtype, seed=N), ("x", "dt", "A", "B", "C")
+    got = []
+    for pitch, shift in ((0, 0), (4, 4), (4, 1), (3, 0)):
+        s = {k: t[k] if k == "A" else t[k][:, 0] for k in names}
+        for k in ("B", "C"):
+            wide = torch.full((N, G * S + pitch + shift), float("nan"), dtype=dtype, device="cuda")
+            s[k] = wide[:, shift:shift + G * S].unflatten(-1, (G, S))
+            s[k].copy_(t[k][:, 0])
+        got.append(ha.ha_la_scan_decode(*(s[k] for k in names), t["h0"].clone(), z=t["z"][:, 0], D=t["D"], dt_bias=t["dt_bias"]))
+    want, last, e, elast = ref.scan(flat(t["x"]), flat(t["dt"]), ref.d(t["A"]), flat(t["B"]), flat(t["C"]), ref.d(t["D"]), flat(t["z"]), ref.d(t["dt_bias"]), True,
+                                    ref.d(t["h0"]), t["seqs"])
+    off("y", got[0][0][:, None], want, ROUND[dtype] * want.abs() + 2 ** -19 * e)
+    off("state", got[0][1], last, 2 ** -19 * elast)
+    for y, state in got[1:]:
+        assert torch.equal(y, got[0][0]) and torch.equal(state, got[0][1])
+
+
+@TYPES
 def test_what_one_sequence_holds_stays_there(dtype):
     ha = _ha()
     cu = [0, 30, 37, 70]
