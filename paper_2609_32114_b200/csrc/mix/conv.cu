@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(ConvParams p) {
     return;
   }
   int t = row * p.run;
-  const int t1 = min(t + p.run, p.seqs.T_total);
+  const int t1 = t + min(p.run, p.seqs.T_total - t);
   int n = seq_of_token(p.seqs, t);
   if (c >= p.C) return;
   Taps<K, V> taps;
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kThreads) conv_back_kernel(ConvParams p) {
     return;
   }
   int t = row * p.run;
-  const int t1 = min(t + p.run, p.seqs.T_total);
+  const int t1 = t + min(p.run, p.seqs.T_total - t);
   int n = seq_of_token(p.seqs, t);
   if (c >= p.C) return;
   Taps<K, V> taps;
@@ -418,7 +418,7 @@ int width_of(const ha_la_conv_args* a, const ConvParams& p, bool back) {
 void shape(ConvParams* p, int V, bool back) {
   p->groups = (p->C + V * kThreads - 1) / (V * kThreads);
   p->run = run_of(p->seqs.T_total, p->C, V, back);
-  p->runs = (p->seqs.T_total + p->run - 1) / p->run;
+  p->runs = (int)(((long long)p->seqs.T_total + p->run - 1) / p->run);
 }
 
 // The workspace is for the narrow threads too, whatever the pointers are: the most runs that either has.
