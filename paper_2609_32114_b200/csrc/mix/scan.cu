@@ -458,8 +458,8 @@ Plan forward_plan(ScanParams* p) {
   p->segs = 1;
   f.units = p->seqs.N;
   if (p->seg_log < 31) {
-    const int L = 1 << p->seg_log;
-    p->segs = (p->seqs.T_row + L - 1) / L;
+    const long long L = 1LL << p->seg_log;
+    p->segs = (int)((p->seqs.T_row + L - 1) / L);
     f.units = p->packed ? (long long)(p->seqs.T_total >> p->seg_log) + p->seqs.N : (long long)p->seqs.N * p->segs;
     const size_t np = padded(p->S);
     f.bytes = align_up((size_t)f.units * p->C * (np + 1) * 4, 256) + align_up((size_t)p->seqs.N * p->C * np * 4, 256);

@@ -19,3 +19,12 @@ def test_convolution_of_the_most_tokens(tokens, channels):
     """The gradients' runs are up to 512 tokens long, each with five sums a channel in 32 bits."""
     have = ha.ha_la_conv_workspace_bytes(mixer.ha_la_conv_args(dtype=0, batch=1, seqlen=tokens, channels=channels, taps=4, activation=0))
     assert have >= -(-tokens // 512) * 5 * channels * 4
+
+
+@pytest.mark.parametrize("tokens,channels,groups", [(2_100_000_000, 4, 4), (2_132_000_000, 1, 1), (MOST, 1, 1), (MOST, 4, 4), (MOST, 18, 18)])
+def test_scan_of_the_most_tokens(tokens, channels, groups):
+    """Few channels are cut into segments, two and a half times as many as SMs at the most, each with a state of up to 16 and a sum of steps a channel."""
+    args = mixer.ha_la_scan_args(dtype=0, batch=1, seqlen=tokens, channels=channels, states=1, groups=groups, softplus=1)
+    have = ha.ha_la_scan_workspace_bytes(args)
+    assert 2 * channels * 17 * 4 <= have <= 400 * channels * 17 * 4 + 1024
+    assert ha.ha_la_scan_workspace_bytes(args, backward=True) >= tokens // 8 * channels * 16 * 4
