@@ -9,7 +9,7 @@ int check(const ha_la_latent_prefill_args* a, mix::PromptParams* p) {
   if (!a) return HA_LA_ERR_INVALID_ARG;
   if (a->dtype != HA_LA_BF16 && a->dtype != HA_LA_FP32) return HA_LA_ERR_INVALID_ARG;
   if (a->batch < 1 || a->num_heads < 1 || a->d_nope < 1 || a->d_rope < 0 || a->d_v < 1 || !(a->scale == a->scale)) return HA_LA_ERR_INVALID_ARG;
-  if (a->d_nope > 256 || a->d_rope > 128 || a->d_v > 256 || a->num_heads > 65535) return HA_LA_ERR_UNSUPPORTED;
+  if (a->d_nope > mix::kMostNope || a->d_rope > mix::kMostRope || a->d_v > mix::kMostValue || a->num_heads > 65535) return HA_LA_ERR_UNSUPPORTED;
   *p = mix::PromptParams{};
   if (!mix::make_seqs(&p->q_seqs, a->cu_seqlens, a->batch, a->seqlen, a->num_seqs, a->max_seqlen) ||
       !mix::make_seqs(&p->k_seqs, a->cu_seqlens_k, a->batch, a->seqlen_k, a->num_seqs, 0))
@@ -41,7 +41,7 @@ int check(const ha_la_latent_decode_args* a, mix::TokenParams* p) {
   if (a->num_seqs < 0 || a->new_tokens < 1 || a->num_heads < 1 || a->d_latent < 1 || a->d_rope < 0 || a->page_size < 1 || (a->page_size & (a->page_size - 1)) ||
       a->num_pages < 0 || a->max_pages < 0 || !(a->scale == a->scale))
     return HA_LA_ERR_INVALID_ARG;
-  if (a->d_latent > 512 || a->d_rope > 128 || (long long)a->new_tokens * a->num_heads > (1 << 20)) return HA_LA_ERR_UNSUPPORTED;
+  if (a->d_latent > mix::kMostLatent || a->d_rope > mix::kMostRope || (long long)a->new_tokens * a->num_heads > (1 << 20)) return HA_LA_ERR_UNSUPPORTED;
   if ((long long)a->num_pages * a->page_size > 0x7fffffffLL || (long long)a->num_seqs * a->new_tokens * a->num_heads > 0x7fffffffLL) return HA_LA_ERR_UNSUPPORTED;
   *p = mix::TokenParams{};
   p->N = a->num_seqs; p->T = a->new_tokens; p->H = a->num_heads; p->dl = a->d_latent; p->dr = a->d_rope;

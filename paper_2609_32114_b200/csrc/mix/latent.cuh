@@ -10,6 +10,7 @@ namespace ha_la {
 namespace mix {
 
 constexpr float kNegInf = -INFINITY;
+constexpr int kMostNope = 256, kMostRope = 128, kMostValue = 256, kMostLatent = 512;      // channels that calls may have
 
 struct PromptParams {
   Seqs q_seqs, k_seqs;

@@ -10,6 +10,7 @@ namespace mix {
 namespace {
 
 constexpr int kRows = 8, kKeys = 32, kThreads = 32 * kRows;
+static_assert(kMostValue <= 8 * 32 && kMostLatent <= 16 * 32, "a lane's channels");
 
 // One CTA: rows r < rows with their limits (keys that row r sees), queries in s_q; `key(j, c)` and `value(j, c)` bring element c of key j.
 template <int CH, typename Key, typename Value, typename Out>
@@ -111,10 +112,11 @@ __global__ void __launch_bounds__(kThreads) latent_token_kernel(TokenParams p) {
              });
 }
 
-template <typename P> cudaError_t go(void (*k)(P), const P& p, long long grid, size_t smem, cudaStream_t stream) {
+// `most`: for the largest head sizes that the library takes, whatever this call's are; a limit of the call's own would be another host thread's to lower.
+template <auto kern, typename P> cudaError_t go(const P& p, long long grid, size_t smem, size_t most, cudaStream_t stream) {
   if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
-  const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(k), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  return e == cudaSuccess ? start(k, dim3((unsigned)grid), kThreads, smem, stream, p) : e;
+  const cudaError_t e = allow_smem<kern>(most);
+  return e == cudaSuccess ? start(kern, dim3((unsigned)grid), kThreads, smem, stream, p) : e;
 }
 
 }  // namespace
@@ -122,12 +124,15 @@ template <typename P> cudaError_t go(void (*k)(P), const P& p, long long grid, s
 cudaError_t launch_prompt_simt(bool bf16, const PromptParams& given, cudaStream_t stream) {
   PromptParams p = given;
   p.blocks = (p.q_seqs.max_len + kRows - 1) / kRows;
-  return go(bf16 ? latent_prompt_kernel<__nv_bfloat16> : latent_prompt_kernel<float>, p, (long long)p.q_seqs.N * p.blocks * p.H, smem_of(p.dn + p.dr, p.dv, false), stream);
+  const long long grid = (long long)p.q_seqs.N * p.blocks * p.H;
+  const size_t smem = smem_of(p.dn + p.dr, p.dv, false), most = smem_of(kMostNope + kMostRope, kMostValue, false);
+  return bf16 ? go<latent_prompt_kernel<__nv_bfloat16>>(p, grid, smem, most, stream) : go<latent_prompt_kernel<float>>(p, grid, smem, most, stream);
 }
 
 cudaError_t launch_token_simt(bool bf16, const TokenParams& p, cudaStream_t stream) {
-  const long long blocks = ((long long)p.T * p.H + kRows - 1) / kRows;
-  return go(bf16 ? latent_token_kernel<__nv_bfloat16> : latent_token_kernel<float>, p, p.N * blocks, smem_of(p.dl + p.dr, p.dl, true), stream);
+  const long long grid = p.N * (((long long)p.T * p.H + kRows - 1) / kRows);
+  const size_t smem = smem_of(p.dl + p.dr, p.dl, true), most = smem_of(kMostLatent + kMostRope, kMostLatent, true);
+  return bf16 ? go<latent_token_kernel<__nv_bfloat16>>(p, grid, smem, most, stream) : go<latent_token_kernel<float>>(p, grid, smem, most, stream);
 }
 
 }  // namespace mix
