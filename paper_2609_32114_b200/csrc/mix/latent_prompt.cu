@@ -157,7 +157,8 @@ latent_prompt_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     __syncwarp();
   } else {
     // ------------------------------------------------------------ softmax: a thread to a query
-    const int t = warp >> 2, quad = warp & 3, row = 32 * quad + lane, i_q = g.r0 + 128 * t + row, limit = seen_by(g, i_q);
+    const int t = warp >> 2, quad = warp & 3, row = 32 * quad + lane, i_q = g.r0 + 128 * t + row;
+    const int limit = i_q < g.q ? seen_by(g, i_q) : 0;     // (rows of the tile behind the sequence hold another's queries, which have no say in when this one is rescaled)
     const uint32_t lanes = static_cast<uint32_t>(32 * quad) << 16, S = tm + kTmS + 128 * t + lanes, O = tm + kTmO + 128 * t + lanes;
     const float to_log2 = p.scale * 1.4426950408889634f;
     const int count = t == 0 ? steps[0] : steps[TILES - 1];
