@@ -337,12 +337,13 @@ latent_token_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         load_columns<NR>(tm + C::kTmS + NR * (tile & 1) + lanes, raw);
         const int j = t * kTile + row;
         float s[NR];
-        const bool partly = (t + 1) * kTile > low + (p.T > 1 ? r0 / p.H : 0);   // (of the block's first token)
+        // (not every row is seen by the block's first token; or columns behind the sequence's hold another's queries, which have no say in when this one is rescaled)
+        const bool partly = rows < NR || (t + 1) * kTile > low + (p.T > 1 ? r0 / p.H : 0);
 #pragma unroll
         for (int r = 0; r < NR; ++r) s[r] = mine ? __uint_as_float(raw[r]) * to_log2 : kNegInf;
         if (partly) {
 #pragma unroll
-          for (int r = 0; r < NR; ++r) s[r] = j < low + (p.T > 1 ? (r0 + r) / p.H : 0) && j < len ? s[r] : kNegInf;
+          for (int r = 0; r < NR; ++r) s[r] = r < rows && j < low + (p.T > 1 ? (r0 + r) / p.H : 0) && j < len ? s[r] : kNegInf;
         }
         bool over = t == walk.t0;
 #pragma unroll

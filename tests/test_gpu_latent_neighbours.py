@@ -3,7 +3,7 @@ no comparison lets through, are elsewhere.)"""
 import pytest
 import torch
 
-from tests.test_gpu_latent import TC, prompt, run_prompt
+from tests.test_gpu_latent import TC, prompt, run_prompt, run_tokens, tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -19,3 +19,17 @@ def test_prompts_beside_large_queries(H, first):
         s["q"][:, first:] *= size
         got = run_prompt(s, 0.07)
         assert torch.equal(got[0][:, :first], want[0][:, :first]) and torch.equal(got[1][:, :first], want[1][:, :first]), size
+
+
+@pytest.mark.parametrize("H,new,lens", [(24, 1, (700, 500, 64)), (9, 1, (2000, 30, 500)), (5, 3, (300, 300, 300)), (40, 2, (1500, 200, 90))])
+def test_new_tokens_beside_large_queries(H, new, lens):
+    """Heads fill up to 16, 32 or 64 columns; what fills the rest are the next sequence's."""
+    t = tokens(list(lens), new, H, 64, torch.bfloat16, seed=H, junk=0.0)
+    want = run_tokens(t, 0.05)
+    for size in (0.0, 5.0, 100.0):
+        for n in range(3):
+            s = dict(t, q=t["q"].clone())
+            s["q"][:n] *= size
+            s["q"][n + 1:] *= size
+            got = run_tokens(s, 0.05)
+            assert torch.equal(got[0][n], want[0][n]) and torch.equal(got[1][n], want[1][n]), (size, n)
