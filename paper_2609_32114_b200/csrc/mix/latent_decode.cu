@@ -327,7 +327,8 @@ latent_token_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       float l[NR];
 #pragma unroll
       for (int r = 0; r < NR; ++r) l[r] = 0.f;
-      if (tid < NR) s_m[tid] = kNegInf;
+      // (columns behind the sequence's hold another's queries: nothing exceeds their maximum, so they have no say in when this one is rescaled)
+      if (tid < NR) s_m[tid] = tid < rows ? kNegInf : INFINITY;
       softmax_sync();
       for (int t = walk.t0; t < walk.t1; ++t, ++tile) {
         wait_for(&scores[tile & 1], (tile >> 1) & 1, abort_flag);
@@ -337,13 +338,12 @@ latent_token_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         load_columns<NR>(tm + C::kTmS + NR * (tile & 1) + lanes, raw);
         const int j = t * kTile + row;
         float s[NR];
-        // (not every row is seen by the block's first token; or columns behind the sequence's hold another's queries, which have no say in when this one is rescaled)
-        const bool partly = rows < NR || (t + 1) * kTile > low + (p.T > 1 ? r0 / p.H : 0);
+        const bool partly = (t + 1) * kTile > low + (p.T > 1 ? r0 / p.H : 0);   // (of the block's first token)
 #pragma unroll
         for (int r = 0; r < NR; ++r) s[r] = mine ? __uint_as_float(raw[r]) * to_log2 : kNegInf;
         if (partly) {
 #pragma unroll
-          for (int r = 0; r < NR; ++r) s[r] = r < rows && j < low + (p.T > 1 ? (r0 + r) / p.H : 0) && j < len ? s[r] : kNegInf;
+          for (int r = 0; r < NR; ++r) s[r] = j < low + (p.T > 1 ? (r0 + r) / p.H : 0) && j < len ? s[r] : kNegInf;
         }
         bool over = t == walk.t0;
 #pragma unroll

@@ -21,13 +21,15 @@ def test_prompts_beside_large_queries(H, first):
         assert torch.equal(got[0][:, :first], want[0][:, :first]) and torch.equal(got[1][:, :first], want[1][:, :first]), size
 
 
-@pytest.mark.parametrize("H,new,lens", [(24, 1, (700, 500, 64)), (9, 1, (2000, 30, 500)), (5, 3, (300, 300, 300)), (40, 2, (1500, 200, 90))])
+@pytest.mark.parametrize("H,new,lens", [(24, 1, (700, 500, 64)), (9, 1, (2000, 30, 500)), (5, 3, (300, 300, 300)), (40, 2, (1500, 200, 90)),
+                                        (24, 1, (4000,) * 16), (9, 1, (4000, 3000) * 8), (5, 3, (2500,) * 24), (40, 2, (3000,) * 12)], ids=str)
 def test_new_tokens_beside_large_queries(H, new, lens):
-    """Heads fill up to 16, 32 or 64 columns; what fills the rest are the next sequence's."""
+    """Heads fill up to 16, 32 or 64 columns; what fills the rest are the next sequence's.  Few sequences, a part of a context to a CTA; many, with several tiles
+    one behind the other, between which the results may be rescaled."""
     t = tokens(list(lens), new, H, 64, torch.bfloat16, seed=H, junk=0.0)
     want = run_tokens(t, 0.05)
     for size in (0.0, 5.0, 100.0):
-        for n in range(3):
+        for n in (0, 1, len(lens) // 2):
             s = dict(t, q=t["q"].clone())
             s["q"][:n] *= size
             s["q"][n + 1:] *= size
