@@ -644,6 +644,16 @@ template <typename F, typename A> int without_lock(F f, const A* args, void* str
   return rc;
 }
 
+// an optional contiguous tensor of that shape, or one with more behind it: longer in the first dimension that is not one
+bool laid_out(const at::Tensor* t, const at::Tensor& like, at::ScalarType type, at::IntArrayRef shape) {
+  if (!t) return true;
+  if (t->device() != like.device() || t->scalar_type() != type || !t->is_contiguous() || t->dim() != (int64_t)shape.size()) return false;
+  const auto have = t->sizes();
+  size_t i = 0;
+  while (i + 1 < shape.size() && shape[i] == 1 && have[i] == 1) ++i;
+  return have[i] >= shape[i] && have.slice(i + 1) == shape.slice(i + 1);
+}
+
 // x [B, T, C] (`token`: [N, C]), w, bias, activation, cu_seqlens
 bool conv_inputs(const at::Tensor* x, const at::Tensor* w, const at::Tensor* bias, PyObject* act, const at::Tensor* cu, bool token, ha_la_conv_args* d, int64_t* N) {
   if (!element(x) || x->dim() != (token ? 2 : 3) || !w || w->dim() != 2) return false;
@@ -671,7 +681,7 @@ PyObject* conv_call(PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
   const at::ScalarType type = x->scalar_type();
   const int64_t C = d.channels, K = d.taps - 1;
-  if (!room(h0, *x, type, N * K * C) || !room(y, *x, type, x->numel()) || !room(hT, *x, type, N * K * C) || !room(sw, *x, at::kInt, 1)) Py_RETURN_NONE;
+  if (!laid_out(h0, *x, type, {N, K, C}) || !laid_out(y, *x, type, x->sizes()) || !laid_out(hT, *x, type, {N, K, C}) || !room(sw, *x, at::kInt, 1)) Py_RETURN_NONE;
   const int want = hT ? 0 : PyObject_IsTrue(a[9]);
   if (want < 0) return nullptr;
   Outputs out(a[11], *x);
@@ -698,8 +708,8 @@ PyObject* conv_backward_call(PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
   const at::ScalarType type = x->scalar_type();
   const int64_t C = d.channels, K = d.taps - 1;
-  if (!same(dy, *x, type, x->sizes()) || !room(h0, *x, type, N * K * C) || !room(dhT, *x, type, N * K * C) || !room(dx, *x, type, x->numel()) ||
-      !room(dw, *x, at::kFloat, C * (K + 1)) || !room(db, *x, at::kFloat, C) || !room(dh0, *x, type, N * K * C) || !scratch_ok(ws, *x) || !room(sw, *x, at::kInt, 1))
+  if (!same(dy, *x, type, x->sizes()) || !laid_out(h0, *x, type, {N, K, C}) || !laid_out(dhT, *x, type, {N, K, C}) || !laid_out(dx, *x, type, x->sizes()) ||
+      !laid_out(dw, *x, at::kFloat, {C, K + 1}) || !laid_out(db, *x, at::kFloat, {C}) || !laid_out(dh0, *x, type, {N, K, C}) || !scratch_ok(ws, *x) || !room(sw, *x, at::kInt, 1))
     Py_RETURN_NONE;
   size_t need = 0;
   if (g_conv_bytes(&d, &need) != HA_LA_OK) Py_RETURN_NONE;
@@ -731,7 +741,7 @@ PyObject* conv_decode_call(PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
   const at::ScalarType type = x->scalar_type();
   const int64_t C = d.channels, K = d.taps - 1;
-  if (!room(st, *x, type, N * K * C) || !room(so, *x, type, N * K * C) || !room(y, *x, type, x->numel())) Py_RETURN_NONE;
+  if (!laid_out(st, *x, type, {N, K, C}) || !laid_out(so, *x, type, {N, K, C}) || !laid_out(y, *x, type, x->sizes())) Py_RETURN_NONE;
   Outputs out(a[7], *x);
   if (!out.set()) return nullptr;
   y = out.take(y, x->sizes(), type);
@@ -776,8 +786,9 @@ PyObject* scan_call(PyObject* const* a, Py_ssize_t n) {
       !unpack(a[7], &bias) || !unpack(a[9], &h0) || !unpack(a[10], &cu) || !unpack(a[12], &y) || !unpack(a[13], &hT) || !unpack(a[15], &ws) || !unpack(a[16], &sw) ||
       !scan_inputs(x, dt, A, B, C, D, z, bias, a[8], cu, false, &d, &N) || !length(a[11], &d.max_seqlen))
     Py_RETURN_NONE;
-  const int64_t ch = d.channels, S = d.states, state = N * ch * S;
-  if (!room(h0, *x, at::kFloat, state) || !room(y, *x, x->scalar_type(), x->numel()) || !room(hT, *x, at::kFloat, state) || !scratch_ok(ws, *x) || !room(sw, *x, at::kInt, 1))
+  const int64_t ch = d.channels, S = d.states;
+  const int64_t state[3] = {N, ch, S};
+  if (!laid_out(h0, *x, at::kFloat, state) || !laid_out(y, *x, x->scalar_type(), x->sizes()) || !laid_out(hT, *x, at::kFloat, state) || !scratch_ok(ws, *x) || !room(sw, *x, at::kInt, 1))
     Py_RETURN_NONE;
   size_t need = 0;
   if (g_scan_bytes(&d, 0, &need) != HA_LA_OK) Py_RETURN_NONE;
@@ -808,10 +819,11 @@ PyObject* scan_backward_call(PyObject* const* a, Py_ssize_t n) {
       !unpack(a[24], &ws) || !unpack(a[25], &sw) || !scan_inputs(x, dt, A, B, C, D, z, bias, a[9], cu, false, &d, &N) || !length(a[13], &d.max_seqlen))
     Py_RETURN_NONE;
   const at::ScalarType type = x->scalar_type(), f32 = at::kFloat;
-  const int64_t ch = d.channels, S = d.states, state = N * ch * S;
-  if (!same(dy, *x, type, x->sizes()) || !room(h0, *x, f32, state) || !room(dhT, *x, f32, state) || !room(dx, *x, type, x->numel()) || !room(ddt, *x, type, x->numel()) ||
-      !room(dA, *x, f32, ch * S) || !room(dB, *x, type, B->numel()) || !room(dC, *x, type, B->numel()) || !room(dD, *x, f32, ch) || !room(dz, *x, type, x->numel()) ||
-      !room(dbias, *x, f32, ch) || !room(dh0, *x, f32, state) || !scratch_ok(ws, *x) || !room(sw, *x, at::kInt, 1))
+  const int64_t ch = d.channels, S = d.states;
+  const int64_t state[3] = {N, ch, S};
+  if (!same(dy, *x, type, x->sizes()) || !laid_out(h0, *x, f32, state) || !laid_out(dhT, *x, f32, state) || !laid_out(dx, *x, type, x->sizes()) || !laid_out(ddt, *x, type, x->sizes()) ||
+      !laid_out(dA, *x, f32, {ch, S}) || !laid_out(dB, *x, type, B->sizes()) || !laid_out(dC, *x, type, B->sizes()) || !laid_out(dD, *x, f32, {ch}) ||
+      !laid_out(dz, *x, type, x->sizes()) || !laid_out(dbias, *x, f32, {ch}) || !laid_out(dh0, *x, f32, state) || !scratch_ok(ws, *x) || !room(sw, *x, at::kInt, 1))
     Py_RETURN_NONE;
   size_t need = 0;
   if (g_scan_bytes(&d, 1, &need) != HA_LA_OK) Py_RETURN_NONE;
@@ -848,8 +860,9 @@ PyObject* scan_decode_call(PyObject* const* a, Py_ssize_t n) {
   if (!unpack(a[0], &x) || !unpack(a[1], &dt) || !unpack(a[2], &A) || !unpack(a[3], &B) || !unpack(a[4], &C) || !unpack(a[5], &st) || !unpack(a[6], &D) ||
       !unpack(a[7], &z) || !unpack(a[8], &bias) || !unpack(a[10], &y) || !unpack(a[11], &so) || !scan_inputs(x, dt, A, B, C, D, z, bias, a[9], nullptr, true, &d, &N))
     Py_RETURN_NONE;
-  const int64_t ch = d.channels, S = d.states, state = N * ch * S;
-  if (!room(st, *x, at::kFloat, state) || !room(so, *x, at::kFloat, state) || !room(y, *x, x->scalar_type(), x->numel())) Py_RETURN_NONE;
+  const int64_t ch = d.channels, S = d.states;
+  const int64_t state[3] = {N, ch, S};
+  if (!laid_out(st, *x, at::kFloat, state) || !laid_out(so, *x, at::kFloat, state) || !laid_out(y, *x, x->scalar_type(), x->sizes())) Py_RETURN_NONE;
   Outputs out(a[12], *x);
   if (!out.set()) return nullptr;
   y = out.take(y, x->sizes(), x->scalar_type());
@@ -882,7 +895,7 @@ PyObject* latent_prefill_call(PyObject* const* a, Py_ssize_t n) {
   const at::IntArrayRef lead_k(keys, 2);
   if (!token_rows(q, *q, qs.slice(0, 2), {H, dq}, &d.q_stride) || !token_rows(kr, *q, lead_k, {dr}, &d.kr_stride) ||
       !head_rows(kn, *q, lead_k, H, &d.kn_stride, &d.kn_head_stride, &dn) || !head_rows(v, *q, lead_k, H, &d.v_stride, &d.v_head_stride, &dv) || dn + dr != dq ||
-      (cuk && !same(cuk, *q, at::kInt, cu->sizes())) || dv > 4096 || !room(o, *q, q->scalar_type(), B * T * H * dv) || !room(lse, *q, at::kFloat, B * T * H) ||
+      (cuk && !same(cuk, *q, at::kInt, cu->sizes())) || dv > 4096 || !laid_out(o, *q, q->scalar_type(), {B, T, H, dv}) || !laid_out(lse, *q, at::kFloat, {B, T, H}) ||
       !room(sw, *q, at::kInt, 1))
     Py_RETURN_NONE;
   d.dtype = q->scalar_type() == at::kFloat;
@@ -918,7 +931,7 @@ PyObject* latent_decode_call(PyObject* const* a, Py_ssize_t n) {
   if (d.d_latent < 1 || d.d_latent > D) Py_RETURN_NONE;
   const int64_t dl = d.d_latent;
   if (!same(cache, *q, q->scalar_type(), {P, page, D}) || !same(table, *q, at::kInt, {N, M}) || !same(lengths, *q, at::kInt, {N}) ||
-      !room(o, *q, q->scalar_type(), N * T * H * dl) || !room(lse, *q, at::kFloat, N * T * H) || !scratch_ok(ws, *q) || !room(sw, *q, at::kInt, 1))
+      !laid_out(o, *q, q->scalar_type(), {N, T, H, dl}) || !laid_out(lse, *q, at::kFloat, {N, T, H}) || !scratch_ok(ws, *q) || !room(sw, *q, at::kInt, 1))
     Py_RETURN_NONE;
   d.dtype = q->scalar_type() == at::kFloat;
   d.num_seqs = (int32_t)N; d.new_tokens = (int32_t)T; d.num_heads = (int32_t)H; d.d_rope = (int32_t)(D - dl);

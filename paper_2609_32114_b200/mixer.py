@@ -4,7 +4,8 @@ state space scan, forward, backward and one token; attention over latent rows, f
 As in `layer`: marshalling only, torch CUDA tensors in and out, everything is computed by the library's kernels on the caller's
 stream, nothing is synchronised, tensors whose type, layout, size or device does not fit raise ValueError before anything is launched,
 and nothing is recorded for autograd.  Inputs with one row to a token may be rows of a wider tensor (slices of a fused projection's
-output along the last dimension); outputs are contiguous.
+output along the last dimension); outputs are contiguous.  States, outputs and their gradients that a caller hands in have the shape that is
+written beside them, or more behind it (a longer first dimension): one with as many elements in another order is refused.
 """
 from __future__ import annotations
 
@@ -144,6 +145,19 @@ def _vector(t, like, name, shape):
         _as(t, like, name, shape, torch.float32)
 
 
+def _laid_out(name, t, like, dtype, shape):
+    """A tensor (or None) that the kernels take by its address: contiguous, of that shape, or with more behind it: longer in the first dimension that is not one.
+    A state with its last dimensions the other way round has as many elements, so those do not tell."""
+    if t is None:
+        return
+    have, shape = tuple(t.shape), tuple(shape)
+    i = next((i for i, n in enumerate(shape) if n != 1), len(shape) - 1)
+    i = next((j for j in range(i) if have[j:j + 1] != (1,)), i)
+    fits = len(have) == len(shape) and have[:i] == shape[:i] and have[i] >= shape[i] and have[i + 1:] == shape[i + 1:]
+    if not (_reachable(t, like) and t.is_contiguous() and t.dtype == dtype and fits):
+        raise ValueError(f"{name}: {t.dtype} {have}, strides {tuple(t.stride())}, on {t.device}; wanted is {dtype} {shape}, contiguous, on {like.device}")
+
+
 def _sequences(x, cu_seqlens, name):
     """(batch, tokens, sequences) of [B, T, ..] or [T, ..]."""
     import torch
@@ -219,8 +233,9 @@ def ha_la_conv(x, w, *, bias=None, activation="silu", h0=None, cu_seqlens=None, 
     import torch
 
     args, N, C, K = _conv_args("ha_la_conv", x, w, bias, activation, cu_seqlens, max_seqlen)
-    for name, t, dt, n in (("h0", h0, x.dtype, N * K * C), ("y", y, x.dtype, x.numel()), ("hT", hT, x.dtype, N * K * C), ("status_word", status_word, torch.int32, 1)):
-        _check_room(name, t, x, dt, n)
+    for name, t, shape in (("h0", h0, (N, K, C)), ("y", y, x.shape), ("hT", hT, (N, K, C))):
+        _laid_out(name, t, x, x.dtype, shape)
+    _check_room("status_word", status_word, x, torch.int32, 1)
     with _On(stream, x) as on:
         y = on.new(y, x.shape, x.dtype)
         if want_hT or hT is not None:
@@ -247,10 +262,11 @@ def ha_la_conv_backward(dy, x, w, *, bias=None, activation="silu", h0=None, dhT=
 
     args, N, C, K = _conv_args("ha_la_conv_backward", x, w, bias, activation, cu_seqlens, max_seqlen)
     _as(dy, x, "dy", x.shape)
-    for name, t, dt, n in (("h0", h0, x.dtype, N * K * C), ("dhT", dhT, x.dtype, N * K * C), ("dx", dx, x.dtype, x.numel()), ("dw", dw, torch.float32, C * (K + 1)),
-                           ("db", db, torch.float32, C), ("dh0", dh0, x.dtype, N * K * C), ("workspace", workspace, None, 0),
-                           ("status_word", status_word, torch.int32, 1)):
-        _check_room(name, t, x, dt, n)
+    for name, t, dt, shape in (("h0", h0, x.dtype, (N, K, C)), ("dhT", dhT, x.dtype, (N, K, C)), ("dx", dx, x.dtype, x.shape), ("dw", dw, torch.float32, (C, K + 1)),
+                               ("db", db, torch.float32, (C,)), ("dh0", dh0, x.dtype, (N, K, C))):
+        _laid_out(name, t, x, dt, shape)
+    _check_room("workspace", workspace, x, None, 0)
+    _check_room("status_word", status_word, x, torch.int32, 1)
     with _On(stream, x) as on:
         dx, dw = on.new(dx, x.shape, x.dtype), on.new(dw, (C, K + 1), torch.float32)
         db = on.new(db, (C,), torch.float32) if bias is not None else None
@@ -276,8 +292,8 @@ def ha_la_conv_decode(x, w, state, *, bias=None, activation="silu", y=None, stat
         raise HaLaError(r, "ha_la_conv_decode")
     args, _, C, K = _conv_args("ha_la_conv_decode", x, w, bias, activation, None, 0, (2,))
     N = x.shape[0]
-    for name, t, n in (("state", state, N * K * C), ("state_out", state_out, N * K * C), ("y", y, x.numel())):
-        _check_room(name, t, x, x.dtype, n)
+    for name, t, shape in (("state", state, (N, K, C)), ("state_out", state_out, (N, K, C)), ("y", y, x.shape)):
+        _laid_out(name, t, x, x.dtype, shape)
     args.batch, args.seqlen = N, 1
     with _On(stream, x) as on:
         y = on.new(y, x.shape, x.dtype)
@@ -326,9 +342,10 @@ def ha_la_scan(x, dt, A, B, C, *, D=None, z=None, dt_bias=None, softplus=True, h
     import torch
 
     args, N, ch, S = _scan_args("ha_la_scan", x, dt, A, B, C, D, z, dt_bias, softplus, cu_seqlens, max_seqlen)
-    for name, t, dt_, n in (("h0", h0, torch.float32, N * ch * S), ("y", y, x.dtype, x.numel()), ("hT", hT, torch.float32, N * ch * S),
-                            ("workspace", workspace, None, 0), ("status_word", status_word, torch.int32, 1)):
-        _check_room(name, t, x, dt_, n)
+    for name, t, dt_, shape in (("h0", h0, torch.float32, (N, ch, S)), ("y", y, x.dtype, x.shape), ("hT", hT, torch.float32, (N, ch, S))):
+        _laid_out(name, t, x, dt_, shape)
+    _check_room("workspace", workspace, x, None, 0)
+    _check_room("status_word", status_word, x, torch.int32, 1)
     with _On(stream, x) as on:
         y = on.new(y, x.shape, x.dtype)
         if want_hT or hT is not None:
@@ -359,11 +376,12 @@ def ha_la_scan_backward(dy, x, dt, A, B, C, *, D=None, z=None, dt_bias=None, sof
     args, N, ch, S = _scan_args("ha_la_scan_backward", x, dt, A, B, C, D, z, dt_bias, softplus, cu_seqlens, max_seqlen)
     _as(dy, x, "dy", x.shape)
     f32 = torch.float32
-    for name, t, dt_, n in (("h0", h0, f32, N * ch * S), ("dhT", dhT, f32, N * ch * S), ("dx", dx, x.dtype, x.numel()), ("ddt", ddt, x.dtype, x.numel()),
-                            ("dA", dA, f32, ch * S), ("dB", dB, x.dtype, B.numel()), ("dC", dC, x.dtype, B.numel()), ("dD", dD, f32, ch),
-                            ("dz", dz, x.dtype, x.numel()), ("ddt_bias", ddt_bias, f32, ch), ("dh0", dh0, f32, N * ch * S), ("workspace", workspace, None, 0),
-                            ("status_word", status_word, torch.int32, 1)):
-        _check_room(name, t, x, dt_, n)
+    for name, t, dt_, shape in (("h0", h0, f32, (N, ch, S)), ("dhT", dhT, f32, (N, ch, S)), ("dx", dx, x.dtype, x.shape), ("ddt", ddt, x.dtype, x.shape),
+                                ("dA", dA, f32, (ch, S)), ("dB", dB, x.dtype, B.shape), ("dC", dC, x.dtype, B.shape), ("dD", dD, f32, (ch,)),
+                                ("dz", dz, x.dtype, x.shape), ("ddt_bias", ddt_bias, f32, (ch,)), ("dh0", dh0, f32, (N, ch, S))):
+        _laid_out(name, t, x, dt_, shape)
+    _check_room("workspace", workspace, x, None, 0)
+    _check_room("status_word", status_word, x, torch.int32, 1)
     with _On(stream, x) as on:
         dx, ddt = on.new(dx, x.shape, x.dtype), on.new(ddt, x.shape, x.dtype)
         dB, dC = on.new(dB, B.shape, x.dtype), on.new(dC, B.shape, x.dtype)
@@ -397,8 +415,8 @@ def ha_la_scan_decode(x, dt, A, B, C, state, *, D=None, z=None, dt_bias=None, so
 
     args, _, ch, S = _scan_args("ha_la_scan_decode", x, dt, A, B, C, D, z, dt_bias, softplus, None, 0, (2,))
     N = x.shape[0]
-    for name, t, dt_, n in (("state", state, torch.float32, N * ch * S), ("state_out", state_out, torch.float32, N * ch * S), ("y", y, x.dtype, x.numel())):
-        _check_room(name, t, x, dt_, n)
+    for name, t, dt_, shape in (("state", state, torch.float32, (N, ch, S)), ("state_out", state_out, torch.float32, (N, ch, S)), ("y", y, x.dtype, x.shape)):
+        _laid_out(name, t, x, dt_, shape)
     args.batch, args.seqlen = N, 1
     with _On(stream, x) as on:
         y = on.new(y, x.shape, x.dtype)
@@ -477,8 +495,9 @@ def ha_la_latent_prefill(q, kn, kr, v, *, scale=1.0, cu_seqlens=None, cu_seqlens
     v_stride, v_head, dv = _heads(v, q, "v", keys, H)
     if dn + dr != dq:
         raise ValueError(f"q: {tuple(q.shape)}; wanted are kn's {dn} and kr's {dr} channels together")
-    for name, t, dt, n in (("o", o, q.dtype, B * T * H * dv), ("lse", lse, torch.float32, B * T * H), ("status_word", status_word, torch.int32, 1)):
-        _check_room(name, t, q, dt, n)
+    _laid_out("o", o, q, q.dtype, (*lead, H, dv))
+    _laid_out("lse", lse, q, torch.float32, (*lead, H))
+    _check_room("status_word", status_word, q, torch.int32, 1)
     args = ha_la_latent_prefill_args(dtype=dtype, batch=B, seqlen=T, seqlen_k=keys[-1], num_heads=H, d_nope=dn, d_rope=dr, d_v=dv, scale=_float(scale, "scale"),
                                      num_seqs=N, max_seqlen=_bound(max_seqlen), cu_seqlens=_ptr(cu_seqlens), cu_seqlens_k=_ptr(cu_seqlens_k),
                                      q_stride=q_stride, kn_stride=kn_stride, kr_stride=kr_stride, v_stride=v_stride, kn_head_stride=kn_head,
@@ -524,9 +543,10 @@ def ha_la_latent_decode(q, cache, page_table, lengths, *, scale=1.0, o=None, lse
     _as(cache, q, "cache", (*cache.shape[:2], d))
     _as(page_table, q, "page_table", (N, page_table.shape[1]), torch.int32)
     _as(lengths, q, "lengths", (N,), torch.int32)
-    for name, t, dt, n in (("o", o, q.dtype, N * new * H * dl), ("lse", lse, torch.float32, N * new * H), ("workspace", workspace, None, 0),
-                           ("status_word", status_word, torch.int32, 1)):
-        _check_room(name, t, q, dt, n)
+    _laid_out("o", o, q, q.dtype, (N, new, H, dl))
+    _laid_out("lse", lse, q, torch.float32, (N, new, H))
+    _check_room("workspace", workspace, q, None, 0)
+    _check_room("status_word", status_word, q, torch.int32, 1)
     args = ha_la_latent_decode_args(dtype=dtype, num_seqs=N, new_tokens=new, num_heads=H, d_latent=dl, d_rope=d - dl, page_size=cache.shape[1],
                                     num_pages=cache.shape[0], max_pages=page_table.shape[1], scale=_float(scale, "scale"), q=_ptr(q), cache=_ptr(cache),
                                     page_table=_ptr(page_table), lengths=_ptr(lengths))
