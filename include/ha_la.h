@@ -486,8 +486,8 @@ int ha_la_scan_decode(const ha_la_scan_args* args, void* cuda_stream);
  * lse = log sum_j e^{s_ij} (natural), for joining results over parts of the keys; NULL: not wanted.  A row that sees no key has
  * o = 0 and lse = -infinity.  What no row of a sequence sees (the rest of its last page, other pages) may hold anything, NaN included.
  * What one of its rows sees has to be finite: a NaN there may reach the rows ahead of it too.
- * A length that is negative or longer than its row of the table counts as zero and is reported through the status word, as is a
- * page that does not exist, whose sequence's results are unspecified.
+ * A length that is negative, longer than its row of the table or above 2^31 - 256 counts as zero and is reported through the status
+ * word, as is a page that does not exist, whose sequence's results are unspecified.
  * Scores, their sums and o's sums are fp32; with bf16 tensors the weights are rounded to bf16 for the product with the values.
  * Tensor cores: bf16 with d_nope = 128, d_rope = 64, d_v = 128, 16-byte aligned with strides that are multiples of 8, scale > 0;
  * decode bf16 with d_latent = 512, d_rope = 64, pages of 16 rows or more, 16-byte aligned, scale > 0.  Everything else runs on the CUDA cores, much slower.    */

@@ -46,11 +46,12 @@ struct TokenParams {
 };
 
 // Cached rows of a sequence; 0 if the length does not fit.
+constexpr int kMostRows = 0x7fffffff - 255;                // (tables may name a page again and again; row numbers are 32 bits, tiles ahead of the last one included)
 __device__ __forceinline__ int rows_of(const TokenParams& p, int n) {
   const int len = p.lengths[n];
-  return len >= 0 && (long long)len <= ((long long)p.max_pages << p.page_log) ? len : 0;
+  return len >= 0 && len <= kMostRows && (long long)len <= ((long long)p.max_pages << p.page_log) ? len : 0;
 }
-// One CTA's threads look at all lengths and pages and report.
+// One CTA's threads look at all lengths and report; a page that does not exist is reported by whoever wants a row of it.
 __device__ __forceinline__ void check_tokens(const TokenParams& p) {
   if (!p.status) return;
   for (int n = threadIdx.x; n < p.N; n += blockDim.x)

@@ -20,3 +20,20 @@ def test_convolution_gradients_of_the_most_tokens():
     assert float(db) == float(torch.tensor(T, dtype=torch.float64).float()) and dh0[0, :, 0].tolist() == [1, 3, 7]
     del x, dx
     torch.cuda.empty_cache()
+
+
+def test_lengths_that_row_numbers_do_not_reach():
+    """A table may name a page as often as it likes, so that its row holds 2^31 cached rows; a length whose last tile would pass 2^31 counts as zero."""
+    import paper_2609_32114_b200 as ha
+
+    page = 1 << 20
+    if torch.cuda.mem_get_info()[0] < 10e9:
+        pytest.skip("needs 10 GB")
+    cache = torch.zeros(2, page, 576, dtype=torch.bfloat16, device="cuda")
+    cache[0, :100] = torch.randn(100, 576, device="cuda").bfloat16()
+    q = torch.randn(2, 1, 16, 576, device="cuda").bfloat16()
+    table = torch.zeros(2, 2048, dtype=torch.int32, device="cuda")
+    want = ha.ha_la_latent_decode(q, cache, table, torch.tensor([100, 0], dtype=torch.int32, device="cuda"), scale=0.05)
+    for length in (2 ** 31 - 1, 2 ** 31 - 64, 2 ** 31 - 255):
+        got = ha.ha_la_latent_decode(q, cache, table, torch.tensor([100, length], dtype=torch.int32, device="cuda"), scale=0.05)
+        assert int(got[2]) == 6 and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
