@@ -141,14 +141,13 @@ __global__ void __launch_bounds__(kThreads, 2) scan_kernel(ScanParams p) {
           if (M == kOut) cv = load_v<SP>(&s_c[b][t0 + j][s0]);
           float y = 0.f;
           if constexpr (SP == 1) {
-            h[0] = fmaf(ex2(du.x * A[0]), h[0], du.y * bv.v[0]);
+            h[0] = fmaf(decay(du.x, A[0]), h[0], du.y * bv.v[0]);
             if (M == kOut) y = h[0] * cv.v[0];
           } else {                                         // (two states to an instruction)
             float2 y2 = make_float2(0.f, 0.f);
 #pragma unroll
             for (int s = 0; s < SP; s += 2) {
-              const float2 g = ptx::mul2(make_float2(du.x, du.x), make_float2(A[s], A[s + 1]));
-              const float2 hn = ptx::fma2(make_float2(ex2(g.x), ex2(g.y)), make_float2(h[s], h[s + 1]),
+              const float2 hn = ptx::fma2(decay2(du.x, make_float2(A[s], A[s + 1])), make_float2(h[s], h[s + 1]),
                                           ptx::mul2(make_float2(du.y, du.y), make_float2(bv.v[s], bv.v[s + 1])));
               h[s] = hn.x;
               h[s + 1] = hn.y;
@@ -345,7 +344,7 @@ __global__ void __launch_bounds__(128) scan_decode_kernel(ScanParams p) {
       float y = 0.f;
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        h[i].v[s] = fmaf(ex2(delta * A.v[s] * kLog2e), h[i].v[s], u * b[i].v[s]);
+        h[i].v[s] = fmaf(decay(delta, A.v[s] * kLog2e), h[i].v[s], u * b[i].v[s]);
         y = fmaf(h[i].v[s], cc[i].v[s], y);
       }
 #pragma unroll

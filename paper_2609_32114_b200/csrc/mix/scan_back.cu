@@ -90,8 +90,7 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
           const float2 du = *reinterpret_cast<const float2*>(du0 + j * CH * 2);
 #pragma unroll
           for (int s = 0; s < SP / 2; ++s) {
-            const float2 x = ptx::mul2(make_float2(du.x, du.x), A[s]);
-            h[j][s] = ptx::fma2(make_float2(ex2(x.x), ex2(x.y)), j ? h[j - 1][s] : first[s], ptx::mul2(make_float2(du.y, du.y), make_float2(bv.v[2 * s], bv.v[2 * s + 1])));
+            h[j][s] = ptx::fma2(decay2(du.x, A[s]), j ? h[j - 1][s] : first[s], ptx::mul2(make_float2(du.y, du.y), make_float2(bv.v[2 * s], bv.v[2 * s + 1])));
           }
         }
 #pragma unroll
@@ -109,8 +108,7 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
             from_b = s ? ptx::fma2(dh[s], b2, from_b) : ptx::mul2(dh[s], b2);
             if (GATE) out = s ? ptx::fma2(h[j][s], c2, out) : ptx::mul2(h[j][s], c2);
             const float2 db = ptx::mul2(dh[s], u2), dc = ptx::mul2(h[j][s], g2);
-            const float2 x = ptx::mul2(make_float2(du.x, du.x), A[s]);   // (made again: kept, decays take as many registers as the states)
-            dh[s] = ptx::mul2(dh[s], make_float2(ex2(x.x), ex2(x.y)));
+            dh[s] = ptx::mul2(dh[s], decay2(du.x, A[s]));    // (made again: kept, decays take as many registers as the states)
             const float2 f = ptx::mul2(dh[s], j ? h[j - 1][s] : first[s]);
             from_a = s ? ptx::fma2(f, A[s], from_a) : ptx::mul2(f, A[s]);
             sum_A[s] = j == kCkpt - 1 ? ptx::mul2(f, make_float2(du.x, du.x)) : ptx::fma2(f, make_float2(du.x, du.x), sum_A[s]);
