@@ -15,6 +15,7 @@ namespace mix {
 namespace {
 
 constexpr int kWarps = 8, kScan = 32 * kWarps, kThreads = kScan + 256, kTile = 16, SP = 4;   // recurrence warps and threads
+constexpr int kFlush = 4;                                  // tiles whose sums over tokens are in 32 bits: more of them lose what each adds to a long sequence's sum
 
 template <typename In, int LS> struct BackShape {
   static constexpr int LC = 32 / LS, CH = kWarps * LC, NP = SP * LS;
@@ -24,7 +25,10 @@ template <typename In, int LS> struct BackShape {
   static constexpr int du = 0, g = du + 2 * kTile * CH * 2, b = g + 2 * kTile * CH, c = b + 2 * kTile * NP, res = c + 2 * kTile * NP,
                        bc = res + 2 * 3 * RES, floats = bc + 2 * kWarps * kTile * 2 * NP;
   static constexpr int kRowB = E * sizeof(In), kQuadB = 4 * sizeof(In), QUADS = 2 * kTile * NP / 4, BC = (QUADS + 255) / 256;
-  static constexpr size_t OFF_ROWS = floats * 4, OFF_BC = OFF_ROWS + 4 * 4 * 256 * kRowB, bytes = OFF_BC + 2 * BC * 256 * kQuadB;
+  static constexpr size_t OFF_ROWS = floats * 4, OFF_BC = OFF_ROWS + 4 * 4 * 256 * kRowB;
+  // ... and in 64 bits, a place to a thread: dA of the recurrence's, dD and the steps' gradients of the helping ones
+  static constexpr size_t OFF_DA = OFF_BC + 2 * BC * 256 * kQuadB, OFF_DD = OFF_DA + SP * kScan * 8, bytes = OFF_DD + 2 * E * 256 * 8;
+  static_assert(bytes <= 227 * 1024 && OFF_DA % 8 == 0, "shared memory");
 };
 
 template <typename In, int LS, bool GATE>
@@ -58,6 +62,9 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
       (&A[s / 2].x)[s % 2] = ok ? p.A[at] * kLog2e : 0.f;
       (&dh[s / 2].x)[s % 2] = ok && p.dhT && q.len >= 0 ? p.dhT[n * state + at] : 0.f;
     }
+    double* const total = reinterpret_cast<double*>(reinterpret_cast<uint8_t*>(sm) + S::OFF_DA) + tid;
+#pragma unroll
+    for (int s = 0; s < SP; ++s) total[s * kScan] = 0;
     const int ck0 = slot_of(p.seqs, n, tok0, kCkptLog, (p.seqs.T_row + kCkpt - 1) / kCkpt);
     constexpr int PARTS = kTile / kCkpt;
     Vec<SP> kept[PARTS] = {};                              // the states in front of a tile's parts, sent for a tile ahead
@@ -125,7 +132,14 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
           for (int e = 0; e < nbc; ++e) s_bc[((buf * kWarps + warp) * kTile + r) * 2 * NP + (pb + e) / SP * NP + s0 + (pb + e) % SP] = to_b[e];
         }
 #pragma unroll
-        for (int s = 0; s < SP / 2; ++s) dA[s] = ptx::add2(dA[s], sum_A[s]);   // (eight tokens at a time: token by token it is off by a third more; in 64 bits by no less)
+        for (int s = 0; s < SP / 2; ++s) dA[s] = ptx::add2(dA[s], sum_A[s]);   // (eight tokens at a time: token by token it is off by a third more)
+      }
+      if (i % kFlush == kFlush - 1) {
+#pragma unroll
+        for (int s = 0; s < SP; ++s) {
+          total[s * kScan] += (&dA[s / 2].x)[s % 2];
+          (&dA[s / 2].x)[s % 2] = 0.f;
+        }
       }
       __syncthreads();
     }
@@ -133,7 +147,7 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
     for (int s = 0; s < SP; ++s)
       if (mine && s0 + s < p.S) {
         const size_t at = n * state + (size_t)(c0 + c) * p.S + s0 + s;
-        p.part_a[at] = (&dA[s / 2].x)[s % 2];
+        p.part_a[at] = (float)(total[s * kScan] + (&dA[s / 2].x)[s % 2]);
         if (p.dh0 && q.len >= 0) p.dh0[at] = (&dh[s / 2].x)[s % 2];
       }
     __syncthreads();
@@ -148,6 +162,17 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
   const In *B = reinterpret_cast<const In*>(p.B) + (size_t)group * p.S, *C = reinterpret_cast<const In*>(p.C_) + (size_t)group * p.S;
   Vec<E> bias = {}, skip = {};
   float dD[E] = {}, dbias[E] = {};
+  double* const totals = reinterpret_cast<double*>(reinterpret_cast<uint8_t*>(sm) + S::OFF_DD);       // [dD, dbias][channel of a thread][thread]
+  auto flush = [&] {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      totals[e * 256 + ht] += dD[e];
+      totals[(E + e) * 256 + ht] += dbias[e];
+      dD[e] = dbias[e] = 0.f;
+    }
+  };
+#pragma unroll
+  for (int e = 0; e < 2 * E; ++e) totals[e * 256 + ht] = 0;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     if (p.dt_bias && e < have) bias.v[e] = p.dt_bias[c0 + c + e];
@@ -271,27 +296,20 @@ __global__ void __launch_bounds__(kThreads) scan_back_kernel(ScanParams p) {
     asm volatile("cp.async.wait_group 1;" ::: "memory");
     if (i + 1 < tiles) put(i + 1);
     if (i > 0) finish(i - 1);
+    if (i % kFlush == 0) flush();
     if (i + 3 < tiles) fetch(i + 3);
     sent();
     if (i < tiles) __syncthreads();
   }
-  // over the rows: through the places of the results, which nobody reads any more but the helping warps themselves
+  // over the rows
+  flush();
   __syncthreads();
-  float* const s_sum = s_res;                              // [row][dD, dbias][channel]
-  if (row < kTile) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      s_sum[(row * 2) * CH + c + e] = dD[e];
-      s_sum[(row * 2 + 1) * CH + c + e] = dbias[e];
-    }
-  }
-  asm volatile("bar.sync 1, 256;" ::: "memory");
   if (ht < 2 * CH) {
-    float sum = 0.f;
+    const int kind = ht / CH, cc = ht % CH;
+    double sum = 0;
 #pragma unroll
-    for (int r = 0; r < kTile; ++r) sum += s_sum[r * 2 * CH + ht];
-    const int cc = ht % CH;
-    if (cc < left) p.part_d[((size_t)n * 2 + ht / CH) * p.C + c0 + cc] = sum;
+    for (int r = 0; r < kTile; ++r) sum += totals[(kind * E + cc % E) * 256 + r * S::TPR + cc / E];
+    if (cc < left) p.part_d[((size_t)n * 2 + kind) * p.C + c0 + cc] = (float)sum;
   }
 }
 

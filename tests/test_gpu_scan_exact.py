@@ -1,4 +1,5 @@
 """How exact the selective scan is where 2^-19 of everything would hide it: steps of every size by themselves, and sums over many tokens."""
+import numpy as np
 import pytest
 import torch
 
@@ -48,3 +49,30 @@ def test_decays_on_the_average():
         assert float(error.abs().max()) <= 2 ** -22 + 2 ** -23 * 2 ** max(octave, 0)
     _, state = _ha().ha_la_scan_decode(zero, zero, A, one, one, st, softplus=False, state_out=torch.empty_like(st))
     assert torch.equal(state, st)                            # nothing passes: not one bit changes
+
+
+def test_gradients_that_add_up_over_many_tokens():
+    """The same token 65,536 times: from the sum's size on, what each adds would be rounded alike, so 32 bits lose what 64 keep.  All terms are positive but one.  Relative:
+    decays of 0.05 to 0.6 are off by 2^-21, which states and their gradients carry on 1.5 times each, so their product by 2^-19; products 2^-21; sums of 8 tokens 8 times 2^-20."""
+    ha, T, ch, S = _ha(), 65536, 6, 3
+    gen = torch.Generator().manual_seed(4)
+    r = lambda *s: 0.5 + 0.5 * torch.rand(*s, generator=gen)                   # noqa: E731
+    x, dt, dy, B, C, D, A = r(ch), r(ch), r(ch), r(1, S), r(1, S), r(ch), -2 * r(ch, S)
+    rows = lambda t: t.cuda().expand(1, T, *t.shape).contiguous()              # noqa: E731
+    got = ha.ha_la_scan_backward(rows(dy), rows(x), rows(dt), A.cuda(), rows(B), rows(C), D=D.cuda(), dt_bias=torch.zeros(ch, device="cuda"), softplus=False)
+    x, dt, dy, B, C, D, A = (t.double().numpy() for t in (x, dt, dy, B, C, D, A))
+    a, u = np.exp(dt[:, None] * A), (dt * x)[:, None] * B
+    h = np.zeros((T + 1, ch, S))
+    for t in range(T):
+        h[t + 1] = a * h[t] + u
+    dh, flow, to_b = np.zeros((ch, S)), np.zeros((ch, S)), np.zeros(ch)
+    for t in reversed(range(T)):
+        dh = C * dy[:, None] + dh
+        to_b += (dh * B).sum(1)
+        dh = dh * a
+        flow += dh * h[t]
+    dA, from_a, from_b = flow * dt[:, None], (flow * A).sum(1), x * to_b
+    off = lambda g, w, m=None: float(((g.double().cpu() - torch.tensor(w)).abs() / torch.tensor(w if m is None else m)).max())       # noqa: E731
+    assert off(got[2], dA) <= 2 ** -18
+    assert off(got[5], T * x * dy) <= 2 ** -21
+    assert off(got[7], from_a + from_b, from_b - from_a) <= 2 ** -18
