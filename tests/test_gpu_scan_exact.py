@@ -3,6 +3,8 @@ import numpy as np
 import pytest
 import torch
 
+from tests import test_gpu_scan as scan
+
 pytestmark = pytest.mark.gpu
 
 
@@ -76,3 +78,9 @@ def test_gradients_that_add_up_over_many_tokens():
     assert off(got[2], dA) <= 2 ** -18
     assert off(got[5], T * x * dy) <= 2 ** -21
     assert off(got[7], from_a + from_b, from_b - from_a) <= 2 ** -18
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+def test_gradients_of_long_sequences(dtype):
+    """Everything of a few thousand random tokens, to the bounds that short sequences keep (sums over tokens in parts of at most 64 in 32 bits, the parts in 64)."""
+    scan.check(scan.inputs(1, 3300, 5, 16, 1, dtype, cu=[0, 1300, 1301, 3300], seed=21, strong=0.3))
