@@ -644,11 +644,13 @@ template <typename F, typename A> int without_lock(F f, const A* args, void* str
   return rc;
 }
 
-// an optional contiguous tensor of that shape, or one with more behind it: longer in the first dimension that is not one
+// an optional contiguous tensor of that shape, or one with more behind it: longer in the first dimension that is not one; or a flat buffer with room
 bool laid_out(const at::Tensor* t, const at::Tensor& like, at::ScalarType type, at::IntArrayRef shape) {
   if (!t) return true;
-  if (t->device() != like.device() || t->scalar_type() != type || !t->is_contiguous() || t->dim() != (int64_t)shape.size()) return false;
+  if (t->device() != like.device() || t->scalar_type() != type || !t->is_contiguous()) return false;
   const auto have = t->sizes();
+  if (have.size() == 1) return have[0] >= c10::multiply_integers(shape);
+  if (have.size() != shape.size()) return false;
   size_t i = 0;
   while (i + 1 < shape.size() && shape[i] == 1 && have[i] == 1) ++i;
   return have[i] >= shape[i] && have.slice(i + 1) == shape.slice(i + 1);
