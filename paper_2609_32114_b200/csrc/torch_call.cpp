@@ -644,16 +644,20 @@ template <typename F, typename A> int without_lock(F f, const A* args, void* str
   return rc;
 }
 
-// an optional contiguous tensor of that shape, or one with more behind it: longer in the first dimension that is not one; or a flat buffer with room
+// an optional contiguous tensor whose elements are in that shape's order as far as its own shape tells: from the last one on dimensions agree, but for the outermost
+// (in front of which there are only ones), which has at least what the wanted ones that are left come to
 bool laid_out(const at::Tensor* t, const at::Tensor& like, at::ScalarType type, at::IntArrayRef shape) {
   if (!t) return true;
   if (t->device() != like.device() || t->scalar_type() != type || !t->is_contiguous()) return false;
   const auto have = t->sizes();
-  if (have.size() == 1) return have[0] >= c10::multiply_integers(shape);
-  if (have.size() != shape.size()) return false;
-  size_t i = 0;
-  while (i + 1 < shape.size() && shape[i] == 1 && have[i] == 1) ++i;
-  return have[i] >= shape[i] && have.slice(i + 1) == shape.slice(i + 1);
+  int64_t i = (int64_t)have.size() - 1, j = (int64_t)shape.size() - 1;
+  for (; i > 0 && j >= 0 && have[i] == shape[j]; --i) --j;
+  if (i < 0 || t->numel() < c10::multiply_integers(shape)) return false;
+  int64_t least = 1;
+  for (int64_t k = 0; k <= j; ++k) least *= shape[k];
+  for (int64_t k = 0; j >= 0 && k < i; ++k)
+    if (have[k] != 1) return false;
+  return j < 0 || have[i] >= least;
 }
 
 // x [B, T, C] (`token`: [N, C]), w, bias, activation, cu_seqlens

@@ -5,7 +5,8 @@ As in `layer`: marshalling only, torch CUDA tensors in and out, everything is co
 stream, nothing is synchronised, tensors whose type, layout, size or device does not fit raise ValueError before anything is launched,
 and nothing is recorded for autograd.  Inputs with one row to a token may be rows of a wider tensor (slices of a fused projection's
 output along the last dimension); outputs are contiguous.  States, outputs and their gradients that a caller hands in have the shape that is
-written beside them, or more behind it (a longer first dimension), or are flat buffers with room for it: another shape is refused, whatever it holds.
+written beside them, outer dimensions taken together if that suits the caller (up to a flat buffer), and may hold more behind it; one whose inner
+dimensions are others is refused, however many elements it has.
 """
 from __future__ import annotations
 
@@ -147,14 +148,15 @@ def _vector(t, like, name, shape):
 
 
 def _laid_out(name, t, like, dtype, shape):
-    """A tensor (or None) that the kernels take by its address: contiguous, of that shape, or with more behind it: longer in the first dimension that is not one;
-    or a flat buffer with room.  A state with its last dimensions the other way round has as many elements, so those do not tell."""
+    """A tensor (or None) that the kernels take by its address: contiguous, and its elements in that shape's order as far as its own shape tells.  From the last one on
+    dimensions agree, but for the outermost (in front of which there are only ones): it has at least what the wanted ones that are left come to."""
     if t is None:
         return
     have, shape = tuple(t.shape), tuple(shape)
-    i = next((i for i, n in enumerate(shape) if n != 1), len(shape) - 1)
-    i = next((j for j in range(i) if have[j:j + 1] != (1,)), i)
-    fits = len(have) == 1 and have[0] >= math.prod(shape) or len(have) == len(shape) and have[:i] == shape[:i] and have[i] >= shape[i] and have[i + 1:] == shape[i + 1:]
+    i, j = len(have) - 1, len(shape) - 1
+    while i > 0 and j >= 0 and have[i] == shape[j]:
+        i, j = i - 1, j - 1
+    fits = i >= 0 and math.prod(have) >= math.prod(shape) and (j < 0 or all(n == 1 for n in have[:i]) and have[i] >= math.prod(shape[:j + 1]))
     if not (_reachable(t, like) and t.is_contiguous() and t.dtype == dtype and fits):
         raise ValueError(f"{name}: {t.dtype} {have}, strides {tuple(t.stride())}, on {t.device}; wanted is {dtype} {shape}, contiguous, on {like.device}")
 
