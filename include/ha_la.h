@@ -430,7 +430,7 @@ int ha_la_conv_decode(const ha_la_conv_args* args, void* cuda_stream);
  *     h <- e^{delta_t A} h + delta_t B_t[j] x_t        y_t = (<C_t[j], h> + D x_t) silu(z_t)      hT = h after the last token
  * D, z and dt_bias may be NULL (no such term).  All arithmetic fp32, y rounded once at the end, states fp32.
  * ha_la_scan_backward: gradients of everything from dy and dhT; the forward pass's states are computed again.  dB and dC are
- * sums over a group's channels, dA, dD and ddt_bias over all tokens.
+ * sums over a group's channels, dA, dD and ddt_bias over all tokens (64 of them in fp32, those sums in 64 bits).
  * ha_la_scan_decode: one token for each of `batch` sequences (seqlen = 1), no workspace; hT may be exactly h0.
  * hT may be exactly h0 in ha_la_scan too, and dh0 exactly dhT.
  * What the inputs must satisfy: finite values, A <= 0, delta >= 0 (so with softplus = 0 dt + dt_bias >= 0).    */

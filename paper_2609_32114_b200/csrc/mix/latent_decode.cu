@@ -9,8 +9,10 @@
 // query's maximum is spread over 64 threads: they take the exact one for a segment's first rows and whenever a score exceeds it by 2^8 (one vote), and
 // each adds up its own weights until the end.
 // The scores of the next 64 rows are made ahead of the products with these rows' values, and shared memory holds two to two and a half such tiles: copies are
-// under way all the time.  (64 contexts of 500 to 16000 rows, 32 heads: 122 us a call; 128 rows at a time, of which shared memory holds one and a quarter, 156.)
-// What bounds it there is the rate at which the copy engine takes its 128-byte pieces: 2800 cycles a tile with nothing else going on (6 TB/s), 3500 beside the products.
+// under way all the time.  (64 contexts of 500 to 16000 rows, 32 heads: 122 to 126 us a call; 128 rows at a time, of which shared memory holds one and a quarter, 156.)
+// Tiles that follow one another take an SM 1.76 us each, 6.2 TB/s over all SMs (148 contexts of 8192 rows less 148 of 4096, with 16 heads 1.63, with 64 2.15); 45.6 of them an
+// SM are 80 us of those 64 contexts'.  The rest is what a call has once: two launches, lengths and pages looked up, the first tiles, which come one by one, and the parts'
+// joining, 10 us by itself.  (One tile an SM: 22 us a call.)
 //
 // Work is cut into units of 64 rows of all sequences one behind the other, in equal parts for the CTAs, one an SM: long and short contexts, few or many,
 // load all of them evenly.  A sequence that several CTAs share leaves unnormalised parts, joined by a second kernel in order.

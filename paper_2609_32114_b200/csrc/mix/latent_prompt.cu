@@ -3,8 +3,9 @@
 // A CTA has 128 TILES queries of a head and goes through the keys 128 at a time: S = Q K^T (128 x 128, twelve steps of 16 channels, the last four of
 // them on the positional key that all heads share), P = 2^(S - m) in bf16 over S's place in tensor memory, O += P V with P as the operand from there.
 // With two tiles of queries the tensor cores work on one while the softmax warps, a thread to a query, are on the other's scores: the products of
-// both are 2560 cycles a round, their exponentials 2048, and K and V are read once for 256 queries.  A round takes some 4200: a tile's own chain of scores, softmax (2000 beside
-// the other tile's) and values.  8192 tokens, 32 heads: 590 us, 1165 TFLOP/s of the causal half.
+// both are 2560 cycles a round, their exponentials 2048, and K and V are read once for 256 queries.  A round takes some 4700, all that is around the rounds
+// included (4096 tokens, 32 heads: 275,000 cycles for 58.8 of them an SM, the tensor cores busy for 53 %): a tile's scores, softmax and values wait for each other.  8192 tokens,
+// 32 heads: 580 us, 1184 TFLOP/s of the causal half; 684 after some seconds of nothing else, when the power cap holds the clocks at 1580 MHz.
 // m need not be the largest score, only near it: O and l are rescaled when a score exceeds m by 2^8, which after the first keys is rare, so O is hardly
 // ever read back.  P <= 2^8 loses nothing in bf16, and l adds up the weights as they are before that rounding, in fp32.
 #include <algorithm>

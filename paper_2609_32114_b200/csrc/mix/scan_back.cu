@@ -3,10 +3,10 @@
 // The states in front of every eight tokens come from a run of the forward recurrence (scan.cu).  Here a CTA goes through a sequence's tokens from the
 // last to the first, 16 at a time, for CH channels: eight warps make eight tokens' states from the kept one, hold them in registers and come back
 // through them, so that the states never go through memory one by one; a decay is made three times in all, which is cheaper than the registers that would
-// keep it (622 us against 667 with decays kept, two rows of 2048 tokens and 4096 channels; 637 since dA is summed by eights).  Eight other warps bring the
+// keep it (622 us against 667 with decays kept, two rows of 2048 tokens and 4096 channels; 634 since dA is summed by eights and in 64 bits).  Eight other warps bring the
 // next 16 tokens and finish the last ones.  Sums over states (dx, ddelta, p) and over channels (dB, dC) cross the lanes of a warp, 10 shuffles a token; dB and
 // dC then go over the warps in shared memory and over the channel blocks in a second kernel, in order.  What bounds it is the length of a token's own chain,
-// products, two sums across lanes, results, with two such warps to a scheduler: issue slots are 53 % used.  (Four warps with two channels to a thread:
+// products, two sums across lanes, results, with two such warps to a scheduler: issue slots are 54 % used.  (Four warps with two channels to a thread:
 // 706 us; kept states sent for one part ahead instead of a tile: 758.)
 #include "scan.cuh"
 
