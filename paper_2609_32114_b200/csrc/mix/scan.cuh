@@ -49,8 +49,8 @@ __device__ __forceinline__ float softplus(float v) {
 
 // A step's decay e^{delta A}, with A2 = A log2(e).  ex2 comes out too small on the average, by 2e-8 of itself for exponents of -1/256 to -1 (half of that below, twice as
 // much above), and where decays are near one that adds up over all the tokens that a state lasts.  The exponent is raised by as much, where it costs nothing: the average
-// is then within 1.2e-8 for all exponents above -1.  Of an exponent of zero 2^x is still exactly one.  (Error of dA, two rows of 2048 tokens, 4096 channels: 1.8e-6 without and 0.8e-6 with it; the plain
-// form's exponentials 0.9e-6.)
+// is then within 1.2e-8 for all exponents above -1.  Of an exponent of zero 2^x is still exactly one.  (Error of dA, two rows of 2048 tokens, 4096 channels: 1.8e-6 without
+// and 0.8e-6 with it; the plain form's exponentials 0.9e-6.)
 constexpr float kRaise = 0x1.8p-26f;
 __device__ __forceinline__ float decay(float delta, float A2) { return ex2(fmaf(delta, A2, kRaise)); }
 __device__ __forceinline__ float2 decay2(float delta, float2 A2) {
